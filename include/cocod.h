@@ -382,6 +382,123 @@ int cocod_debug_normals(void *stream, uint64_t seed, uint32_t tag, uint32_t work
  */
 int cocod_debug_copy(void *stream, const float *src, float *dst, uint64_t n);
 
+/*
+ * ---- Operators for the caller's own models (COCOD_GRAD_EXTERNAL) -----------------------------------
+ *
+ * A caller whose gradient comes from a model of its own needs the products, the loss and the stored
+ * activations of that model for all W workers at a time.  A group is a worker (or an expert): group g
+ * owns the rows offsets[g] .. offsets[g + 1] - 1 of every row-wise array and its own matrix.  Batches may
+ * be of any sizes, empty ones included; offsets lie in device memory, so a replayed graph or a router
+ * may change them without the host knowing.  Rows in front of offsets[0] and from offsets[groups] on are
+ * neither read nor written.  Offsets ought to ascend; entries outside 0 .. rows are taken as the nearer
+ * end, and with offsets that do not ascend no access leaves the arrays but the results are undefined.
+ *
+ * The calls need no context.  Each only enqueues on `stream` (a hipStream_t of any device, NULL = the
+ * null stream of the current device), allocates nothing, keeps nothing and may be captured into a graph.
+ * The caller's workspace belongs to a call until the stream has passed it: two calls or two graphs that
+ * may run at the same time need two.  Descriptions are read during the call.  Arrays are row-major
+ * with a pitch ("ld", elements from row to row) of their own; any alignment to whole elements and any
+ * pitch work.  16-bit operands that start on 16 bytes, with pitches, group strides and a summed axis that
+ * are multiples of 8, are the fast ones; of such a row the whole 16-byte piece that holds its last
+ * element is read.  Row-wise arrays may be NULL where rows is 0.  Outputs must not overlap other arguments.  Sums are kept in fp32 (fp32 operands are multiplied
+ * at fp32 accuracy) and rounded once.
+ */
+typedef enum cocod_dtype {
+    COCOD_F32 = 0,
+    COCOD_BF16 = 1,              /* the upper 16 bits of an fp32 */
+    COCOD_F16 = 2                /* IEEE half */
+} cocod_dtype;
+
+enum {
+    COCOD_GROUPED_RELU_OUT = 1u,    /* forward: y = max(x w, 0) */
+    COCOD_GROUPED_RELU_IN = 2u      /* x is the output of a relu: the input's gradient is taken through it */
+};
+enum { COCOD_GROUPED_FORWARD = 0, COCOD_GROUPED_INPUT_GRAD = 1, COCOD_GROUPED_WEIGHT_GRAD = 2 };
+
+/*
+ * One linear layer of all groups, y_g = x_g w_g.  A call reads the fields it names; the others are
+ * ignored.  w may lie inside the workers' models ([W][stride], w_stride = stride) and dw inside the gradient that
+ * cocod_external_step or cocod_external_step_bf16 takes.
+ */
+typedef struct cocod_grouped {
+    uint32_t struct_size;           /* sizeof(cocod_grouped); checked */
+    uint32_t dtype;                 /* cocod_dtype of x, w, y, dy, dx */
+    uint32_t groups;                /* 1 .. 65535 */
+    uint32_t flags;                 /* COCOD_GROUPED_RELU_* */
+    uint64_t rows;                  /* rows of x, y, dy, dx in memory, < 2^31; 0 is legal */
+    uint32_t inner, outer;          /* columns of x, columns of y; 1 .. 2^30 */
+    const int64_t *offsets;         /* device, [groups + 1], 8-byte aligned */
+    const void *x;   uint64_t ldx;          /* [rows][inner] */
+    const uint8_t *x_codes;  uint64_t ld_codes;    /* where x is NULL: x as cocod_checkpoint_store left it, [rows][inner] */
+    const uint8_t *x_scales; uint64_t ld_scales;   /*   and its scales, [rows][ceil(inner / 32)] */
+    const void *w;   uint64_t ldw, w_stride;       /* [groups][inner][outer]; w_stride 0: one matrix for all groups */
+    void *y;         uint64_t ldy;          /* [rows][outer] */
+    const void *dy;  uint64_t lddy;         /* [rows][outer] gradient at y */
+    void *dx;        uint64_t lddx;         /* [rows][inner] gradient at x */
+    void *dw;        uint64_t lddw, dw_stride;     /* [groups][inner][outer] gradient at w, a matrix of its own for every group */
+    uint32_t dw_dtype;              /* dtype, or COCOD_F32 */
+    uint32_t reserved;
+    void *workspace;                /* device, 16-byte aligned; NULL: long sums of small results are not split over the chip */
+    uint64_t workspace_bytes;
+} cocod_grouped;
+
+/* Bytes of workspace with which the call of this direction splits its sums (0: it would not); reads the sizes only. */
+int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *bytes);
+/* y_g = x_g w_g, through a relu with COCOD_GROUPED_RELU_OUT (a NaN stays one). */
+int cocod_grouped_forward(void *stream, const cocod_grouped *g);
+/* dx_g = dy_g w_g^T; with COCOD_GROUPED_RELU_IN zero where x (x NULL: its codes) is not above zero. */
+int cocod_grouped_input_grad(void *stream, const cocod_grouped *g);
+/* dw_g = x_g^T dy_g (x NULL: the product takes the codes and scales as they are); zero for a group without rows. */
+int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g);
+
+enum { COCOD_CROSS_ENTROPY_SUM = 1u };      /* a group's loss is the sum of its rows' losses, not their mean */
+
+/*
+ * Softmax cross-entropy of logits h_g e_g^T over a vocabulary, without the logits in memory, and the gradients of
+ * grad_scale * (loss of the group).  A row whose target is not in 0 .. vocab - 1 has none: its loss and its
+ * row of dh are zero, it does not count in the mean, and nothing of its h is used.  A group without
+ * targets has loss 0 and gradient 0.  16-bit types: the slopes at the logits are rounded to the type before the products.
+ */
+typedef struct cocod_cross_entropy_call {
+    uint32_t struct_size;           /* sizeof(cocod_cross_entropy_call); checked */
+    uint32_t dtype;                 /* cocod_dtype of h, e, dh, de */
+    uint32_t groups;                /* 1 .. 65535 */
+    uint32_t flags;                 /* COCOD_CROSS_ENTROPY_* */
+    uint64_t rows;                  /* < 2^31; 0 is legal */
+    uint32_t dim, vocab;            /* 1 .. 2^30 */
+    const int64_t *offsets;         /* device, [groups + 1], 8-byte aligned */
+    const void *h;   uint64_t ldh;              /* [rows][dim] hidden states */
+    const void *e;   uint64_t lde, e_stride;    /* [groups][vocab][dim]; e_stride 0: one table for all groups */
+    const int32_t *targets;         /* device, [rows] */
+    float *loss;                    /* device, [rows] */
+    float *group_loss;              /* device, [groups]; may be NULL */
+    void *dh;        uint64_t lddh;             /* [rows][dim]; NULL: not wanted */
+    void *de;        uint64_t ldde, de_stride;  /* [groups][vocab][dim], a table of its own for every group; NULL: not wanted */
+    float grad_scale;               /* finite */
+    uint32_t piece;                 /* vocabulary entries whose slopes are in memory at a time, rounded down to a multiple of 256 (at least
+                                       256); 0: as many as make 2^28 values */
+    void *workspace;                /* device, 256-byte aligned */
+    uint64_t workspace_bytes;
+} cocod_cross_entropy_call;
+
+/* Bytes of workspace that the call needs; reads the sizes, piece, and whether dh and de are NULL. */
+int cocod_cross_entropy_workspace(const cocod_cross_entropy_call *c, uint64_t *bytes);
+int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c);
+
+/*
+ * Activations in 8 bits from the forward to the backward pass.  32 consecutive values of a row (the last ones of a
+ * row may be fewer) share a scale 2^e, stored as e + 127: the smallest power of two, not below 2^-117 (COCOD_F16: 2^-15), for
+ * which their largest finite magnitude is at most 448 * 2^e.  A value is stored as the e4m3 code (1 + 4 + 3
+ * bits, bias 7, no infinities) nearest to value / 2^e, ties to the even code; what is not zero becomes no
+ * zero but at least the smallest code; magnitudes above 1.875 * 2^127 (COCOD_F16: 1.875 * 2^15) are stored as that;
+ * infinities and NaN become NaN and do not count for the scale.  Every stored value is a value of the
+ * type it came from, so load is exact.  The codes of a row are followed by nothing: pitches may be any.
+ */
+int cocod_checkpoint_store(void *stream, int dtype, uint64_t rows, uint64_t cols, const void *x, uint64_t ldx,
+                           uint8_t *codes, uint64_t ld_codes, uint8_t *scales, uint64_t ld_scales);
+int cocod_checkpoint_load(void *stream, int dtype, uint64_t rows, uint64_t cols, const uint8_t *codes, uint64_t ld_codes,
+                          const uint8_t *scales, uint64_t ld_scales, void *x, uint64_t ldx);
+
 /* Last error text of ctx, or of the last failed cocod_create / context-free call when ctx is NULL.
    Never NULL; owned by the library; valid until the next call on the same context / thread. */
 const char *cocod_last_error(const cocod_ctx *ctx);

@@ -13,6 +13,10 @@ OK, ERR_INVALID, ERR_STATE, ERR_HIP, ERR_NOMEM, ERR_UNSUPPORTED = 0, -1, -2, -3,
 GRAD_QUADRATIC, GRAD_MLP, GRAD_EXTERNAL = 0, 1, 2
 SCHED_OVERLAP, SCHED_SERIAL, SCHED_FUSED, SCHED_HEAD = 0, 1, 2, 3
 FLAG_DRY_RUN = 1
+F32, BF16, F16 = 0, 1, 2
+GROUPED_RELU_OUT, GROUPED_RELU_IN = 1, 2
+GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD = 0, 1, 2
+CROSS_ENTROPY_SUM = 1
 
 
 class Config(C.Structure):
@@ -29,6 +33,51 @@ class Config(C.Structure):
         ("mlp_in", C.c_uint32), ("mlp_hidden", C.c_uint32), ("mlp_out", C.c_uint32), ("mlp_batch", C.c_uint32),
         ("flags", C.c_uint32),
     ]
+
+
+class _Call(C.Structure):
+    """A description of a call: fields by name, addresses unwrapped, struct_size filled in."""
+
+    def __init__(self, **fields):
+        super().__init__()
+        self.struct_size = C.sizeof(self)
+        self.set(**fields)
+
+    def set(self, **fields):
+        types = dict(self._fields_)
+        for name, value in fields.items():
+            if name not in types:
+                raise TypeError("%s has no field %s" % (type(self).__name__, name))
+            setattr(self, name, _addr(value) if types[name] is C.c_void_p else value)
+
+
+class Grouped(_Call):
+    """Mirror of struct cocod_grouped.  It holds addresses only: the tensors are the caller's to keep."""
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("groups", C.c_uint32), ("flags", C.c_uint32),
+        ("rows", C.c_uint64), ("inner", C.c_uint32), ("outer", C.c_uint32), ("offsets", C.c_void_p),
+        ("x", C.c_void_p), ("ldx", C.c_uint64), ("x_codes", C.c_void_p), ("ld_codes", C.c_uint64),
+        ("x_scales", C.c_void_p), ("ld_scales", C.c_uint64),
+        ("w", C.c_void_p), ("ldw", C.c_uint64), ("w_stride", C.c_uint64), ("y", C.c_void_p), ("ldy", C.c_uint64),
+        ("dy", C.c_void_p), ("lddy", C.c_uint64), ("dx", C.c_void_p), ("lddx", C.c_uint64),
+        ("dw", C.c_void_p), ("lddw", C.c_uint64), ("dw_stride", C.c_uint64), ("dw_dtype", C.c_uint32), ("reserved", C.c_uint32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class CrossEntropy(_Call):
+    """Mirror of struct cocod_cross_entropy_call (grad_scale 1 unless given)."""
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("groups", C.c_uint32), ("flags", C.c_uint32),
+        ("rows", C.c_uint64), ("dim", C.c_uint32), ("vocab", C.c_uint32), ("offsets", C.c_void_p),
+        ("h", C.c_void_p), ("ldh", C.c_uint64), ("e", C.c_void_p), ("lde", C.c_uint64), ("e_stride", C.c_uint64),
+        ("targets", C.c_void_p), ("loss", C.c_void_p), ("group_loss", C.c_void_p),
+        ("dh", C.c_void_p), ("lddh", C.c_uint64), ("de", C.c_void_p), ("ldde", C.c_uint64), ("de_stride", C.c_uint64),
+        ("grad_scale", C.c_float), ("piece", C.c_uint32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+    def __init__(self, **fields):
+        super().__init__(**{"grad_scale": 1.0, **fields})
 
 
 class CocodError(RuntimeError):
@@ -83,6 +132,14 @@ def lib():
             "cocod_mlp_workspace": ([vp, P(vp), P(vp), P(vp), P(vp), P(vp), P(u32)], i32),
             "cocod_step_timing": ([vp, i32], i32),
             "cocod_step_timing_read": ([vp, P(C.c_double), P(u32)], i32),
+            "cocod_grouped_workspace": ([P(Grouped), i32, P(u64)], i32),
+            "cocod_grouped_forward": ([vp, P(Grouped)], i32),
+            "cocod_grouped_input_grad": ([vp, P(Grouped)], i32),
+            "cocod_grouped_weight_grad": ([vp, P(Grouped)], i32),
+            "cocod_cross_entropy_workspace": ([P(CrossEntropy), P(u64)], i32),
+            "cocod_cross_entropy": ([vp, P(CrossEntropy)], i32),
+            "cocod_checkpoint_store": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
+            "cocod_checkpoint_load": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_debug_copy": ([vp, vp, vp, u64], i32),
             "cocod_debug_normals": ([vp, u64, u32, u32, u32, u64, u64, i32, vp], i32),
         }
@@ -128,6 +185,46 @@ def debug_normals(stream, seed, tag, worker, step, j0, n, fast, out):
 
 def debug_copy(stream, src, dst, n):
     _check(lib().cocod_debug_copy(_addr(stream), _addr(src), _addr(dst), n))
+
+
+# ---- operators for the caller's own models -----------------------------------------------------
+
+def grouped_workspace(layer, direction):
+    """Bytes with which this direction of the layer splits its sums over the chip."""
+    out = C.c_uint64()
+    _check(lib().cocod_grouped_workspace(C.byref(layer), direction, C.byref(out)))
+    return out.value
+
+
+def grouped_forward(stream, layer):
+    return _check(lib().cocod_grouped_forward(_addr(stream), C.byref(layer)))
+
+
+def grouped_input_grad(stream, layer):
+    return _check(lib().cocod_grouped_input_grad(_addr(stream), C.byref(layer)))
+
+
+def grouped_weight_grad(stream, layer):
+    return _check(lib().cocod_grouped_weight_grad(_addr(stream), C.byref(layer)))
+
+
+def cross_entropy_workspace(call):
+    """Bytes of workspace that cross_entropy(stream, call) needs."""
+    out = C.c_uint64()
+    _check(lib().cocod_cross_entropy_workspace(C.byref(call), C.byref(out)))
+    return out.value
+
+
+def cross_entropy(stream, call):
+    return _check(lib().cocod_cross_entropy(_addr(stream), C.byref(call)))
+
+
+def checkpoint_store(stream, dtype, rows, cols, x, ldx, codes, ld_codes, scales, ld_scales):
+    return _check(lib().cocod_checkpoint_store(_addr(stream), dtype, rows, cols, _addr(x), ldx, _addr(codes), ld_codes, _addr(scales), ld_scales))
+
+
+def checkpoint_load(stream, dtype, rows, cols, codes, ld_codes, scales, ld_scales, x, ldx):
+    return _check(lib().cocod_checkpoint_load(_addr(stream), dtype, rows, cols, _addr(codes), ld_codes, _addr(scales), ld_scales, _addr(x), ldx))
 
 
 # ---- the five entry points of the round, by their C names -----------------------------------

@@ -355,6 +355,17 @@ int mean_before_line6(cocod_ctx *ctx)
 
 }  // namespace
 
+int cocod::set_error(int code, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    g_err = buf;
+    return code;
+}
+
 extern "C" {
 
 int cocod_version(void) { return 1000; }

@@ -1,0 +1,345 @@
+// Mean softmax cross-entropy of ragged batches over a large vocabulary, and its gradient, without the logits in memory.
+//
+//   z = h E_g^T,  loss_r = log sum_v exp z_rv - z_r,t(r),  L_g = sum_r loss_r / n_g,
+//   dL/dz_rv = (exp(z_rv - norm_r) - [v = t(r)]) / n_g,  dh = dz E_g,  dE_g = dz^T h
+//
+// Rows without a target take no part: the others are gathered to the front of their group, so that no product sees a row that is
+// masked (whatever its values are) and masked rows cost nothing.  The vocabulary is gone through twice: once for maximum and sum
+// of exponentials of every row, tile by tile in the products' epilogue, and once more, piece by piece, for dz, of which one piece
+// at a time is in memory in the element type, for the two products that follow it.  The logits are formed twice, 8 instead of 6
+// products' worth of work; kept in 16 bits they would be rows x vocab x 2 bytes (2 GiB at 8192 x 131072).
+//
+// dz is rounded to the element type before the products (fp32: not): each of its values is off by at most half a step, which leaves
+// the gradients, themselves rounded once more, within 1.4 times the error of that last rounding.
+#include "operator_call.hpp"
+
+#include <cmath>
+
+namespace cocod {
+namespace {
+
+const Dtype kTypes[] = {Dtype::F32, Dtype::BF16, Dtype::F16};
+constexpr uint32_t kPieceUnit = 256;
+constexpr uint64_t kPieceElements = 1ull << 28;      // of dz in memory at a time, unless the caller says otherwise
+
+struct Rows {
+    const int64_t *offsets;
+    uint32_t groups;
+    uint64_t rows;
+    const int32_t *target;
+    uint32_t vocab;
+};
+
+__device__ __forceinline__ uint64_t clamped(const Rows &p, uint32_t i)
+{
+    const int64_t v = p.offsets[i];
+    return v < 0 ? 0 : static_cast<uint64_t>(v) > p.rows ? p.rows : static_cast<uint64_t>(v);
+}
+__device__ __forceinline__ bool has_target(const Rows &p, uint64_t r)
+{
+    return static_cast<uint32_t>(p.target[r]) < p.vocab;          // negative ones are large
+}
+
+// One block per group: the rows with a target, in order, to the front of the group's part of `index`; kNoRow behind them.
+constexpr int kCompactThreads = 1024;
+__global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, uint32_t *index, int32_t *target, int64_t *ends)
+{
+    __shared__ uint32_t counts[kCompactThreads / 64];
+    const uint32_t g = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint64_t begin = clamped(p, g), next = clamped(p, g + 1), end = next > begin ? next : begin;
+    uint64_t at = begin;
+    for (uint64_t r0 = begin; r0 < end; r0 += kCompactThreads) {
+        const uint64_t r = r0 + threadIdx.x;
+        const bool in = r < end && has_target(p, r);
+        const unsigned long long votes = __ballot(in);
+        if (lane == 0) counts[wave] = __popcll(votes);
+        __syncthreads();
+        uint32_t before = 0, all = 0;
+        for (int w = 0; w < kCompactThreads / 64; ++w) { if (w < static_cast<int>(wave)) before += counts[w]; all += counts[w]; }
+        if (in) {
+            const uint64_t to = at + before + __popcll(votes & ((1ull << lane) - 1));
+            index[to] = static_cast<uint32_t>(r);
+            target[to] = p.target[r];
+        }
+        at += all;
+        __syncthreads();
+    }
+    for (uint64_t r = at + threadIdx.x; r < end; r += kCompactThreads) index[r] = kNoRow;
+    if (threadIdx.x == 0) ends[g] = static_cast<int64_t>(at);
+}
+
+// Row r of the gathered hidden states (pitch a multiple of 8, zeros behind dim); rows without a target get loss 0 and gradient 0.
+template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Rows p, const uint32_t *index, const E *h, uint64_t ldh, uint32_t dim,
+                                                                        E *out, uint64_t pitch, float *loss, E *dh, uint64_t lddh)
+{
+    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+    const uint32_t lane = threadIdx.x % 64;
+    if (r < clamped(p, 0) || r >= clamped(p, p.groups)) return;
+    const uint32_t from = index[r];
+    if (from != kNoRow) {
+        const E *src = h + from * ldh;
+        E *dst = out + r * pitch;
+        constexpr uint32_t V = 16 / sizeof(E);
+        if ((reinterpret_cast<uintptr_t>(src) & 15) == 0 && dim % V == 0) {
+            for (uint32_t j = lane * V; j < dim; j += 64 * V) *reinterpret_cast<float4 *>(dst + j) = *reinterpret_cast<const float4 *>(src + j);
+            for (uint32_t j = dim + lane; j < pitch; j += 64) dst[j] = 0;
+        } else {
+            for (uint32_t j = lane; j < pitch; j += 64) dst[j] = j < dim ? src[j] : E(0);
+        }
+    }
+    if (!has_target(p, r)) {
+        if (lane == 0) loss[r] = 0.0f;
+        if (dh) for (uint32_t j = lane; j < dim; j += 64) dh[r * lddh + j] = 0;
+    }
+}
+
+// norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss.  64 rows per block,
+// four threads a row.
+__global__ __launch_bounds__(256) void norm_kernel(const Rows p, const uint32_t *index, const float2 *stats, uint32_t tiles, const float *target_logit,
+                                                   float *norm, float *loss)
+{
+    __shared__ float2 part[4][64];
+    const uint32_t x = threadIdx.x % 64, y = threadIdx.x / 64;
+    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * 64 + x;
+    const bool in = r >= clamped(p, 0) && r < clamped(p, p.groups) && index[r] != kNoRow;
+    float top = -INFINITY, sum = 0.0f;
+    if (in) {
+        for (uint32_t t = y; t < tiles; t += 4) {
+            const float2 s = stats[t * p.rows + r];
+            const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
+            sum = sum * expf(top - base) + s.y * expf(s.x - base);
+            top = m;
+        }
+    }
+    part[y][x] = make_float2(top, sum);
+    __syncthreads();
+    if (y != 0 || !in) return;
+    #pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float2 s = part[w][x];
+        const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
+        sum = sum * expf(top - base) + s.y * expf(s.x - base);
+        top = m;
+    }
+    const float n = top + logf(sum);
+    norm[r] = n;
+    loss[index[r]] = n - target_logit[r];
+}
+
+// One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits, and every row's gradient factor.
+__global__ __launch_bounds__(256) void mean_kernel(const Rows p, const uint32_t *index, const int64_t *ends, const float *loss, float *group_loss, int sum_only,
+                                                   float scale, float *row_scale)
+{
+    __shared__ double part[256];
+    const uint32_t g = blockIdx.x;
+    const uint64_t begin = clamped(p, g), end = static_cast<uint64_t>(ends[g]);
+    const float n = static_cast<float>(end - begin);
+    double s = 0.0;
+    for (uint64_t r = begin + threadIdx.x; r < end; r += 256) {
+        if (index[r] != kNoRow) s += loss[index[r]];             // (offsets that do not ascend may leave holes)
+        row_scale[r] = sum_only ? scale : scale / n;
+    }
+    part[threadIdx.x] = s;
+    __syncthreads();
+    for (int d = 128; d > 0; d >>= 1) {
+        if (static_cast<int>(threadIdx.x) < d) part[threadIdx.x] += part[threadIdx.x + d];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0 && group_loss) group_loss[g] = static_cast<float>(end > begin ? (sum_only ? part[0] : part[0] / static_cast<double>(end - begin)) : 0.0);
+}
+
+// The caller's memory, carved up.
+struct Workspace {
+    uint64_t index, target, ends, norm, target_logit, row_scale, hidden, stats, slope, sum, part, bytes;
+    uint64_t pitch, piece, sum_pitch;
+    uint32_t pieces;
+    ProductPlan logits, slopes, to_hidden, to_table;
+};
+
+Workspace carve(const cocod_cross_entropy_call *c)
+{
+    Workspace w{};
+    const Dtype t = kTypes[c->dtype];
+    const uint64_t s = dtype_bytes(t), rows = c->rows;
+    const bool grads = c->dh || c->de;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
+    w.pitch = (static_cast<uint64_t>(c->dim) + 7) / 8 * 8;
+    uint64_t piece = c->piece ? c->piece : kPieceElements / (rows ? rows : 1);
+    const uint64_t whole = (static_cast<uint64_t>(c->vocab) + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
+    piece = (piece < kPieceUnit ? kPieceUnit : piece) / kPieceUnit * kPieceUnit;
+    if (piece > whole) piece = whole;
+    w.pieces = static_cast<uint32_t>((whole + piece - 1) / piece);
+    w.piece = c->piece ? piece : (whole / kPieceUnit + w.pieces - 1) / w.pieces * kPieceUnit;      // of equal size
+    w.pieces = static_cast<uint32_t>((whole + w.piece - 1) / w.piece);
+    const uint32_t n = static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab);
+    w.logits = plan_product(Layout::Rows_NK, t, rows, c->groups, 0, c->vocab, c->dim);
+    w.slopes = plan_product(Layout::Rows_NK, t, rows, c->groups, 0, n, c->dim);
+    w.logits.splits = w.slopes.splits = 1;                     // exponentials need the whole sum
+    w.to_hidden = plan_product(Layout::Rows_KN, t, rows, c->groups, 0, c->dim, n);
+    w.to_table = plan_product(Layout::Weights, t, rows, c->groups, n, c->dim, 0);
+    w.index = take(rows * 4);
+    w.target = take(rows * 4);
+    w.ends = take(c->groups * 8ull);
+    w.norm = take(rows * 4);
+    w.target_logit = take(rows * 4);
+    w.row_scale = take(rows * 4);
+    w.hidden = take(rows * w.pitch * s);
+    const uint32_t narrow = w.logits.tile == Tile::Small ? 64 : 128;         // the large tile may have to give way to the medium one
+    w.stats = take((static_cast<uint64_t>(c->vocab) + narrow - 1) / narrow * rows * 8);
+    if (grads) {
+        w.slope = take(rows * w.piece * s);
+        w.sum_pitch = part_pitch(c->dim);
+        if (c->dh && w.pieces > 1) w.sum = take(rows * w.sum_pitch * 4);
+        uint64_t part = 0;
+        if (c->dh) part = part_bytes(w.to_hidden, Layout::Rows_KN, rows, c->groups, 0, c->dim);
+        if (c->de) { const uint64_t q = part_bytes(w.to_table, Layout::Weights, rows, c->groups, n, c->dim); part = part > q ? part : q; }
+        w.part = take(part);
+    }
+    w.bytes = at;
+    return w;
+}
+
+int check(const cocod_cross_entropy_call *c)
+{
+    if (!c) return set_error(COCOD_ERR_INVALID, "the description is NULL");
+    if (c->struct_size != sizeof(cocod_cross_entropy_call))
+        return set_error(COCOD_ERR_INVALID, "struct_size %u does not match this library (%zu)", c->struct_size, sizeof(cocod_cross_entropy_call));
+    if (int rc = check_dtype(c->dtype)) return rc;
+    if (c->flags & ~COCOD_CROSS_ENTROPY_SUM) return set_error(COCOD_ERR_INVALID, "unknown flag bits 0x%x", c->flags);
+    if (c->groups < 1 || c->groups > kMaxGroups) return set_error(COCOD_ERR_INVALID, "groups must be in 1..65535");
+    if (c->rows > kMaxRows) return set_error(COCOD_ERR_INVALID, "rows must be below 2^31");
+    if (c->dim < 1 || c->dim > kMaxWidth || c->vocab < 1 || c->vocab > kMaxWidth) return set_error(COCOD_ERR_INVALID, "dim and vocab must be in 1..2^30");
+    if (!std::isfinite(c->grad_scale)) return set_error(COCOD_ERR_INVALID, "grad_scale is not finite");
+    return COCOD_OK;
+}
+
+template <class E> hipError_t launch_gather(hipStream_t s, const Rows &rows, const uint32_t *index, const cocod_cross_entropy_call *c, void *hidden, uint64_t pitch)
+{
+    hipLaunchKernelGGL(gather_kernel<E>, dim3(static_cast<uint32_t>((rows.rows + 3) / 4)), dim3(256), 0, s, rows, index, static_cast<const E *>(c->h), c->ldh, c->dim,
+                       static_cast<E *>(hidden), pitch, c->loss, static_cast<E *>(c->dh), c->lddh);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace cocod
+
+using namespace cocod;
+
+extern "C" {
+
+int cocod_cross_entropy_workspace(const cocod_cross_entropy_call *c, uint64_t *bytes)
+{
+    if (!bytes) return set_error(COCOD_ERR_INVALID, "bytes is NULL");
+    if (int rc = check(c)) return rc;
+    *bytes = carve(c).bytes;
+    return COCOD_OK;
+}
+
+int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
+{
+    if (int rc = check(c)) return rc;
+    const Dtype t = kTypes[c->dtype];
+    const uint64_t s = dtype_bytes(t);
+    if (!c->offsets || (reinterpret_cast<uintptr_t>(c->offsets) & 7)) return set_error(COCOD_ERR_INVALID, "offsets is NULL or not 8-byte aligned");
+    if (int rc = check_matrix("h", c->h, c->dim, c->ldh, s, c->rows)) return rc;
+    if (int rc = check_matrix("e", c->e, c->dim, c->lde, s)) return rc;
+    if (int rc = check_stride("e", c->e_stride, c->groups, c->vocab, c->dim, c->lde, true)) return rc;
+    if (int rc = check_matrix("targets", c->targets, 1, 1, 4, c->rows)) return rc;
+    if (int rc = check_matrix("loss", c->loss, 1, 1, 4, c->rows)) return rc;
+    if (c->group_loss) if (int rc = check_matrix("group_loss", c->group_loss, 1, 1, 4)) return rc;
+    if (c->dh) if (int rc = check_matrix("dh", c->dh, c->dim, c->lddh, s)) return rc;
+    if (c->de) {
+        if (int rc = check_matrix("de", c->de, c->dim, c->ldde, s)) return rc;
+        if (int rc = check_stride("de", c->de_stride, c->groups, c->vocab, c->dim, c->ldde, false)) return rc;
+    }
+    const Workspace w = carve(c);
+    if (!c->workspace || (reinterpret_cast<uintptr_t>(c->workspace) & 255)) return set_error(COCOD_ERR_INVALID, "workspace is NULL or not 256-byte aligned");
+    if (c->workspace_bytes < w.bytes)
+        return set_error(COCOD_ERR_INVALID, "workspace holds %llu bytes, %llu are needed", (unsigned long long)c->workspace_bytes, (unsigned long long)w.bytes);
+    const Extent all[] = {
+        {"workspace", c->workspace, w.bytes}, {"loss", c->loss, c->rows * 4}, {"group_loss", c->group_loss, c->groups * 4ull},
+        {"dh", c->dh, matrix_bytes(c->rows, c->dim, c->lddh, s)},
+        {"de", c->de, c->de ? stack_bytes(c->groups, c->de_stride, c->vocab, c->dim, c->ldde, s) : 0},
+        {"h", c->h, matrix_bytes(c->rows, c->dim, c->ldh, s)}, {"e", c->e, stack_bytes(c->groups, c->e_stride, c->vocab, c->dim, c->lde, s)},
+        {"targets", c->targets, c->rows * 4}, {"offsets", c->offsets, (c->groups + 1ull) * 8},
+    };
+    for (int i = 0; i < 5; ++i)
+        if (int rc = check_apart(all[i], all + i + 1, 9 - i - 1)) return rc;
+
+    const hipStream_t q = static_cast<hipStream_t>(stream);
+    const OnStreamDevice device(q);
+    const char *const what = "cocod_cross_entropy";
+    if (device.status() != hipSuccess) return launch_status(device.status(), what);
+    uint8_t *ws = static_cast<uint8_t *>(c->workspace);
+    uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
+    int64_t *ends = reinterpret_cast<int64_t *>(ws + w.ends);
+    float *norm = reinterpret_cast<float *>(ws + w.norm), *row_scale = reinterpret_cast<float *>(ws + w.row_scale);
+    int32_t *target = reinterpret_cast<int32_t *>(ws + w.target);
+    const Rows rows = {c->offsets, c->groups, c->rows, c->targets, c->vocab};
+    const float unslope = t == Dtype::F16 ? 0x1p-14f : 1.0f;   // fp16 slopes are kept times 2^14
+    const int sum_only = (c->flags & COCOD_CROSS_ENTROPY_SUM) != 0;
+
+    hipLaunchKernelGGL(compact_kernel, dim3(c->groups), dim3(kCompactThreads), 0, q, rows, index, target, ends);
+    if (c->rows) {
+        const hipError_t e = t == Dtype::F32 ? launch_gather<float>(q, rows, index, c, ws + w.hidden, w.pitch) : launch_gather<uint16_t>(q, rows, index, c, ws + w.hidden, w.pitch);
+        if (e != hipSuccess) return launch_status(e, what);
+    }
+    ProductParams z{};
+    z.a = ws + w.hidden; z.lda = w.pitch;
+    z.b = c->e; z.ldb = c->lde; z.b_group = c->e_stride;
+    z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
+    z.k = c->dim; z.splits = 1; z.target = target;
+    if (c->rows) {
+        ProductParams p = z;
+        p.n = c->vocab;
+        p.stats = reinterpret_cast<float2 *>(ws + w.stats);
+        p.target_logit = reinterpret_cast<float *>(ws + w.target_logit);
+        const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, p);
+        if (int rc = launch_status(launch_logits(q, t, Finish::Stats, tile, p), what)) return rc;
+        const uint32_t tiles = (c->vocab + tile_cols(t, tile) - 1) / tile_cols(t, tile);
+        hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + 63) / 64)), dim3(256), 0, q, rows, index, p.stats, tiles, p.target_logit, norm, c->loss);
+    }
+    hipLaunchKernelGGL(mean_kernel, dim3(c->groups), dim3(256), 0, q, rows, index, ends, c->loss, c->group_loss, sum_only, c->grad_scale * unslope, row_scale);
+    if (int rc = launch_status(hipGetLastError(), what)) return rc;
+    if (!c->dh && !c->de) return COCOD_OK;
+
+    for (uint32_t i = 0; i < w.pieces; ++i) {
+        const uint64_t v0 = i * w.piece;
+        const uint32_t n = static_cast<uint32_t>(c->vocab - v0 < w.piece ? c->vocab - v0 : w.piece);
+        const uint8_t *e = static_cast<const uint8_t *>(c->e) + v0 * c->lde * s;
+        if (c->rows) {
+            ProductParams p = z;
+            p.b = e; p.n = n; p.v0 = static_cast<uint32_t>(v0);
+            p.norm = norm;
+            p.out = ws + w.slope; p.ldc = w.piece; p.ldc_zero = (n + 7) / 8 * 8;
+            if (int rc = launch_status(launch_logits(q, t, Finish::Slope, settle_tile(t, Layout::Rows_NK, w.slopes.tile, p), p), what)) return rc;
+        }
+        ProductParams p{};
+        p.offsets = c->offsets; p.ends = ends; p.groups = c->groups; p.rows = c->rows;
+        p.a = ws + w.slope; p.lda = w.piece;
+        p.n = c->dim;
+        p.part = reinterpret_cast<float *>(ws + w.part); p.ld_part = part_pitch(c->dim);
+        if (c->dh && c->rows) {
+            ProductParams d = p;
+            d.b = e; d.ldb = c->lde; d.b_group = c->e_stride;
+            d.k = n; d.a_zero_padded = 1;
+            d.out = c->dh; d.ldc = c->lddh; d.out_row = index; d.row_scale = row_scale;
+            if (w.pieces > 1) { d.sum = reinterpret_cast<float *>(ws + w.sum); d.ld_sum = w.sum_pitch; d.sum_read = i > 0; d.sum_write = i + 1 < w.pieces; }
+            d.splits = w.to_hidden.splits;
+            if (int rc = launch_status(launch_store(q, t, Layout::Rows_KN, settle_tile(t, Layout::Rows_KN, w.to_hidden.tile, d), d), what)) return rc;
+        }
+        if (c->de) {
+            ProductParams d = p;
+            d.b = ws + w.hidden; d.ldb = w.pitch;
+            d.m = n;
+            d.out = static_cast<uint8_t *>(c->de) + v0 * c->ldde * s; d.ldc = c->ldde; d.out_group = c->de_stride;
+            d.scale = c->grad_scale * unslope; d.mean = !sum_only;
+            d.splits = w.to_table.splits;
+            if (int rc = launch_status(launch_store(q, t, Layout::Weights, settle_tile(t, Layout::Weights, w.to_table.tile, d), d), what)) return rc;
+        }
+    }
+    return COCOD_OK;
+}
+
+}  // extern "C"

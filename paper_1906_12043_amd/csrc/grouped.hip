@@ -1,0 +1,206 @@
+// Grouped products of ragged batches: argument checks, choice of the tile, and the three directions of a layer.
+#include "operator_call.hpp"
+
+namespace cocod {
+
+ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k)
+{
+    const bool weights = layout == Layout::Weights;
+    const uint64_t high = weights ? m : (rows + groups - 1) / groups;       // rows of C of one group, on average
+    const uint64_t terms = weights ? (rows + groups - 1) / groups : k;
+    auto tiles = [&](uint64_t bm, uint64_t bn) { return groups * ((high + bm - 1) / bm) * ((n + bn - 1) / bn); };
+    ProductPlan plan{Tile::Medium, 1};
+    if (high <= 48 || (tiles(128, 128) < 64 && terms <= 4096)) plan.tile = Tile::Small;
+    else if (type != Dtype::F32 && high >= 192 && n >= 192 && tiles(256, 256) >= 200) plan.tile = Tile::Large;
+    const uint64_t slice = plan.tile == Tile::Small ? (type == Dtype::F32 ? 64 : 128) : type == Dtype::F32 ? 32 : 64;
+    const uint64_t have = plan.tile == Tile::Small ? tiles(32, 64) : plan.tile == Tile::Medium ? tiles(128, 128) : tiles(256, 256);
+    const uint64_t want = plan.tile == Tile::Small ? 512 : 256, most = terms / (4 * slice);
+    if (have * 2 <= want && most >= 2) {
+        uint64_t s = want / have;
+        s = s < most ? s : most;
+        plan.splits = static_cast<uint32_t>(s < 32 ? s : 32);
+    }
+    return plan;
+}
+
+uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n)
+{
+    if (plan.splits <= 1) return 0;
+    return plan.splits * (layout == Layout::Weights ? static_cast<uint64_t>(groups) * m : rows) * part_pitch(n) * sizeof(float);
+}
+
+namespace {
+
+const Dtype kTypes[] = {Dtype::F32, Dtype::BF16, Dtype::F16};
+
+int check_shape(const cocod_grouped *g)
+{
+    if (!g) return set_error(COCOD_ERR_INVALID, "the description is NULL");
+    if (g->struct_size != sizeof(cocod_grouped))
+        return set_error(COCOD_ERR_INVALID, "struct_size %u does not match this library (%zu)", g->struct_size, sizeof(cocod_grouped));
+    if (int rc = check_dtype(g->dtype)) return rc;
+    if (g->flags & ~(COCOD_GROUPED_RELU_OUT | COCOD_GROUPED_RELU_IN)) return set_error(COCOD_ERR_INVALID, "unknown flag bits 0x%x", g->flags);
+    if (g->groups < 1 || g->groups > kMaxGroups) return set_error(COCOD_ERR_INVALID, "groups must be in 1..65535");
+    if (g->rows > kMaxRows) return set_error(COCOD_ERR_INVALID, "rows must be below 2^31");
+    if (g->inner < 1 || g->inner > kMaxWidth || g->outer < 1 || g->outer > kMaxWidth) return set_error(COCOD_ERR_INVALID, "inner and outer must be in 1..2^30");
+    if (!g->offsets || (reinterpret_cast<uintptr_t>(g->offsets) & 7)) return set_error(COCOD_ERR_INVALID, "offsets is NULL or not 8-byte aligned");
+    return COCOD_OK;
+}
+
+ProductPlan plan_of(const cocod_grouped *g, Layout layout)
+{
+    const Dtype t = kTypes[g->dtype];
+    if (layout == Layout::Rows_KN) return plan_product(layout, t, g->rows, g->groups, 0, g->outer, g->inner);
+    if (layout == Layout::Rows_NK) return plan_product(layout, t, g->rows, g->groups, 0, g->inner, g->outer);
+    return plan_product(layout, t, g->rows, g->groups, g->inner, g->outer, 0);
+}
+uint64_t workspace_of(const cocod_grouped *g, Layout layout, const ProductPlan &plan)
+{
+    return part_bytes(plan, layout, g->rows, g->groups, g->inner, layout == Layout::Rows_NK ? g->inner : g->outer);
+}
+
+int check_codes(const cocod_grouped *g)
+{
+    if (int rc = check_matrix("x_codes", g->x_codes, g->inner, g->ld_codes, 1, g->rows)) return rc;
+    return check_matrix("x_scales", g->x_scales, (static_cast<uint64_t>(g->inner) + 31) / 32, g->ld_scales, 1, g->rows);
+}
+
+// The parameters that all directions share, the split sums' memory, and the launch.
+int start(const cocod_grouped *g, Layout layout, ProductParams &p, ProductPlan &plan, const Extent &out, const Extent *in, int n_in)
+{
+    const Dtype t = kTypes[g->dtype];
+    plan = plan_of(g, layout);
+    const uint64_t need = workspace_of(g, layout, plan);
+    const bool own = g->workspace && need;
+    if (own && (reinterpret_cast<uintptr_t>(g->workspace) & 15)) return set_error(COCOD_ERR_INVALID, "workspace is not 16-byte aligned");
+    if (own && g->workspace_bytes < need)
+        return set_error(COCOD_ERR_INVALID, "workspace holds %llu bytes, %llu are needed", (unsigned long long)g->workspace_bytes, (unsigned long long)need);
+    if (!own) plan.splits = 1;                     // the sums are then formed by one block each
+    const Extent ws = {"workspace", own ? g->workspace : nullptr, need};
+    const Extent offsets = {"offsets", g->offsets, (static_cast<uint64_t>(g->groups) + 1) * 8};
+    if (int rc = check_apart(out, in, n_in)) return rc;
+    if (int rc = check_apart(out, &offsets, 1)) return rc;
+    if (int rc = check_apart(ws, &out, 1)) return rc;
+    if (int rc = check_apart(ws, in, n_in)) return rc;
+    if (int rc = check_apart(ws, &offsets, 1)) return rc;
+    p.offsets = g->offsets;
+    p.groups = g->groups;
+    p.rows = g->rows;
+    p.scale = 1.0f;
+    p.part = own ? static_cast<float *>(g->workspace) : nullptr;
+    p.splits = plan.splits;
+    p.ld_part = part_pitch(p.n);
+    plan.tile = settle_tile(t, layout, plan.tile, p);
+    return COCOD_OK;
+}
+
+int run(void *stream, const cocod_grouped *g, Layout layout, const ProductParams &p, const ProductPlan &plan, const char *what)
+{
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const OnStreamDevice device(s);
+    if (device.status() != hipSuccess) return launch_status(device.status(), what);
+    return launch_status(launch_store(s, kTypes[g->dtype], layout, plan.tile, p), what);
+}
+
+}  // namespace
+}  // namespace cocod
+
+using namespace cocod;
+
+extern "C" {
+
+int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *bytes)
+{
+    if (!bytes) return set_error(COCOD_ERR_INVALID, "bytes is NULL");
+    if (int rc = check_shape(g)) return rc;
+    if (direction < COCOD_GROUPED_FORWARD || direction > COCOD_GROUPED_WEIGHT_GRAD) return set_error(COCOD_ERR_INVALID, "unknown direction %d", direction);
+    const Layout layout = direction == COCOD_GROUPED_FORWARD ? Layout::Rows_KN : direction == COCOD_GROUPED_INPUT_GRAD ? Layout::Rows_NK : Layout::Weights;
+    *bytes = workspace_of(g, layout, plan_of(g, layout));
+    return COCOD_OK;
+}
+
+int cocod_grouped_forward(void *stream, const cocod_grouped *g)
+{
+    if (int rc = check_shape(g)) return rc;
+    const uint64_t s = dtype_bytes(kTypes[g->dtype]);
+    if (int rc = check_matrix("x", g->x, g->inner, g->ldx, s, g->rows)) return rc;
+    if (int rc = check_matrix("w", g->w, g->outer, g->ldw, s)) return rc;
+    if (int rc = check_stride("w", g->w_stride, g->groups, g->inner, g->outer, g->ldw, true)) return rc;
+    if (int rc = check_matrix("y", g->y, g->outer, g->ldy, s, g->rows)) return rc;
+    ProductParams p{};
+    p.a = g->x; p.lda = g->ldx;
+    p.b = g->w; p.ldb = g->ldw; p.b_group = g->w_stride;
+    p.n = g->outer; p.k = g->inner;
+    p.out = g->y; p.ldc = g->ldy;
+    p.relu = (g->flags & COCOD_GROUPED_RELU_OUT) != 0;
+    const Extent in[] = {{"x", g->x, matrix_bytes(g->rows, g->inner, g->ldx, s)}, {"w", g->w, stack_bytes(g->groups, g->w_stride, g->inner, g->outer, g->ldw, s)}};
+    ProductPlan plan;
+    if (int rc = start(g, Layout::Rows_KN, p, plan, {"y", g->y, matrix_bytes(g->rows, g->outer, g->ldy, s)}, in, 2)) return rc;
+    return g->rows ? run(stream, g, Layout::Rows_KN, p, plan, "cocod_grouped_forward") : COCOD_OK;
+}
+
+int cocod_grouped_input_grad(void *stream, const cocod_grouped *g)
+{
+    if (int rc = check_shape(g)) return rc;
+    const uint64_t s = dtype_bytes(kTypes[g->dtype]);
+    if (int rc = check_matrix("dy", g->dy, g->outer, g->lddy, s, g->rows)) return rc;
+    if (int rc = check_matrix("w", g->w, g->outer, g->ldw, s)) return rc;
+    if (int rc = check_stride("w", g->w_stride, g->groups, g->inner, g->outer, g->ldw, true)) return rc;
+    if (int rc = check_matrix("dx", g->dx, g->inner, g->lddx, s, g->rows)) return rc;
+    ProductParams p{};
+    p.a = g->dy; p.lda = g->lddy;
+    p.b = g->w; p.ldb = g->ldw; p.b_group = g->w_stride;
+    p.n = g->inner; p.k = g->outer;
+    p.out = g->dx; p.ldc = g->lddx;
+    Extent in[4] = {{"dy", g->dy, matrix_bytes(g->rows, g->outer, g->lddy, s)}, {"w", g->w, stack_bytes(g->groups, g->w_stride, g->inner, g->outer, g->ldw, s)}};
+    if (g->flags & COCOD_GROUPED_RELU_IN) {
+        if (g->x) {
+            if (int rc = check_matrix("x", g->x, g->inner, g->ldx, s, g->rows)) return rc;
+            p.mask = g->x; p.ld_mask = g->ldx;
+            in[2] = {"x", g->x, matrix_bytes(g->rows, g->inner, g->ldx, s)};
+        } else {
+            if (int rc = check_matrix("x_codes", g->x_codes, g->inner, g->ld_codes, 1, g->rows)) return rc;
+            p.mask_codes = g->x_codes; p.ld_mask = g->ld_codes;
+            in[2] = {"x_codes", g->x_codes, matrix_bytes(g->rows, g->inner, g->ld_codes, 1)};
+        }
+    }
+    ProductPlan plan;
+    if (int rc = start(g, Layout::Rows_NK, p, plan, {"dx", g->dx, matrix_bytes(g->rows, g->inner, g->lddx, s)}, in, 3)) return rc;
+    return g->rows ? run(stream, g, Layout::Rows_NK, p, plan, "cocod_grouped_input_grad") : COCOD_OK;
+}
+
+int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g)
+{
+    if (int rc = check_shape(g)) return rc;
+    const uint64_t s = dtype_bytes(kTypes[g->dtype]);
+    if (g->dw_dtype != g->dtype && g->dw_dtype != COCOD_F32) return set_error(COCOD_ERR_INVALID, "dw_dtype must be the element type or COCOD_F32");
+    const uint64_t so = dtype_bytes(kTypes[g->dw_dtype]);
+    ProductParams p{};
+    Extent in[3];
+    int n_in = 1;
+    if (g->x) {
+        if (int rc = check_matrix("x", g->x, g->inner, g->ldx, s, g->rows)) return rc;
+        p.a = g->x; p.lda = g->ldx;
+        in[0] = {"x", g->x, matrix_bytes(g->rows, g->inner, g->ldx, s)};
+    } else {
+        if (int rc = check_codes(g)) return rc;
+        p.a_codes = g->x_codes; p.ld_codes = g->ld_codes;
+        p.a_scales = g->x_scales; p.ld_scales = g->ld_scales;
+        in[0] = {"x_codes", g->x_codes, matrix_bytes(g->rows, g->inner, g->ld_codes, 1)};
+        in[1] = {"x_scales", g->x_scales, matrix_bytes(g->rows, (static_cast<uint64_t>(g->inner) + 31) / 32, g->ld_scales, 1)};
+        n_in = 2;
+    }
+    if (int rc = check_matrix("dy", g->dy, g->outer, g->lddy, s, g->rows)) return rc;
+    if (int rc = check_matrix("dw", g->dw, g->outer, g->lddw, so)) return rc;
+    if (int rc = check_stride("dw", g->dw_stride, g->groups, g->inner, g->outer, g->lddw, false)) return rc;
+    in[n_in++] = {"dy", g->dy, matrix_bytes(g->rows, g->outer, g->lddy, s)};
+    p.b = g->dy; p.ldb = g->lddy;
+    p.m = g->inner; p.n = g->outer;
+    p.out = g->dw; p.ldc = g->lddw; p.out_group = g->dw_stride;
+    p.out_f32 = g->dw_dtype == COCOD_F32;
+    ProductPlan plan;
+    if (int rc = start(g, Layout::Weights, p, plan, {"dw", g->dw, stack_bytes(g->groups, g->dw_stride, g->inner, g->outer, g->lddw, so)}, in, n_in)) return rc;
+    return run(stream, g, Layout::Weights, p, plan, "cocod_grouped_weight_grad");
+}
+
+}  // extern "C"

@@ -5,6 +5,9 @@
 
 namespace cocod {
 
+// Text of cocod_last_error(NULL) for a call without a context; returns code.
+int set_error(int code, const char *fmt, ...);
+
 // One block of the local-step kernel serves one chunk: up to kChunkElems
 // consecutive elements of ONE tensor of one worker, one 16-byte quad per thread.
 constexpr uint32_t kStepThreads = 256;

@@ -1,0 +1,758 @@
+// Grouped matrix products on the matrix cores: C = A B for every group of a ragged batch, one launch for all groups.
+//
+// A block computes a BM x BN tile of C.  Slices of BK terms of both operands pass through LDS, two buffers, one barrier per
+// slice; the next slice is on its way while this one is multiplied.  The matrix instruction is 32x32x16 with the operands
+// exchanged (C^T = B^T A^T), so that a lane holds one row of C and runs of four consecutive columns of it.
+//
+// In LDS an operand lies as it does in memory: with the summed axis contiguous ([BX][BK], read as 16-byte pieces of eight
+// terms) or with the other axis contiguous ([BK][BX], read by the transposing 8-byte LDS loads, which give a lane four
+// terms of one column).  16-byte chunks are permuted inside a row so that the lanes of one read hit all banks.
+#pragma once
+#include "product.hpp"
+
+#include <type_traits>
+
+namespace cocod {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 hf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 hf8 __attribute__((ext_vector_type(8)));
+typedef float v2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef u4 __attribute__((aligned(2))) u4_any;       // 16 bytes at any element's address
+typedef u2 __attribute__((aligned(1))) u2_any;
+
+constexpr uint32_t kXcdCount = 8;
+constexpr uint32_t kBandTiles = 8;                   // row tiles that take turns in front of one column tile
+
+// fp32 operands go in as three bf16 planes, exactly (8 + 8 + 8 bits), times 2^24 so that the last bit of the smallest numbers is
+// a normal bf16 too; sums come out times 2^48.  Where that leaves the range, or an operand is not finite, the sum is not finite,
+// and the tile is formed again with fp32 products.
+constexpr float kPlaneScale = 0x1p24f, kPlaneUnscale = 0x1p-48f;
+
+struct Bf16 {
+    typedef uint16_t elem;
+    static constexpr Dtype dtype = Dtype::BF16;
+    static constexpr int planes = 1;
+    static __device__ __forceinline__ f16v mfma(u4 a, u4 b, f16v c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, bf2)); }
+    static __device__ __forceinline__ float exp(float x) { return __expf(x); }
+    static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
+    {
+        return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true))
+                    : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, false));
+    }
+};
+struct F16 {
+    typedef uint16_t elem;
+    static constexpr Dtype dtype = Dtype::F16;
+    static constexpr int planes = 1;
+    static __device__ __forceinline__ f16v mfma(u4 a, u4 b, f16v c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, hf2)); }
+    static __device__ __forceinline__ float exp(float x) { return __expf(x); }
+    static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
+    {
+        return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, scale, true))
+                    : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, scale, false));
+    }
+};
+struct F32 : Bf16 {
+    typedef float elem;
+    static constexpr Dtype dtype = Dtype::F32;
+    static constexpr int planes = 3;
+    static __device__ __forceinline__ float exp(float x) { return expf(x); }     // __expf is off by |x| 2^-24
+};
+
+// Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
+template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
+
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_> struct TileShape {
+    static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
+    static constexpr int threads = 64 * WM * WN * WK;
+    static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;       // 32x32 blocks of a wave
+};
+
+// How a tile of [ROWS][COLS] 16-bit elements lies in LDS.  KC: the summed axis is the contiguous one.
+template <bool KC, int BX, int BK> struct LdsTile {
+    static constexpr int ROWS = KC ? BX : BK, COLS = KC ? BK : BX, CH = COLS / 8;
+    static constexpr int bytes = ROWS * COLS * 2;
+    static __device__ __forceinline__ uint32_t swizzle(uint32_t row)
+    {
+        if (KC) return CH >= 16 ? row & 15 : CH == 8 ? row & 7 : (row >> 1) & 3;
+        return CH >= 16 ? (row & 3) << 2 : CH == 8 ? (row & 2) << 1 : 0;
+    }
+    // eight terms k0 + 8 (lane / 32) .. of the element x0 + lane % 32 of the other axis
+    static __device__ __forceinline__ u4 fragment(const uint8_t *lds, uint32_t x0, uint32_t k0, uint32_t lane)
+    {
+        if constexpr (KC) {
+            const uint32_t row = x0 + lane % 32, c = k0 / 8 + lane / 32;
+            return *reinterpret_cast<const u4 *>(lds + row * (COLS * 2) + ((c ^ swizzle(row)) * 16));
+        } else {
+            const uint32_t i = lane % 16, row = k0 + 8 * (lane / 32) + i / 4, c = (x0 + (lane & 16)) / 8 + (i % 4) / 2;
+            const uint8_t *at = lds + row * (COLS * 2) + ((c ^ swizzle(row)) * 16) + (i % 2) * 8;
+            union { s4 h[2]; u4 v; } out;
+            out.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at);
+            out.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(at + 4 * COLS * 2));
+            return out.v;
+        }
+    }
+};
+
+__device__ __forceinline__ u4 zero4() { return u4{0, 0, 0, 0}; }
+
+// One operand's part of a slice on its way to LDS through registers: any alignment, any type, bounds checked element by element
+// where a chunk of eight is not whole.
+enum { kDirect = 0, kRegs = 1, kCodes = 2 };
+__device__ __attribute__((aligned(16))) const unsigned int kZeroChunk[4] = {0, 0, 0, 0};
+
+template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader {
+    typedef LdsTile<KC, BX, BK> L;
+    typedef typename T::elem elem;
+    static constexpr int planes = HOW == kCodes ? 1 : T::planes;
+    static constexpr int N = L::ROWS * L::CH / THREADS;             // 16-byte chunks per thread
+    static_assert(N >= 1 && N * THREADS == L::ROWS * L::CH, "whole chunks per thread");
+    static constexpr int bytes = planes * L::bytes;
+    static constexpr int RAW = HOW == kDirect ? 1 : (sizeof(elem) == 4 && HOW == kRegs ? 2 : 1);
+
+    const elem *src;                  // element (0, 0) of the operand's matrix of this group
+    uint64_t ld;
+    const uint8_t *codes, *scales;
+    uint64_t ld_codes, ld_scales;
+    uint32_t x0, x_end;               // the other axis: first element of the tile, end
+    uint32_t k_end;                   // end of the summed axis
+    u4 raw[HOW == kDirect ? 1 : N][RAW];
+    float sc[HOW == kCodes ? N : 1];
+    uint32_t off[HOW == kDirect ? N : 1];
+
+    __device__ __forceinline__ static uint32_t chunk(int i) { return i * THREADS + threadIdx.x; }
+
+    __device__ __forceinline__ void start()
+    {
+        if constexpr (HOW == kDirect) {
+            // rows (or chunks of columns) past the end repeat the last one: their products are not stored
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
+                if (KC) { const uint32_t last = x_end - 1 - x0; row = row < last ? row : last; }
+                else    { const uint32_t last = (x_end - 1 - x0) / 8; c = c < last ? c : last; }
+                off[i] = (row * static_cast<uint32_t>(ld) + c * 8) * 2;
+            }
+        }
+    }
+
+    // request the slice that begins at term k0
+    __device__ __forceinline__ void request(uint8_t *lds, uint32_t k0)
+    {
+        if constexpr (HOW == kDirect) {
+            const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
+            const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+            const bool whole = k0 + BK <= k_end;
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const char *from = base + off[i];
+                if (!whole) {
+                    const uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
+                    if (k0 + (KC ? c * 8 : row) >= k_end) from = reinterpret_cast<const char *>(kZeroChunk);
+                }
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+            }
+        } else {
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
+                const uint32_t r = (KC ? x0 : k0) + row, r_end = KC ? x_end : k_end, q = (KC ? k0 : x0) + c * 8, q_end = KC ? k_end : x_end;
+                #pragma unroll
+                for (int j = 0; j < RAW; ++j) raw[i][j] = zero4();
+                if constexpr (HOW == kCodes) sc[i] = 1.0f;
+                if (r < r_end && q < q_end) {
+                    if constexpr (HOW == kCodes) {
+                        const uint8_t *at = codes + r * ld_codes + q;
+                        sc[i] = __uint_as_float(static_cast<unsigned>(scales[r * ld_scales + q / 32]) << 23);
+                        if (q + 8 <= q_end) {
+                            const u2 v = *reinterpret_cast<const u2_any *>(at);
+                            raw[i][0] = u4{v.x, v.y, 0, 0};
+                        } else {
+                            u4 v = zero4();
+                            #pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (q + e < q_end) v[e / 4] |= static_cast<unsigned>(at[e]) << (8 * (e % 4));
+                            raw[i][0] = v;
+                        }
+                    } else {
+                        const elem *at = src + r * ld + q;
+                        if (q + 8 <= q_end) {
+                            #pragma unroll
+                            for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(at)[j];
+                        } else {
+                            #pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (q + e < q_end) {
+                                    if constexpr (sizeof(elem) == 4) raw[i][e / 4][e % 4] = __float_as_uint(at[e]);
+                                    else                             raw[i][0][e / 2] |= static_cast<unsigned>(at[e]) << (16 * (e % 2));
+                                }
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // put the requested slice into LDS (behind the products of the slice before)
+    __device__ __forceinline__ void deliver(uint8_t *lds)
+    {
+        if constexpr (HOW == kDirect) return;
+        #pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint8_t *at = lds + chunk(i) * 16;
+            if constexpr (HOW == kCodes) {
+                *reinterpret_cast<u4 *>(at) = u4{T::codes(raw[i][0].x, sc[i], false), T::codes(raw[i][0].x, sc[i], true),
+                                                 T::codes(raw[i][0].y, sc[i], false), T::codes(raw[i][0].y, sc[i], true)};
+            } else if constexpr (T::planes == 1) {
+                *reinterpret_cast<u4 *>(at) = raw[i][0];
+            } else {
+                u4 p[3];
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float a = __uint_as_float(raw[i][j / 2][2 * j % 4]) * kPlaneScale, b = __uint_as_float(raw[i][j / 2][2 * j % 4 + 1]) * kPlaneScale;
+                    #pragma unroll
+                    for (int pl = 0; pl < 3; ++pl) {
+                        const unsigned pair = T::pack(a, b);
+                        p[pl][j] = pair;
+                        a -= __uint_as_float(pair << 16);
+                        b -= __uint_as_float(pair & 0xffff0000u);
+                    }
+                }
+                #pragma unroll
+                for (int pl = 0; pl < 3; ++pl) *reinterpret_cast<u4 *>(at + pl * L::bytes) = p[pl];
+            }
+        }
+    }
+
+    // element (x of the other axis, term k) in fp32, zero outside (the exact path for sums that are not finite)
+    __device__ __forceinline__ float element(uint32_t x, uint32_t k) const
+    {
+        if (x >= x_end || k >= k_end) return 0.0f;
+        const uint64_t r = KC ? x : k, q = KC ? k : x;
+        if constexpr (HOW == kCodes)
+            return __uint_as_float(T::codes(codes[r * ld_codes + q], __uint_as_float(static_cast<unsigned>(scales[r * ld_scales + q / 32]) << 23), false) << 16);
+        else
+            return static_cast<float>(src[r * ld + q]);
+    }
+};
+
+// Where a block's tile lies.
+struct Place { uint32_t group; uint32_t n0; uint64_t row0; uint32_t rows; uint32_t m0; uint32_t terms; };
+
+__device__ __forceinline__ uint64_t bound_at(const ProductParams &p, uint32_t i)
+{
+    const int64_t v = p.offsets[i];
+    return v < 0 ? 0 : static_cast<uint64_t>(v) > p.rows ? p.rows : static_cast<uint64_t>(v);
+}
+__device__ __forceinline__ uint64_t length_at(const ProductParams &p, uint32_t g)
+{
+    const uint64_t a = bound_at(p, g), next = bound_at(p, g + 1);
+    uint64_t b = next;
+    if (p.ends) { const int64_t e = p.ends[g]; b = e < 0 ? 0 : static_cast<uint64_t>(e) < next ? static_cast<uint64_t>(e) : next; }
+    return b > a ? b - a : 0;
+}
+
+// Blocks go round the eight dies in turn: each die gets a run of consecutive tiles, which share operands in its cache.
+// In a band of row tiles the row tiles take turns in front of one column tile.
+__device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t row_tiles, uint32_t col_tiles, uint32_t &row_tile, uint32_t &col_tile)
+{
+    const uint32_t total = row_tiles * col_tiles;
+    if (block >= total) return false;
+    const uint32_t x = block % kXcdCount, q = total / kXcdCount, r = total % kXcdCount;
+    const uint32_t idx = x * q + (x < r ? x : r) + block / kXcdCount;
+    const uint32_t band = idx / (kBandTiles * col_tiles), in = idx - band * kBandTiles * col_tiles;
+    const uint32_t left = row_tiles - band * kBandTiles, high = left < kBandTiles ? left : kBandTiles;
+    row_tile = band * kBandTiles + in % high;
+    col_tile = in / high;
+    return true;
+}
+
+// The row tiles of all groups in order; every wave scans the groups' lengths for itself, 64 at a time.
+template <int BM> __device__ __forceinline__ bool place_rows(const ProductParams &p, uint32_t block, uint32_t col_tiles, Place &at, int BN)
+{
+    const uint32_t lane = threadIdx.x % 64;
+    uint32_t total = 0, incl = 0, tiles = 0;
+    uint64_t first = 0, len = 0;
+    auto scan = [&](uint32_t g0) {
+        const uint32_t g = g0 + lane;
+        first = 0; len = 0;
+        if (g < p.groups) { first = bound_at(p, g); len = length_at(p, g); }
+        tiles = static_cast<uint32_t>((len + BM - 1) / BM);
+        incl = tiles;
+        #pragma unroll
+        for (int d = 1; d < 64; d <<= 1) { const uint32_t v = __shfl_up(incl, d, 64); if (lane >= static_cast<uint32_t>(d)) incl += v; }
+        return __shfl(incl, 63, 64);
+    };
+    for (uint32_t g0 = 0; g0 < p.groups; g0 += 64) total += scan(g0);
+    uint32_t row_tile, col_tile;
+    if (!tile_of_block(block, __builtin_amdgcn_readfirstlane(total), col_tiles, row_tile, col_tile)) return false;
+    uint32_t g0 = 0;
+    if (p.groups > 64)
+        for (;; g0 += 64) {
+            if (g0 >= p.groups) return false;                  // offsets that do not ascend
+            const uint32_t n = scan(g0);
+            if (row_tile < n) break;
+            row_tile -= n;
+        }
+    const unsigned long long beyond = __ballot(incl > row_tile);
+    if (!beyond) return false;
+    const uint32_t who = __ffsll(beyond) - 1;
+    const uint32_t tile = row_tile - (__shfl(incl, who, 64) - __shfl(tiles, who, 64));
+    at.group = __builtin_amdgcn_readfirstlane(g0 + who);
+    const uint64_t f = __shfl(first, who, 64), l = __shfl(len, who, 64);
+    const uint64_t r0 = f + static_cast<uint64_t>(tile) * BM, left = f + l - r0;
+    at.row0 = (static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(r0 >> 32))) << 32) | __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(r0));
+    at.rows = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(left < BM ? left : BM));
+    at.n0 = col_tile * BN;
+    at.m0 = 0;
+    at.terms = p.k;
+    return true;
+}
+
+template <int BM> __device__ __forceinline__ bool place_weights(const ProductParams &p, uint32_t block, uint32_t col_tiles, Place &at, int BN)
+{
+    const uint32_t per = (p.m + BM - 1) / BM;
+    uint32_t row_tile, col_tile;
+    if (!tile_of_block(block, per * p.groups, col_tiles, row_tile, col_tile)) return false;
+    at.group = row_tile / per;
+    at.m0 = row_tile % per * BM;
+    at.rows = p.m - at.m0 < BM ? p.m - at.m0 : BM;
+    at.n0 = col_tile * BN;
+    at.row0 = bound_at(p, at.group);
+    at.terms = static_cast<uint32_t>(length_at(p, at.group));
+    return true;
+}
+
+// ---- what happens to four consecutive columns of a row of C ----------------------------------------------
+
+template <class T> __device__ __forceinline__ void store_values(void *out, uint64_t at, f4 v, uint32_t count, bool f32)
+{
+    if (f32 || sizeof(typename T::elem) == 4) {
+        float *o = static_cast<float *>(out) + at;
+        if (count == 4 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) { *reinterpret_cast<f4 *>(o) = v; return; }
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) if (j < count) o[j] = v[j];
+    } else {
+        uint16_t *o = static_cast<uint16_t *>(out) + at;
+        const unsigned lo = T::pack(v.x, v.y), hi = T::pack(v.z, v.w);
+        if (count == 4 && (reinterpret_cast<uintptr_t>(o) & 7) == 0) { *reinterpret_cast<u2 *>(o) = u2{lo, hi}; return; }
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) if (j < count) o[j] = static_cast<uint16_t>((j < 2 ? lo : hi) >> (16 * (j % 2)));
+    }
+}
+
+template <class T> __device__ __forceinline__ bool above_zero(const ProductParams &p, uint64_t row, uint32_t col)
+{
+    if (p.mask_codes) { const uint8_t c = p.mask_codes[row * p.ld_mask + col]; return c != 0 && c < 0x7f; }
+    if constexpr (sizeof(typename T::elem) == 4) return static_cast<const float *>(p.mask)[row * p.ld_mask + col] > 0.0f;
+    else {
+        // sign clear, not zero, not NaN
+        const uint16_t b = static_cast<const uint16_t *>(p.mask)[row * p.ld_mask + col];
+        return b != 0 && b <= (std::is_same<T, F16>::value ? 0x7c00 : 0x7f80);
+    }
+}
+
+// row: of all groups (Weights: group * m + row of C_g); local: row of C_g
+template <class T, bool WEIGHTS>
+__device__ __forceinline__ void finish_quad(const ProductParams &p, uint32_t group, uint64_t row, uint32_t local, uint32_t col, f4 v, float factor)
+{
+    const uint32_t count = p.n - col < 4 ? p.n - col : 4;
+    if (!WEIGHTS && p.out_row && p.out_row[row] == kNoRow) return;
+    if (p.sum) {
+        float *s = p.sum + row * p.ld_sum + col;               // ld_sum is a multiple of 4, the columns behind n are its own
+        if (p.sum_read) v += *reinterpret_cast<const f4 *>(s);
+        if (p.sum_write) { *reinterpret_cast<f4 *>(s) = v; return; }
+    }
+    if (!WEIGHTS && p.row_scale) factor = p.row_scale[row];
+    v *= factor;
+    if (p.relu) {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];
+    }
+    if (p.mask || p.mask_codes) {
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) if (j < count && !above_zero<T>(p, row, col + j)) v[j] = 0.0f;
+    }
+    const uint64_t at = WEIGHTS ? group * p.out_group + static_cast<uint64_t>(local) * p.ldc + col
+                                : (p.out_row ? static_cast<uint64_t>(p.out_row[row]) : row) * p.ldc + col;
+    store_values<T>(p.out, at, v, count, p.out_f32 != 0);
+}
+
+__device__ __forceinline__ float group_factor(const ProductParams &p, uint32_t group)
+{
+    if (!p.mean) return p.scale;
+    const uint64_t len = length_at(p, group);
+    return len ? p.scale / static_cast<float>(len) : 0.0f;
+}
+
+// ---- the kernel ---------------------------------------------------------------------------------------------
+
+template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product {
+    static constexpr bool WEIGHTS = LAYOUT == Layout::Weights;
+    static constexpr bool A_KC = !WEIGHTS, B_KC = LAYOUT == Layout::Rows_NK;
+    typedef Loader<T, HOW_A, A_KC, S::BM, S::BK, S::threads> LoadA;
+    typedef Loader<T, HOW_B, B_KC, S::BN, S::BK, S::threads> LoadB;
+    static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
+    static constexpr bool DIRECT = HOW_A == kDirect || HOW_B == kDirect;
+    static constexpr int stage = LoadA::bytes + LoadB::bytes;
+    static constexpr int join_bytes = S::WK > 1 ? S::threads * S::MB * S::NB * 16 * 4 : 0;
+    static constexpr int lds_bytes = 2 * stage > join_bytes ? 2 * stage : join_bytes;
+
+    // multiply the slice in `cur` while the next one is requested into `next`
+    static __device__ __forceinline__ void slice(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, LoadA &la, LoadB &lb, bool more,
+                                                 uint32_t k_next, f16v (&acc)[SUMS][S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane)
+    {
+        if (more) { la.request(next, k_next); lb.request(next + LoadA::bytes, k_next); }
+        #pragma unroll
+        for (int kk = 0; kk < S::BK / 16 / S::WK; ++kk) {
+            const uint32_t k0 = (kk * S::WK + wk) * 16;
+            u4 fa[PA][S::MB], fb[PB][S::NB];
+            #pragma unroll
+            for (int pl = 0; pl < PA; ++pl)
+                #pragma unroll
+                for (int i = 0; i < S::MB; ++i) fa[pl][i] = LoadA::L::fragment(cur + pl * LoadA::L::bytes, (wm * S::MB + i) * 32, k0, lane);
+            #pragma unroll
+            for (int pl = 0; pl < PB; ++pl)
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j) fb[pl][j] = LoadB::L::fragment(cur + LoadA::bytes + pl * LoadB::L::bytes, (wn * S::NB + j) * 32, k0, lane);
+            #pragma unroll
+            for (int i = 0; i < S::MB; ++i)
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j) {
+                    acc[0][i][j] = T::mfma(fb[0][j], fa[0][i], acc[0][i][j]);
+                    if constexpr (PB == 3) {
+                        f16v s = acc[1][i][j];
+                        if constexpr (PA == 3) {
+                            s = T::mfma(fb[0][j], fa[2][i], s);
+                            s = T::mfma(fb[2][j], fa[0][i], s);
+                            s = T::mfma(fb[1][j], fa[1][i], s);
+                            s = T::mfma(fb[0][j], fa[1][i], s);
+                        } else {
+                            s = T::mfma(fb[2][j], fa[0][i], s);
+                        }
+                        acc[1][i][j] = T::mfma(fb[1][j], fa[0][i], s);
+                    }
+                }
+        }
+    }
+};
+
+// The slice that goes to LDS by itself has arrived (its loads count as vector memory, which a barrier alone need not wait for).
+template <bool DIRECT> __device__ __forceinline__ void slice_barrier()
+{
+    if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// quads of a wave: all of its own, or (waves that share the terms) a share of the common tile's
+template <class S> constexpr int kQuads = S::MB * S::NB * 4 / S::WK;
+
+template <class T, Layout LAYOUT, class S, Finish FINISH, int HOW_A, int HOW_B>
+__global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams p)
+{
+    typedef Product<T, LAYOUT, S, HOW_A, HOW_B> P;
+    constexpr bool WEIGHTS = P::WEIGHTS;
+    constexpr int stats_bytes = FINISH == Finish::Stats ? S::WN * S::WK * S::BM * 8 : 0;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::lds_bytes > stats_bytes ? P::lds_bytes : stats_bytes];
+    Place at;
+    const uint32_t col_tiles = (p.n + S::BN - 1) / S::BN;
+    if (!(WEIGHTS ? place_weights<S::BM>(p, blockIdx.x, col_tiles, at, S::BN) : place_rows<S::BM>(p, blockIdx.x, col_tiles, at, S::BN))) return;
+
+    typedef typename T::elem elem;
+    typename P::LoadA la;
+    typename P::LoadB lb;
+    la.ld = p.lda; la.ld_codes = p.ld_codes; la.ld_scales = p.ld_scales;
+    la.src = static_cast<const elem *>(p.a) + at.row0 * p.lda;
+    la.codes = p.a_codes + at.row0 * p.ld_codes;
+    la.scales = p.a_scales + at.row0 * p.ld_scales;
+    la.x0 = at.m0; la.x_end = at.m0 + at.rows; la.k_end = at.terms;
+    lb.ld = p.ldb;
+    lb.src = static_cast<const elem *>(p.b) + (WEIGHTS ? at.row0 * p.ldb : at.group * p.b_group);
+    lb.x0 = at.n0; lb.x_end = p.n; lb.k_end = at.terms;
+    la.start();
+    lb.start();
+
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t wk = wave % S::WK, wn = wave / S::WK % S::WN, wm = wave / S::WK / S::WN;
+    f16v acc[P::SUMS][S::MB][S::NB];
+    #pragma unroll
+    for (int s = 0; s < P::SUMS; ++s)
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) acc[s][i][j] = f16v{0};
+
+    // this split's slices
+    uint32_t slices = (at.terms + S::BK - 1) / S::BK, slice0 = 0;
+    if (p.splits > 1) {
+        const uint32_t per = (slices + p.splits - 1) / p.splits;
+        slice0 = per * blockIdx.y < slices ? per * blockIdx.y : slices;
+        slices = slices - slice0 < per ? slices - slice0 : per;
+    }
+    if (slices) {
+        la.request(lds, slice0 * S::BK); lb.request(lds + P::LoadA::bytes, slice0 * S::BK);
+        la.deliver(lds); lb.deliver(lds + P::LoadA::bytes);
+    }
+    slice_barrier<P::DIRECT>();
+    for (uint32_t t = 0; t < slices; ++t) {
+        uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
+        const bool more = t + 1 < slices;
+        P::slice(cur, next, la, lb, more, (slice0 + t + 1) * S::BK, acc, wm, wn, wk, lane);
+        if (more) { la.deliver(next); lb.deliver(next + P::LoadA::bytes); }
+        slice_barrier<P::DIRECT>();
+    }
+
+    float unscale = 1.0f;
+    if constexpr (P::PB == 3) {
+        unscale = P::PA == 3 ? kPlaneUnscale : 1.0f / kPlaneScale;
+        bool fine = true;
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) {
+                acc[0][i][j] += acc[P::SUMS - 1][i][j];
+                #pragma unroll
+                for (int r = 0; r < 16; ++r) fine = fine && __builtin_isfinite(acc[0][i][j][r]);
+            }
+        if (__syncthreads_or(!fine)) {
+            // the same sums with fp32 products: what is not finite then is so by fp32 arithmetic
+            unscale = 1.0f;
+            #pragma unroll
+            for (int i = 0; i < S::MB; ++i)
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j) acc[0][i][j] = f16v{0};
+            const uint32_t k_end = (slice0 + slices) * S::BK < at.terms ? (slice0 + slices) * S::BK : at.terms;
+            #pragma unroll 1
+            for (uint32_t k0 = slice0 * S::BK + 2 * wk; k0 < k_end; k0 += 2 * S::WK) {
+                const uint32_t k = k0 + lane / 32;
+                float a[S::MB], b[S::NB];
+                #pragma unroll
+                for (int i = 0; i < S::MB; ++i) a[i] = k < k_end ? la.element(at.m0 + (wm * S::MB + i) * 32 + lane % 32, k) : 0.0f;
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j) b[j] = k < k_end ? lb.element(at.n0 + (wn * S::NB + j) * 32 + lane % 32, k) : 0.0f;
+                #pragma unroll
+                for (int i = 0; i < S::MB; ++i)
+                    #pragma unroll
+                    for (int j = 0; j < S::NB; ++j) acc[0][i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j], a[i], acc[0][i][j], 0, 0, 0);
+            }
+        }
+    }
+
+    // quads: row block i, column 4 q' of the wave's columns
+    constexpr int QN = kQuads<S>;
+    f4 quad[QN];
+    if constexpr (S::WK == 1) {
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j)
+                #pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    quad[(i * S::NB + j) * 4 + g] = f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]} * unscale;
+    } else {
+        // the waves' sums over their terms meet in LDS, in the order of the waves
+        static_assert(S::WM == 1 && S::WN == 1, "waves share the terms of one tile");
+        f4 *share = reinterpret_cast<f4 *>(lds);
+        constexpr int ALL = S::MB * S::NB * 4;
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j)
+                #pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    share[(wk * ALL + (i * S::NB + j) * 4 + g) * 64 + lane] = f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]};
+        __syncthreads();
+        #pragma unroll
+        for (int q = 0; q < QN; ++q) {
+            f4 s = share[(wk * QN + q) * 64 + lane];
+            #pragma unroll
+            for (int w = 1; w < S::WK; ++w) s += share[(w * ALL + wk * QN + q) * 64 + lane];
+            quad[q] = s * unscale;
+        }
+        if (FINISH == Finish::Stats) __syncthreads();
+    }
+    // quad q: row and column
+    const uint32_t q0 = S::WK == 1 ? 0 : wk * QN;
+    auto row_of = [&](int q) { return (wm * S::MB + (q0 + q) / (4 * S::NB)) * 32 + lane % 32; };
+    auto col_of = [&](int q) { return at.n0 + (wn * S::NB + (q0 + q) / 4 % S::NB) * 32 + (q0 + q) % 4 * 8 + 4 * (lane / 32); };
+
+    if constexpr (FINISH == Finish::Store) {
+        if (p.splits > 1) {
+            const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+            #pragma unroll
+            for (int q = 0; q < QN; ++q) {
+                const uint32_t r = row_of(q), c = col_of(q);
+                if (r >= at.rows || c >= p.n) continue;
+                const uint64_t row = WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r;
+                *reinterpret_cast<f4 *>(p.part + (blockIdx.y * all + row) * p.ld_part + c) = quad[q];
+            }
+            return;
+        }
+        const float factor = group_factor(p, at.group);
+        #pragma unroll
+        for (int q = 0; q < QN; ++q) {
+            const uint32_t r = row_of(q), c = col_of(q);
+            if (r >= at.rows || c >= p.n) continue;
+            finish_quad<T, WEIGHTS>(p, at.group, WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r, at.m0 + r, c, quad[q], factor);
+        }
+    } else if constexpr (FINISH == Finish::Stats) {
+        // per row block: maximum and sum over the wave's columns (a lane and the one 32 further on hold a row), then over the waves
+        constexpr int PER = S::WK == 1 ? 4 * S::NB : QN, BLOCKS = QN / PER;
+        float2 *share = reinterpret_cast<float2 *>(lds);       // the operand buffers are free: the loop ended with a barrier
+        #pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const uint32_t r = row_of(i * PER);
+            const int32_t target = r < at.rows ? p.target[at.row0 + r] : -1;
+            float top = -INFINITY;
+            #pragma unroll
+            for (int q = i * PER; q < (i + 1) * PER; ++q)
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t c = col_of(q) + j;
+                    if (c >= p.n) quad[q][j] = -INFINITY;
+                    else if (static_cast<int32_t>(p.v0 + c) == target) p.target_logit[at.row0 + r] = quad[q][j];
+                    top = fmaxf(top, quad[q][j]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float base = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f;
+            #pragma unroll
+            for (int q = i * PER; q < (i + 1) * PER; ++q)
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) sum += T::exp(quad[q][j] - base);
+            sum += __shfl_xor(sum, 32, 64);
+            if (lane < 32) share[(wn * S::WK + wk) * S::BM + r] = make_float2(top, sum);
+        }
+        __syncthreads();
+        for (uint32_t r = threadIdx.x; r < at.rows; r += S::threads) {
+            float top = -INFINITY, sum = 0.0f;
+            #pragma unroll
+            for (int w = 0; w < S::WN * S::WK; ++w) top = fmaxf(top, share[w * S::BM + r].x);
+            const float base = top == -INFINITY ? 0.0f : top;
+            #pragma unroll
+            for (int w = 0; w < S::WN * S::WK; ++w) {
+                const float2 s = share[w * S::BM + r];
+                // a part whose columns all lie past the end has nothing to add; a NaN stays one
+                if (s.x != -INFINITY || s.y != s.y) sum += s.y * T::exp(s.x - base);
+            }
+            p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
+        }
+    } else {
+        #pragma unroll
+        for (int q = 0; q < QN; ++q) {
+            const uint32_t r = row_of(q), c = col_of(q);
+            if (r >= at.rows || c >= p.ldc_zero) continue;
+            const float norm = p.norm[at.row0 + r];
+            const int32_t target = p.target[at.row0 + r];
+            f4 v;
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = (T::exp(quad[q][j] - norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
+                if (c + j >= p.n) v[j] = 0.0f;
+            }
+            store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
+        }
+    }
+}
+
+// The splits' sums, in order, and what a block without splits does with them.
+template <class T, bool WEIGHTS> __global__ __launch_bounds__(256) void join_kernel(const ProductParams p)
+{
+    const uint32_t quads = (p.n + 3) / 4;
+    const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+    const uint64_t first = WEIGHTS ? 0 : bound_at(p, 0), end = WEIGHTS ? all : bound_at(p, p.groups);
+    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const uint64_t row = first + i / quads;
+    if (row >= end) return;
+    const uint32_t col = static_cast<uint32_t>(i % quads) * 4;
+    f4 v = *reinterpret_cast<const f4 *>(p.part + row * p.ld_part + col);
+    for (uint32_t s = 1; s < p.splits; ++s) v += *reinterpret_cast<const f4 *>(p.part + (s * all + row) * p.ld_part + col);
+    const uint32_t group = WEIGHTS ? static_cast<uint32_t>(row / p.m) : 0;
+    finish_quad<T, WEIGHTS>(p, group, row, WEIGHTS ? static_cast<uint32_t>(row % p.m) : 0, col, v, WEIGHTS ? group_factor(p, group) : p.scale);
+}
+
+template <class T, Layout LAYOUT, class S, Finish FINISH, int HOW_A, int HOW_B>
+hipError_t launch_one(hipStream_t stream, const ProductParams &p)
+{
+    const uint64_t col_tiles = (p.n + S::BN - 1) / S::BN;
+    const uint64_t row_tiles = LAYOUT == Layout::Weights ? static_cast<uint64_t>(p.groups) * ((p.m + S::BM - 1) / S::BM) : p.rows / S::BM + p.groups;
+    const uint64_t blocks = row_tiles * col_tiles;
+    if (blocks * S::threads >= (1ull << 32)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((product_kernel<T, LAYOUT, S, FINISH, HOW_A, HOW_B>), dim3(static_cast<uint32_t>(blocks), p.splits), dim3(S::threads), 0, stream, p);
+    if (p.splits > 1) {
+        const uint64_t all = LAYOUT == Layout::Weights ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+        const uint64_t join = (all * ((p.n + 3) / 4) + 255) / 256;
+        if (join * 256 >= (1ull << 32)) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL((join_kernel<T, LAYOUT == Layout::Weights>), dim3(static_cast<uint32_t>(join)), dim3(256), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
+typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
+typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
+typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
+typedef TileShape<32, 64, 64, 1, 1, 4> Small32;
+
+template <class T, Layout LAYOUT, Finish FINISH>
+hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
+{
+    constexpr bool WEIGHTS = LAYOUT == Layout::Weights;
+    if constexpr (T::planes == 3) {
+        if constexpr (WEIGHTS)
+            if (!p.a) return tile == Tile::Small ? launch_one<T, LAYOUT, Small32, FINISH, kCodes, kRegs>(stream, p)
+                                                 : launch_one<T, LAYOUT, Medium32, FINISH, kCodes, kRegs>(stream, p);
+        return tile == Tile::Small ? launch_one<T, LAYOUT, Small32, FINISH, kRegs, kRegs>(stream, p)
+                                   : launch_one<T, LAYOUT, Medium32, FINISH, kRegs, kRegs>(stream, p);
+    } else {
+        const bool b_direct = direct_b(LAYOUT, p);
+        if constexpr (WEIGHTS)
+            if (!p.a) {
+                if (b_direct) return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kDirect>(stream, p)
+                                                         : launch_one<T, LAYOUT, Medium16, FINISH, kCodes, kDirect>(stream, p);
+                return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kRegs>(stream, p)
+                                           : launch_one<T, LAYOUT, Medium16, FINISH, kCodes, kRegs>(stream, p);
+            }
+        if (b_direct && direct_a(LAYOUT, p)) {
+            if (tile == Tile::Large) return launch_one<T, LAYOUT, Large16, FINISH, kDirect, kDirect>(stream, p);
+            return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kDirect, kDirect>(stream, p)
+                                       : launch_one<T, LAYOUT, Medium16, FINISH, kDirect, kDirect>(stream, p);
+        }
+        return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kRegs, kRegs>(stream, p)
+                                   : launch_one<T, LAYOUT, Medium16, FINISH, kRegs, kRegs>(stream, p);
+    }
+}
+
+template <class T> hipError_t launch_store(hipStream_t stream, Layout layout, Tile tile, const ProductParams &p)
+{
+    if (layout == Layout::Rows_KN) return launch_layout<T, Layout::Rows_KN, Finish::Store>(stream, tile, p);
+    if (layout == Layout::Rows_NK) return launch_layout<T, Layout::Rows_NK, Finish::Store>(stream, tile, p);
+    return launch_layout<T, Layout::Weights, Finish::Store>(stream, tile, p);
+}
+
+template <class T> hipError_t launch_logits(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p)
+{
+    return finish == Finish::Stats ? launch_layout<T, Layout::Rows_NK, Finish::Stats>(stream, tile, p)
+                                   : launch_layout<T, Layout::Rows_NK, Finish::Slope>(stream, tile, p);
+}
+
+}  // namespace
+}  // namespace cocod
