@@ -1,7 +1,44 @@
 // Grouped products of ragged batches: argument checks, choice of the tile, and the three directions of a layer.
 #include "operator_call.hpp"
+#include "product_finish.hpp"
 
 namespace cocod {
+namespace {
+
+// The splits' sums, in order, and what a block without splits does with them.
+template <class T, bool WEIGHTS> __global__ __launch_bounds__(256) void join_kernel(const ProductParams p)
+{
+    const uint32_t quads = (p.n + 3) / 4;
+    const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+    const uint64_t first = WEIGHTS ? 0 : bound_at(p, 0), end = WEIGHTS ? all : bound_at(p, p.groups);
+    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const uint64_t row = first + i / quads;
+    if (row >= end) return;
+    const uint32_t col = static_cast<uint32_t>(i % quads) * 4;
+    f4 v = *reinterpret_cast<const f4 *>(p.part + row * p.ld_part + col);
+    for (uint32_t s = 1; s < p.splits; ++s) v += *reinterpret_cast<const f4 *>(p.part + (s * all + row) * p.ld_part + col);
+    const uint32_t group = WEIGHTS ? static_cast<uint32_t>(row / p.m) : 0;
+    finish_quad<T, WEIGHTS>(p, group, row, WEIGHTS ? static_cast<uint32_t>(row % p.m) : 0, col, v, WEIGHTS ? group_factor(p, group) : p.scale);
+}
+
+template <class T> hipError_t launch_join_of(hipStream_t stream, bool weights, uint32_t blocks, const ProductParams &p)
+{
+    if (weights) hipLaunchKernelGGL((join_kernel<T, true>), dim3(blocks), dim3(256), 0, stream, p);
+    else         hipLaunchKernelGGL((join_kernel<T, false>), dim3(blocks), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const ProductParams &p)
+{
+    const bool weights = layout == Layout::Weights;
+    const uint64_t blocks = ((weights ? static_cast<uint64_t>(p.groups) * p.m : p.rows) * ((p.n + 3) / 4) + 255) / 256;
+    if (blocks * 256 >= (1ull << 32)) return hipErrorInvalidConfiguration;
+    const uint32_t n = static_cast<uint32_t>(blocks);
+    return type == Dtype::BF16 ? launch_join_of<Bf16>(stream, weights, n, p)
+           : type == Dtype::F16 ? launch_join_of<F16>(stream, weights, n, p) : launch_join_of<F32>(stream, weights, n, p);
+}
 
 ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k)
 {

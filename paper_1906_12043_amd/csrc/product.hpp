@@ -106,10 +106,13 @@ ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t grou
 // Bytes of ProductParams::part (0 with one split), whose rows hold part_pitch(n) floats.
 inline uint64_t part_pitch(uint32_t n) { return (static_cast<uint64_t>(n) + 3) / 4 * 4; }
 uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n);
+hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const ProductParams &p);
+
 inline hipError_t launch_store(hipStream_t stream, Dtype type, Layout layout, Tile tile, const ProductParams &p)
 {
-    return type == Dtype::BF16 ? launch_store_bf16(stream, layout, tile, p)
-           : type == Dtype::F16 ? launch_store_f16(stream, layout, tile, p) : launch_store_f32(stream, layout, tile, p);
+    const hipError_t e = type == Dtype::BF16 ? launch_store_bf16(stream, layout, tile, p)
+                         : type == Dtype::F16 ? launch_store_f16(stream, layout, tile, p) : launch_store_f32(stream, layout, tile, p);
+    return e != hipSuccess || p.splits <= 1 ? e : launch_join(stream, type, layout, p);
 }
 inline hipError_t launch_logits(hipStream_t stream, Dtype type, Finish finish, Tile tile, const ProductParams &p)
 {
