@@ -19,7 +19,8 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 // Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_> struct TileShape {
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2> struct TileShape {
+    static constexpr int STAGES = STAGES_;
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
     static constexpr int threads = 64 * WM * WN * WK;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;       // 32x32 blocks of a wave
@@ -31,7 +32,7 @@ template <bool KC, int BX, int BK> struct LdsTile {
     static constexpr int bytes = ROWS * COLS * 2;
     static __device__ __forceinline__ uint32_t swizzle(uint32_t row)
     {
-        if (KC) return CH >= 16 ? row & 15 : CH == 8 ? row & 7 : (row >> 1) & 3;
+        if (KC) return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3;      // sixteen rows of one chunk: sixteen places
         return CH >= 16 ? (row & 3) << 2 : CH == 8 ? (row & 2) << 1 : 0;
     }
     // eight terms k0 + 8 (lane / 32) .. of the element x0 + lane % 32 of the other axis
@@ -149,6 +150,16 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                 }
             }
         }
+    }
+
+    // chunks FIRST .. LAST - 1 of a slice that lies within the sum: nothing to check
+    template <int FIRST, int LAST> __device__ __forceinline__ void request_whole(uint8_t *lds, uint32_t k0, uint32_t wave)
+    {
+        const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
+        #pragma unroll
+        for (int i = FIRST; i < LAST; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
+                                             (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
     }
 
     // put the requested slice into LDS (behind the products of the slice before)
@@ -278,8 +289,62 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
     static constexpr bool DIRECT = HOW_A == kDirect || HOW_B == kDirect;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
-    static constexpr int join_bytes = S::WK > 1 ? S::threads * S::MB * S::NB * 16 * 4 : 0;
-    static constexpr int lds_bytes = 2 * stage > join_bytes ? 2 * stage : join_bytes;
+    static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 2 * (S::NB * 32 + 4) * 4;
+    static constexpr bool DEEP = HOW_A == kDirect && HOW_B == kDirect && S::STAGES > 2;
+    static constexpr int stages = DEEP ? S::STAGES : 2;
+    static constexpr int lds_bytes = stages * stage > join_bytes ? stages * stage : join_bytes;
+
+    // The deep pipeline of operands that go to LDS by themselves.  Iteration t multiplies slice t, whose first fragments are in
+    // registers already, reads every next fragment while the matrix cores work on the one before, the first of slice t + 1 among them,
+    // and requests slice t + stages - 1 into the buffer that slice t - 1 has left.
+    static constexpr int STEPS = S::BK / 16 / S::WK;
+    struct Fragments { u4 a[S::MB], b[S::NB]; };
+    static __device__ __forceinline__ void read(Fragments &f, const uint8_t *lds, uint32_t k0, uint32_t wm, uint32_t wn, uint32_t lane)
+    {
+        #pragma unroll
+        for (int j = 0; j < S::NB; ++j) f.b[j] = LoadB::L::fragment(lds + LoadA::bytes, (wn * S::NB + j) * 32, k0, lane);
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i) f.a[i] = LoadA::L::fragment(lds, (wm * S::MB + i) * 32, k0, lane);
+    }
+    template <bool WHOLE>
+    static __device__ __forceinline__ void deep_slice(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
+                                                      bool more, uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
+                                                      uint32_t wave)
+    {
+        if (!WHOLE && more) { la.request(fill, k_fill); lb.request(fill + LoadA::bytes, k_fill); }
+        deep_steps<WHOLE, 0>(cur, next, fill, la, lb, k_fill, f, acc, wm, wn, wk, lane, wave);
+    }
+    // Step kk of a slice: its share of the requests and the reads of the next step's fragments, between its first products.
+    template <bool WHOLE, int kk>
+    static __device__ __forceinline__ void deep_steps(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
+                                                      uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
+                                                      uint32_t wave)
+    {
+        if constexpr (kk < STEPS) {
+            constexpr int A0 = kk * LoadA::N / STEPS, A1 = (kk + 1) * LoadA::N / STEPS, B0 = kk * LoadB::N / STEPS, B1 = (kk + 1) * LoadB::N / STEPS;
+            if constexpr (WHOLE) {
+                la.template request_whole<A0, A1>(fill, k_fill, wave);
+                lb.template request_whole<B0, B1>(fill + LoadA::bytes, k_fill, wave);
+            }
+            if (kk + 1 < STEPS) read(f[(kk + 1) % 2], cur, ((kk + 1) * S::WK + wk) * 16, wm, wn, lane);
+            else                read(f[(kk + 1) % 2], next, wk * 16, wm, wn, lane);
+            #pragma unroll
+            for (int i = 0; i < S::MB; ++i)
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j) acc[i][j] = T::mfma(f[kk % 2].b[j], f[kk % 2].a[i], acc[i][j]);
+            // the reads between the first products, so that the last of them has arrived when the next step begins; then the requests
+            constexpr int READS = S::MB * (A_KC ? 1 : 2) + S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB, PER = (READS + PRODUCTS - 1) / PRODUCTS;
+            constexpr int ASKED = WHOLE ? A1 - A0 + B1 - B0 : 0, LATE = (READS + PER - 1) / PER < PRODUCTS ? PRODUCTS - (READS + PER - 1) / PER : 1, ASK = (ASKED + LATE - 1) / LATE;
+            #pragma unroll
+            for (int r = 0; r < PRODUCTS; ++r) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (r * PER < READS) __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+                if constexpr (ASK > 0) if (r >= PRODUCTS - LATE) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            deep_steps<WHOLE, kk + 1>(cur, next, fill, la, lb, k_fill, f, acc, wm, wn, wk, lane, wave);
+        }
+    }
 
     // multiply the slice in `cur` while the next one is requested into `next`
     static __device__ __forceinline__ void slice(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, LoadA &la, LoadB &lb, bool more,
@@ -327,16 +392,133 @@ template <bool DIRECT> __device__ __forceinline__ void slice_barrier()
     __syncthreads();
 }
 
-// quads of a wave: all of its own, or (waves that share the terms) a share of the common tile's
-template <class S> constexpr int kQuads = S::MB * S::NB * 4 / S::WK;
+// All but the last LEFT requests of every wave have arrived in LDS, and every wave has its fragments of earlier slices.
+template <int LEFT> __device__ __forceinline__ void slices_arrived()
+{
+    static_assert(LEFT < 64, "the wait's counter");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Rows of a tile that lies within C, eight columns of a row per lane: what finish (below) does to four, with its decisions taken once.
+template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
+    char *to;                         // first row of the tile (column 0 of C)
+    uint64_t pitch;                   // bytes
+    bool f32, part, aligned;
+    float factor;
+
+    __device__ __forceinline__ RowFinish(const ProductParams &p, const Place &at, float factor_)
+    {
+        part = FINISH == Finish::Store && p.splits > 1;
+        f32 = part || p.out_f32 || sizeof(typename T::elem) == 4;
+        factor = factor_;
+        const uint64_t size = f32 ? 4 : 2;
+        const uint64_t local = WEIGHTS ? at.m0 : at.row0;
+        if (part) {
+            const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+            pitch = p.ld_part * 4;
+            to = reinterpret_cast<char *>(p.part + (blockIdx.y * all + (WEIGHTS ? static_cast<uint64_t>(at.group) * p.m : 0) + local) * p.ld_part);
+        } else {
+            pitch = p.ldc * size;
+            to = static_cast<char *>(p.out) + (WEIGHTS ? at.group * p.out_group * size : 0) + (p.out_row && !WEIGHTS ? 0 : local * pitch);
+        }
+        aligned = ((reinterpret_cast<uintptr_t>(to) | pitch) & 15) == 0;
+        if (!part && !WEIGHTS && FINISH == Finish::Store) {
+            if (p.mask) aligned = aligned && ((reinterpret_cast<uintptr_t>(p.mask) | p.ld_mask * sizeof(typename T::elem)) & 15) == 0;
+            if (p.mask_codes) aligned = aligned && ((reinterpret_cast<uintptr_t>(p.mask_codes) | p.ld_mask) & 7) == 0;
+        }
+    }
+
+    // rows r0 + first, r0 + first + PASS, ... of 32; v: the lane's columns in the turned tile, PITCH floats a row
+    template <int PASS, int PITCH> __device__ __forceinline__ void rows(const ProductParams &p, const Place &at, uint32_t r0, uint32_t first, uint32_t c, const float *v) const
+    {
+        // what belongs to a row is fetched once, by the lane of its number
+        const uint32_t lane = threadIdx.x % 64, mine = r0 + lane % 32;
+        const uint64_t my_row = at.row0 + mine;
+        float row_factor = factor;
+        uint32_t row_number = 0;
+        bool is_in = mine < at.rows;
+        if (!WEIGHTS && !part && is_in) {
+            if (FINISH == Finish::Slope) { row_factor = p.norm[my_row]; row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
+            if (FINISH == Finish::Store && p.row_scale) row_factor = p.row_scale[my_row];
+            if (FINISH == Finish::Store && p.out_row) row_number = p.out_row[my_row];
+        }
+        #pragma unroll 4
+        for (uint32_t k = 0; k < 32; k += PASS) {
+            const uint32_t r = k + first;
+            const float f = WEIGHTS ? factor : __shfl(row_factor, r, 64);
+            const uint32_t number = WEIGHTS ? 0 : __shfl(row_number, r, 64);
+            f4 a = *reinterpret_cast<const f4 *>(v + r * PITCH), b = *reinterpret_cast<const f4 *>(v + r * PITCH + 4);
+            if (r0 + r >= at.rows) continue;
+            const uint64_t row = at.row0 + r0 + r;
+            char *at_row = to + static_cast<uint64_t>(r0 + r) * pitch;
+            if constexpr (FINISH == Finish::Slope) {
+                #pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    a[j] = (T::exp(a[j] - f) - (c + j == number ? 1.0f : 0.0f)) * slope_scale<T>();
+                    b[j] = (T::exp(b[j] - f) - (c + 4 + j == number ? 1.0f : 0.0f)) * slope_scale<T>();
+                }
+            } else if (!part) {
+                if (!WEIGHTS) {
+                    if (p.out_row) { if (number == kNoRow) continue; at_row = to + number * pitch; }
+                    if (p.sum) {
+                        float *s = p.sum + row * p.ld_sum + c;
+                        if (p.sum_read) { a += *reinterpret_cast<const f4 *>(s); b += *reinterpret_cast<const f4 *>(s + 4); }
+                        if (p.sum_write) { *reinterpret_cast<f4 *>(s) = a; *reinterpret_cast<f4 *>(s + 4) = b; continue; }
+                    }
+                }
+                a *= f;
+                b *= f;
+                if (!WEIGHTS && p.relu) {
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j) { a[j] = a[j] < 0.0f ? 0.0f : a[j]; b[j] = b[j] < 0.0f ? 0.0f : b[j]; }
+                }
+                if (!WEIGHTS && (p.mask || p.mask_codes)) mask(p, row, c, a, b);
+            }
+            if (f32) {
+                f4 *o = reinterpret_cast<f4 *>(at_row) + c / 4;
+                o[0] = a;
+                o[1] = b;
+            } else {
+                reinterpret_cast<u4 *>(at_row)[c / 8] = u4{T::pack(a.x, a.y), T::pack(a.z, a.w), T::pack(b.x, b.y), T::pack(b.z, b.w)};
+            }
+        }
+    }
+
+    __device__ __forceinline__ void mask(const ProductParams &p, uint64_t row, uint32_t c, f4 &a, f4 &b) const
+    {
+        if (p.mask_codes) {
+            const u2 m = *reinterpret_cast<const u2 *>(p.mask_codes + row * p.ld_mask + c);
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if ((m.x >> (8 * j) & 0xffu) - 1u >= 0x7eu) a[j] = 0.0f;          // 1 .. 0x7e are above zero
+                if ((m.y >> (8 * j) & 0xffu) - 1u >= 0x7eu) b[j] = 0.0f;
+            }
+        } else if constexpr (sizeof(typename T::elem) == 4) {
+            const float *m = static_cast<const float *>(p.mask) + row * p.ld_mask + c;
+            const f4 x = *reinterpret_cast<const f4 *>(m), y = *reinterpret_cast<const f4 *>(m + 4);
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) { if (!(x[j] > 0.0f)) a[j] = 0.0f; if (!(y[j] > 0.0f)) b[j] = 0.0f; }
+        } else {
+            constexpr unsigned most = std::is_same<T, F16>::value ? 0x7c00u : 0x7f80u;
+            const u4 m = *reinterpret_cast<const u4 *>(static_cast<const uint16_t *>(p.mask) + row * p.ld_mask + c);
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (((m[j / 2] >> (16 * (j % 2))) & 0xffffu) - 1u >= most) a[j] = 0.0f;
+                if (((m[2 + j / 2] >> (16 * (j % 2))) & 0xffffu) - 1u >= most) b[j] = 0.0f;
+            }
+        }
+    }
+};
 
 template <class T, Layout LAYOUT, class S, Finish FINISH, int HOW_A, int HOW_B>
 __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams p)
 {
     typedef Product<T, LAYOUT, S, HOW_A, HOW_B> P;
     constexpr bool WEIGHTS = P::WEIGHTS;
-    constexpr int stats_bytes = FINISH == Finish::Stats ? S::WN * S::WK * S::BM * 8 : 0;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[P::lds_bytes > stats_bytes ? P::lds_bytes : stats_bytes];
+    static_assert(S::WN * S::BM * 8 <= P::lds_bytes, "the statistics' waves meet in the operands' buffers");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[P::lds_bytes];
     Place at;
     const uint32_t col_tiles = (p.n + S::BN - 1) / S::BN;
     if (!(WEIGHTS ? place_weights<S::BM>(p, blockIdx.x, col_tiles, at, S::BN) : place_rows<S::BM>(p, blockIdx.x, col_tiles, at, S::BN))) return;
@@ -372,6 +554,41 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         slice0 = per * blockIdx.y < slices ? per * blockIdx.y : slices;
         slices = slices - slice0 < per ? slices - slice0 : per;
     }
+    if constexpr (P::DEEP) {
+        static_assert(P::STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
+        constexpr int NI = P::LoadA::N + P::LoadB::N, ST = P::stages;
+        #pragma unroll
+        for (int i = 0; i < ST - 1; ++i)
+            if (static_cast<uint32_t>(i) < slices) { la.request(lds + i * P::stage, (slice0 + i) * S::BK); lb.request(lds + i * P::stage + P::LoadA::bytes, (slice0 + i) * S::BK); }
+        typename P::Fragments f[2];
+        slices_arrived<0>();
+        P::read(f[0], lds, wk * 16, wm, wn, lane);
+        // (keeps the compiler from joining these reads with the loop's last ones at the head of the loop, where nothing hides them)
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i) asm volatile("" : "+v"(f[0].a[i]));
+        #pragma unroll
+        for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[j]));
+        uint32_t at_cur = 0, at_next = P::stage, at_fill = (ST - 1) * P::stage;
+        auto advance = [&] {
+            at_cur = at_next;
+            at_next = at_next + P::stage == ST * P::stage ? 0 : at_next + P::stage;
+            at_fill = at_fill + P::stage == ST * P::stage ? 0 : at_fill + P::stage;
+        };
+        uint32_t t = 0;
+        // slice t + 1 has arrived, and every wave has left slice t - 1
+        for (; (slice0 + t + ST) * S::BK <= at.terms && t + ST - 1 < slices; ++t) {
+            slices_arrived<NI * (ST - 3)>();
+            P::template deep_slice<true>(lds + at_cur, lds + at_next, lds + at_fill, la, lb, true, (slice0 + t + ST - 1) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
+            advance();
+        }
+        #pragma unroll 1
+        for (; t < slices; ++t) {
+            slices_arrived<0>();
+            P::template deep_slice<false>(lds + at_cur, lds + at_next, lds + at_fill, la, lb, t + ST - 1 < slices, (slice0 + t + ST - 1) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
+            advance();
+        }
+        slices_arrived<0>();
+    } else {
     if (slices) {
         la.request(lds, slice0 * S::BK); lb.request(lds + P::LoadA::bytes, slice0 * S::BK);
         la.deliver(lds); lb.deliver(lds + P::LoadA::bytes);
@@ -383,6 +600,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         P::slice(cur, next, la, lb, more, (slice0 + t + 1) * S::BK, acc, wm, wn, wk, lane);
         if (more) { la.deliver(next); lb.deliver(next + P::LoadA::bytes); }
         slice_barrier<P::DIRECT>();
+    }
     }
 
     float unscale = 1.0f;
@@ -421,119 +639,150 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         }
     }
 
-    // quads: row block i, column 4 q' of the wave's columns
-    constexpr int QN = kQuads<S>;
-    f4 quad[QN];
-    if constexpr (S::WK == 1) {
-        #pragma unroll
-        for (int i = 0; i < S::MB; ++i)
+    // Four consecutive columns of a row, r in the tile and c in C.
+    const float factor = FINISH == Finish::Store && p.splits <= 1 ? group_factor(p, at.group) : 1.0f;
+    auto finish = [&](uint32_t r, uint32_t c, f4 v) {
+        if constexpr (FINISH == Finish::Store) {
+            if (r >= at.rows || c >= p.n) return;
+            const uint64_t row = WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r;
+            if (p.splits > 1) {
+                const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
+                *reinterpret_cast<f4 *>(p.part + (blockIdx.y * all + row) * p.ld_part + c) = v;
+            } else {
+                finish_quad<T, WEIGHTS>(p, at.group, row, at.m0 + r, c, v, factor);
+            }
+        } else if constexpr (FINISH == Finish::Slope) {
+            if (r >= at.rows || c >= p.ldc_zero) return;
+            const float norm = p.norm[at.row0 + r];
+            const int32_t target = p.target[at.row0 + r];
             #pragma unroll
-            for (int j = 0; j < S::NB; ++j)
-                #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    quad[(i * S::NB + j) * 4 + g] = f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]} * unscale;
-    } else {
-        // the waves' sums over their terms meet in LDS, in the order of the waves
-        static_assert(S::WM == 1 && S::WN == 1, "waves share the terms of one tile");
-        f4 *share = reinterpret_cast<f4 *>(lds);
-        constexpr int ALL = S::MB * S::NB * 4;
+            for (int j = 0; j < 4; ++j) {
+                v[j] = (T::exp(v[j] - norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
+                if (c + j >= p.n) v[j] = 0.0f;
+            }
+            store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
+        }
+    };
+
+    if constexpr (S::WK > 1) {
+        // the waves' sums over their terms meet in LDS, row by row, in the order of the waves
+        static_assert(S::WM == 1 && S::WN == 1 && S::MB == 1, "waves share the terms of one tile");
+        constexpr int PITCH = S::BN + 4, LANES = S::BN / 4;
+        float *part = reinterpret_cast<float *>(lds);
         #pragma unroll
-        for (int i = 0; i < S::MB; ++i)
+        for (int j = 0; j < S::NB; ++j)
             #pragma unroll
-            for (int j = 0; j < S::NB; ++j)
-                #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    share[(wk * ALL + (i * S::NB + j) * 4 + g) * 64 + lane] = f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]};
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f4 *>(part + (wk * S::BM + lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) =
+                    f4{acc[0][0][j][4 * g], acc[0][0][j][4 * g + 1], acc[0][0][j][4 * g + 2], acc[0][0][j][4 * g + 3]};
         __syncthreads();
         #pragma unroll
-        for (int q = 0; q < QN; ++q) {
-            f4 s = share[(wk * QN + q) * 64 + lane];
+        for (uint32_t r = threadIdx.x / LANES; r < S::BM; r += S::threads / LANES) {
+            const uint32_t q = threadIdx.x % LANES * 4, c = at.n0 + q;
+            f4 v = *reinterpret_cast<const f4 *>(part + r * PITCH + q);
             #pragma unroll
-            for (int w = 1; w < S::WK; ++w) s += share[(w * ALL + wk * QN + q) * 64 + lane];
-            quad[q] = s * unscale;
-        }
-        if (FINISH == Finish::Stats) __syncthreads();
-    }
-    // quad q: row and column
-    const uint32_t q0 = S::WK == 1 ? 0 : wk * QN;
-    auto row_of = [&](int q) { return (wm * S::MB + (q0 + q) / (4 * S::NB)) * 32 + lane % 32; };
-    auto col_of = [&](int q) { return at.n0 + (wn * S::NB + (q0 + q) / 4 % S::NB) * 32 + (q0 + q) % 4 * 8 + 4 * (lane / 32); };
-
-    if constexpr (FINISH == Finish::Store) {
-        if (p.splits > 1) {
-            const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
-            #pragma unroll
-            for (int q = 0; q < QN; ++q) {
-                const uint32_t r = row_of(q), c = col_of(q);
-                if (r >= at.rows || c >= p.n) continue;
-                const uint64_t row = WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r;
-                *reinterpret_cast<f4 *>(p.part + (blockIdx.y * all + row) * p.ld_part + c) = quad[q];
+            for (int w = 1; w < S::WK; ++w) v += *reinterpret_cast<const f4 *>(part + (w * S::BM + r) * PITCH + q);
+            v *= unscale;
+            if constexpr (FINISH == Finish::Stats) {
+                static_assert(LANES <= 64 && 64 % LANES == 0, "a row within a wave");
+                const int32_t target = r < at.rows ? p.target[at.row0 + r] : -1;
+                float top = -INFINITY;
+                #pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    if (c + j >= p.n) v[j] = -INFINITY;
+                    else if (static_cast<int32_t>(p.v0 + c + j) == target) p.target_logit[at.row0 + r] = v[j];
+                    top = fmaxf(top, v[j]);
+                }
+                #pragma unroll
+                for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+                const float base = top == -INFINITY ? 0.0f : top;
+                float sum = (T::exp(v[0] - base) + T::exp(v[1] - base)) + (T::exp(v[2] - base) + T::exp(v[3] - base));
+                #pragma unroll
+                for (int d = 1; d < LANES; d <<= 1) sum += __shfl_xor(sum, d, 64);
+                if (q == 0 && r < at.rows) p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
+            } else {
+                finish(r, c, v);
             }
-            return;
-        }
-        const float factor = group_factor(p, at.group);
-        #pragma unroll
-        for (int q = 0; q < QN; ++q) {
-            const uint32_t r = row_of(q), c = col_of(q);
-            if (r >= at.rows || c >= p.n) continue;
-            finish_quad<T, WEIGHTS>(p, at.group, WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r, at.m0 + r, c, quad[q], factor);
         }
     } else if constexpr (FINISH == Finish::Stats) {
         // per row block: maximum and sum over the wave's columns (a lane and the one 32 further on hold a row), then over the waves
-        constexpr int PER = S::WK == 1 ? 4 * S::NB : QN, BLOCKS = QN / PER;
         float2 *share = reinterpret_cast<float2 *>(lds);       // the operand buffers are free: the loop ended with a barrier
+        const uint32_t c0 = at.n0 + wn * S::NB * 32 + 4 * (lane / 32);
+        const bool whole = at.n0 + S::BN <= p.n;
         #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) {
-            const uint32_t r = row_of(i * PER);
-            const int32_t target = r < at.rows ? p.target[at.row0 + r] : -1;
-            float top = -INFINITY;
-            #pragma unroll
-            for (int q = i * PER; q < (i + 1) * PER; ++q)
+        for (int i = 0; i < S::MB; ++i) {
+            const uint32_t r = (wm * S::MB + i) * 32 + lane % 32;
+            const int32_t target = r < at.rows ? p.target[at.row0 + r] - static_cast<int32_t>(p.v0) : -1;
+            if (__ballot(target >= static_cast<int32_t>(at.n0) && target < static_cast<int32_t>(at.n0 + S::BN))) {
                 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t c = col_of(q) + j;
-                    if (c >= p.n) quad[q][j] = -INFINITY;
-                    else if (static_cast<int32_t>(p.v0 + c) == target) p.target_logit[at.row0 + r] = quad[q][j];
-                    top = fmaxf(top, quad[q][j]);
-                }
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+                for (int j = 0; j < S::NB; ++j)
+                    #pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        if (static_cast<int32_t>(c0 + j * 32 + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
+            }
+            float top = -INFINITY, sum = 0.0f;
+            if (!whole) {
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j)
+                    #pragma unroll
+                    for (int x = 0; x < 16; ++x) if (c0 + j * 32 + 8 * (x / 4) + x % 4 >= p.n) acc[0][i][j][x] = -INFINITY;
+            }
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j)
+                #pragma unroll
+                for (int x = 0; x < 16; ++x) top = fmaxf(top, acc[0][i][j][x]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64)) * unscale;
             const float base = top == -INFINITY ? 0.0f : top;
-            float sum = 0.0f;
             #pragma unroll
-            for (int q = i * PER; q < (i + 1) * PER; ++q)
+            for (int j = 0; j < S::NB; ++j) {
                 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += T::exp(quad[q][j] - base);
+                for (int x = 0; x < 16; ++x) sum += T::exp(acc[0][i][j][x] * unscale - base);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             sum += __shfl_xor(sum, 32, 64);
-            if (lane < 32) share[(wn * S::WK + wk) * S::BM + r] = make_float2(top, sum);
+            if (lane < 32) share[wn * S::BM + r] = make_float2(top, sum);
+            __builtin_amdgcn_sched_barrier(0);                 // one row block's values at a time
         }
         __syncthreads();
         for (uint32_t r = threadIdx.x; r < at.rows; r += S::threads) {
             float top = -INFINITY, sum = 0.0f;
             #pragma unroll
-            for (int w = 0; w < S::WN * S::WK; ++w) top = fmaxf(top, share[w * S::BM + r].x);
+            for (int w = 0; w < S::WN; ++w) top = fmaxf(top, share[w * S::BM + r].x);
             const float base = top == -INFINITY ? 0.0f : top;
             #pragma unroll
-            for (int w = 0; w < S::WN * S::WK; ++w) {
+            for (int w = 0; w < S::WN; ++w) {
                 const float2 s = share[w * S::BM + r];
-                // a part whose columns all lie past the end has nothing to add; a NaN stays one
-                if (s.x != -INFINITY || s.y != s.y) sum += s.y * T::exp(s.x - base);
+                sum += s.y * T::exp(s.x - base);               // (a part without columns: 0 times 0; a NaN stays one)
             }
             p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
         }
     } else {
+        // 32 rows at a time turn in the wave's own part of LDS, so that consecutive lanes take consecutive columns.  Tiles that lie
+        // within C with every row on 16 bytes are finished eight columns at a time, without a decision per element.
+        constexpr int PITCH = S::NB * 32 + 4, LANES = S::NB * 4, PASS = 64 / LANES;     // rows of one pass
+        float *mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+        const uint32_t q = lane % LANES * 8, c = at.n0 + wn * S::NB * 32 + q;
+        const RowFinish<T, WEIGHTS, FINISH> whole(p, at, factor);
+        const bool fast = at.n0 + S::BN <= p.n && whole.aligned;
         #pragma unroll
-        for (int q = 0; q < QN; ++q) {
-            const uint32_t r = row_of(q), c = col_of(q);
-            if (r >= at.rows || c >= p.ldc_zero) continue;
-            const float norm = p.norm[at.row0 + r];
-            const int32_t target = p.target[at.row0 + r];
-            f4 v;
+        for (int i = 0; i < S::MB; ++i) {
             #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = (T::exp(quad[q][j] - norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
-                if (c + j >= p.n) v[j] = 0.0f;
+            for (int j = 0; j < S::NB; ++j)
+                #pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f4 *>(mine + (lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) =
+                        f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]} * unscale;
+            __builtin_amdgcn_wave_barrier();
+            const uint32_t r0 = (wm * S::MB + i) * 32;
+            if (fast) {
+                whole.template rows<PASS, PITCH>(p, at, r0, lane / LANES, c, mine + q);
+            } else {
+                #pragma unroll 1
+                for (uint32_t r = lane / LANES; r < 32; r += PASS)
+                    #pragma unroll
+                    for (int h = 0; h < 2; ++h) finish(r0 + r, c + 4 * h, *reinterpret_cast<const f4 *>(mine + r * PITCH + q + 4 * h));
             }
-            store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
+            __builtin_amdgcn_wave_barrier();
         }
     }
 }
@@ -549,7 +798,7 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
     return hipGetLastError();
 }
 
-typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
+typedef TileShape<256, 256, 32, 2, 2, 1, 4> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
