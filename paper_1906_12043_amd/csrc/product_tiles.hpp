@@ -798,7 +798,7 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
     return hipGetLastError();
 }
 
-typedef TileShape<256, 256, 32, 2, 2, 1, 4> Large16;
+typedef TileShape<256, 256, 32, 2, 4, 1, 4> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
