@@ -19,8 +19,7 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 // Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2> struct TileShape {
-    static constexpr int STAGES = STAGES_;
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_> struct TileShape {
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
     static constexpr int threads = 64 * WM * WN * WK;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;       // 32x32 blocks of a wave
@@ -152,12 +151,12 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
         }
     }
 
-    // chunks FIRST .. LAST - 1 of a slice that lies within the sum: nothing to check
-    template <int FIRST, int LAST> __device__ __forceinline__ void request_whole(uint8_t *lds, uint32_t k0, uint32_t wave)
+    // a slice that lies within the sum: nothing to check
+    __device__ __forceinline__ void request_whole(uint8_t *lds, uint32_t k0, uint32_t wave)
     {
         const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
         #pragma unroll
-        for (int i = FIRST; i < LAST; ++i)
+        for (int i = 0; i < N; ++i)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
                                              (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
     }
@@ -281,6 +280,15 @@ template <int BM> __device__ __forceinline__ bool place_weights(const ProductPar
 
 // ---- the kernel ---------------------------------------------------------------------------------------------
 
+// All but the last LEFT requests of every wave have arrived in LDS, and every wave has the fragments it has read.
+template <int LEFT> __device__ __forceinline__ void slices_arrived()
+{
+    static_assert(LEFT < 64, "the wait's counter");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product {
     static constexpr bool WEIGHTS = LAYOUT == Layout::Weights;
     static constexpr bool A_KC = !WEIGHTS, B_KC = LAYOUT == Layout::Rows_NK;
@@ -290,13 +298,13 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     static constexpr bool DIRECT = HOW_A == kDirect || HOW_B == kDirect;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
     static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 2 * (S::NB * 32 + 4) * 4;
-    static constexpr bool DEEP = HOW_A == kDirect && HOW_B == kDirect && S::STAGES > 2;
-    static constexpr int stages = DEEP ? S::STAGES : 2;
-    static constexpr int lds_bytes = stages * stage > join_bytes ? stages * stage : join_bytes;
+    static constexpr bool AHEAD = HOW_A == kDirect && HOW_B == kDirect;
+    static constexpr int lds_bytes = 2 * stage > join_bytes ? 2 * stage : join_bytes;
 
-    // The deep pipeline of operands that go to LDS by themselves.  Iteration t multiplies slice t, whose first fragments are in
-    // registers already, reads every next fragment while the matrix cores work on the one before, the first of slice t + 1 among them,
-    // and requests slice t + stages - 1 into the buffer that slice t - 1 has left.
+    // The pipeline of operands that go to LDS by themselves.  While the matrix cores work on one step of 16 terms (times WK), the fragments of the next
+    // step are read.  In front of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes
+    // the slice after the next one, which then has a whole slice's time to arrive; and the next slice, requested that long ago, is there, so
+    // that its first fragments are read beside the last step's products.
     static constexpr int STEPS = S::BK / 16 / S::WK;
     struct Fragments { u4 a[S::MB], b[S::NB]; };
     static __device__ __forceinline__ void read(Fragments &f, const uint8_t *lds, uint32_t k0, uint32_t wm, uint32_t wn, uint32_t lane)
@@ -306,43 +314,42 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
         #pragma unroll
         for (int i = 0; i < S::MB; ++i) f.a[i] = LoadA::L::fragment(lds, (wm * S::MB + i) * 32, k0, lane);
     }
-    template <bool WHOLE>
-    static __device__ __forceinline__ void deep_slice(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
-                                                      bool more, uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
-                                                      uint32_t wave)
-    {
-        if (!WHOLE && more) { la.request(fill, k_fill); lb.request(fill + LoadA::bytes, k_fill); }
-        deep_steps<WHOLE, 0>(cur, next, fill, la, lb, k_fill, f, acc, wm, wn, wk, lane, wave);
-    }
-    // Step kk of a slice: its share of the requests and the reads of the next step's fragments, between its first products.
-    template <bool WHOLE, int kk>
-    static __device__ __forceinline__ void deep_steps(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
-                                                      uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
-                                                      uint32_t wave)
+    // (fill is cur: a name of its own tells the compiler that reads need not wait for what is requested into it; the meeting of the
+    // waves keeps the reads of the old slice in front)
+    template <bool WHOLE, int kk = 0>
+    static __device__ __forceinline__ void steps(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
+                                                 bool more, uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
+                                                 uint32_t wave)
     {
         if constexpr (kk < STEPS) {
-            constexpr int A0 = kk * LoadA::N / STEPS, A1 = (kk + 1) * LoadA::N / STEPS, B0 = kk * LoadB::N / STEPS, B1 = (kk + 1) * LoadB::N / STEPS;
-            if constexpr (WHOLE) {
-                la.template request_whole<A0, A1>(fill, k_fill, wave);
-                lb.template request_whole<B0, B1>(fill + LoadA::bytes, k_fill, wave);
+            constexpr bool LAST = kk + 1 == STEPS;
+            if constexpr (LAST) {
+                slices_arrived<0>();
+                if constexpr (WHOLE) {
+                    la.request_whole(fill, k_fill, wave);
+                    lb.request_whole(fill + LoadA::bytes, k_fill, wave);
+                } else if (more) {
+                    la.request(fill, k_fill);
+                    lb.request(fill + LoadA::bytes, k_fill);
+                }
             }
-            if (kk + 1 < STEPS) read(f[(kk + 1) % 2], cur, ((kk + 1) * S::WK + wk) * 16, wm, wn, lane);
-            else                read(f[(kk + 1) % 2], next, wk * 16, wm, wn, lane);
+            if (LAST) read(f[0], next, wk * 16, wm, wn, lane);
+            else      read(f[(kk + 1) % 2], cur, ((kk + 1) * S::WK + wk) * 16, wm, wn, lane);
             #pragma unroll
             for (int i = 0; i < S::MB; ++i)
                 #pragma unroll
                 for (int j = 0; j < S::NB; ++j) acc[i][j] = T::mfma(f[kk % 2].b[j], f[kk % 2].a[i], acc[i][j]);
-            // the reads between the first products, so that the last of them has arrived when the next step begins; then the requests
+            // the reads between the first products, so that the last of them has arrived when the next step begins, the requests beside them
             constexpr int READS = S::MB * (A_KC ? 1 : 2) + S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB, PER = (READS + PRODUCTS - 1) / PRODUCTS;
-            constexpr int ASKED = WHOLE ? A1 - A0 + B1 - B0 : 0, LATE = (READS + PER - 1) / PER < PRODUCTS ? PRODUCTS - (READS + PER - 1) / PER : 1, ASK = (ASKED + LATE - 1) / LATE;
+            constexpr int ASK = LAST && WHOLE ? (LoadA::N + LoadB::N + PRODUCTS - 1) / PRODUCTS : 0;
             #pragma unroll
             for (int r = 0; r < PRODUCTS; ++r) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                 if (r * PER < READS) __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
-                if constexpr (ASK > 0) if (r >= PRODUCTS - LATE) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
+                if constexpr (ASK > 0) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
-            deep_steps<WHOLE, kk + 1>(cur, next, fill, la, lb, k_fill, f, acc, wm, wn, wk, lane, wave);
+            steps<WHOLE, kk + 1>(cur, next, fill, la, lb, more, k_fill, f, acc, wm, wn, wk, lane, wave);
         }
     }
 
@@ -390,15 +397,6 @@ template <bool DIRECT> __device__ __forceinline__ void slice_barrier()
 {
     if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-}
-
-// All but the last LEFT requests of every wave have arrived in LDS, and every wave has its fragments of earlier slices.
-template <int LEFT> __device__ __forceinline__ void slices_arrived()
-{
-    static_assert(LEFT < 64, "the wait's counter");
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 }
 
 // Rows of a tile that lies within C, eight columns of a row per lane: what finish (below) does to four, with its decisions taken once.
@@ -554,38 +552,29 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         slice0 = per * blockIdx.y < slices ? per * blockIdx.y : slices;
         slices = slices - slice0 < per ? slices - slice0 : per;
     }
-    if constexpr (P::DEEP) {
+    if constexpr (P::AHEAD) {
         static_assert(P::STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
-        constexpr int NI = P::LoadA::N + P::LoadB::N, ST = P::stages;
+        const uint32_t k0 = slice0 * S::BK;
         #pragma unroll
-        for (int i = 0; i < ST - 1; ++i)
-            if (static_cast<uint32_t>(i) < slices) { la.request(lds + i * P::stage, (slice0 + i) * S::BK); lb.request(lds + i * P::stage + P::LoadA::bytes, (slice0 + i) * S::BK); }
+        for (uint32_t i = 0; i < 2; ++i)
+            if (i < slices) { la.request(lds + i * P::stage, k0 + i * S::BK); lb.request(lds + i * P::stage + P::LoadA::bytes, k0 + i * S::BK); }
         typename P::Fragments f[2];
-        slices_arrived<0>();
+        if (slices > 1) slices_arrived<P::LoadA::N + P::LoadB::N>(); else slices_arrived<0>();
         P::read(f[0], lds, wk * 16, wm, wn, lane);
         // (keeps the compiler from joining these reads with the loop's last ones at the head of the loop, where nothing hides them)
         #pragma unroll
         for (int i = 0; i < S::MB; ++i) asm volatile("" : "+v"(f[0].a[i]));
         #pragma unroll
         for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[j]));
-        uint32_t at_cur = 0, at_next = P::stage, at_fill = (ST - 1) * P::stage;
-        auto advance = [&] {
-            at_cur = at_next;
-            at_next = at_next + P::stage == ST * P::stage ? 0 : at_next + P::stage;
-            at_fill = at_fill + P::stage == ST * P::stage ? 0 : at_fill + P::stage;
-        };
         uint32_t t = 0;
-        // slice t + 1 has arrived, and every wave has left slice t - 1
-        for (; (slice0 + t + ST) * S::BK <= at.terms && t + ST - 1 < slices; ++t) {
-            slices_arrived<NI * (ST - 3)>();
-            P::template deep_slice<true>(lds + at_cur, lds + at_next, lds + at_fill, la, lb, true, (slice0 + t + ST - 1) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
-            advance();
+        for (; t + 2 < slices && k0 + (t + 3) * S::BK <= at.terms; ++t) {
+            uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
+            P::template steps<true>(cur, next, cur, la, lb, true, k0 + (t + 2) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
         }
         #pragma unroll 1
         for (; t < slices; ++t) {
-            slices_arrived<0>();
-            P::template deep_slice<false>(lds + at_cur, lds + at_next, lds + at_fill, la, lb, t + ST - 1 < slices, (slice0 + t + ST - 1) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
-            advance();
+            uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
+            P::template steps<false>(cur, next, cur, la, lb, t + 2 < slices, k0 + (t + 2) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
         }
         slices_arrived<0>();
     } else {
@@ -798,7 +787,7 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
     return hipGetLastError();
 }
 
-typedef TileShape<256, 256, 32, 2, 4, 1, 4> Large16;
+typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
