@@ -2,6 +2,8 @@
 #include "operator_call.hpp"
 #include "product_finish.hpp"
 
+#include <cmath>
+
 namespace cocod {
 namespace {
 
@@ -40,24 +42,37 @@ hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const Prod
            : type == Dtype::F16 ? launch_join_of<F16>(stream, weights, n, p) : launch_join_of<F32>(stream, weights, n, p);
 }
 
-ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k)
+// The tile and the number of splits that are expected to take least time.  A compute unit takes ceil(blocks / 256) blocks one after the other (where it
+// holds several at a time they share it), each `per_slice` for every slice of its sum and `per_tile` once, in us; a launch costs 5, joining splits 4 and
+// their traffic at 4 TB/s.  Fitted to 54 products of 1 to 16 groups, 1 to 8192 rows and widths 512 to 32000, every tile with 1 to 16 splits: the choice
+// costs 1 % more time than the best one in the mean, 21 % at most.  For instance, us (large / medium / small tile, best splits in brackets):
+// bf16 16 groups of one row, 1024 x 1024: 16 (4) / 12 (4) / 8 (1); 4 of 64 rows, 2048 x 2048: 22 (4) / 18 (4) / 14 (1); 16 of 512 rows, 1024 x
+// 1024: 33 (1) / 26 (1) / 50 (1); 16 of 500 rows, 2048 x 1024, input gradient: 40 (1) / 47 (1) / 93 (1); 4 of 768 rows, 32000 x 1024: 239 (4) / 266 (8) /
+// 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); fp32 4 of 250 rows, 512 x 768: - / 25 (4) / 17 (1); one of 2048 rows, 2048 x 2048: - / 130 (1) / 180 (1).
+struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile; };
+constexpr TileCost kCost16[] = {{256, 256, 64, 1.36, 3.9}, {128, 128, 64, 0.45, 1.2}, {32, 64, 128, 0.27, 0.4}};
+constexpr TileCost kCost32[] = {{0, 0, 0, 0, 0}, {128, 128, 32, 1.73, 3.5}, {32, 64, 64, 0.62, 1.2}};
+constexpr uint32_t kMaxSplits = 16;
+
+ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split)
 {
     const bool weights = layout == Layout::Weights;
-    const uint64_t high = weights ? m : (rows + groups - 1) / groups;       // rows of C of one group, on average
-    const uint64_t terms = weights ? (rows + groups - 1) / groups : k;
-    auto tiles = [&](uint64_t bm, uint64_t bn) { return groups * ((high + bm - 1) / bm) * ((n + bn - 1) / bn); };
-    ProductPlan plan{Tile::Medium, 1};
-    if (high <= 48 || (tiles(128, 128) < 64 && terms <= 4096)) plan.tile = Tile::Small;
-    else if (type != Dtype::F32 && high >= 192 && n >= 192 && tiles(256, 256) >= 200) plan.tile = Tile::Large;
-    const uint64_t slice = plan.tile == Tile::Small ? (type == Dtype::F32 ? 64 : 128) : type == Dtype::F32 ? 32 : 64;
-    const uint64_t have = plan.tile == Tile::Small ? tiles(32, 64) : plan.tile == Tile::Medium ? tiles(128, 128) : tiles(256, 256);
-    const uint64_t want = plan.tile == Tile::Small ? 512 : 256, most = terms / (4 * slice);
-    if (have * 2 <= want && most >= 2) {
-        uint64_t s = want / have;
-        s = s < most ? s : most;
-        plan.splits = static_cast<uint32_t>(s < 32 ? s : 32);
+    const double mean_rows = static_cast<double>(rows) / groups, terms = weights ? mean_rows : k;
+    const double cells = weights ? static_cast<double>(groups) * m * n : static_cast<double>(rows) * n;
+    ProductPlan best{Tile::Medium, 1};
+    double least = 1e300;
+    for (uint32_t tile = type == Dtype::F32 ? 1 : 0; tile < 3; ++tile) {
+        const TileCost &c = (type == Dtype::F32 ? kCost32 : kCost16)[tile];
+        // ragged groups end half a tile short, in the mean
+        const double high = weights || groups == 1 ? std::ceil((weights ? m : mean_rows) / c.bm) : std::fmax(1.0, mean_rows / c.bm + 0.5);
+        const double tiles = groups * high * std::ceil(static_cast<double>(n) / c.bn);
+        for (uint32_t splits = 1; splits <= (may_split ? kMaxSplits : 1u); splits *= 2) {
+            const double turns = std::fmax(1.0, std::ceil(tiles * splits / 256.0 - 1e-9)), slices = std::fmax(1.0, std::ceil(terms / c.bk / splits));
+            const double us = 5.0 + turns * (slices * c.per_slice + c.per_tile) + (splits > 1 ? 4.0 + cells * 4.0 * (splits + 1) / 4.0e6 : 0.0);
+            if (us < least) { least = us; best = {static_cast<Tile>(tile), splits}; }
+        }
     }
-    return plan;
+    return best;
 }
 
 uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n)
@@ -84,12 +99,12 @@ int check_shape(const cocod_grouped *g)
     return COCOD_OK;
 }
 
-ProductPlan plan_of(const cocod_grouped *g, Layout layout)
+ProductPlan plan_of(const cocod_grouped *g, Layout layout, bool may_split)
 {
     const Dtype t = kTypes[g->dtype];
-    if (layout == Layout::Rows_KN) return plan_product(layout, t, g->rows, g->groups, 0, g->outer, g->inner);
-    if (layout == Layout::Rows_NK) return plan_product(layout, t, g->rows, g->groups, 0, g->inner, g->outer);
-    return plan_product(layout, t, g->rows, g->groups, g->inner, g->outer, 0);
+    if (layout == Layout::Rows_KN) return plan_product(layout, t, g->rows, g->groups, 0, g->outer, g->inner, may_split);
+    if (layout == Layout::Rows_NK) return plan_product(layout, t, g->rows, g->groups, 0, g->inner, g->outer, may_split);
+    return plan_product(layout, t, g->rows, g->groups, g->inner, g->outer, 0, may_split);
 }
 uint64_t workspace_of(const cocod_grouped *g, Layout layout, const ProductPlan &plan)
 {
@@ -106,13 +121,13 @@ int check_codes(const cocod_grouped *g)
 int start(const cocod_grouped *g, Layout layout, ProductParams &p, ProductPlan &plan, const Extent &out, const Extent *in, int n_in)
 {
     const Dtype t = kTypes[g->dtype];
-    plan = plan_of(g, layout);
+    plan = plan_of(g, layout, true);
     const uint64_t need = workspace_of(g, layout, plan);
     const bool own = g->workspace && need;
     if (own && (reinterpret_cast<uintptr_t>(g->workspace) & 15)) return set_error(COCOD_ERR_INVALID, "workspace is not 16-byte aligned");
     if (own && g->workspace_bytes < need)
         return set_error(COCOD_ERR_INVALID, "workspace holds %llu bytes, %llu are needed", (unsigned long long)g->workspace_bytes, (unsigned long long)need);
-    if (!own) plan.splits = 1;                     // the sums are then formed by one block each
+    if (!own) plan = plan_of(g, layout, false);    // the sums are then formed by one block each
     const Extent ws = {"workspace", own ? g->workspace : nullptr, need};
     const Extent offsets = {"offsets", g->offsets, (static_cast<uint64_t>(g->groups) + 1) * 8};
     if (int rc = check_apart(out, in, n_in)) return rc;
@@ -152,7 +167,7 @@ int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *byt
     if (int rc = check_shape(g)) return rc;
     if (direction < COCOD_GROUPED_FORWARD || direction > COCOD_GROUPED_WEIGHT_GRAD) return set_error(COCOD_ERR_INVALID, "unknown direction %d", direction);
     const Layout layout = direction == COCOD_GROUPED_FORWARD ? Layout::Rows_KN : direction == COCOD_GROUPED_INPUT_GRAD ? Layout::Rows_NK : Layout::Weights;
-    *bytes = workspace_of(g, layout, plan_of(g, layout));
+    *bytes = workspace_of(g, layout, plan_of(g, layout, true));
     return COCOD_OK;
 }
 

@@ -94,15 +94,15 @@ inline bool direct_b(Layout layout, const ProductParams &p)
 {
     return direct_operand(p.b, p.ldb, layout == Layout::Weights ? 0 : p.b_group, layout != Layout::Rows_NK || p.k % 8 == 0);
 }
-// The tile that a launch takes where `planned` was planned: the large one needs operands that go to LDS directly.
+// The tile that a launch takes where `planned` was planned: the large one needs operands that go to LDS directly (or codes).
 inline Tile settle_tile(Dtype type, Layout layout, Tile planned, const ProductParams &p)
 {
-    return planned == Tile::Large && (type == Dtype::F32 || !direct_a(layout, p) || !direct_b(layout, p)) ? Tile::Medium : planned;
+    return planned == Tile::Large && (type == Dtype::F32 || (p.a && !direct_a(layout, p)) || !direct_b(layout, p)) ? Tile::Medium : planned;
 }
 
 // Tile and splits of a product, from its sizes alone.
 struct ProductPlan { Tile tile; uint32_t splits; };
-ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k);
+ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split);
 // Bytes of ProductParams::part (0 with one split), whose rows hold part_pitch(n) floats.
 inline uint64_t part_pitch(uint32_t n) { return (static_cast<uint64_t>(n) + 3) / 4 * 4; }
 uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n);

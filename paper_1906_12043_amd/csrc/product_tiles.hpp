@@ -53,8 +53,8 @@ template <bool KC, int BX, int BK> struct LdsTile {
 
 __device__ __forceinline__ u4 zero4() { return u4{0, 0, 0, 0}; }
 
-// One operand's part of a slice on its way to LDS through registers: any alignment, any type, bounds checked element by element
-// where a chunk of eight is not whole.
+// How an operand gets from memory into LDS: 16-byte pieces that the loads themselves put there; through registers, with any alignment and any
+// type; or as codes of 8 bits with a scale for every 32, expanded on the way.
 enum { kDirect = 0, kRegs = 1, kCodes = 2 };
 __device__ __attribute__((aligned(16))) const unsigned int kZeroChunk[4] = {0, 0, 0, 0};
 
@@ -77,12 +77,15 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
     float sc[HOW == kCodes ? N : 1];
     uint32_t off[HOW == kDirect ? N : 1];
 
+    bool fits;                        // every chunk of a slice within the sum lies within the operand
+
     __device__ __forceinline__ static uint32_t chunk(int i) { return i * THREADS + threadIdx.x; }
 
     __device__ __forceinline__ void start()
     {
+        // rows (direct: chunks of columns, too) past the end repeat the last one: their products are not stored
+        fits = HOW == kDirect || KC || x0 + BX <= x_end;
         if constexpr (HOW == kDirect) {
-            // rows (or chunks of columns) past the end repeat the last one: their products are not stored
             #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
@@ -151,17 +154,35 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
         }
     }
 
-    // a slice that lies within the sum: nothing to check
+    // a slice that lies within the sum, of an operand that fits: nothing to check
     __device__ __forceinline__ void request_whole(uint8_t *lds, uint32_t k0, uint32_t wave)
     {
-        const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
-        #pragma unroll
-        for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
-                                             (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+        if constexpr (HOW == kDirect) {
+            const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
+            #pragma unroll
+            for (int i = 0; i < N; ++i)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
+                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+        } else {
+            #pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t row = chunk(i) / L::CH;
+                const uint32_t c = (chunk(i) % L::CH) ^ L::swizzle(row), last = x_end - 1 - x0;
+                if (KC) row = row < last ? row : last;
+                const uint64_t r = (KC ? x0 : k0) + row, q = (KC ? k0 : x0) + c * 8;
+                if constexpr (HOW == kCodes) {
+                    const u2 v = *reinterpret_cast<const u2_any *>(codes + r * ld_codes + q);
+                    raw[i][0] = u4{v.x, v.y, 0, 0};
+                    sc[i] = __uint_as_float(static_cast<unsigned>(scales[r * ld_scales + q / 32]) << 23);
+                } else {
+                    #pragma unroll
+                    for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(src + r * ld + q)[j];
+                }
+            }
+        }
     }
 
-    // put the requested slice into LDS (behind the products of the slice before)
+    // put the requested slice into LDS
     __device__ __forceinline__ void deliver(uint8_t *lds)
     {
         if constexpr (HOW == kDirect) return;
@@ -205,16 +226,18 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
 };
 
 // Where a block's tile lies.
-struct Place { uint32_t group; uint32_t n0; uint64_t row0; uint32_t rows; uint32_t m0; uint32_t terms; };
+struct Place { uint32_t group; uint32_t n0; uint64_t row0; uint32_t rows; uint32_t m0; uint32_t terms; uint32_t split; };
 
-// Blocks go round the eight dies in turn: each die gets a run of consecutive tiles, which share operands in its cache.
-// In a band of row tiles the row tiles take turns in front of one column tile.
-__device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t row_tiles, uint32_t col_tiles, uint32_t &row_tile, uint32_t &col_tile)
+// Blocks go round the eight dies in turn: each die gets a run of consecutive tiles (of one split after another), which share operands
+// in its cache.  In a band of row tiles the row tiles take turns in front of one column tile.
+__device__ __forceinline__ bool tile_of_block(uint32_t row_tiles, uint32_t col_tiles, uint32_t splits, uint32_t &row_tile, uint32_t &col_tile, uint32_t &split)
 {
-    const uint32_t total = row_tiles * col_tiles;
-    if (block >= total) return false;
-    const uint32_t x = block % kXcdCount, q = total / kXcdCount, r = total % kXcdCount;
-    const uint32_t idx = x * q + (x < r ? x : r) + block / kXcdCount;
+    const uint32_t tiles = row_tiles * col_tiles, total = tiles * splits;
+    if (blockIdx.x >= total) return false;
+    const uint32_t x = blockIdx.x % kXcdCount, q = total / kXcdCount, r = total % kXcdCount;
+    uint32_t idx = x * q + (x < r ? x : r) + blockIdx.x / kXcdCount;
+    split = idx / tiles;
+    idx -= split * tiles;
     const uint32_t band = idx / (kBandTiles * col_tiles), in = idx - band * kBandTiles * col_tiles;
     const uint32_t left = row_tiles - band * kBandTiles, high = left < kBandTiles ? left : kBandTiles;
     row_tile = band * kBandTiles + in % high;
@@ -223,7 +246,7 @@ __device__ __forceinline__ bool tile_of_block(uint32_t block, uint32_t row_tiles
 }
 
 // The row tiles of all groups in order; every wave scans the groups' lengths for itself, 64 at a time.
-template <int BM> __device__ __forceinline__ bool place_rows(const ProductParams &p, uint32_t block, uint32_t col_tiles, Place &at, int BN)
+template <int BM> __device__ __forceinline__ bool place_rows(const ProductParams &p, uint32_t col_tiles, Place &at, int BN)
 {
     const uint32_t lane = threadIdx.x % 64;
     uint32_t total = 0, incl = 0, tiles = 0;
@@ -240,7 +263,7 @@ template <int BM> __device__ __forceinline__ bool place_rows(const ProductParams
     };
     for (uint32_t g0 = 0; g0 < p.groups; g0 += 64) total += scan(g0);
     uint32_t row_tile, col_tile;
-    if (!tile_of_block(block, __builtin_amdgcn_readfirstlane(total), col_tiles, row_tile, col_tile)) return false;
+    if (!tile_of_block(__builtin_amdgcn_readfirstlane(total), col_tiles, p.splits, row_tile, col_tile, at.split)) return false;
     uint32_t g0 = 0;
     if (p.groups > 64)
         for (;; g0 += 64) {
@@ -264,11 +287,11 @@ template <int BM> __device__ __forceinline__ bool place_rows(const ProductParams
     return true;
 }
 
-template <int BM> __device__ __forceinline__ bool place_weights(const ProductParams &p, uint32_t block, uint32_t col_tiles, Place &at, int BN)
+template <int BM> __device__ __forceinline__ bool place_weights(const ProductParams &p, uint32_t col_tiles, Place &at, int BN)
 {
     const uint32_t per = (p.m + BM - 1) / BM;
     uint32_t row_tile, col_tile;
-    if (!tile_of_block(block, per * p.groups, col_tiles, row_tile, col_tile)) return false;
+    if (!tile_of_block(per * p.groups, col_tiles, p.splits, row_tile, col_tile, at.split)) return false;
     at.group = row_tile / per;
     at.m0 = row_tile % per * BM;
     at.rows = p.m - at.m0 < BM ? p.m - at.m0 : BM;
@@ -295,34 +318,67 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     typedef Loader<T, HOW_A, A_KC, S::BM, S::BK, S::threads> LoadA;
     typedef Loader<T, HOW_B, B_KC, S::BN, S::BK, S::threads> LoadB;
     static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
-    static constexpr bool DIRECT = HOW_A == kDirect || HOW_B == kDirect;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
     static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 2 * (S::NB * 32 + 4) * 4;
-    static constexpr bool AHEAD = HOW_A == kDirect && HOW_B == kDirect;
     static constexpr int lds_bytes = 2 * stage > join_bytes ? 2 * stage : join_bytes;
 
-    // The pipeline of operands that go to LDS by themselves.  While the matrix cores work on one step of 16 terms (times WK), the fragments of the next
-    // step are read.  In front of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes
-    // the slice after the next one, which then has a whole slice's time to arrive; and the next slice, requested that long ago, is there, so
-    // that its first fragments are read beside the last step's products.
+    // The pipeline.  While the matrix cores work on one step of 16 terms (times WK), the fragments of the next step are read.  In front
+    // of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes the slice after the
+    // next one, which then has a whole slice's time to arrive; and the next slice, requested that long ago, is there, so that its first
+    // fragments are read beside the last step's products.  An operand that passes through registers is requested at the same place and
+    // put into LDS a step before the waves meet.
     static constexpr int STEPS = S::BK / 16 / S::WK;
-    struct Fragments { u4 a[S::MB], b[S::NB]; };
+    static_assert(STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
+    struct Fragments { u4 a[PA][S::MB], b[PB][S::NB]; };
+    typedef f16v Sums[SUMS][S::MB][S::NB];
+
     static __device__ __forceinline__ void read(Fragments &f, const uint8_t *lds, uint32_t k0, uint32_t wm, uint32_t wn, uint32_t lane)
     {
         #pragma unroll
-        for (int j = 0; j < S::NB; ++j) f.b[j] = LoadB::L::fragment(lds + LoadA::bytes, (wn * S::NB + j) * 32, k0, lane);
+        for (int pl = 0; pl < PB; ++pl)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) f.b[pl][j] = LoadB::L::fragment(lds + LoadA::bytes + pl * LoadB::L::bytes, (wn * S::NB + j) * 32, k0, lane);
         #pragma unroll
-        for (int i = 0; i < S::MB; ++i) f.a[i] = LoadA::L::fragment(lds, (wm * S::MB + i) * 32, k0, lane);
+        for (int pl = 0; pl < PA; ++pl)
+            #pragma unroll
+            for (int i = 0; i < S::MB; ++i) f.a[pl][i] = LoadA::L::fragment(lds + pl * LoadA::L::bytes, (wm * S::MB + i) * 32, k0, lane);
     }
-    // (fill is cur: a name of its own tells the compiler that reads need not wait for what is requested into it; the meeting of the
-    // waves keeps the reads of the old slice in front)
+
+    static __device__ __forceinline__ void multiply(const Fragments &f, Sums &acc)
+    {
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) {
+                acc[0][i][j] = T::mfma(f.b[0][j], f.a[0][i], acc[0][i][j]);
+                if constexpr (PB == 3) {
+                    f16v s = acc[1][i][j];
+                    if constexpr (PA == 3) {
+                        s = T::mfma(f.b[0][j], f.a[2][i], s);
+                        s = T::mfma(f.b[2][j], f.a[0][i], s);
+                        s = T::mfma(f.b[1][j], f.a[1][i], s);
+                        s = T::mfma(f.b[0][j], f.a[1][i], s);
+                    } else {
+                        s = T::mfma(f.b[2][j], f.a[0][i], s);
+                    }
+                    acc[1][i][j] = T::mfma(f.b[1][j], f.a[0][i], s);
+                }
+            }
+    }
+
+    // Step kk of the slice in `cur`.  (fill is cur: a name of its own tells the compiler that reads need not wait for what is requested into
+    // it; the meeting of the waves keeps the reads of the old slice in front.)  WHOLE: the slice that is requested needs no checks.
     template <bool WHOLE, int kk = 0>
-    static __device__ __forceinline__ void steps(const uint8_t *__restrict__ cur, const uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
-                                                 bool more, uint32_t k_fill, Fragments (&f)[2], f16v (&acc)[S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
+    static __device__ __forceinline__ void steps(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
+                                                 bool more, uint32_t k_fill, Fragments (&f)[2], Sums &acc, uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
                                                  uint32_t wave)
     {
         if constexpr (kk < STEPS) {
             constexpr bool LAST = kk + 1 == STEPS;
+            if constexpr (kk + 2 == STEPS) {
+                la.deliver(next);
+                lb.deliver(next + LoadA::bytes);
+            }
             if constexpr (LAST) {
                 slices_arrived<0>();
                 if constexpr (WHOLE) {
@@ -335,69 +391,21 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
             }
             if (LAST) read(f[0], next, wk * 16, wm, wn, lane);
             else      read(f[(kk + 1) % 2], cur, ((kk + 1) * S::WK + wk) * 16, wm, wn, lane);
-            #pragma unroll
-            for (int i = 0; i < S::MB; ++i)
-                #pragma unroll
-                for (int j = 0; j < S::NB; ++j) acc[i][j] = T::mfma(f[kk % 2].b[j], f[kk % 2].a[i], acc[i][j]);
+            multiply(f[kk % 2], acc);
             // the reads between the first products, so that the last of them has arrived when the next step begins, the requests beside them
-            constexpr int READS = S::MB * (A_KC ? 1 : 2) + S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB, PER = (READS + PRODUCTS - 1) / PRODUCTS;
-            constexpr int ASK = LAST && WHOLE ? (LoadA::N + LoadB::N + PRODUCTS - 1) / PRODUCTS : 0;
+            constexpr int READS = PA * S::MB * (A_KC ? 1 : 2) + PB * S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB * (PB == 1 ? 1 : PA == 3 ? 6 : 3);
+            constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, ASKED = LoadA::N * LoadA::RAW + LoadB::N * LoadB::RAW, ASK = LAST && WHOLE ? (ASKED + PRODUCTS - 1) / PRODUCTS : 0;
             #pragma unroll
             for (int r = 0; r < PRODUCTS; ++r) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                 if (r * PER < READS) __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
-                if constexpr (ASK > 0) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
+                if constexpr (ASK > 0) if (r * ASK < ASKED) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             steps<WHOLE, kk + 1>(cur, next, fill, la, lb, more, k_fill, f, acc, wm, wn, wk, lane, wave);
         }
     }
-
-    // multiply the slice in `cur` while the next one is requested into `next`
-    static __device__ __forceinline__ void slice(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, LoadA &la, LoadB &lb, bool more,
-                                                 uint32_t k_next, f16v (&acc)[SUMS][S::MB][S::NB], uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane)
-    {
-        if (more) { la.request(next, k_next); lb.request(next + LoadA::bytes, k_next); }
-        #pragma unroll
-        for (int kk = 0; kk < S::BK / 16 / S::WK; ++kk) {
-            const uint32_t k0 = (kk * S::WK + wk) * 16;
-            u4 fa[PA][S::MB], fb[PB][S::NB];
-            #pragma unroll
-            for (int pl = 0; pl < PA; ++pl)
-                #pragma unroll
-                for (int i = 0; i < S::MB; ++i) fa[pl][i] = LoadA::L::fragment(cur + pl * LoadA::L::bytes, (wm * S::MB + i) * 32, k0, lane);
-            #pragma unroll
-            for (int pl = 0; pl < PB; ++pl)
-                #pragma unroll
-                for (int j = 0; j < S::NB; ++j) fb[pl][j] = LoadB::L::fragment(cur + LoadA::bytes + pl * LoadB::L::bytes, (wn * S::NB + j) * 32, k0, lane);
-            #pragma unroll
-            for (int i = 0; i < S::MB; ++i)
-                #pragma unroll
-                for (int j = 0; j < S::NB; ++j) {
-                    acc[0][i][j] = T::mfma(fb[0][j], fa[0][i], acc[0][i][j]);
-                    if constexpr (PB == 3) {
-                        f16v s = acc[1][i][j];
-                        if constexpr (PA == 3) {
-                            s = T::mfma(fb[0][j], fa[2][i], s);
-                            s = T::mfma(fb[2][j], fa[0][i], s);
-                            s = T::mfma(fb[1][j], fa[1][i], s);
-                            s = T::mfma(fb[0][j], fa[1][i], s);
-                        } else {
-                            s = T::mfma(fb[2][j], fa[0][i], s);
-                        }
-                        acc[1][i][j] = T::mfma(fb[1][j], fa[0][i], s);
-                    }
-                }
-        }
-    }
 };
-
-// The slice that goes to LDS by itself has arrived (its loads count as vector memory, which a barrier alone need not wait for).
-template <bool DIRECT> __device__ __forceinline__ void slice_barrier()
-{
-    if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-}
 
 // Rows of a tile that lies within C, eight columns of a row per lane: what finish (below) does to four, with its decisions taken once.
 template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
@@ -416,7 +424,7 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         if (part) {
             const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
             pitch = p.ld_part * 4;
-            to = reinterpret_cast<char *>(p.part + (blockIdx.y * all + (WEIGHTS ? static_cast<uint64_t>(at.group) * p.m : 0) + local) * p.ld_part);
+            to = reinterpret_cast<char *>(p.part + (at.split * all + (WEIGHTS ? static_cast<uint64_t>(at.group) * p.m : 0) + local) * p.ld_part);
         } else {
             pitch = p.ldc * size;
             to = static_cast<char *>(p.out) + (WEIGHTS ? at.group * p.out_group * size : 0) + (p.out_row && !WEIGHTS ? 0 : local * pitch);
@@ -519,7 +527,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
     __shared__ __attribute__((aligned(16))) uint8_t lds[P::lds_bytes];
     Place at;
     const uint32_t col_tiles = (p.n + S::BN - 1) / S::BN;
-    if (!(WEIGHTS ? place_weights<S::BM>(p, blockIdx.x, col_tiles, at, S::BN) : place_rows<S::BM>(p, blockIdx.x, col_tiles, at, S::BN))) return;
+    if (!(WEIGHTS ? place_weights<S::BM>(p, col_tiles, at, S::BN) : place_rows<S::BM>(p, col_tiles, at, S::BN))) return;
 
     typedef typename T::elem elem;
     typename P::LoadA la;
@@ -549,48 +557,44 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
     uint32_t slices = (at.terms + S::BK - 1) / S::BK, slice0 = 0;
     if (p.splits > 1) {
         const uint32_t per = (slices + p.splits - 1) / p.splits;
-        slice0 = per * blockIdx.y < slices ? per * blockIdx.y : slices;
+        slice0 = per * at.split < slices ? per * at.split : slices;
         slices = slices - slice0 < per ? slices - slice0 : per;
     }
-    if constexpr (P::AHEAD) {
-        static_assert(P::STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
+    if (slices) {
         const uint32_t k0 = slice0 * S::BK;
-        #pragma unroll
-        for (uint32_t i = 0; i < 2; ++i)
-            if (i < slices) { la.request(lds + i * P::stage, k0 + i * S::BK); lb.request(lds + i * P::stage + P::LoadA::bytes, k0 + i * S::BK); }
+        la.request(lds, k0);
+        lb.request(lds + P::LoadA::bytes, k0);
+        la.deliver(lds);
+        lb.deliver(lds + P::LoadA::bytes);
+        if (slices > 1) {
+            la.request(lds + P::stage, k0 + S::BK);
+            lb.request(lds + P::stage + P::LoadA::bytes, k0 + S::BK);
+        }
         typename P::Fragments f[2];
-        if (slices > 1) slices_arrived<P::LoadA::N + P::LoadB::N>(); else slices_arrived<0>();
+        if (HOW_A == kDirect && HOW_B == kDirect && slices > 1) slices_arrived<P::LoadA::N + P::LoadB::N>(); else slices_arrived<0>();
         P::read(f[0], lds, wk * 16, wm, wn, lane);
         // (keeps the compiler from joining these reads with the loop's last ones at the head of the loop, where nothing hides them)
         #pragma unroll
-        for (int i = 0; i < S::MB; ++i) asm volatile("" : "+v"(f[0].a[i]));
+        for (int pl = 0; pl < P::PA; ++pl)
+            #pragma unroll
+            for (int i = 0; i < S::MB; ++i) asm volatile("" : "+v"(f[0].a[pl][i]));
         #pragma unroll
-        for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[j]));
+        for (int pl = 0; pl < P::PB; ++pl)
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[pl][j]));
         uint32_t t = 0;
-        for (; t + 2 < slices && k0 + (t + 3) * S::BK <= at.terms; ++t) {
-            uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
-            P::template steps<true>(cur, next, cur, la, lb, true, k0 + (t + 2) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
-        }
+        if (la.fits && lb.fits)
+            for (; t + 2 < slices && k0 + (t + 3) * S::BK <= at.terms; ++t) {
+                uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
+                P::template steps<true>(cur, next, cur, la, lb, true, k0 + (t + 2) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            }
         #pragma unroll 1
         for (; t < slices; ++t) {
             uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
-            P::template steps<false>(cur, next, cur, la, lb, t + 2 < slices, k0 + (t + 2) * S::BK, f, acc[0], wm, wn, wk, lane, wave);
+            P::template steps<false>(cur, next, cur, la, lb, t + 2 < slices, k0 + (t + 2) * S::BK, f, acc, wm, wn, wk, lane, wave);
         }
-        slices_arrived<0>();
-    } else {
-    if (slices) {
-        la.request(lds, slice0 * S::BK); lb.request(lds + P::LoadA::bytes, slice0 * S::BK);
-        la.deliver(lds); lb.deliver(lds + P::LoadA::bytes);
     }
-    slice_barrier<P::DIRECT>();
-    for (uint32_t t = 0; t < slices; ++t) {
-        uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
-        const bool more = t + 1 < slices;
-        P::slice(cur, next, la, lb, more, (slice0 + t + 1) * S::BK, acc, wm, wn, wk, lane);
-        if (more) { la.deliver(next); lb.deliver(next + P::LoadA::bytes); }
-        slice_barrier<P::DIRECT>();
-    }
-    }
+    slices_arrived<0>();                                       // LDS is free
 
     float unscale = 1.0f;
     if constexpr (P::PB == 3) {
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             const uint64_t row = WEIGHTS ? static_cast<uint64_t>(at.group) * p.m + at.m0 + r : at.row0 + r;
             if (p.splits > 1) {
                 const uint64_t all = WEIGHTS ? static_cast<uint64_t>(p.groups) * p.m : p.rows;
-                *reinterpret_cast<f4 *>(p.part + (blockIdx.y * all + row) * p.ld_part + c) = v;
+                *reinterpret_cast<f4 *>(p.part + (at.split * all + row) * p.ld_part + c) = v;
             } else {
                 finish_quad<T, WEIGHTS>(p, at.group, row, at.m0 + r, c, v, factor);
             }
@@ -655,14 +659,14 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
 
     if constexpr (S::WK > 1) {
         // the waves' sums over their terms meet in LDS, row by row, in the order of the waves
-        static_assert(S::WM == 1 && S::WN == 1 && S::MB == 1, "waves share the terms of one tile");
+        static_assert(S::WM == 1 && S::MB == 1, "waves share the terms of 32 rows");
         constexpr int PITCH = S::BN + 4, LANES = S::BN / 4;
         float *part = reinterpret_cast<float *>(lds);
         #pragma unroll
         for (int j = 0; j < S::NB; ++j)
             #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<f4 *>(part + (wk * S::BM + lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) =
+                *reinterpret_cast<f4 *>(part + (wk * S::BM + lane % 32) * PITCH + (wn * S::NB + j) * 32 + 8 * g + 4 * (lane / 32)) =
                     f4{acc[0][0][j][4 * g], acc[0][0][j][4 * g + 1], acc[0][0][j][4 * g + 2], acc[0][0][j][4 * g + 3]};
         __syncthreads();
         #pragma unroll
@@ -781,9 +785,9 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
 {
     const uint64_t col_tiles = (p.n + S::BN - 1) / S::BN;
     const uint64_t row_tiles = LAYOUT == Layout::Weights ? static_cast<uint64_t>(p.groups) * ((p.m + S::BM - 1) / S::BM) : p.rows / S::BM + p.groups;
-    const uint64_t blocks = row_tiles * col_tiles;
+    const uint64_t blocks = row_tiles * col_tiles * p.splits;
     if (blocks * S::threads >= (1ull << 32)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((product_kernel<T, LAYOUT, S, FINISH, HOW_A, HOW_B>), dim3(static_cast<uint32_t>(blocks), p.splits), dim3(S::threads), 0, stream, p);
+    hipLaunchKernelGGL((product_kernel<T, LAYOUT, S, FINISH, HOW_A, HOW_B>), dim3(static_cast<uint32_t>(blocks)), dim3(S::threads), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -791,7 +795,7 @@ typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
-typedef TileShape<32, 64, 64, 1, 1, 4> Small32;
+typedef TileShape<32, 64, 64, 1, 2, 2> Small32;
 
 template <class T, Layout LAYOUT, Finish FINISH>
 hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
@@ -807,6 +811,7 @@ hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
         const bool b_direct = direct_b(LAYOUT, p);
         if constexpr (WEIGHTS)
             if (!p.a) {
+                if (b_direct && tile == Tile::Large) return launch_one<T, LAYOUT, Large16, FINISH, kCodes, kDirect>(stream, p);
                 if (b_direct) return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kDirect>(stream, p)
                                                          : launch_one<T, LAYOUT, Medium16, FINISH, kCodes, kDirect>(stream, p);
                 return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kRegs>(stream, p)
