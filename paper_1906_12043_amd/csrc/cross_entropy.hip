@@ -40,9 +40,11 @@ __device__ __forceinline__ bool has_target(const Rows &p, uint64_t r)
     return static_cast<uint32_t>(p.target[r]) < p.vocab;          // negative ones are large
 }
 
-// One block per group: the rows with a target, in order, to the front of the group's part of `index`; kNoRow behind them.
+// One block per group: the rows with a target, in order, to the front of the group's part of `index`; kNoRow behind them.  And every such row's
+// gradient factor.
 constexpr int kCompactThreads = 1024;
-__global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, uint32_t *index, int32_t *target, int64_t *ends)
+__global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, uint32_t *index, int32_t *target, int64_t *ends, int sum_only, float scale,
+                                                                  float *row_scale)
 {
     __shared__ uint32_t counts[kCompactThreads / 64];
     const uint32_t g = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -65,6 +67,8 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, 
         __syncthreads();
     }
     for (uint64_t r = at + threadIdx.x; r < end; r += kCompactThreads) index[r] = kNoRow;
+    const float factor = sum_only ? scale : scale / static_cast<float>(at - begin);
+    for (uint64_t r = begin + threadIdx.x; r < at; r += kCompactThreads) row_scale[r] = factor;
     if (threadIdx.x == 0) ends[g] = static_cast<int64_t>(at);
 }
 
@@ -93,59 +97,63 @@ template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Ro
     }
 }
 
-// norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss.  64 rows per block,
-// four threads a row.
-__global__ __launch_bounds__(256) void norm_kernel(const Rows p, const uint32_t *index, const float2 *stats, uint32_t tiles, const float *target_logit,
-                                                   float *norm, float *loss)
+// norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss, also in the place of the
+// target's logit.  Sixteen rows per block, sixteen threads a row.
+constexpr int kNormRows = 16, kNormThreads = 16, kNormAhead = 4;
+__device__ __forceinline__ void add_part(float &top, float &sum, float2 s)
 {
-    __shared__ float2 part[4][64];
-    const uint32_t x = threadIdx.x % 64, y = threadIdx.x / 64;
-    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * 64 + x;
+    const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
+    sum = sum * expf(top - base) + s.y * expf(s.x - base);
+    top = m;
+}
+__global__ __launch_bounds__(kNormRows * kNormThreads) void norm_kernel(const Rows p, const uint32_t *index, const float2 *stats, uint32_t tiles, float *target_logit,
+                                                                        float *norm, float *loss)
+{
+    __shared__ float2 part[kNormThreads][kNormRows];
+    const uint32_t x = threadIdx.x % kNormRows, y = threadIdx.x / kNormRows;
+    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * kNormRows + x;
     const bool in = r >= clamped(p, 0) && r < clamped(p, p.groups) && index[r] != kNoRow;
     float top = -INFINITY, sum = 0.0f;
     if (in) {
-        for (uint32_t t = y; t < tiles; t += 4) {
-            const float2 s = stats[t * p.rows + r];
-            const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
-            sum = sum * expf(top - base) + s.y * expf(s.x - base);
-            top = m;
+        for (uint32_t t = y; t < tiles; t += kNormThreads * kNormAhead) {
+            float2 s[kNormAhead];
+            #pragma unroll
+            for (int i = 0; i < kNormAhead; ++i) {
+                const uint32_t u = t + i * kNormThreads;
+                s[i] = u < tiles ? stats[u * p.rows + r] : make_float2(-INFINITY, 0.0f);
+            }
+            #pragma unroll
+            for (int i = 0; i < kNormAhead; ++i) add_part(top, sum, s[i]);
         }
     }
     part[y][x] = make_float2(top, sum);
     __syncthreads();
     if (y != 0 || !in) return;
     #pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        const float2 s = part[w][x];
-        const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
-        sum = sum * expf(top - base) + s.y * expf(s.x - base);
-        top = m;
-    }
+    for (int w = 1; w < kNormThreads; ++w) add_part(top, sum, part[w][x]);
     const float n = top + logf(sum);
     norm[r] = n;
-    loss[index[r]] = n - target_logit[r];
+    const float l = n - target_logit[r];
+    target_logit[r] = l;
+    loss[index[r]] = l;
 }
 
-// One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits, and every row's gradient factor.
-__global__ __launch_bounds__(256) void mean_kernel(const Rows p, const uint32_t *index, const int64_t *ends, const float *loss, float *group_loss, int sum_only,
-                                                   float scale, float *row_scale)
+// One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits.
+constexpr int kMeanThreads = 1024;
+__global__ __launch_bounds__(kMeanThreads) void mean_kernel(const Rows p, const int64_t *ends, const float *loss, float *group_loss, int sum_only)
 {
-    __shared__ double part[256];
+    __shared__ double part[kMeanThreads];
     const uint32_t g = blockIdx.x;
     const uint64_t begin = clamped(p, g), end = static_cast<uint64_t>(ends[g]);
-    const float n = static_cast<float>(end - begin);
     double s = 0.0;
-    for (uint64_t r = begin + threadIdx.x; r < end; r += 256) {
-        if (index[r] != kNoRow) s += loss[index[r]];             // (offsets that do not ascend may leave holes)
-        row_scale[r] = sum_only ? scale : scale / n;
-    }
+    for (uint64_t r = begin + threadIdx.x; r < end; r += kMeanThreads) s += loss[r];
     part[threadIdx.x] = s;
     __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
+    for (int d = kMeanThreads / 2; d > 0; d >>= 1) {
         if (static_cast<int>(threadIdx.x) < d) part[threadIdx.x] += part[threadIdx.x + d];
         __syncthreads();
     }
-    if (threadIdx.x == 0 && group_loss) group_loss[g] = static_cast<float>(end > begin ? (sum_only ? part[0] : part[0] / static_cast<double>(end - begin)) : 0.0);
+    if (threadIdx.x == 0) group_loss[g] = static_cast<float>(end > begin ? (sum_only ? part[0] : part[0] / static_cast<double>(end - begin)) : 0.0);
 }
 
 // The caller's memory, carved up.
@@ -279,7 +287,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     const float unslope = t == Dtype::F16 ? 0x1p-14f : 1.0f;   // fp16 slopes are kept times 2^14
     const int sum_only = (c->flags & COCOD_CROSS_ENTROPY_SUM) != 0;
 
-    hipLaunchKernelGGL(compact_kernel, dim3(c->groups), dim3(kCompactThreads), 0, q, rows, index, target, ends);
+    hipLaunchKernelGGL(compact_kernel, dim3(c->groups), dim3(kCompactThreads), 0, q, rows, index, target, ends, sum_only, c->grad_scale * unslope, row_scale);
     if (c->rows) {
         const hipError_t e = t == Dtype::F32 ? launch_gather<float>(q, rows, index, c, ws + w.hidden, w.pitch) : launch_gather<uint16_t>(q, rows, index, c, ws + w.hidden, w.pitch);
         if (e != hipSuccess) return launch_status(e, what);
@@ -297,9 +305,10 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
         const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, p);
         if (int rc = launch_status(launch_logits(q, t, Finish::Stats, tile, p), what)) return rc;
         const uint32_t tiles = (c->vocab + tile_cols(t, tile) - 1) / tile_cols(t, tile);
-        hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + 63) / 64)), dim3(256), 0, q, rows, index, p.stats, tiles, p.target_logit, norm, c->loss);
+        hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + kNormRows - 1) / kNormRows)), dim3(kNormRows * kNormThreads), 0, q, rows, index, p.stats, tiles, p.target_logit, norm, c->loss);
     }
-    hipLaunchKernelGGL(mean_kernel, dim3(c->groups), dim3(256), 0, q, rows, index, ends, c->loss, c->group_loss, sum_only, c->grad_scale * unslope, row_scale);
+    if (c->group_loss)
+        hipLaunchKernelGGL(mean_kernel, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, ends, reinterpret_cast<const float *>(ws + w.target_logit), c->group_loss, sum_only);
     if (int rc = launch_status(hipGetLastError(), what)) return rc;
     if (!c->dh && !c->de) return COCOD_OK;
 

@@ -50,7 +50,7 @@ hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const Prod
 // 1024: 33 (1) / 26 (1) / 50 (1); 16 of 500 rows, 2048 x 1024, input gradient: 40 (1) / 47 (1) / 93 (1); 4 of 768 rows, 32000 x 1024: 239 (4) / 266 (8) /
 // 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); fp32 4 of 250 rows, 512 x 768: - / 25 (4) / 17 (1); one of 2048 rows, 2048 x 2048: - / 130 (1) / 180 (1).
 struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile; };
-constexpr TileCost kCost16[] = {{256, 256, 64, 1.36, 3.9}, {128, 128, 64, 0.45, 1.2}, {32, 64, 128, 0.27, 0.4}};
+constexpr TileCost kCost16[] = {{256, 256, 64, 1.36, 3.9}, {128, 128, 64, 0.5, 1.2}, {32, 64, 128, 0.27, 0.4}};
 constexpr TileCost kCost32[] = {{0, 0, 0, 0, 0}, {128, 128, 32, 1.73, 3.5}, {32, 64, 64, 0.62, 1.2}};
 constexpr uint32_t kMaxSplits = 16;
 

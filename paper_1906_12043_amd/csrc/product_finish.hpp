@@ -26,6 +26,8 @@ typedef u2 __attribute__((aligned(1))) u2_any;
 // and the tile is formed again with fp32 products.
 constexpr float kPlaneScale = 0x1p24f, kPlaneUnscale = 0x1p-48f;
 
+constexpr float kLog2e = 1.44269504f;
+
 struct Bf16 {
     typedef uint16_t elem;
     static constexpr Dtype dtype = Dtype::BF16;
@@ -35,7 +37,8 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, bf2)); }
-    static __device__ __forceinline__ float exp(float x) { return __expf(x); }
+    // e^(x - base): one rounding of the exponent, which is off by 2^-24 of |x| and |base|
+    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -kLog2e * base)); }
     static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
     {
         return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true))
@@ -51,7 +54,8 @@ struct F16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, hf2)); }
-    static __device__ __forceinline__ float exp(float x) { return __expf(x); }
+    // e^(x - base): one rounding of the exponent, which is off by 2^-24 of |x| and |base|
+    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -kLog2e * base)); }
     static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
     {
         return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, scale, true))
@@ -62,7 +66,7 @@ struct F32 : Bf16 {
     typedef float elem;
     static constexpr Dtype dtype = Dtype::F32;
     static constexpr int planes = 3;
-    static __device__ __forceinline__ float exp(float x) { return expf(x); }     // __expf is off by |x| 2^-24
+    static __device__ __forceinline__ float exp(float x, float base) { return expf(x - base); }
 };
 
 __device__ __forceinline__ uint64_t bound_at(const ProductParams &p, uint32_t i)

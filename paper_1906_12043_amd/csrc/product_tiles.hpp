@@ -329,6 +329,8 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     // put into LDS a step before the waves meet.
     static constexpr int STEPS = S::BK / 16 / S::WK;
     static_assert(STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
+    // where both operands pass through registers, these are free for the next request as soon as they are in LDS
+    static constexpr bool EARLY = HOW_A != kDirect && HOW_B != kDirect;
     struct Fragments { u4 a[PA][S::MB], b[PB][S::NB]; };
     typedef f16v Sums[SUMS][S::MB][S::NB];
 
@@ -379,8 +381,8 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
                 la.deliver(next);
                 lb.deliver(next + LoadA::bytes);
             }
-            if constexpr (LAST) {
-                slices_arrived<0>();
+            if constexpr (LAST) slices_arrived<EARLY ? 63 : 0>();
+            if constexpr (EARLY ? kk + 2 == STEPS : LAST) {
                 if constexpr (WHOLE) {
                     la.request_whole(fill, k_fill, wave);
                     lb.request_whole(fill + LoadA::bytes, k_fill, wave);
@@ -394,7 +396,7 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
             multiply(f[kk % 2], acc);
             // the reads between the first products, so that the last of them has arrived when the next step begins, the requests beside them
             constexpr int READS = PA * S::MB * (A_KC ? 1 : 2) + PB * S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB * (PB == 1 ? 1 : PA == 3 ? 6 : 3);
-            constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, ASKED = LoadA::N * LoadA::RAW + LoadB::N * LoadB::RAW, ASK = LAST && WHOLE ? (ASKED + PRODUCTS - 1) / PRODUCTS : 0;
+            constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, ASKED = LoadA::N * LoadA::RAW + LoadB::N * LoadB::RAW, ASK = (EARLY ? kk + 2 == STEPS : LAST) && WHOLE ? (ASKED + PRODUCTS - 1) / PRODUCTS : 0;
             #pragma unroll
             for (int r = 0; r < PRODUCTS; ++r) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
@@ -444,8 +446,8 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         const uint64_t my_row = at.row0 + mine;
         float row_factor = factor;
         uint32_t row_number = 0;
-        bool is_in = mine < at.rows;
-        if (!WEIGHTS && !part && is_in) {
+        const bool by_row = !WEIGHTS && !part && (FINISH == Finish::Slope || p.row_scale || p.out_row);
+        if (by_row && mine < at.rows) {
             if (FINISH == Finish::Slope) { row_factor = p.norm[my_row]; row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
             if (FINISH == Finish::Store && p.row_scale) row_factor = p.row_scale[my_row];
             if (FINISH == Finish::Store && p.out_row) row_number = p.out_row[my_row];
@@ -453,18 +455,21 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         #pragma unroll 4
         for (uint32_t k = 0; k < 32; k += PASS) {
             const uint32_t r = k + first;
-            const float f = WEIGHTS ? factor : __shfl(row_factor, r, 64);
-            const uint32_t number = WEIGHTS ? 0 : __shfl(row_number, r, 64);
+            const float f = by_row ? __shfl(row_factor, r, 64) : factor;
+            const uint32_t number = by_row ? __shfl(row_number, r, 64) : 0;
             f4 a = *reinterpret_cast<const f4 *>(v + r * PITCH), b = *reinterpret_cast<const f4 *>(v + r * PITCH + 4);
             if (r0 + r >= at.rows) continue;
             const uint64_t row = at.row0 + r0 + r;
             char *at_row = to + static_cast<uint64_t>(r0 + r) * pitch;
             if constexpr (FINISH == Finish::Slope) {
                 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    a[j] = (T::exp(a[j] - f) - (c + j == number ? 1.0f : 0.0f)) * slope_scale<T>();
-                    b[j] = (T::exp(b[j] - f) - (c + 4 + j == number ? 1.0f : 0.0f)) * slope_scale<T>();
+                for (uint32_t j = 0; j < 4; ++j) { a[j] = T::exp(a[j], f); b[j] = T::exp(b[j], f); }
+                if (number - c < 8) {                          // the target is one of these columns
+                    #pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) { if (number - c == j) a[j] -= 1.0f; if (number - c == 4 + j) b[j] -= 1.0f; }
                 }
+                a *= slope_scale<T>();
+                b *= slope_scale<T>();
             } else if (!part) {
                 if (!WEIGHTS) {
                     if (p.out_row) { if (number == kNoRow) continue; at_row = to + number * pitch; }
@@ -650,7 +655,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             const int32_t target = p.target[at.row0 + r];
             #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = (T::exp(v[j] - norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
+                v[j] = (T::exp(v[j], norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
                 if (c + j >= p.n) v[j] = 0.0f;
             }
             store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
@@ -689,7 +694,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 #pragma unroll
                 for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
                 const float base = top == -INFINITY ? 0.0f : top;
-                float sum = (T::exp(v[0] - base) + T::exp(v[1] - base)) + (T::exp(v[2] - base) + T::exp(v[3] - base));
+                float sum = (T::exp(v[0], base) + T::exp(v[1], base)) + (T::exp(v[2], base) + T::exp(v[3], base));
                 #pragma unroll
                 for (int d = 1; d < LANES; d <<= 1) sum += __shfl_xor(sum, d, 64);
                 if (q == 0 && r < at.rows) p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
@@ -729,7 +734,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) {
                 #pragma unroll
-                for (int x = 0; x < 16; ++x) sum += T::exp(acc[0][i][j][x] * unscale - base);
+                for (int x = 0; x < 16; ++x) sum += T::exp(acc[0][i][j][x] * unscale, base);
                 __builtin_amdgcn_sched_barrier(0);
             }
             sum += __shfl_xor(sum, 32, 64);
@@ -745,7 +750,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int w = 0; w < S::WN; ++w) {
                 const float2 s = share[w * S::BM + r];
-                sum += s.y * T::exp(s.x - base);               // (a part without columns: 0 times 0; a NaN stays one)
+                sum += s.y * T::exp(s.x, base);               // (a part without columns: 0 times 0; a NaN stays one)
             }
             p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
         }
@@ -794,7 +799,7 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
 typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
-typedef TileShape<128, 128, 32, 2, 2, 1> Medium32;
+typedef TileShape<128, 128, 32, 2, 4, 1> Medium32;
 typedef TileShape<32, 64, 64, 1, 2, 2> Small32;
 
 template <class T, Layout LAYOUT, Finish FINISH>
