@@ -20,6 +20,7 @@ typedef float v2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s4 lds_s4;
 typedef u4 __attribute__((aligned(2))) u4_any;       // 16 bytes at any element's address
 typedef u2 __attribute__((aligned(1))) u2_any;
+typedef u4 __attribute__((aligned(1))) u4_bytes;
 
 // fp32 operands go in as three bf16 planes, exactly (8 + 8 + 8 bits), times 2^24 so that the last bit of the smallest numbers is
 // a normal bf16 too; sums come out times 2^48.  Where that leaves the range, or an operand is not finite, the sum is not finite,

@@ -62,8 +62,10 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
     typedef LdsTile<KC, BX, BK> L;
     typedef typename T::elem elem;
     static constexpr int planes = HOW == kCodes ? 1 : T::planes;
-    static constexpr int N = L::ROWS * L::CH / THREADS;             // 16-byte chunks per thread
-    static_assert(N >= 1 && N * THREADS == L::ROWS * L::CH, "whole chunks per thread");
+    static constexpr int CHUNKS = L::ROWS * L::CH / THREADS;        // 16-byte chunks of LDS per thread
+    static_assert(CHUNKS >= 1 && CHUNKS * THREADS == L::ROWS * L::CH, "whole chunks per thread");
+    static constexpr int W = HOW == kCodes && CHUNKS % 2 == 0 ? 2 : 1;   // chunks per load: sixteen codes are two
+    static constexpr int N = CHUNKS / W;                            // loads per thread
     static constexpr int bytes = planes * L::bytes;
     static constexpr int RAW = HOW == kDirect ? 1 : (sizeof(elem) == 4 && HOW == kRegs ? 2 : 1);
 
@@ -75,48 +77,50 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
     uint32_t k_end;                   // end of the summed axis
     u4 raw[HOW == kDirect ? 1 : N][RAW];
     float sc[HOW == kCodes ? N : 1];
-    uint32_t off[HOW == kDirect ? N : 1];
+    uint32_t off[N], scale_off[HOW == kCodes ? N : 1];      // of a thread's chunks in a slice (bytes / elements / codes; scales)
 
     bool fits;                        // every chunk of a slice within the sum lies within the operand
 
-    __device__ __forceinline__ static uint32_t chunk(int i) { return i * THREADS + threadIdx.x; }
+    // load i of this thread: row of the tile, first chunk (pairs of chunks stay side by side in LDS)
+    __device__ __forceinline__ static uint32_t row_of(int i) { return (i * THREADS + threadIdx.x) / (L::CH / W); }
+    __device__ __forceinline__ static uint32_t place_of(int i) { return (i * THREADS + threadIdx.x) * W; }
+    __device__ __forceinline__ static uint32_t chunk_of(int i) { return (place_of(i) % L::CH) ^ L::swizzle(row_of(i)); }
+    static_assert(W == 1 || !KC, "the permutation of whole pairs");
 
     __device__ __forceinline__ void start()
     {
         // rows (direct: chunks of columns, too) past the end repeat the last one: their products are not stored
-        fits = HOW == kDirect || KC || x0 + BX <= x_end;
-        if constexpr (HOW == kDirect) {
-            #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
-                if (KC) { const uint32_t last = x_end - 1 - x0; row = row < last ? row : last; }
-                else    { const uint32_t last = (x_end - 1 - x0) / 8; c = c < last ? c : last; }
-                off[i] = (row * static_cast<uint32_t>(ld) + c * 8) * 2;
+        const uint64_t pitch = HOW == kCodes ? ld_codes : ld;
+        fits = HOW == kDirect || ((KC || x0 + BX <= x_end) && pitch <= (1u << 22) && (HOW != kCodes || ld_scales <= (1u << 22)));
+        #pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t row = row_of(i), c = chunk_of(i);
+            if (KC) { const uint32_t last = x_end - 1 - x0; row = row < last ? row : last; }
+            else if (HOW == kDirect) { const uint32_t last = (x_end - 1 - x0) / 8; c = c < last ? c : last; }
+            off[i] = (row * static_cast<uint32_t>(pitch) + c * 8) * (HOW == kDirect ? 2 : 1);
+            if constexpr (HOW == kCodes) {
+                static_assert(!KC && BX % 32 == 0, "codes of whole blocks, rows summed over");
+                scale_off[i] = row * static_cast<uint32_t>(ld_scales) + c / 4;
             }
         }
     }
 
-    // request the slice that begins at term k0
-    __device__ __forceinline__ void request(uint8_t *lds, uint32_t k0)
+    // request the slice that begins at term k0, zeros behind the sum's end
+    __device__ __forceinline__ void request(uint8_t *lds, uint32_t k0, uint32_t wave)
     {
         if constexpr (HOW == kDirect) {
             const char *base = reinterpret_cast<const char *>(src) + 2 * (KC ? static_cast<uint64_t>(x0) * ld + k0 : static_cast<uint64_t>(k0) * ld + x0);
-            const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-            const bool whole = k0 + BK <= k_end;
             #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const char *from = base + off[i];
-                if (!whole) {
-                    const uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
-                    if (k0 + (KC ? c * 8 : row) >= k_end) from = reinterpret_cast<const char *>(kZeroChunk);
-                }
+                const uint32_t row = row_of(i), c = chunk_of(i);
+                const char *from = k0 + (KC ? c * 8 : row) < k_end ? base + off[i] : reinterpret_cast<const char *>(kZeroChunk);
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                                  (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
             }
         } else {
             #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t row = chunk(i) / L::CH, c = (chunk(i) % L::CH) ^ L::swizzle(row);
+                const uint32_t row = row_of(i), c = chunk_of(i);
                 const uint32_t r = (KC ? x0 : k0) + row, r_end = KC ? x_end : k_end, q = (KC ? k0 : x0) + c * 8, q_end = KC ? k_end : x_end;
                 #pragma unroll
                 for (int j = 0; j < RAW; ++j) raw[i][j] = zero4();
@@ -125,16 +129,11 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                     if constexpr (HOW == kCodes) {
                         const uint8_t *at = codes + r * ld_codes + q;
                         sc[i] = __uint_as_float(static_cast<unsigned>(scales[r * ld_scales + q / 32]) << 23);
-                        if (q + 8 <= q_end) {
-                            const u2 v = *reinterpret_cast<const u2_any *>(at);
-                            raw[i][0] = u4{v.x, v.y, 0, 0};
-                        } else {
-                            u4 v = zero4();
-                            #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (q + e < q_end) v[e / 4] |= static_cast<unsigned>(at[e]) << (8 * (e % 4));
-                            raw[i][0] = v;
-                        }
+                        u4 v = zero4();
+                        #pragma unroll
+                        for (int e = 0; e < 8 * W; ++e)
+                            if (q + e < q_end) v[e / 4] |= static_cast<unsigned>(at[e]) << (8 * (e % 4));
+                        raw[i][0] = v;
                     } else {
                         const elem *at = src + r * ld + q;
                         if (q + 8 <= q_end) {
@@ -164,22 +163,30 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
                                                  (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
         } else {
+            const uint64_t r = KC ? x0 : k0, q = KC ? k0 : x0;
             #pragma unroll
             for (int i = 0; i < N; ++i) {
-                uint32_t row = chunk(i) / L::CH;
-                const uint32_t c = (chunk(i) % L::CH) ^ L::swizzle(row), last = x_end - 1 - x0;
-                if (KC) row = row < last ? row : last;
-                const uint64_t r = (KC ? x0 : k0) + row, q = (KC ? k0 : x0) + c * 8;
                 if constexpr (HOW == kCodes) {
-                    const u2 v = *reinterpret_cast<const u2_any *>(codes + r * ld_codes + q);
-                    raw[i][0] = u4{v.x, v.y, 0, 0};
-                    sc[i] = __uint_as_float(static_cast<unsigned>(scales[r * ld_scales + q / 32]) << 23);
+                    const uint8_t *at = codes + r * ld_codes + q + off[i];
+                    if constexpr (W == 2) {
+                        raw[i][0] = *reinterpret_cast<const u4_bytes *>(at);
+                    } else {
+                        const u2 v = *reinterpret_cast<const u2_any *>(at);
+                        raw[i][0] = u4{v.x, v.y, 0, 0};
+                    }
+                    sc[i] = __uint_as_float(static_cast<unsigned>((scales + r * ld_scales + q / 32)[scale_off[i]]) << 23);
                 } else {
                     #pragma unroll
-                    for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(src + r * ld + q)[j];
+                    for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(src + r * ld + q + off[i])[j];
                 }
             }
         }
+    }
+
+    __device__ __forceinline__ void ask(uint8_t *lds, uint32_t k0, uint32_t wave)
+    {
+        if (fits && k0 + BK <= k_end) request_whole(lds, k0, wave);
+        else                          request(lds, k0, wave);
     }
 
     // put the requested slice into LDS
@@ -188,10 +195,12 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
         if constexpr (HOW == kDirect) return;
         #pragma unroll
         for (int i = 0; i < N; ++i) {
-            uint8_t *at = lds + chunk(i) * 16;
+            uint8_t *at = lds + place_of(i) * 16;
             if constexpr (HOW == kCodes) {
-                *reinterpret_cast<u4 *>(at) = u4{T::codes(raw[i][0].x, sc[i], false), T::codes(raw[i][0].x, sc[i], true),
-                                                 T::codes(raw[i][0].y, sc[i], false), T::codes(raw[i][0].y, sc[i], true)};
+                #pragma unroll
+                for (int w = 0; w < W; ++w)
+                    reinterpret_cast<u4 *>(at)[w] = u4{T::codes(raw[i][0][2 * w], sc[i], false), T::codes(raw[i][0][2 * w], sc[i], true),
+                                                       T::codes(raw[i][0][2 * w + 1], sc[i], false), T::codes(raw[i][0][2 * w + 1], sc[i], true)};
             } else if constexpr (T::planes == 1) {
                 *reinterpret_cast<u4 *>(at) = raw[i][0];
             } else {
@@ -387,8 +396,8 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
                     la.request_whole(fill, k_fill, wave);
                     lb.request_whole(fill + LoadA::bytes, k_fill, wave);
                 } else if (more) {
-                    la.request(fill, k_fill);
-                    lb.request(fill + LoadA::bytes, k_fill);
+                    la.ask(fill, k_fill, wave);
+                    lb.ask(fill + LoadA::bytes, k_fill, wave);
                 }
             }
             if (LAST) read(f[0], next, wk * 16, wm, wn, lane);
@@ -567,13 +576,13 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
     }
     if (slices) {
         const uint32_t k0 = slice0 * S::BK;
-        la.request(lds, k0);
-        lb.request(lds + P::LoadA::bytes, k0);
+        la.ask(lds, k0, wave);
+        lb.ask(lds + P::LoadA::bytes, k0, wave);
         la.deliver(lds);
         lb.deliver(lds + P::LoadA::bytes);
         if (slices > 1) {
-            la.request(lds + P::stage, k0 + S::BK);
-            lb.request(lds + P::stage + P::LoadA::bytes, k0 + S::BK);
+            la.ask(lds + P::stage, k0 + S::BK, wave);
+            lb.ask(lds + P::stage + P::LoadA::bytes, k0 + S::BK, wave);
         }
         typename P::Fragments f[2];
         if (HOW_A == kDirect && HOW_B == kDirect && slices > 1) slices_arrived<P::LoadA::N + P::LoadB::N>(); else slices_arrived<0>();
