@@ -40,11 +40,42 @@ __device__ __forceinline__ bool has_target(const Rows &p, uint64_t r)
     return static_cast<uint32_t>(p.target[r]) < p.vocab;          // negative ones are large
 }
 
+// A row's gathered copy (pitch a multiple of 8, zeros behind dim) by the lanes of a wave.
+template <class E> struct Hidden {
+    const E *h;
+    uint64_t ldh;
+    uint32_t dim;
+    E *out;
+    uint64_t pitch;
+    float *loss;
+    E *dh;                            // may be null
+    uint64_t lddh;
+};
+template <class E> __device__ __forceinline__ void gather_row(const Hidden<E> &p, uint64_t r, uint32_t from, uint32_t lane)
+{
+    const E *src = p.h + from * p.ldh;
+    E *dst = p.out + r * p.pitch;
+    constexpr uint32_t V = 16 / sizeof(E);
+    if ((reinterpret_cast<uintptr_t>(src) & 15) == 0 && p.dim % V == 0) {
+        for (uint32_t j = lane * V; j < p.dim; j += 64 * V) *reinterpret_cast<float4 *>(dst + j) = *reinterpret_cast<const float4 *>(src + j);
+        for (uint32_t j = p.dim + lane; j < p.pitch; j += 64) dst[j] = 0;
+    } else {
+        for (uint32_t j = lane; j < p.pitch; j += 64) dst[j] = j < p.dim ? src[j] : E(0);
+    }
+}
+// A row without a target: loss 0, gradient 0.
+template <class E> __device__ __forceinline__ void clear_row(const Hidden<E> &p, uint64_t r, uint32_t lane)
+{
+    if (lane == 0) p.loss[r] = 0.0f;
+    if (p.dh) for (uint32_t j = lane; j < p.dim; j += 64) p.dh[r * p.lddh + j] = 0;
+}
+
 // One block per group: the rows with a target, in order, to the front of the group's part of `index`; kNoRow behind them.  And every such row's
-// gradient factor.
+// gradient factor.  GATHER: the rows themselves, too (a launch less where there is little to copy).
 constexpr int kCompactThreads = 1024;
+template <class E, bool GATHER>
 __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, uint32_t *index, int32_t *target, int64_t *ends, int sum_only, float scale,
-                                                                  float *row_scale)
+                                                                  float *row_scale, const Hidden<E> hidden)
 {
     __shared__ uint32_t counts[kCompactThreads / 64];
     const uint32_t g = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -70,57 +101,51 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, 
     const float factor = sum_only ? scale : scale / static_cast<float>(at - begin);
     for (uint64_t r = begin + threadIdx.x; r < at; r += kCompactThreads) row_scale[r] = factor;
     if (threadIdx.x == 0) ends[g] = static_cast<int64_t>(at);
+    if constexpr (GATHER) {                                    // (the barrier that ended the loop ordered the block's own writes of index)
+        for (uint64_t r = begin + wave; r < end; r += kCompactThreads / 64) {
+            if (r < at) gather_row(hidden, r, index[r], lane);
+            if (!has_target(p, r)) clear_row(hidden, r, lane);
+        }
+    }
 }
 
-// Row r of the gathered hidden states (pitch a multiple of 8, zeros behind dim); rows without a target get loss 0 and gradient 0.
-template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Rows p, const uint32_t *index, const E *h, uint64_t ldh, uint32_t dim,
-                                                                        E *out, uint64_t pitch, float *loss, E *dh, uint64_t lddh)
+// The gathered rows by a launch of their own, a wave a row.
+template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Rows p, const uint32_t *index, const Hidden<E> hidden)
 {
     const uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
     const uint32_t lane = threadIdx.x % 64;
     if (r < clamped(p, 0) || r >= clamped(p, p.groups)) return;
-    const uint32_t from = index[r];
-    if (from != kNoRow) {
-        const E *src = h + from * ldh;
-        E *dst = out + r * pitch;
-        constexpr uint32_t V = 16 / sizeof(E);
-        if ((reinterpret_cast<uintptr_t>(src) & 15) == 0 && dim % V == 0) {
-            for (uint32_t j = lane * V; j < dim; j += 64 * V) *reinterpret_cast<float4 *>(dst + j) = *reinterpret_cast<const float4 *>(src + j);
-            for (uint32_t j = dim + lane; j < pitch; j += 64) dst[j] = 0;
-        } else {
-            for (uint32_t j = lane; j < pitch; j += 64) dst[j] = j < dim ? src[j] : E(0);
-        }
-    }
-    if (!has_target(p, r)) {
-        if (lane == 0) loss[r] = 0.0f;
-        if (dh) for (uint32_t j = lane; j < dim; j += 64) dh[r * lddh + j] = 0;
-    }
+    if (index[r] != kNoRow) gather_row(hidden, r, index[r], lane);
+    if (!has_target(p, r)) clear_row(hidden, r, lane);
 }
 
 // norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss, also in the place of the
-// target's logit.  Sixteen rows per block, sixteen threads a row.
-constexpr int kNormRows = 16, kNormThreads = 16, kNormAhead = 4;
+// target's logit.  ROWS rows per pass of a block, sixteen threads a row.
+constexpr int kNormThreads = 16, kNormAhead = 4;
+struct Norms {
+    const uint32_t *index;
+    const float2 *stats;              // [tiles][rows]
+    uint32_t tiles;
+    float *target_logit, *norm, *loss;
+};
 __device__ __forceinline__ void add_part(float &top, float &sum, float2 s)
 {
     const float m = fmaxf(top, s.x), base = m == -INFINITY ? 0.0f : m;
     sum = sum * expf(top - base) + s.y * expf(s.x - base);
     top = m;
 }
-__global__ __launch_bounds__(kNormRows * kNormThreads) void norm_kernel(const Rows p, const uint32_t *index, const float2 *stats, uint32_t tiles, float *target_logit,
-                                                                        float *norm, float *loss)
+// the loss of row r in the threads with y == 0 (others: 0)
+template <int ROWS> __device__ __forceinline__ float norm_rows(const Rows &p, const Norms &n, uint64_t r, bool in, float2 (&part)[kNormThreads][ROWS])
 {
-    __shared__ float2 part[kNormThreads][kNormRows];
-    const uint32_t x = threadIdx.x % kNormRows, y = threadIdx.x / kNormRows;
-    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * kNormRows + x;
-    const bool in = r >= clamped(p, 0) && r < clamped(p, p.groups) && index[r] != kNoRow;
+    const uint32_t x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
     float top = -INFINITY, sum = 0.0f;
     if (in) {
-        for (uint32_t t = y; t < tiles; t += kNormThreads * kNormAhead) {
+        for (uint32_t t = y; t < n.tiles; t += kNormThreads * kNormAhead) {
             float2 s[kNormAhead];
             #pragma unroll
             for (int i = 0; i < kNormAhead; ++i) {
                 const uint32_t u = t + i * kNormThreads;
-                s[i] = u < tiles ? stats[u * p.rows + r] : make_float2(-INFINITY, 0.0f);
+                s[i] = u < n.tiles ? n.stats[u * p.rows + r] : make_float2(-INFINITY, 0.0f);
             }
             #pragma unroll
             for (int i = 0; i < kNormAhead; ++i) add_part(top, sum, s[i]);
@@ -128,33 +153,59 @@ __global__ __launch_bounds__(kNormRows * kNormThreads) void norm_kernel(const Ro
     }
     part[y][x] = make_float2(top, sum);
     __syncthreads();
-    if (y != 0 || !in) return;
-    #pragma unroll
-    for (int w = 1; w < kNormThreads; ++w) add_part(top, sum, part[w][x]);
-    const float n = top + logf(sum);
-    norm[r] = n;
-    const float l = n - target_logit[r];
-    target_logit[r] = l;
-    loss[index[r]] = l;
+    float l = 0.0f;
+    if (y == 0 && in) {
+        #pragma unroll
+        for (int w = 1; w < kNormThreads; ++w) add_part(top, sum, part[w][x]);
+        const float norm = top + logf(sum);
+        n.norm[r] = norm;
+        l = norm - n.target_logit[r];
+        n.target_logit[r] = l;
+        n.loss[n.index[r]] = l;
+    }
+    __syncthreads();
+    return l;
 }
 
-// One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits.
-constexpr int kMeanThreads = 1024;
-__global__ __launch_bounds__(kMeanThreads) void mean_kernel(const Rows p, const int64_t *ends, const float *loss, float *group_loss, int sum_only)
+constexpr int kNormRows = 16;
+__global__ __launch_bounds__(kNormRows * kNormThreads) void norm_kernel(const Rows p, const Norms n)
 {
+    __shared__ float2 part[kNormThreads][kNormRows];
+    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * kNormRows + threadIdx.x % kNormRows;
+    norm_rows<kNormRows>(p, n, r, r >= clamped(p, 0) && r < clamped(p, p.groups) && n.index[r] != kNoRow, part);
+}
+
+// One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits.  NORMS: the rows' losses, too (a launch less where a
+// block has little to do).
+constexpr int kMeanThreads = 1024;
+template <bool NORMS> __global__ __launch_bounds__(kMeanThreads) void mean_kernel(const Rows p, const Norms n, const int64_t *ends, float *group_loss, int sum_only)
+{
+    constexpr int ROWS = kMeanThreads / kNormThreads;
     __shared__ double part[kMeanThreads];
+    __shared__ float2 parts[kNormThreads][NORMS ? ROWS : 1];
     const uint32_t g = blockIdx.x;
     const uint64_t begin = clamped(p, g), end = static_cast<uint64_t>(ends[g]);
     double s = 0.0;
-    for (uint64_t r = begin + threadIdx.x; r < end; r += kMeanThreads) s += loss[r];
+    if constexpr (NORMS) {
+        for (uint64_t r0 = begin; r0 < end; r0 += ROWS) {
+            const uint64_t r = r0 + threadIdx.x % ROWS;
+            s += norm_rows<ROWS>(p, n, r, r < end && n.index[r] != kNoRow, parts);         // (offsets that do not ascend may leave holes)
+        }
+    } else {
+        for (uint64_t r = begin + threadIdx.x; r < end; r += kMeanThreads) s += n.target_logit[r];
+    }
     part[threadIdx.x] = s;
     __syncthreads();
     for (int d = kMeanThreads / 2; d > 0; d >>= 1) {
         if (static_cast<int>(threadIdx.x) < d) part[threadIdx.x] += part[threadIdx.x + d];
         __syncthreads();
     }
-    if (threadIdx.x == 0) group_loss[g] = static_cast<float>(end > begin ? (sum_only ? part[0] : part[0] / static_cast<double>(end - begin)) : 0.0);
+    if (threadIdx.x == 0 && group_loss) group_loss[g] = static_cast<float>(end > begin ? (sum_only ? part[0] : part[0] / static_cast<double>(end - begin)) : 0.0);
 }
+
+// Up to so many bytes of hidden states per group, and so many statistics per thread of a group's block, one block of 1024 threads does the small work of a group
+// together with what precedes or follows it; beyond, kernels of their own spread it over the chip.
+constexpr uint64_t kGatherHere = 256u << 10, kStatsHere = 4;
 
 // The caller's memory, carved up.
 struct Workspace {
@@ -221,10 +272,20 @@ int check(const cocod_cross_entropy_call *c)
     return COCOD_OK;
 }
 
-template <class E> hipError_t launch_gather(hipStream_t s, const Rows &rows, const uint32_t *index, const cocod_cross_entropy_call *c, void *hidden, uint64_t pitch)
+template <class E> hipError_t launch_gather(hipStream_t s, const Rows &rows, const cocod_cross_entropy_call *c, const Workspace &w, uint8_t *ws, float scale)
 {
-    hipLaunchKernelGGL(gather_kernel<E>, dim3(static_cast<uint32_t>((rows.rows + 3) / 4)), dim3(256), 0, s, rows, index, static_cast<const E *>(c->h), c->ldh, c->dim,
-                       static_cast<E *>(hidden), pitch, c->loss, static_cast<E *>(c->dh), c->lddh);
+    const Hidden<E> hidden = {static_cast<const E *>(c->h), c->ldh, c->dim, reinterpret_cast<E *>(ws + w.hidden), w.pitch, c->loss, static_cast<E *>(c->dh), c->lddh};
+    uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
+    int32_t *target = reinterpret_cast<int32_t *>(ws + w.target);
+    int64_t *ends = reinterpret_cast<int64_t *>(ws + w.ends);
+    float *row_scale = reinterpret_cast<float *>(ws + w.row_scale);
+    const int sum_only = (c->flags & COCOD_CROSS_ENTROPY_SUM) != 0;
+    if (c->rows * w.pitch * sizeof(E) <= kGatherHere * c->groups) {
+        hipLaunchKernelGGL((compact_kernel<E, true>), dim3(c->groups), dim3(kCompactThreads), 0, s, rows, index, target, ends, sum_only, scale, row_scale, hidden);
+    } else {
+        hipLaunchKernelGGL((compact_kernel<E, false>), dim3(c->groups), dim3(kCompactThreads), 0, s, rows, index, target, ends, sum_only, scale, row_scale, hidden);
+        hipLaunchKernelGGL(gather_kernel<E>, dim3(static_cast<uint32_t>((rows.rows + 3) / 4)), dim3(256), 0, s, rows, index, hidden);
+    }
     return hipGetLastError();
 }
 
@@ -287,28 +348,28 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     const float unslope = t == Dtype::F16 ? 0x1p-14f : 1.0f;   // fp16 slopes are kept times 2^14
     const int sum_only = (c->flags & COCOD_CROSS_ENTROPY_SUM) != 0;
 
-    hipLaunchKernelGGL(compact_kernel, dim3(c->groups), dim3(kCompactThreads), 0, q, rows, index, target, ends, sum_only, c->grad_scale * unslope, row_scale);
-    if (c->rows) {
-        const hipError_t e = t == Dtype::F32 ? launch_gather<float>(q, rows, index, c, ws + w.hidden, w.pitch) : launch_gather<uint16_t>(q, rows, index, c, ws + w.hidden, w.pitch);
-        if (e != hipSuccess) return launch_status(e, what);
-    }
+    const float scale = c->grad_scale * unslope;
+    if (int rc = launch_status(t == Dtype::F32 ? launch_gather<float>(q, rows, c, w, ws, scale) : launch_gather<uint16_t>(q, rows, c, w, ws, scale), what)) return rc;
     ProductParams z{};
     z.a = ws + w.hidden; z.lda = w.pitch;
     z.b = c->e; z.ldb = c->lde; z.b_group = c->e_stride;
     z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
     z.k = c->dim; z.splits = 1; z.target = target;
+    Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), 0, reinterpret_cast<float *>(ws + w.target_logit), norm, c->loss};
+    bool here = true;
     if (c->rows) {
         ProductParams p = z;
         p.n = c->vocab;
         p.stats = reinterpret_cast<float2 *>(ws + w.stats);
-        p.target_logit = reinterpret_cast<float *>(ws + w.target_logit);
+        p.target_logit = norms.target_logit;
         const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, p);
         if (int rc = launch_status(launch_logits(q, t, Finish::Stats, tile, p), what)) return rc;
-        const uint32_t tiles = (c->vocab + tile_cols(t, tile) - 1) / tile_cols(t, tile);
-        hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + kNormRows - 1) / kNormRows)), dim3(kNormRows * kNormThreads), 0, q, rows, index, p.stats, tiles, p.target_logit, norm, c->loss);
+        norms.tiles = (c->vocab + tile_cols(t, tile) - 1) / tile_cols(t, tile);
+        here = c->rows * norms.tiles <= kStatsHere * kMeanThreads * c->groups;
+        if (!here) hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + kNormRows - 1) / kNormRows)), dim3(kNormRows * kNormThreads), 0, q, rows, norms);
     }
-    if (c->group_loss)
-        hipLaunchKernelGGL(mean_kernel, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, ends, reinterpret_cast<const float *>(ws + w.target_logit), c->group_loss, sum_only);
+    if (here)                hipLaunchKernelGGL(mean_kernel<true>, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
+    else if (c->group_loss)  hipLaunchKernelGGL(mean_kernel<false>, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
     if (int rc = launch_status(hipGetLastError(), what)) return rc;
     if (!c->dh && !c->de) return COCOD_OK;
 
@@ -342,7 +403,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
             d.b = ws + w.hidden; d.ldb = w.pitch;
             d.m = n;
             d.out = static_cast<uint8_t *>(c->de) + v0 * c->ldde * s; d.ldc = c->ldde; d.out_group = c->de_stride;
-            d.scale = c->grad_scale * unslope; d.mean = !sum_only;
+            d.scale = scale; d.mean = !sum_only;
             d.splits = w.to_table.splits;
             if (int rc = launch_status(launch_store(q, t, Layout::Weights, settle_tile(t, Layout::Weights, w.to_table.tile, d), d), what)) return rc;
         }
