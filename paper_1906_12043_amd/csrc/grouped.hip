@@ -44,25 +44,28 @@ hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const Prod
 
 // The tile and the number of splits that are expected to take least time.  A compute unit takes ceil(blocks / 256) blocks one after the other (where it
 // holds several at a time they share it), each `per_slice` for every slice of its sum and `per_tile` once, in us; a launch costs 5, joining splits 4 and
-// their traffic at 4 TB/s.  Fitted to 54 products of 1 to 16 groups, 1 to 8192 rows and widths 512 to 32000, every tile with 1 to 16 splits: the choice
-// costs 1 % more time than the best one in the mean, 21 % at most.  For instance, us (large / medium / small tile, best splits in brackets):
+// their traffic at 4 TB/s.  Fitted to 111 products of 1 to 64 groups, 1 to 8192 rows and widths 300 to 32000, every tile with 1 to 16 splits: the choice
+// costs 2 % more time than the best one in the mean.  For instance, us (large / medium / small tile, best splits in brackets):
 // bf16 16 groups of one row, 1024 x 1024: 16 (4) / 12 (4) / 8 (1); 4 of 64 rows, 2048 x 2048: 22 (4) / 18 (4) / 14 (1); 16 of 512 rows, 1024 x
 // 1024: 33 (1) / 26 (1) / 50 (1); 16 of 500 rows, 2048 x 1024, input gradient: 40 (1) / 47 (1) / 93 (1); 4 of 768 rows, 32000 x 1024: 239 (4) / 266 (8) /
-// 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); fp32 4 of 250 rows, 512 x 768: - / 25 (4) / 17 (1); one of 2048 rows, 2048 x 2048: - / 130 (1) / 180 (1).
+// 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); through registers one row, 4095 x 2047: - / 18 (8) / 14 (8), 2048 rows, 2047 x 2047: - / 46 (1) /
+// 77 (1); fp32 16 of 250 rows, 1024 x 1024: - / 56 (1) / 97 (1), 8 of 8 rows, 2048 x 2048: - / 58 (4) / 31 (2).
 struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile; };
-constexpr TileCost kCost16[] = {{256, 256, 64, 1.36, 3.9}, {128, 128, 64, 0.5, 1.2}, {32, 64, 128, 0.27, 0.4}};
-constexpr TileCost kCost32[] = {{0, 0, 0, 0, 0}, {128, 128, 32, 1.73, 3.5}, {32, 64, 64, 0.62, 1.2}};
+constexpr TileCost kCostDirect[] = {{256, 256, 64, 1.15, 5.2}, {128, 128, 64, 0.40, 1.4}, {32, 64, 128, 0.25, 0.5}};
+constexpr TileCost kCostRegs[] = {{0, 0, 0, 0, 0}, {128, 128, 64, 0.81, 3.4}, {32, 64, 128, 0.50, 0.65}};
+constexpr TileCost kCost32[] = {{0, 0, 0, 0, 0}, {128, 128, 32, 1.25, 3.7}, {32, 64, 64, 0.57, 1.3}};
 constexpr uint32_t kMaxSplits = 16;
 
-ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split)
+ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split)
 {
     const bool weights = layout == Layout::Weights;
     const double mean_rows = static_cast<double>(rows) / groups, terms = weights ? mean_rows : k;
     const double cells = weights ? static_cast<double>(groups) * m * n : static_cast<double>(rows) * n;
+    const TileCost *const costs = type == Dtype::F32 ? kCost32 : direct ? kCostDirect : kCostRegs;
     ProductPlan best{Tile::Medium, 1};
     double least = 1e300;
-    for (uint32_t tile = type == Dtype::F32 ? 1 : 0; tile < 3; ++tile) {
-        const TileCost &c = (type == Dtype::F32 ? kCost32 : kCost16)[tile];
+    for (uint32_t tile = costs[0].bm ? 0 : 1; tile < 3; ++tile) {
+        const TileCost &c = costs[tile];
         // ragged groups end half a tile short, in the mean
         const double high = weights || groups == 1 ? std::ceil((weights ? m : mean_rows) / c.bm) : std::fmax(1.0, mean_rows / c.bm + 0.5);
         const double tiles = groups * high * std::ceil(static_cast<double>(n) / c.bn);
@@ -102,9 +105,10 @@ int check_shape(const cocod_grouped *g)
 ProductPlan plan_of(const cocod_grouped *g, Layout layout, bool may_split)
 {
     const Dtype t = kTypes[g->dtype];
-    if (layout == Layout::Rows_KN) return plan_product(layout, t, g->rows, g->groups, 0, g->outer, g->inner, may_split);
-    if (layout == Layout::Rows_NK) return plan_product(layout, t, g->rows, g->groups, 0, g->inner, g->outer, may_split);
-    return plan_product(layout, t, g->rows, g->groups, g->inner, g->outer, 0, may_split);
+    const bool k8 = g->inner % 8 == 0, n8 = g->outer % 8 == 0;       // as dense arrays
+    if (layout == Layout::Rows_KN) return plan_product(layout, t, k8 && n8, g->rows, g->groups, 0, g->outer, g->inner, may_split);
+    if (layout == Layout::Rows_NK) return plan_product(layout, t, n8, g->rows, g->groups, 0, g->inner, g->outer, may_split);
+    return plan_product(layout, t, k8 && n8, g->rows, g->groups, g->inner, g->outer, 0, may_split);
 }
 uint64_t workspace_of(const cocod_grouped *g, Layout layout, const ProductPlan &plan)
 {

@@ -100,9 +100,9 @@ inline Tile settle_tile(Dtype type, Layout layout, Tile planned, const ProductPa
     return planned == Tile::Large && (type == Dtype::F32 || (p.a && !direct_a(layout, p)) || !direct_b(layout, p)) ? Tile::Medium : planned;
 }
 
-// Tile and splits of a product, from its sizes alone.
+// Tile and splits of a product, from its sizes alone; direct: 16-bit operands are expected to go to LDS directly.
 struct ProductPlan { Tile tile; uint32_t splits; };
-ProductPlan plan_product(Layout layout, Dtype type, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split);
+ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split);
 // Bytes of ProductParams::part (0 with one split), whose rows hold part_pitch(n) floats.
 inline uint64_t part_pitch(uint32_t n) { return (static_cast<uint64_t>(n) + 3) / 4 * 4; }
 uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n);

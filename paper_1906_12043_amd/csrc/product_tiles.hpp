@@ -79,7 +79,10 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
     float sc[HOW == kCodes ? N : 1];
     uint32_t off[N], scale_off[HOW == kCodes ? N : 1];      // of a thread's chunks in a slice (bytes / elements / codes; scales)
 
-    bool fits;                        // every chunk of a slice within the sum lies within the operand
+    uint32_t down[HOW != kDirect && !KC ? N : 1];           // elements by which a load of a cut chunk lies too far back
+    bool fits;                        // slices within the sum can be loaded without checks
+    bool cut;                         // some chunk is cut
+    bool moved = false;               //   and the requested slice was loaded that way
 
     // load i of this thread: row of the tile, first chunk (pairs of chunks stay side by side in LDS)
     __device__ __forceinline__ static uint32_t row_of(int i) { return (i * THREADS + threadIdx.x) / (L::CH / W); }
@@ -89,19 +92,32 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
 
     __device__ __forceinline__ void start()
     {
-        // rows (direct: chunks of columns, too) past the end repeat the last one: their products are not stored
+        // Rows past the end repeat the last one, chunks of columns past the end the last one: their products are not stored.  A chunk that
+        // the end of a row cuts is loaded from as far back as it has to and moved down on its way to LDS (direct: it is read to its
+        // end, which lies within the pitch).
         const uint64_t pitch = HOW == kCodes ? ld_codes : ld;
-        fits = HOW == kDirect || ((KC || x0 + BX <= x_end) && pitch <= (1u << 22) && (HOW != kCodes || ld_scales <= (1u << 22)));
+        constexpr uint32_t E = 8 * W;
+        fits = HOW == kDirect || ((KC || x_end >= E) && pitch <= (1u << 22) && (HOW != kCodes || ld_scales <= (1u << 22)));
+        cut = HOW != kDirect && !KC && x0 + BX > x_end;
         #pragma unroll
         for (int i = 0; i < N; ++i) {
-            uint32_t row = row_of(i), c = chunk_of(i);
-            if (KC) { const uint32_t last = x_end - 1 - x0; row = row < last ? row : last; }
-            else if (HOW == kDirect) { const uint32_t last = (x_end - 1 - x0) / 8; c = c < last ? c : last; }
-            off[i] = (row * static_cast<uint32_t>(pitch) + c * 8) * (HOW == kDirect ? 2 : 1);
-            if constexpr (HOW == kCodes) {
-                static_assert(!KC && BX % 32 == 0, "codes of whole blocks, rows summed over");
-                scale_off[i] = row * static_cast<uint32_t>(ld_scales) + c / 4;
+            uint32_t row = row_of(i), q = chunk_of(i) * 8, back = 0;
+            if (KC) {
+                const uint32_t last = x_end - 1 - x0;
+                row = row < last ? row : last;
+            } else if (HOW == kDirect) {
+                const uint32_t last = (x_end - 1 - x0) / 8 * 8;
+                q = q < last ? q : last;
+            } else {
+                if constexpr (HOW == kCodes) {
+                    static_assert(BX % 32 == 0, "codes of whole blocks, rows summed over");
+                    const uint32_t last = x_end - 1 - x0;
+                    scale_off[i] = row * static_cast<uint32_t>(ld_scales) + (q < last ? q : last) / 32;
+                }
+                if (x0 + q + E > x_end) back = x0 + q + E - x_end;
+                down[i] = back < E ? back : 0;
             }
+            off[i] = (row * static_cast<uint32_t>(pitch) + q - back) * (HOW == kDirect ? 2 : 1);
         }
     }
 
@@ -118,6 +134,7 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                                                  (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
             }
         } else {
+            moved = false;
             #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const uint32_t row = row_of(i), c = chunk_of(i);
@@ -167,7 +184,7 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
             #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if constexpr (HOW == kCodes) {
-                    const uint8_t *at = codes + r * ld_codes + q + off[i];
+                    const uint8_t *at = codes + r * ld_codes + q + static_cast<int32_t>(off[i]);
                     if constexpr (W == 2) {
                         raw[i][0] = *reinterpret_cast<const u4_bytes *>(at);
                     } else {
@@ -177,10 +194,32 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                     sc[i] = __uint_as_float(static_cast<unsigned>((scales + r * ld_scales + q / 32)[scale_off[i]]) << 23);
                 } else {
                     #pragma unroll
-                    for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(src + r * ld + q + off[i])[j];
+                    for (int j = 0; j < RAW; ++j) raw[i][j] = reinterpret_cast<const u4_any *>(src + r * ld + q + static_cast<int32_t>(off[i]))[j];
                 }
             }
+            moved = cut;
         }
+    }
+
+    // the elements of load i by down[i] towards the first
+    __device__ __forceinline__ void move_down(int i)
+    {
+        constexpr int SIZE = HOW == kCodes ? 1 : sizeof(elem), WORDS = 8 * W * SIZE / 4;
+        unsigned w[WORDS + 1];
+        #pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = raw[i][j / 4][j % 4];
+        w[WORDS] = 0;
+        const uint32_t bytes = down[i] * SIZE;
+        #pragma unroll
+        for (int step = 1; step < WORDS; step <<= 1)
+            #pragma unroll
+            for (int j = 0; j < WORDS; ++j) w[j] = bytes & (4 * step) ? (j + step < WORDS ? w[j + step] : 0) : w[j];
+        if constexpr (SIZE < 4) {
+            #pragma unroll
+            for (int j = 0; j < WORDS; ++j) w[j] = __builtin_amdgcn_alignbyte(w[j + 1], w[j], bytes & 3);
+        }
+        #pragma unroll
+        for (int j = 0; j < WORDS; ++j) raw[i][j / 4][j % 4] = w[j];
     }
 
     __device__ __forceinline__ void ask(uint8_t *lds, uint32_t k0, uint32_t wave)
@@ -193,6 +232,12 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
     __device__ __forceinline__ void deliver(uint8_t *lds)
     {
         if constexpr (HOW == kDirect) return;
+        if constexpr (HOW != kDirect && !KC) {
+            if (moved) {
+                #pragma unroll
+                for (int i = 0; i < N; ++i) move_down(i);
+            }
+        }
         #pragma unroll
         for (int i = 0; i < N; ++i) {
             uint8_t *at = lds + place_of(i) * 16;
