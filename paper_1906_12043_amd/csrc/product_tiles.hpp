@@ -19,7 +19,8 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 // Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_> struct TileShape {
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2> struct TileShape {
+    static constexpr int STAGES = STAGES_;           // slices in LDS
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
     static constexpr int threads = 64 * WM * WN * WK;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;       // 32x32 blocks of a wave
@@ -374,11 +375,13 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
     static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 2 * (S::NB * 32 + 4) * 4;
-    static constexpr int lds_bytes = 2 * stage > join_bytes ? 2 * stage : join_bytes;
+    static constexpr int ST = S::STAGES, REQUESTS = LoadA::N + LoadB::N;
+    static_assert(ST == 2 || (HOW_A == kDirect && HOW_B == kDirect), "operands in registers hold one slice");
+    static constexpr int lds_bytes = ST * stage > join_bytes ? ST * stage : join_bytes;
 
     // The pipeline.  While the matrix cores work on one step of 16 terms (times WK), the fragments of the next step are read.  In front
-    // of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes the slice after the
-    // next one, which then has a whole slice's time to arrive; and the next slice, requested that long ago, is there, so that its first
+    // of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes the slice STAGES
+    // further on, which then has the time of STAGES - 1 slices to arrive; and the next slice, requested that long ago, is there, so that its first
     // fragments are read beside the last step's products.  An operand that passes through registers is requested at the same place and
     // put into LDS a step before the waves meet.
     static constexpr int STEPS = S::BK / 16 / S::WK;
@@ -435,7 +438,7 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
                 la.deliver(next);
                 lb.deliver(next + LoadA::bytes);
             }
-            if constexpr (LAST) slices_arrived<EARLY ? 63 : 0>();
+            if constexpr (LAST) { if (WHOLE) slices_arrived<EARLY ? 63 : (ST - 2) * REQUESTS>(); else slices_arrived<EARLY ? 63 : 0>(); }
             if constexpr (EARLY ? kk + 2 == STEPS : LAST) {
                 if constexpr (WHOLE) {
                     la.request_whole(fill, k_fill, wave);
@@ -625,12 +628,14 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         lb.ask(lds + P::LoadA::bytes, k0, wave);
         la.deliver(lds);
         lb.deliver(lds + P::LoadA::bytes);
-        if (slices > 1) {
-            la.ask(lds + P::stage, k0 + S::BK, wave);
-            lb.ask(lds + P::stage + P::LoadA::bytes, k0 + S::BK, wave);
-        }
+        #pragma unroll
+        for (uint32_t i = 1; i < P::ST; ++i)
+            if (i < slices) {
+                la.ask(lds + i * P::stage, k0 + i * S::BK, wave);
+                lb.ask(lds + i * P::stage + P::LoadA::bytes, k0 + i * S::BK, wave);
+            }
         typename P::Fragments f[2];
-        if (HOW_A == kDirect && HOW_B == kDirect && slices > 1) slices_arrived<P::LoadA::N + P::LoadB::N>(); else slices_arrived<0>();
+        if (HOW_A == kDirect && HOW_B == kDirect && slices >= P::ST) slices_arrived<(P::ST - 1) * P::REQUESTS>(); else slices_arrived<0>();
         P::read(f[0], lds, wk * 16, wm, wn, lane);
         // (keeps the compiler from joining these reads with the loop's last ones at the head of the loop, where nothing hides them)
         #pragma unroll
@@ -641,16 +646,17 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         for (int pl = 0; pl < P::PB; ++pl)
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[pl][j]));
-        uint32_t t = 0;
+        uint32_t t = 0, cur = 0, next = P::stage;
+        auto turn = [&] { cur = next; next = next + P::stage == P::ST * P::stage ? 0 : next + P::stage; };
         if (la.fits && lb.fits)
-            for (; t + 2 < slices && k0 + (t + 3) * S::BK <= at.terms; ++t) {
-                uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
-                P::template steps<true>(cur, next, cur, la, lb, true, k0 + (t + 2) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            for (; t + P::ST < slices && k0 + (t + P::ST + 1) * S::BK <= at.terms; ++t) {
+                P::template steps<true>(lds + cur, lds + next, lds + cur, la, lb, true, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
+                turn();
             }
         #pragma unroll 1
         for (; t < slices; ++t) {
-            uint8_t *cur = lds + (t & 1) * P::stage, *next = lds + (~t & 1) * P::stage;
-            P::template steps<false>(cur, next, cur, la, lb, t + 2 < slices, k0 + (t + 2) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            P::template steps<false>(lds + cur, lds + next, lds + cur, la, lb, t + P::ST < slices, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            turn();
         }
     }
     slices_arrived<0>();                                       // LDS is free
@@ -853,6 +859,9 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
 typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
+// short sums and few blocks: a slice more in flight (one row, 4096 x 4096: 10.1 us instead of 11.0; the other tiles lose by four slices of 32: 8 groups
+// of 8192 rows, 4096 x 4096, input gradient 1962 us instead of 1840: of a row of 64 bytes the other half of the line is fetched again)
+typedef TileShape<32, 64, 128, 1, 1, 4, 3> Small16Direct;
 typedef TileShape<128, 128, 32, 2, 4, 1> Medium32;
 typedef TileShape<32, 64, 64, 1, 2, 2> Small32;
 
@@ -878,7 +887,7 @@ hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
             }
         if (b_direct && direct_a(LAYOUT, p)) {
             if (tile == Tile::Large) return launch_one<T, LAYOUT, Large16, FINISH, kDirect, kDirect>(stream, p);
-            return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kDirect, kDirect>(stream, p)
+            return tile == Tile::Small ? launch_one<T, LAYOUT, Small16Direct, FINISH, kDirect, kDirect>(stream, p)
                                        : launch_one<T, LAYOUT, Medium16, FINISH, kDirect, kDirect>(stream, p);
         }
         return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kRegs, kRegs>(stream, p)
