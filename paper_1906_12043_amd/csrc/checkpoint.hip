@@ -59,60 +59,139 @@ template <class T> __device__ __forceinline__ float widen(typename T::elem v)
     else return __uint_as_float(static_cast<unsigned>(v) << 16);
 }
 
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+typedef short s2 __attribute__((ext_vector_type(2)));
+
+// Eight values: bit patterns of magnitudes (16-bit types: two to a word) reduced without unpacking them.
+template <class T> struct Eight {
+    static constexpr bool wide = sizeof(typename T::elem) == 4;
+    static constexpr int WORDS = wide ? 8 : 4;
+    unsigned w[WORDS];
+
+    static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b)
+    {
+        return wide ? (a > b ? a : b) : __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+    }
+    static __device__ __forceinline__ unsigned smaller(unsigned a, unsigned b)
+    {
+        return wide ? (a < b ? a : b) : __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+    }
+    __device__ __forceinline__ unsigned magnitude(int i) const { return w[i] & (wide ? 0x7fffffffu : 0x7fff7fffu); }
+    // the largest magnitude
+    __device__ __forceinline__ unsigned largest() const
+    {
+        unsigned m = magnitude(0);
+        #pragma unroll
+        for (int i = 1; i < WORDS; ++i) m = larger(m, magnitude(i));
+        return wide ? m : (m >> 16 > (m & 0xffffu) ? m >> 16 : m & 0xffffu);
+    }
+    // the smallest magnitude that is not zero, less one (all ones: none)
+    __device__ __forceinline__ unsigned smallest_less_one() const
+    {
+        unsigned m = ~0u;
+        #pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            m = smaller(m, wide ? magnitude(i) - 1 : __builtin_bit_cast(unsigned, __builtin_bit_cast(us2, magnitude(i)) - us2{1, 1}));
+        return wide ? m : (m >> 16 < (m & 0xffffu) ? m >> 16 : m & 0xffffu);
+    }
+    __device__ __forceinline__ float value(int i) const
+    {
+        if constexpr (wide) return __uint_as_float(w[i]);
+        else return widen<T>(static_cast<uint16_t>(w[i / 2] >> (16 * (i % 2))));
+    }
+};
+
+// bit pattern of a magnitude as fp32 bits
+template <class T> __device__ __forceinline__ unsigned bits32(unsigned m)
+{
+    if constexpr (sizeof(typename T::elem) == 4) return m;
+    else return __float_as_uint(widen<T>(static_cast<uint16_t>(m)));
+}
+
+// Two values as codes of value / scale in the low half of a word.
+template <class T> __device__ __forceinline__ unsigned two_codes(const Eight<T> &v, int i, float scale)
+{
+    s2 out;
+    if constexpr (Eight<T>::wide)                    out = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2{0, 0}, __uint_as_float(v.w[2 * i]), __uint_as_float(v.w[2 * i + 1]), scale, false);
+    else if constexpr (std::is_same<T, F16>::value)  out = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(s2{0, 0}, __builtin_bit_cast(hf2, v.w[i]), scale, false);
+    else                                             out = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s2{0, 0}, __builtin_bit_cast(bf2, v.w[i]), scale, false);
+    return static_cast<unsigned short>(out[0]);
+}
+
+// Codes value by value, for a thread that holds something not finite, beyond the largest stored magnitude or below half the smallest code.
+template <class T> __device__ __noinline__ u2 rare_codes(const Eight<T> v, float scale)
+{
+    u2 code = {0, 0};
+    #pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        float x = v.value(0);
+        #pragma unroll
+        for (int j = 1; j < 8; ++j) if (j == i) x = v.value(j);
+        const unsigned b = __float_as_uint(x), m = b & 0x7fffffffu, sign = b >> 24 & 0x80u;
+        unsigned c;
+        if (m >= 0x7f800000u) {
+            c = 0x7fu | sign;
+        } else {
+            const float y = m > Range<T>::most ? __uint_as_float(Range<T>::most | (b & 0x80000000u)) : x;
+            c = static_cast<unsigned short>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2{0, 0}, y, 0.0f, scale, false)[0]) & 0xffu;
+            if (m != 0 && (c & 0x7fu) == 0) c = 1u | sign;
+        }
+        code[i / 4] |= c << (8 * (i % 4));
+    }
+    return code;
+}
+
 template <class T> __global__ __launch_bounds__(kCheckpointThreads) void store_kernel(const CheckpointParams p)
 {
     typedef typename T::elem elem;
+    constexpr unsigned infinity = sizeof(elem) == 4 ? 0x7f800000u : std::is_same<T, F16>::value ? 0x7c00u : 0x7f80u;
     for (Walk at(p); at.row < p.rows; at.next(p)) {            // four threads of a block of 32 leave together
         const uint32_t q = at.chunk * 8;
         const elem *x = static_cast<const elem *>(p.x) + at.row * p.ldx + q;
-        float v[8];
+        Eight<T> v;
         if (q + 8 <= p.cols) {
-            union { u4 w[sizeof(elem) / 2]; elem e[8]; } raw;
             #pragma unroll
-            for (unsigned j = 0; j < sizeof(elem) / 2; ++j) raw.w[j] = reinterpret_cast<const u4_any *>(x)[j];
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = widen<T>(raw.e[j]);
+            for (int j = 0; j < Eight<T>::WORDS / 4; ++j) {
+                const u4 four = reinterpret_cast<const u4_any *>(x)[j];
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) v.w[4 * j + i] = four[i];
+            }
         } else {
             #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = q + j < p.cols ? widen<T>(x[j]) : 0.0f;
+            for (int j = 0; j < Eight<T>::WORDS; ++j) {
+                if constexpr (Eight<T>::wide) v.w[j] = q + j < p.cols ? __float_as_uint(x[j]) : 0u;
+                else v.w[j] = (q + 2 * j < p.cols ? x[2 * j] : 0u) | (q + 2 * j + 1 < p.cols ? static_cast<unsigned>(x[2 * j + 1]) << 16 : 0u);
+            }
         }
-        unsigned top = 0;
-        #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned m = __float_as_uint(v[j]) & 0x7fffffffu;
-            if (m < 0x7f800000u && m > top) top = m;
+        unsigned top = v.largest();
+        if (top >= infinity) {                                 // what is not finite does not count
+            top = 0;
+            #pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned m = sizeof(elem) == 4 ? v.magnitude(j) : v.magnitude(j / 2) >> (16 * (j % 2)) & 0xffffu;
+                if (m < infinity && m > top) top = m;
+            }
         }
         unsigned other = __shfl_xor(top, 1, 64);
         top = other > top ? other : top;
         other = __shfl_xor(top, 2, 64);
-        top = other > top ? other : top;
+        top = bits32<T>(other > top ? other : top);
         // top = f 2^t with f in [1, 2): 448 = 1.75 * 2^8
         int e = static_cast<int>(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
         e = e < Range<T>::low ? Range<T>::low : e;
         const float scale = __uint_as_float(static_cast<unsigned>(e + 127) << 23);
-        unsigned code[2] = {0, 0};
-        #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            float pair[2];
-            #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned b = __float_as_uint(v[j + i]), m = b & 0x7fffffffu;
-                pair[i] = m > Range<T>::most && m < 0x7f800000u ? __uint_as_float(Range<T>::most | (b & 0x80000000u)) : v[j + i];
-            }
-            typedef short s2 __attribute__((ext_vector_type(2)));
-            const s2 two = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2{0, 0}, pair[0], pair[1], scale, false);
-            unsigned c = static_cast<unsigned short>(two.x);
-            #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned b = __float_as_uint(v[j + i]), m = b & 0x7fffffffu;
-                if (m >= 0x7f800000u) c = (c & ~(0xffu << (8 * i))) | ((0x7fu | (b >> 24 & 0x80u)) << (8 * i));
-                else if (m != 0 && (c & (0x7fu << (8 * i))) == 0) c |= (1u | (b >> 24 & 0x80u)) << (8 * i);
-            }
-            code[j / 4] |= c << (8 * (j % 4));
+        // 2^(e - 10) and less would round to no code at all
+        const unsigned least = bits32<T>(v.smallest_less_one() + 1), half = e < -116 ? 0x00800000u : static_cast<unsigned>(e + 117) << 23;
+        const bool none = v.smallest_less_one() == (sizeof(elem) == 4 ? ~0u : 0xffffu);
+        u2 code;
+        if (v.largest() >= infinity || top > Range<T>::most || (!none && least <= half)) {
+            code = rare_codes(v, scale);
+        } else {
+            code = u2{two_codes(v, 0, scale) | two_codes(v, 1, scale) << 16, two_codes(v, 2, scale) | two_codes(v, 3, scale) << 16};
         }
         uint8_t *to = p.codes + at.row * p.ld_codes + q;
         if (q + 8 <= p.cols) {
-            *reinterpret_cast<u2_any *>(to) = u2{code[0], code[1]};
+            *reinterpret_cast<u2_any *>(to) = code;
         } else {
             #pragma unroll
             for (int j = 0; j < 8; ++j) if (q + j < p.cols) to[j] = static_cast<uint8_t>(code[j / 4] >> (8 * (j % 4)));
