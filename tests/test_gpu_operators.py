@@ -157,6 +157,32 @@ def test_large_tiles_and_splits(dtype, case):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("bounds, rows, k, n", [
+    ([1, 2999], 3000, 72, 4104), ([1, 2999], 3000, 4104, 72), ([0, 5990], 6000, 72, 136), ([0, 5990], 6000, 136, 72), ([0, 690], 700, 73, 4101),
+    ([0, 690], 700, 4101, 73), ([0, 100, 100, 390, 500, 700], 700, 4104, 520), ([0, 100, 100, 390, 500, 700], 700, 2056, 72)])
+def test_every_tile(dtype, bounds, rows, k, n):
+    """Sizes at which the three tiles are taken in each direction, with operands of whole and of odd rows."""
+    gen, t, groups = generator(rows + k), oh.TYPES[dtype][1], len(bounds) - 1
+    x, dy, w = oh.matrix(rows, k, 0, t, gen), oh.matrix(rows, n, 0, t, gen), oh.stack(groups, k, n, 0, 0, t, gen)
+    written = oh.inside(bounds, rows)
+    buf, y = oh.output((rows, n), 0, t)
+    oh.call("forward", oh.layer(dtype, bounds, rows, k, n, x=x, w=w, y=y, flags=P.GROUPED_RELU_OUT))
+    out, mag, terms = oh.exact_product("forward", bounds, x, w)
+    close(y[written], out.clamp(min=0)[written], oh.product_bound(out, mag, terms, t)[written])
+    assert oh.untouched(buf, y, written)
+    buf, dx = oh.output((rows, k), 0, t)
+    oh.call("input_grad", oh.layer(dtype, bounds, rows, k, n, x=x, dy=dy, w=w, dx=dx, flags=P.GROUPED_RELU_IN))
+    out, mag, terms = oh.exact_product("input_grad", bounds, dy, w)
+    close(dx[written], (out * (x > 0))[written], oh.product_bound(out, mag, terms, t)[written])
+    assert oh.untouched(buf, dx, written)
+    for to in {t, torch.float32}:
+        buf, dw = oh.output((groups, k, n), 0, to)
+        oh.call("weight_grad", oh.layer(dtype, bounds, rows, k, n, x=x, dy=dy, dw=dw))
+        out, mag, terms = oh.exact_product("weight_grad", bounds, x, dy)
+        close(dw, out, oh.product_bound(out, mag, terms, to))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("case", [0, 1, 3, 4, 5, 7])
 def test_products_from_codes(dtype, case):
     bounds, rows, k, n, pad = SHAPES[case]
@@ -208,6 +234,109 @@ def test_not_finite_and_extreme_operands(dtype):
         y = torch.empty((rows, n), dtype=torch.float32 if dtype == "fp32" else t, device="cuda")
         oh.call("forward", oh.layer(dtype, [0, rows], rows, k, n, x=xs, w=ws, y=y))
         assert torch.equal(y, (xs.double() @ ws[0].double()).to(t)), (a, b)
+
+
+@pytest.mark.parametrize("dtype, lo, up", [("fp16", -24, 10), ("bf16", -133, 60), ("fp32", -149, 60)])
+def test_subnormal_operands_and_results(dtype, lo, up):
+    """The smallest numbers of a type, whose sums fp32 holds exactly, are neither lost as operands nor as results."""
+    t, gen, rows, k, n = oh.TYPES[dtype][1], generator(11), 150, 96, 80
+    r = torch.randint(-1, 2, (rows, k), generator=gen, device="cuda").double()
+    sign = torch.sign(torch.randn(1, k, n, generator=gen, device="cuda")).double()
+    for a, b in ((lo, up), (0, lo)):
+        x, w = (r * 2.0 ** a).to(t), (sign * 2.0 ** b).to(t)
+        y = torch.empty((rows, n), dtype=t, device="cuda")
+        oh.call("forward", oh.layer(dtype, [0, rows], rows, k, n, x=x, w=w, y=y))
+        assert bool(x.any()) and bool(w.any()) and torch.equal(y, (x.double() @ w[0].double()).to(t)), (a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("width", list(range(129, 137)) + [7, 9, 1023])
+def test_widths_that_cut_a_chunk(dtype, width):
+    """Rows of every length modulo 8, both as the axis that is summed over and as the one that is not; rows before, between and
+    behind the groups; and the same layer with its activations in codes."""
+    (kind, t), gen, bounds, rows = oh.TYPES[dtype], generator(width), [1, 60, 60, 205], 207
+    other = 136
+    for k, n in ((width, other), (other, width), (width, width)):
+        x, dy, w = oh.matrix(rows, k, 0, t, gen), oh.matrix(rows, n, 0, t, gen), oh.stack(3, k, n, 0, 0, t, gen)
+        written = oh.inside(bounds, rows)
+        buf, y = oh.output((rows, n), 0, t)
+        oh.call("forward", oh.layer(dtype, bounds, rows, k, n, x=x, w=w, y=y))
+        out, mag, terms = oh.exact_product("forward", bounds, x, w)
+        close(y[written], out[written], oh.product_bound(out, mag, terms, t)[written])
+        assert oh.untouched(buf, y, written)
+        buf, dx = oh.output((rows, k), 0, t)
+        oh.call("input_grad", oh.layer(dtype, bounds, rows, k, n, x=x, dy=dy, w=w, dx=dx, flags=P.GROUPED_RELU_IN))
+        out, mag, terms = oh.exact_product("input_grad", bounds, dy, w)
+        close(dx[written], (out * (x > 0))[written], oh.product_bound(out, mag, terms, t)[written])
+        codes = torch.empty((rows, k), dtype=torch.uint8, device="cuda")
+        scales = torch.empty((rows, -(-k // 32)), dtype=torch.uint8, device="cuda")
+        P.checkpoint_store(torch.cuda.current_stream(), kind, rows, k, x, k, codes, k, scales, scales.shape[1])
+        back = torch.empty_like(x)
+        P.checkpoint_load(torch.cuda.current_stream(), kind, rows, k, codes, k, scales, scales.shape[1], back, k)
+        for source, value in ((dict(x=x), x), (dict(x_codes=codes, x_scales=scales), back)):
+            buf, dw = oh.output((3, k, n), 0, torch.float32)
+            oh.call("weight_grad", oh.layer(dtype, bounds, rows, k, n, dy=dy, dw=dw, **source))
+            out, mag, terms = oh.exact_product("weight_grad", bounds, value, dy)
+            close(dw, out, oh.product_bound(out, mag, terms, torch.float32))
+            assert oh.untouched(buf, dw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("bounds, rows, k, n", [([0, 900, 2100, 4000], 4000, 1304, 2568), ([5, 900, 2100, 4000], 4010, 1313, 2571), ([0, 3000], 3000, 96, 40), ([0, 2999], 3001, 65, 33)])
+def test_codes_in_every_tile(dtype, bounds, rows, k, n):
+    (kind, t), gen = oh.TYPES[dtype], generator(rows)
+    x, dy = torch.relu(oh.matrix(rows, k, 0, t, gen)), oh.matrix(rows, n, 0, t, gen)
+    codes = torch.empty((rows, k), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((rows, -(-k // 32)), dtype=torch.uint8, device="cuda")
+    P.checkpoint_store(torch.cuda.current_stream(), kind, rows, k, x, k, codes, k, scales, scales.shape[1])
+    back = torch.empty_like(x)
+    P.checkpoint_load(torch.cuda.current_stream(), kind, rows, k, codes, k, scales, scales.shape[1], back, k)
+    for workspace in (False, True):
+        dw = torch.empty((len(bounds) - 1, k, n), device="cuda")
+        oh.call("weight_grad", oh.layer(dtype, bounds, rows, k, n, dy=dy, dw=dw, x_codes=codes, x_scales=scales), workspace)
+        out, mag, terms = oh.exact_product("weight_grad", bounds, back, dy)
+        close(dw, out, oh.product_bound(out, mag, terms, torch.float32))
+
+
+def test_thousands_of_groups():
+    t, gen, groups, k, n = torch.bfloat16, generator(12), 5000, 24, 40
+    length = torch.randint(0, 4, (groups,), generator=gen, device="cuda")
+    bounds = [0] + torch.cumsum(length, 0).tolist()
+    rows = bounds[-1]
+    x, dy, w = oh.matrix(rows, k, 0, t, gen), oh.matrix(rows, n, 0, t, gen), oh.stack(groups, k, n, 0, 0, t, gen)
+    group = torch.repeat_interleave(torch.arange(groups, device="cuda"), length)
+    y, dw = torch.empty((rows, n), dtype=t, device="cuda"), torch.empty((groups, k, n), device="cuda")
+    oh.call("forward", oh.layer("bf16", bounds, rows, k, n, x=x, w=w, y=y))
+    oh.call("weight_grad", oh.layer("bf16", bounds, rows, k, n, x=x, dy=dy, dw=dw))
+    wide = w.double()[group]
+    out = (x.double()[:, :, None] * wide).sum(1)
+    close(y, out, oh.product_bound(out, (x.double()[:, :, None] * wide).abs().sum(1), k, t))
+    each = x.double()[:, :, None] * dy.double()[:, None, :]
+    out, mag = torch.zeros((groups, k, n), dtype=torch.float64, device="cuda"), torch.zeros((groups, k, n), dtype=torch.float64, device="cuda")
+    out.index_add_(0, group, each)
+    mag.index_add_(0, group, each.abs())
+    close(dw, out, oh.product_bound(out, mag, 4, torch.float32))
+
+
+def test_gradients_of_a_layer_against_differences():
+    """f(x, w) = <x w, dy> is linear in either argument: differences are exact but for rounding.  fp32, |f| below 100: each value of f is a float64
+    sum of fp32 results off by at most 72 2^-23 sum |x w| |dy| < 2e-3 at a step of one, so a quotient by 2e-3, and <dx, d> as much."""
+    gen, t, bounds, rows, k, n = generator(13), torch.float32, [0, 20, 50], 50, 64, 48
+    x, dy, w = oh.matrix(rows, k, 0, t, gen, 0.3), oh.matrix(rows, n, 0, t, gen, 0.3), oh.stack(2, k, n, 0, 0, t, gen, 0.3)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    oh.call("input_grad", oh.layer("fp32", bounds, rows, k, n, dy=dy, w=w, dx=dx))
+    oh.call("weight_grad", oh.layer("fp32", bounds, rows, k, n, x=x, dy=dy, dw=dw))
+
+    def f(xx, ww):
+        y = torch.empty((rows, n), device="cuda")
+        oh.call("forward", oh.layer("fp32", bounds, rows, k, n, x=xx, w=ww, y=y))
+        return (y.double() * dy.double()).sum().item()
+
+    for _ in range(3):
+        d = torch.randn(rows, k, generator=gen, device="cuda") * 0.3
+        assert abs((f(x + d, w) - f(x - d, w)) / 2 - (dx.double() * d.double()).sum().item()) < 4e-3
+        d = torch.randn(2, k, n, generator=gen, device="cuda") * 0.3
+        assert abs((f(x, w + d) - f(x, w - d)) / 2 - (dw.double() * d.double()).sum().item()) < 4e-3
 
 
 def test_shared_weights_pitches_and_offsets_beyond_32_bits():
@@ -272,6 +401,12 @@ LOSSES = [
     ([0, 257], 257, 200, 2049, 0, 600, 0.5),
     ([0, 5, 10], 10, 40, 300, 0, 0, 1.0),
     ([0, 1500, 2100], 2100, 72, 5000, 0, 0, 0.05),
+    ([3, 300], 310, 203, 3001, 0, 1024, 0.0),
+    ([0, 10, 700, 2900, 4000], 4000, 136, 2000, 8, 1024, 0.3),
+    # the large tile; the medium one, and it with odd rows
+    ([1, 2999], 3000, 72, 4104, 0, 0, 0.1),
+    ([0, 5990], 6000, 72, 136, 0, 0, 0.1),
+    ([0, 690], 700, 73, 4101, 0, 0, 0.1),
 ]
 
 
@@ -319,6 +454,10 @@ def test_loss_and_gradients(dtype, case, total):
     P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, loss=only, dh=one, grad_scale=scale, piece=piece,
                                                                        flags=P.CROSS_ENTROPY_SUM if total else 0))
     assert torch.equal(one[written], dh[written])
+    table = torch.empty_like(e)
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, loss=only, de=table, grad_scale=scale, piece=piece,
+                                                                       flags=P.CROSS_ENTROPY_SUM if total else 0))
+    assert torch.equal(table, de)
 
 
 def test_loss_gradient_against_differences():
@@ -515,6 +654,30 @@ def test_replays_of_a_captured_step_have_the_eager_bits():
             for t, e in zip((k.loss, k.group_loss, k.h2), eager[1:]):
                 assert torch.equal(t, e), turn
     k.ctx.close()
+
+
+def test_the_null_stream_and_another_thread():
+    import threading
+    gen, bounds, rows, k, n = generator(40), [0, 30, 90], 90, 64, 72
+    x, w = oh.matrix(rows, k, 0, torch.bfloat16, gen), oh.stack(2, k, n, 0, 0, torch.bfloat16, gen)
+    y = [torch.empty((rows, n), dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    calls = [oh.layer("bf16", bounds, rows, k, n, x=x, w=w, y=out) for out in y]
+    torch.cuda.synchronize()
+    P.grouped_forward(None, calls[0])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+
+    def other():
+        P.grouped_forward(side, calls[1])
+        with pytest.raises(P.CocodError, match="y is NULL"):
+            calls[2].set(y=None)
+            P.grouped_forward(side, calls[2])
+
+    worker = threading.Thread(target=other)
+    worker.start()
+    worker.join()
+    torch.cuda.synchronize()
+    assert torch.equal(y[0], y[1])
 
 
 def test_two_streams_at_once():

@@ -1,5 +1,7 @@
 """Grouped products, vocabulary loss, 8-bit checkpoints: what the host refuses, and the sizes it plans; no GPU call is made."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 
@@ -69,6 +71,23 @@ def test_grouped_struct_and_null():
     refused(P.grouped_workspace, grouped(), 3, text="direction")
     with pytest.raises(TypeError):
         P.Grouped(no_such_field=1)
+
+
+def test_descriptions_match_the_header(tmp_path):
+    """Size and place of every field, from a C compiler."""
+    names = {"cocod_grouped": P.Grouped, "cocod_cross_entropy_call": P.CrossEntropy}
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "cocod.h"', "int main(void) {"]
+    for name, mirror in names.items():
+        lines.append('printf("%s %%zu\\n", sizeof(%s));' % (name, name))
+        lines += ['printf("%s.%s %%zu\\n", offsetof(%s, %s));' % (name, f, name, f) for f, _ in mirror._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["return 0; }"]))
+    subprocess.run(["gcc", "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include"), str(src), "-o", str(exe)], check=True)
+    got = dict(line.split() for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
+    for name, mirror in names.items():
+        assert int(got[name]) == C.sizeof(mirror)
+        for f, _ in mirror._fields_:
+            assert int(got["%s.%s" % (name, f)]) == getattr(mirror, f).offset, f
 
 
 def test_grouped_workspace_is_needed_in_full_or_not_given():
