@@ -50,10 +50,12 @@ hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const Prod
 // 1024: 33 (1) / 26 (1) / 50 (1); 16 of 500 rows, 2048 x 1024, input gradient: 40 (1) / 47 (1) / 93 (1); 4 of 768 rows, 32000 x 1024: 239 (4) / 266 (8) /
 // 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); through registers one row, 4095 x 2047: - / 18 (8) / 14 (8), 2048 rows, 2047 x 2047: - / 46 (1) /
 // 77 (1); fp32 16 of 250 rows, 1024 x 1024: - / 56 (1) / 97 (1), 8 of 8 rows, 2048 x 2048: - / 58 (4) / 31 (2).
-struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile; };
-constexpr TileCost kCostDirect[] = {{256, 256, 64, 1.15, 5.2}, {128, 128, 64, 0.40, 1.4}, {32, 64, 128, 0.25, 0.5}};
-constexpr TileCost kCostRegs[] = {{0, 0, 0, 0, 0}, {128, 128, 64, 0.81, 3.4}, {32, 64, 128, 0.50, 0.65}};
-constexpr TileCost kCost32[] = {{0, 0, 0, 0, 0}, {128, 128, 32, 1.25, 3.7}, {32, 64, 64, 0.57, 1.3}};
+struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile; Tile tile; uint32_t most_turns; };
+constexpr TileCost kCostDirect[] = {{256, 256, 64, 1.15, 5.2, Tile::Large, ~0u}, {128, 128, 64, 0.40, 1.4, Tile::Medium, ~0u},
+                                    {32, 64, 128, 0.25, 0.5, Tile::Small, ~0u}, {128, 128, 64, 0.56, 1.4, Tile::Deep, 1}};
+constexpr TileCost kCostRegs[] = {{128, 128, 64, 0.81, 3.4, Tile::Medium, ~0u}, {32, 64, 128, 0.50, 0.65, Tile::Small, ~0u}};
+constexpr TileCost kCost32[] = {{128, 128, 32, 1.25, 3.7, Tile::Medium, ~0u}, {32, 64, 64, 0.57, 1.3, Tile::Small, ~0u}};
+constexpr double kAlone = 1.75;       // a medium tile that has its compute unit to itself: per slice so much more than its share
 constexpr uint32_t kMaxSplits = 16;
 
 ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split)
@@ -62,17 +64,20 @@ ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, 
     const double mean_rows = static_cast<double>(rows) / groups, terms = weights ? mean_rows : k;
     const double cells = weights ? static_cast<double>(groups) * m * n : static_cast<double>(rows) * n;
     const TileCost *const costs = type == Dtype::F32 ? kCost32 : direct ? kCostDirect : kCostRegs;
+    const uint32_t n_costs = type != Dtype::F32 && direct ? 4 : 2;
     ProductPlan best{Tile::Medium, 1};
     double least = 1e300;
-    for (uint32_t tile = costs[0].bm ? 0 : 1; tile < 3; ++tile) {
-        const TileCost &c = costs[tile];
+    for (uint32_t i = 0; i < n_costs; ++i) {
+        const TileCost &c = costs[i];
         // ragged groups end half a tile short, in the mean
         const double high = weights || groups == 1 ? std::ceil((weights ? m : mean_rows) / c.bm) : std::fmax(1.0, mean_rows / c.bm + 0.5);
         const double tiles = groups * high * std::ceil(static_cast<double>(n) / c.bn);
         for (uint32_t splits = 1; splits <= (may_split ? kMaxSplits : 1u); splits *= 2) {
             const double turns = std::fmax(1.0, std::ceil(tiles * splits / 256.0 - 1e-9)), slices = std::fmax(1.0, std::ceil(terms / c.bk / splits));
-            const double us = 5.0 + turns * (slices * c.per_slice + c.per_tile) + (splits > 1 ? 4.0 + cells * 4.0 * (splits + 1) / 4.0e6 : 0.0);
-            if (us < least) { least = us; best = {static_cast<Tile>(tile), splits}; }
+            if (turns > c.most_turns) continue;
+            const double alone = direct && type != Dtype::F32 && c.tile == Tile::Medium && turns == 1.0 ? kAlone : 1.0;
+            const double us = 5.0 + turns * (slices * c.per_slice * alone + c.per_tile) + (splits > 1 ? 4.0 + cells * 4.0 * (splits + 1) / 4.0e6 : 0.0);
+            if (us < least) { least = us; best = {c.tile, splits}; }
         }
     }
     return best;

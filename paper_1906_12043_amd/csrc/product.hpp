@@ -67,7 +67,7 @@ struct ProductParams {
 };
 
 // Tile shapes a launch can take (plan_product picks one).
-enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2 };
+enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3 };
 
 // C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats or Slope), one launch, with splits one more that joins
 // them.  hipErrorInvalidConfiguration: the grid would exceed a launch's limits.
@@ -94,9 +94,11 @@ inline bool direct_b(Layout layout, const ProductParams &p)
 {
     return direct_operand(p.b, p.ldb, layout == Layout::Weights ? 0 : p.b_group, layout != Layout::Rows_NK || p.k % 8 == 0);
 }
-// The tile that a launch takes where `planned` was planned: the large one needs operands that go to LDS directly (or codes).
+// The tile that a launch takes where `planned` was planned: the large and the deep one need operands that go to LDS directly (the large one
+// also takes codes).
 inline Tile settle_tile(Dtype type, Layout layout, Tile planned, const ProductParams &p)
 {
+    if (planned == Tile::Deep && (type == Dtype::F32 || !direct_a(layout, p) || !direct_b(layout, p))) return Tile::Medium;
     return planned == Tile::Large && (type == Dtype::F32 || (p.a && !direct_a(layout, p)) || !direct_b(layout, p)) ? Tile::Medium : planned;
 }
 

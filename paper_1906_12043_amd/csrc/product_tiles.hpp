@@ -866,6 +866,10 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
 
 typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
+// where every compute unit has one block at most: the medium tile with four slices in LDS instead of two (and room for a second block).  2048 x 2048 x
+// 2048: 25 us instead of 29, 4 groups of 1024 rows, 2048 to 512 columns: 22 instead of 26, out of memory 23 instead of 33; with 512 blocks (16 groups of 512
+// rows, 1024 x 1024) 30 instead of 24
+typedef TileShape<128, 128, 64, 2, 4, 1, 4> Deep16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 // short sums and few blocks: a slice more in flight (one row, 4096 x 4096: 10.1 us instead of 11.0; the other tiles lose by four slices of 32: 8 groups
 // of 8192 rows, 4096 x 4096, input gradient 1962 us instead of 1840: of a row of 64 bytes the other half of the line is fetched again)
@@ -895,6 +899,7 @@ hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
             }
         if (b_direct && direct_a(LAYOUT, p)) {
             if (tile == Tile::Large) return launch_one<T, LAYOUT, Large16, FINISH, kDirect, kDirect>(stream, p);
+            if (tile == Tile::Deep) return launch_one<T, LAYOUT, Deep16, FINISH, kDirect, kDirect>(stream, p);
             return tile == Tile::Small ? launch_one<T, LAYOUT, Small16Direct, FINISH, kDirect, kDirect>(stream, p)
                                        : launch_one<T, LAYOUT, Medium16, FINISH, kDirect, kDirect>(stream, p);
         }
