@@ -22,6 +22,7 @@ enum class Layout { Rows_KN, Rows_NK, Weights };
 enum class Finish {
     Store,       // relu, mask, scale, running sum; store in the element type or fp32
     Stats,       // logits: maximum and sum of exponentials of the tile's part of every row, and the target's logit
+    Keep,        //   the same, and the exponentials stored (bf16: in fp16 times 2^14; pitch and columns to the end of the last tile are the buffer's)
     Slope        // logits: softmax minus one-hot, stored in the element type
 };
 
@@ -69,7 +70,7 @@ struct ProductParams {
 // Tile shapes a launch can take (plan_product picks one).
 enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3 };
 
-// C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats or Slope), one launch, with splits one more that joins
+// C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats, Keep or Slope), one launch, with splits one more that joins
 // them.  hipErrorInvalidConfiguration: the grid would exceed a launch's limits.
 hipError_t launch_store_bf16(hipStream_t stream, Layout layout, Tile tile, const ProductParams &p);
 hipError_t launch_store_f16(hipStream_t stream, Layout layout, Tile tile, const ProductParams &p);

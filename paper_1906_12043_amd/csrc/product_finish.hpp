@@ -27,7 +27,9 @@ typedef u4 __attribute__((aligned(1))) u4_bytes;
 // and the tile is formed again with fp32 products.
 constexpr float kPlaneScale = 0x1p24f, kPlaneUnscale = 0x1p-48f;
 
+// exp(x, base): e^(x - base); in 16 bits the instruction for powers of two, off by 2^-23 of |x - base| beside its own last bit
 constexpr float kLog2e = 1.44269504f;
+constexpr float kKeepScale = 0x1p14f, kKeepUnscale = 0x1p-14f;   // of exponentials, at most 1, kept in fp16: exact to 2^-11 down to 2^-28 of the largest
 
 struct Bf16 {
     typedef uint16_t elem;
@@ -38,8 +40,7 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, bf2)); }
-    // e^(x - base): one rounding of the exponent, which is off by 2^-24 of |x| and |base|
-    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -kLog2e * base)); }
+    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
     static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
     {
         return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true))
@@ -55,8 +56,7 @@ struct F16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, hf2)); }
-    // e^(x - base): one rounding of the exponent, which is off by 2^-24 of |x| and |base|
-    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -kLog2e * base)); }
+    static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
     static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
     {
         return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, scale, true))
@@ -99,6 +99,13 @@ template <class T> __device__ __forceinline__ void store_values(void *out, uint6
         #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) if (j < count) o[j] = static_cast<uint16_t>((j < 2 ? lo : hi) >> (16 * (j % 2)));
     }
+}
+
+// Exponentials between the two passes over the vocabulary: fp32 as they are, for bf16 slopes in fp16, whose eleven bits leave the rounding to eight alone.
+template <class T> __device__ __forceinline__ void keep_values(void *out, uint64_t at, f4 v)
+{
+    if constexpr (sizeof(typename T::elem) == 4) *reinterpret_cast<f4 *>(static_cast<float *>(out) + at) = v;
+    else *reinterpret_cast<u2 *>(static_cast<uint16_t *>(out) + at) = u2{F16::pack(v.x * kKeepScale, v.y * kKeepScale), F16::pack(v.z * kKeepScale, v.w * kKeepScale)};
 }
 
 template <class T> __device__ __forceinline__ bool above_zero(const ProductParams &p, uint64_t row, uint32_t col)

@@ -749,7 +749,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int w = 1; w < S::WK; ++w) v += *reinterpret_cast<const f4 *>(part + (w * S::BM + r) * PITCH + q);
             v *= unscale;
-            if constexpr (FINISH == Finish::Stats) {
+            if constexpr (FINISH == Finish::Stats || FINISH == Finish::Keep) {
                 static_assert(LANES <= 64 && 64 % LANES == 0, "a row within a wave");
                 const int32_t target = r < at.rows ? p.target[at.row0 + r] : -1;
                 float top = -INFINITY;
@@ -762,7 +762,9 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 #pragma unroll
                 for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
                 const float base = top == -INFINITY ? 0.0f : top;
-                float sum = (T::exp(v[0], base) + T::exp(v[1], base)) + (T::exp(v[2], base) + T::exp(v[3], base));
+                v = f4{T::exp(v[0], base), T::exp(v[1], base), T::exp(v[2], base), T::exp(v[3], base)};
+                if (FINISH == Finish::Keep && r < at.rows) keep_values<T>(p.out, (at.row0 + r) * p.ldc + c, v);
+                float sum = (v[0] + v[1]) + (v[2] + v[3]);
                 #pragma unroll
                 for (int d = 1; d < LANES; d <<= 1) sum += __shfl_xor(sum, d, 64);
                 if (q == 0 && r < at.rows) p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
@@ -770,9 +772,11 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 finish(r, c, v);
             }
         }
-    } else if constexpr (FINISH == Finish::Stats) {
-        // per row block: maximum and sum over the wave's columns (a lane and the one 32 further on hold a row), then over the waves
-        float2 *share = reinterpret_cast<float2 *>(lds);       // the operand buffers are free: the loop ended with a barrier
+    } else if constexpr (FINISH == Finish::Stats || FINISH == Finish::Keep) {
+        // The maximum over the wave's columns (a lane and the one 32 further on hold a row), over the waves, and the sums of exponentials below the tile's
+        // maximum; kept or not, the same bits.
+        constexpr bool KEEP = FINISH == Finish::Keep;
+        float *tops = reinterpret_cast<float *>(lds), *sums = tops + S::WN * S::BM;        // the operand buffers are free
         const uint32_t c0 = at.n0 + wn * S::NB * 32 + 4 * (lane / 32);
         const bool whole = at.n0 + S::BN <= p.n;
         #pragma unroll
@@ -786,7 +790,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                     for (int x = 0; x < 16; ++x)
                         if (static_cast<int32_t>(c0 + j * 32 + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
             }
-            float top = -INFINITY, sum = 0.0f;
+            float top = -INFINITY;
             if (!whole) {
                 #pragma unroll
                 for (int j = 0; j < S::NB; ++j)
@@ -798,28 +802,52 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 #pragma unroll
                 for (int x = 0; x < 16; ++x) top = fmaxf(top, acc[0][i][j][x]);
             top = fmaxf(top, __shfl_xor(top, 32, 64)) * unscale;
+            if (lane < 32) tops[wn * S::BM + r] = top;
+            __builtin_amdgcn_sched_barrier(0);                 // one row block's values at a time
+        }
+        __syncthreads();
+        constexpr int PITCH = S::NB * 32 + 4, LANES = S::NB * 8;
+        static_assert(2 * S::WN * S::BM * 4 + S::threads / 64 * 32 * PITCH * 4 <= P::lds_bytes, "statistics and the waves' turned rows");
+        float *mine = sums + S::WN * S::BM + wave * 32 * PITCH;
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i) {
+            const uint32_t r0 = (wm * S::MB + i) * 32, r = r0 + lane % 32;
+            float top = -INFINITY, sum = 0.0f;
+            #pragma unroll
+            for (int w = 0; w < S::WN; ++w) top = fmaxf(top, tops[w * S::BM + r]);
             const float base = top == -INFINITY ? 0.0f : top;
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) {
                 #pragma unroll
-                for (int x = 0; x < 16; ++x) sum += T::exp(acc[0][i][j][x] * unscale, base);
+                for (int g = 0; g < 4; ++g) {
+                    f4 e;
+                    #pragma unroll
+                    for (int x = 0; x < 4; ++x) e[x] = T::exp(acc[0][i][j][4 * g + x] * unscale, base);
+                    sum += (e[0] + e[1]) + (e[2] + e[3]);
+                    if (KEEP) *reinterpret_cast<f4 *>(mine + (lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) = e;
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             sum += __shfl_xor(sum, 32, 64);
-            if (lane < 32) share[wn * S::BM + r] = make_float2(top, sum);
-            __builtin_amdgcn_sched_barrier(0);                 // one row block's values at a time
+            if (lane < 32) sums[wn * S::BM + r] = sum;
+            if constexpr (KEEP) {
+                __builtin_amdgcn_wave_barrier();
+                #pragma unroll 4
+                for (uint32_t k = lane / LANES; k < 32; k += 64 / LANES) {
+                    const uint32_t q = lane % LANES * 4;
+                    const f4 e = *reinterpret_cast<const f4 *>(mine + k * PITCH + q);
+                    if (r0 + k < at.rows) keep_values<T>(p.out, (at.row0 + r0 + k) * p.ldc + at.n0 + wn * S::NB * 32 + q, e);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
         }
         __syncthreads();
         for (uint32_t r = threadIdx.x; r < at.rows; r += S::threads) {
             float top = -INFINITY, sum = 0.0f;
             #pragma unroll
-            for (int w = 0; w < S::WN; ++w) top = fmaxf(top, share[w * S::BM + r].x);
-            const float base = top == -INFINITY ? 0.0f : top;
+            for (int w = 0; w < S::WN; ++w) top = fmaxf(top, tops[w * S::BM + r]);
             #pragma unroll
-            for (int w = 0; w < S::WN; ++w) {
-                const float2 s = share[w * S::BM + r];
-                sum += s.y * T::exp(s.x, base);               // (a part without columns: 0 times 0; a NaN stays one)
-            }
+            for (int w = 0; w < S::WN; ++w) sum += sums[w * S::BM + r];
             p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
         }
     } else {
@@ -917,8 +945,10 @@ template <class T> hipError_t launch_store(hipStream_t stream, Layout layout, Ti
 
 template <class T> hipError_t launch_logits(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p)
 {
-    return finish == Finish::Stats ? launch_layout<T, Layout::Rows_NK, Finish::Stats>(stream, tile, p)
-                                   : launch_layout<T, Layout::Rows_NK, Finish::Slope>(stream, tile, p);
+    if (finish == Finish::Stats) return launch_layout<T, Layout::Rows_NK, Finish::Stats>(stream, tile, p);
+    if constexpr (!std::is_same<T, F16>::value)                // (its slopes would be rounded twice to the same eleven bits)
+        if (finish == Finish::Keep) return launch_layout<T, Layout::Rows_NK, Finish::Keep>(stream, tile, p);
+    return finish == Finish::Slope ? launch_layout<T, Layout::Rows_NK, Finish::Slope>(stream, tile, p) : hipErrorInvalidValue;
 }
 
 }  // namespace

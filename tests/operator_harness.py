@@ -203,6 +203,8 @@ def loss_bounds(out, t, dim, vocab):
     error (|x| + 2 steps of 2^-23 at an argument x below the maximum, whose mean over the terms is below 32), and by the additions (a lane
     adds up to 128 values, then lanes, waves and tiles: fewer than 256 + vocab / 64).  So norm is off by at most
     r = d + (300 + vocab / 64) 2^-23 + |norm| 2^-23, the loss by r + d, and a probability by the factor r + d + 40 steps.
+    Between two passes an exponential relative to its tile's maximum may be held in 11 bits (bf16, 2^-11 of it and not below steps of 2^-38) or 24,
+    and is multiplied by a second exponential, with errors like the first's: 80 steps and 2^-11 of the probability.
     A slope is rounded by half a step of the type (fp16: times 2^14, not below steps of 2^-38).  The two products add what products add.
     """
     u = half_step(t)
@@ -211,8 +213,8 @@ def loss_bounds(out, t, dim, vocab):
         d = (dim + 8) * STEP * (hh.abs() @ ee.abs().t()).amax(1)
         r = d + (300 + vocab / 64) * STEP + norm.abs() * STEP
         bound["loss"][ids] = r + d + STEP * (out["loss"][ids] + norm.abs())
-        off = prob * (r + d + 40 * STEP)[:, None] * 1.01 + STEP
-        off = off * (prob > 0) + (u if t != torch.float32 else STEP) * dz.abs() + (2.0 ** -39 if t == torch.float16 else 0.0)
+        off = prob * (r + d + 80 * STEP + (2.0 ** -11 if t == torch.bfloat16 else 0.0))[:, None] * 1.01 + STEP
+        off = off * (prob > 0) + (u if t != torch.float32 else STEP) * dz.abs() + (2.0 ** -39 if t != torch.float32 else 0.0)
         for key, at, left, right, terms in (("dh", ids, (off, dz), ee, vocab), ("de", g, (off.t(), dz.t()), hh, len(ids))):
             far = left[0] @ right.abs() + (terms + 8) * STEP * ((left[1].abs() + left[0]) @ right.abs())
             bound[key][at] = abs(scale) * far * (1 + u) + (u + 4 * STEP) * out[key][at].abs() + torch.finfo(t).smallest_normal * torch.finfo(t).eps
