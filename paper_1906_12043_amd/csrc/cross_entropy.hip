@@ -205,15 +205,15 @@ template <bool NORMS> __global__ __launch_bounds__(kMeanThreads) void mean_kerne
 }
 
 // Slopes from kept exponentials, in their place: exp(z - top) exp(top - norm) - [v = t], top the tile's maximum.  Eight columns a thread.
-template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Rows p, const Norms n, const int32_t *target, void *slopes, uint64_t pitch, uint32_t vocab,
-                                                                       uint32_t vocab_end, uint32_t tile_cols, uint32_t parts)
+template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Rows p, const Norms n, const int32_t *target, void *slopes, uint64_t pitch, uint32_t v0,
+                                                                       uint32_t columns, uint32_t columns_end, uint32_t tile_cols, uint32_t parts)
 {
     typedef typename T::elem elem;
     const uint64_t r = blockIdx.x / parts;
     const uint32_t c = (blockIdx.x % parts * 256 + threadIdx.x) * 8;
-    if (c >= vocab_end || r < clamped(p, 0) || r >= clamped(p, p.groups) || n.index[r] == kNoRow) return;
+    if (c >= columns_end || r < clamped(p, 0) || r >= clamped(p, p.groups) || n.index[r] == kNoRow) return;
     const float factor = expf(n.stats[static_cast<uint64_t>(c / tile_cols) * p.rows + r].x - n.norm[r]);
-    const uint32_t number = static_cast<uint32_t>(target[r]) - c;
+    const uint32_t number = static_cast<uint32_t>(target[r]) - v0 - c;
     elem *at = static_cast<elem *>(slopes) + r * pitch + c;
     float v[8];
     if constexpr (sizeof(elem) == 4) {
@@ -227,7 +227,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Row
     #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
         if (number == j) v[j] -= 1.0f;
-        if (c + j >= vocab) v[j] = 0.0f;
+        if (c + j >= columns) v[j] = 0.0f;
     }
     if constexpr (sizeof(elem) == 4) {
         *reinterpret_cast<f4 *>(at) = f4{v[0], v[1], v[2], v[3]};
@@ -246,7 +246,7 @@ struct Workspace {
     uint64_t index, target, ends, norm, target_logit, row_scale, hidden, stats, slope, sum, part, bytes;
     uint64_t pitch, piece, sum_pitch;
     uint32_t pieces;
-    bool keep;                        // the exponentials of the first pass stay, as slopes to be
+    bool keep;                        // the last piece's exponentials stay from the first pass, as slopes to be
     ProductPlan logits, slopes, to_hidden, to_table;
 };
 
@@ -290,7 +290,7 @@ Workspace carve(const cocod_cross_entropy_call *c)
         if (c->de) { const uint64_t q = part_bytes(w.to_table, Layout::Weights, rows, c->groups, n, c->dim); part = part > q ? part : q; }
         w.part = take(part);
     }
-    w.keep = grads && rows != 0 && w.pieces == 1 && t != Dtype::F16 && rows * ((whole / 8 + 255) / 256) * 256 < (1ull << 32);
+    w.keep = grads && rows != 0 && t != Dtype::F16 && rows * ((w.piece / 8 + 255) / 256) * 256 < (1ull << 32);
     w.bytes = at;
     return w;
 }
@@ -394,18 +394,28 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     z.k = c->dim; z.splits = 1; z.target = target;
     Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), 0, reinterpret_cast<float *>(ws + w.target_logit), norm, c->loss};
     bool here = true;
-    uint32_t cols = 0;
+    uint32_t cols = 0, kept_v0 = static_cast<uint32_t>((w.pieces - 1) * w.piece);
+    uint64_t kept_tile0 = 0;
     if (c->rows) {
         ProductParams p = z;
         p.n = c->vocab;
         p.stats = reinterpret_cast<float2 *>(ws + w.stats);
         p.target_logit = norms.target_logit;
         const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, p);
-        p.out = ws + w.slope;
-        p.ldc = w.piece;
-        if (int rc = launch_status(launch_logits(q, t, w.keep ? Finish::Keep : Finish::Stats, tile, p), what)) return rc;
         cols = tile_cols(t, tile);
-        norms.tiles = (c->vocab + tile_cols(t, tile) - 1) / tile_cols(t, tile);
+        kept_tile0 = kept_v0 / cols;                           // (pieces are whole tiles)
+        p.n = w.keep ? kept_v0 : c->vocab;
+        if (p.n) if (int rc = launch_status(launch_logits(q, t, Finish::Stats, tile, p), what)) return rc;
+        if (w.keep) {
+            p.b = static_cast<const uint8_t *>(c->e) + static_cast<uint64_t>(kept_v0) * c->lde * s;
+            p.n = c->vocab - kept_v0;
+            p.v0 = kept_v0;
+            p.stats += kept_tile0 * c->rows;
+            p.out = ws + w.slope;
+            p.ldc = w.piece;
+            if (int rc = launch_status(launch_logits(q, t, Finish::Keep, tile, p), what)) return rc;
+        }
+        norms.tiles = (c->vocab + cols - 1) / cols;
         here = c->rows * norms.tiles <= kStatsHere * kMeanThreads * c->groups;
         if (!here) hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + kNormRows - 1) / kNormRows)), dim3(kNormRows * kNormThreads), 0, q, rows, norms);
     }
@@ -414,15 +424,17 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     if (int rc = launch_status(hipGetLastError(), what)) return rc;
     if (!c->dh && !c->de) return COCOD_OK;
 
-    for (uint32_t i = 0; i < w.pieces; ++i) {
-        const uint64_t v0 = i * w.piece;
+    for (uint32_t i = 0; i < w.pieces; ++i) {                  // the last piece first: its exponentials are there
+        const uint64_t v0 = (w.pieces - 1 - i) * w.piece;
         const uint32_t n = static_cast<uint32_t>(c->vocab - v0 < w.piece ? c->vocab - v0 : w.piece);
         const uint8_t *e = static_cast<const uint8_t *>(c->e) + v0 * c->lde * s;
-        if (w.keep) {
+        if (w.keep && i == 0) {
             const uint32_t end = (n + 7) / 8 * 8, parts = (end / 8 + 255) / 256;
             const dim3 grid(static_cast<uint32_t>(c->rows * parts));
-            if (t == Dtype::F32) hipLaunchKernelGGL(slope_kernel<F32>, grid, dim3(256), 0, q, rows, norms, target, ws + w.slope, w.piece, n, end, cols, parts);
-            else                 hipLaunchKernelGGL(slope_kernel<Bf16>, grid, dim3(256), 0, q, rows, norms, target, ws + w.slope, w.piece, n, end, cols, parts);
+            Norms kept = norms;
+            kept.stats += kept_tile0 * c->rows;
+            if (t == Dtype::F32) hipLaunchKernelGGL(slope_kernel<F32>, grid, dim3(256), 0, q, rows, kept, target, ws + w.slope, w.piece, kept_v0, n, end, cols, parts);
+            else                 hipLaunchKernelGGL(slope_kernel<Bf16>, grid, dim3(256), 0, q, rows, kept, target, ws + w.slope, w.piece, kept_v0, n, end, cols, parts);
             if (int rc = launch_status(hipGetLastError(), what)) return rc;
         } else if (c->rows) {
             ProductParams p = z;
