@@ -1,8 +1,13 @@
 // Grouped matrix products on the matrix cores: C = A B for every group of a ragged batch, one launch for all groups.
 //
-// A block computes a BM x BN tile of C.  Slices of BK terms of both operands pass through LDS, two buffers, one barrier per
-// slice; the next slice is on its way while this one is multiplied.  The matrix instruction is 32x32x16 with the operands
-// exchanged (C^T = B^T A^T), so that a lane holds one row of C and runs of four consecutive columns of it.
+// A block computes a BM x BN tile of C.  Slices of BK terms of both operands pass through LDS, several on their way at a time, one meeting of the
+// waves per slice.  The matrix instruction is 32x32x16 with the operands exchanged (C^T = B^T A^T), so that a lane holds one row of C and runs of four
+// consecutive columns of it.
+//
+// What bounds it: long sums the chip's power (8 groups of 8192 rows, 4096 x 4096 bf16: forward 1924 us, 1.14 PFLOP/s, at 1.75 GHz with the
+// matrix cores busy 68 % of the time; without loads to LDS 1.41, without reads from it 1.40, without both 1.94 PFLOP/s), short ones the start and end
+// of blocks and the latency of slices out of memory, few rows the stream of the weights (16 matrices of 1024 x 1024, a row each: 9.4 us,
+// 3.6 TB/s).
 //
 // In LDS an operand lies as it does in memory: with the summed axis contiguous ([BX][BK], read as 16-byte pieces of eight
 // terms) or with the other axis contiguous ([BK][BX], read by the transposing 8-byte LDS loads, which give a lane four
