@@ -400,7 +400,8 @@ int cocod_debug_copy(void *stream, const float *src, float *dst, uint64_t n);
  * with a pitch ("ld", elements from row to row) of their own; any alignment to whole elements and any
  * pitch work.  16-bit operands that start on 16 bytes, with pitches, group strides and a summed axis that
  * are multiples of 8, are the fast ones; of such a row the whole 16-byte piece that holds its last
- * element is read.  Row-wise arrays may be NULL where rows is 0.  Outputs must not overlap other arguments.  Sums are kept in fp32 (fp32 operands are multiplied
+ * element is read.  Row-wise arrays may be NULL where rows is 0.  COCOD_ERR_UNSUPPORTED: the result has more tiles than one
+ * launch holds (2^32 threads: 2^24 tiles of 128 x 128, or of 32 x 64 where groups have few rows, a tile begun per group counted).  Outputs must not overlap other arguments.  Sums are kept in fp32 (fp32 operands are multiplied
  * at fp32 accuracy) and rounded once.
  */
 typedef enum cocod_dtype {
@@ -464,7 +465,7 @@ typedef struct cocod_cross_entropy_call {
     uint32_t dtype;                 /* cocod_dtype of h, e, dh, de */
     uint32_t groups;                /* 1 .. 65535 */
     uint32_t flags;                 /* COCOD_CROSS_ENTROPY_* */
-    uint64_t rows;                  /* < 2^31; 0 is legal */
+    uint64_t rows;                  /* < 2^26; 0 is legal */
     uint32_t dim, vocab;            /* 1 .. 2^30 */
     const int64_t *offsets;         /* device, [groups + 1], 8-byte aligned */
     const void *h;   uint64_t ldh;              /* [rows][dim] hidden states */

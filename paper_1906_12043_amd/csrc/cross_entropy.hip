@@ -21,6 +21,7 @@ namespace {
 
 const Dtype kTypes[] = {Dtype::F32, Dtype::BF16, Dtype::F16};
 constexpr uint32_t kPieceUnit = 256;
+constexpr uint64_t kMaxLossRows = 1ull << 26;        // a wave a row in one launch
 constexpr uint64_t kPieceElements = 1ull << 28;      // of dz in memory at a time, unless the caller says otherwise
 
 struct Rows {
@@ -303,7 +304,7 @@ int check(const cocod_cross_entropy_call *c)
     if (int rc = check_dtype(c->dtype)) return rc;
     if (c->flags & ~COCOD_CROSS_ENTROPY_SUM) return set_error(COCOD_ERR_INVALID, "unknown flag bits 0x%x", c->flags);
     if (c->groups < 1 || c->groups > kMaxGroups) return set_error(COCOD_ERR_INVALID, "groups must be in 1..65535");
-    if (c->rows > kMaxRows) return set_error(COCOD_ERR_INVALID, "rows must be below 2^31");
+    if (c->rows >= kMaxLossRows) return set_error(COCOD_ERR_INVALID, "rows must be below 2^26");
     if (c->dim < 1 || c->dim > kMaxWidth || c->vocab < 1 || c->vocab > kMaxWidth) return set_error(COCOD_ERR_INVALID, "dim and vocab must be in 1..2^30");
     if (!std::isfinite(c->grad_scale)) return set_error(COCOD_ERR_INVALID, "grad_scale is not finite");
     return COCOD_OK;
@@ -389,7 +390,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     if (int rc = launch_status(t == Dtype::F32 ? launch_gather<float>(q, rows, c, w, ws, scale) : launch_gather<uint16_t>(q, rows, c, w, ws, scale), what)) return rc;
     ProductParams z{};
     z.a = ws + w.hidden; z.lda = w.pitch;
-    z.b = c->e; z.ldb = c->lde; z.b_group = c->e_stride;
+    z.b = c->e; z.ldb = c->lde; z.b_group = c->groups > 1 ? c->e_stride : 0;
     z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
     z.k = c->dim; z.splits = 1; z.target = target;
     Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), 0, reinterpret_cast<float *>(ws + w.target_logit), norm, c->loss};
@@ -450,7 +451,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
         p.part = reinterpret_cast<float *>(ws + w.part); p.ld_part = part_pitch(c->dim);
         if (c->dh && c->rows) {
             ProductParams d = p;
-            d.b = e; d.ldb = c->lde; d.b_group = c->e_stride;
+            d.b = e; d.ldb = c->lde; d.b_group = z.b_group;
             d.k = n; d.a_zero_padded = 1;
             d.out = c->dh; d.ldc = c->lddh; d.out_row = index; d.row_scale = row_scale;
             if (w.pieces > 1) { d.sum = reinterpret_cast<float *>(ws + w.sum); d.ld_sum = w.sum_pitch; d.sum_read = i > 0; d.sum_write = i + 1 < w.pieces; }

@@ -190,7 +190,7 @@ int cocod_grouped_forward(void *stream, const cocod_grouped *g)
     if (int rc = check_matrix("y", g->y, g->outer, g->ldy, s, g->rows)) return rc;
     ProductParams p{};
     p.a = g->x; p.lda = g->ldx;
-    p.b = g->w; p.ldb = g->ldw; p.b_group = g->w_stride;
+    p.b = g->w; p.ldb = g->ldw; p.b_group = g->groups > 1 ? g->w_stride : 0;
     p.n = g->outer; p.k = g->inner;
     p.out = g->y; p.ldc = g->ldy;
     p.relu = (g->flags & COCOD_GROUPED_RELU_OUT) != 0;
@@ -210,7 +210,7 @@ int cocod_grouped_input_grad(void *stream, const cocod_grouped *g)
     if (int rc = check_matrix("dx", g->dx, g->inner, g->lddx, s, g->rows)) return rc;
     ProductParams p{};
     p.a = g->dy; p.lda = g->lddy;
-    p.b = g->w; p.ldb = g->ldw; p.b_group = g->w_stride;
+    p.b = g->w; p.ldb = g->ldw; p.b_group = g->groups > 1 ? g->w_stride : 0;
     p.n = g->inner; p.k = g->outer;
     p.out = g->dx; p.ldc = g->lddx;
     Extent in[4] = {{"dy", g->dy, matrix_bytes(g->rows, g->outer, g->lddy, s)}, {"w", g->w, stack_bytes(g->groups, g->w_stride, g->inner, g->outer, g->ldw, s)}};

@@ -104,6 +104,13 @@ def test_grouped_workspace_is_needed_in_full_or_not_given():
     assert P.grouped_workspace(many, P.GROUPED_FORWARD) == 0
 
 
+def test_results_of_more_tiles_than_a_launch_are_refused():
+    # 65535 groups of 15 rows, 2^14 columns: (983025 / 32 + 65535) * 256 tiles of 256 threads
+    wide = grouped(groups=65535, rows=65535 * 15, inner=8, outer=1 << 14, ldx=8, ldw=1 << 14, ldy=1 << 14, w_stride=1 << 17,
+                   x=1 << 50, w=1 << 52, y=1 << 54)
+    refused(P.grouped_forward, None, wide, status=P.ERR_UNSUPPORTED, text="tiles")
+
+
 def test_no_rows_need_no_gpu():
     P.grouped_forward(None, grouped(rows=0))
     P.grouped_input_grad(None, grouped(rows=0, dy=None, dx=None))
@@ -120,7 +127,7 @@ def loss_call(**more):
 
 
 @pytest.mark.parametrize("change, text", [
-    (dict(dtype=7), "element type"), (dict(groups=0), "groups"), (dict(flags=2), "flag"), (dict(rows=1 << 31), "rows"), (dict(dim=0), "dim"),
+    (dict(dtype=7), "element type"), (dict(groups=0), "groups"), (dict(flags=2), "flag"), (dict(rows=1 << 26), "rows"), (dict(dim=0), "dim"),
     (dict(vocab=0), "dim and vocab"), (dict(vocab=(1 << 30) + 1), "dim and vocab"), (dict(grad_scale=float("nan")), "grad_scale"),
     (dict(offsets=A + 2), "offsets"), (dict(h=None), "h is NULL"), (dict(ldh=63), "rows of h"), (dict(e=3 * A + 1), "e is not aligned"),
     (dict(e_stride=63999), "overlap"), (dict(targets=None), "targets"), (dict(targets=4 * A + 2), "targets"), (dict(loss=None), "loss"),
