@@ -39,6 +39,10 @@ struct Bf16 {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, bf2)); }
     static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
     static __device__ __forceinline__ unsigned codes(unsigned four, float scale, bool high)
@@ -54,6 +58,10 @@ struct F16 {
     static __device__ __forceinline__ f16v mfma(u4 a, u4 b, f16v c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ unsigned pack(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2{a, b}, hf2)); }
     static __device__ __forceinline__ float exp(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }

@@ -1,11 +1,11 @@
 // Grouped matrix products on the matrix cores: C = A B for every group of a ragged batch, one launch for all groups.
 //
 // A block computes a BM x BN tile of C.  Slices of BK terms of both operands pass through LDS, several on their way at a time, one meeting of the
-// waves per slice.  The matrix instruction is 32x32x16 with the operands exchanged (C^T = B^T A^T), so that a lane holds one row of C and runs of four
+// waves per slice.  The matrix instruction, 32x32x16 or 16x16x32, has the operands exchanged (C^T = B^T A^T), so that a lane holds one row of C and runs of four
 // consecutive columns of it.
 //
-// What bounds it: long sums the chip's power (8 groups of 8192 rows, 4096 x 4096 bf16: forward 1924 us, 1.14 PFLOP/s, at 1.75 GHz with the
-// matrix cores busy 68 % of the time; without loads to LDS 1.41, without reads from it 1.40, without both 1.94 PFLOP/s), short ones the start and end
+// What bounds it: long sums the chip's power (8 groups of 8192 rows, 4096 x 4096 bf16: forward 1796 us, 1.22 PFLOP/s; with
+// 32x32x16 1.14 at 1.75 GHz, without loads to LDS 1.41, without reads from it 1.40, without both 1.94 PFLOP/s), short ones the start and end
 // of blocks and the latency of slices out of memory, few rows the stream of the weights (16 matrices of 1024 x 1024, a row each: 9.4 us,
 // 3.6 TB/s).
 //
@@ -24,11 +24,12 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 // Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2> struct TileShape {
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2, int MI_ = 32> struct TileShape {
     static constexpr int STAGES = STAGES_;           // slices in LDS
+    static constexpr int MI = MI_, MK = MI == 32 ? 16 : 32, X = MI * MI / 64;        // the matrix instruction: MI x MI x MK, X values a lane
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
     static constexpr int threads = 64 * WM * WN * WK;
-    static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;       // 32x32 blocks of a wave
+    static constexpr int MB = BM / WM / MI, NB = BN / WN / MI;       // blocks of a wave
 };
 
 // How a tile of [ROWS][COLS] 16-bit elements lies in LDS.  KC: the summed axis is the contiguous one.
@@ -40,14 +41,14 @@ template <bool KC, int BX, int BK> struct LdsTile {
         if (KC) return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3;      // sixteen rows of one chunk: sixteen places
         return CH >= 16 ? (row & 3) << 2 : CH == 8 ? (row & 2) << 1 : 0;
     }
-    // eight terms k0 + 8 (lane / 32) .. of the element x0 + lane % 32 of the other axis
-    static __device__ __forceinline__ u4 fragment(const uint8_t *lds, uint32_t x0, uint32_t k0, uint32_t lane)
+    // eight terms k0 + 8 (lane / MI) .. of the element x0 + lane % MI of the other axis
+    template <int MI> static __device__ __forceinline__ u4 fragment(const uint8_t *lds, uint32_t x0, uint32_t k0, uint32_t lane)
     {
         if constexpr (KC) {
-            const uint32_t row = x0 + lane % 32, c = k0 / 8 + lane / 32;
+            const uint32_t row = x0 + lane % MI, c = k0 / 8 + lane / MI;
             return *reinterpret_cast<const u4 *>(lds + row * (COLS * 2) + ((c ^ swizzle(row)) * 16));
         } else {
-            const uint32_t i = lane % 16, row = k0 + 8 * (lane / 32) + i / 4, c = (x0 + (lane & 16)) / 8 + (i % 4) / 2;
+            const uint32_t i = lane % 16, row = k0 + 8 * (lane / MI) + i / 4, c = (x0 + (lane % MI - i)) / 8 + (i % 4) / 2;
             const uint8_t *at = lds + row * (COLS * 2) + ((c ^ swizzle(row)) * 16) + (i % 2) * 8;
             union { s4 h[2]; u4 v; } out;
             out.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at);
@@ -379,72 +380,82 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     typedef Loader<T, HOW_B, B_KC, S::BN, S::BK, S::threads> LoadB;
     static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
-    static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 2 * (S::NB * 32 + 4) * 4;
+    static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 64 * S::MI * (S::NB * S::MI + 4) * 4;
     static constexpr int ST = S::STAGES, REQUESTS = LoadA::N + LoadB::N;
     static_assert(ST == 2 || (HOW_A == kDirect && HOW_B == kDirect), "operands in registers hold one slice");
     static constexpr int lds_bytes = ST * stage > join_bytes ? ST * stage : join_bytes;
 
-    // The pipeline.  While the matrix cores work on one step of 16 terms (times WK), the fragments of the next step are read.  In front
-    // of a slice's last step all waves meet: their last fragments of the slice are in registers, so its buffer takes the slice STAGES
+    // The pipeline.  While the matrix cores work on one part of a step of MK terms (times WK), the fragments of the next part are read: of B
+    // those of a step, of A those of PARTS of its row blocks, two where all of them twice would not leave registers for the sums.  In front of a
+    // slice's last part all waves meet: their last fragments of the slice are in registers, so its buffer takes the slice STAGES
     // further on, which then has the time of STAGES - 1 slices to arrive; and the next slice, requested that long ago, is there, so that its first
-    // fragments are read beside the last step's products.  An operand that passes through registers is requested at the same place and
-    // put into LDS a step before the waves meet.
-    static constexpr int STEPS = S::BK / 16 / S::WK;
-    static_assert(STEPS % 2 == 0, "the first fragments of a slice are always the same registers'");
+    // fragments are read beside the last part's products.  An operand that passes through registers is requested at the same place and
+    // put into LDS a part before the waves meet.
+    typedef typename std::conditional<S::MI == 32, f16v, f4>::type Block;
+    typedef Block Sums[SUMS][S::MB][S::NB];
+    static constexpr int STEPS = S::BK / S::MK / S::WK;
+    static constexpr int PARTS = SUMS * S::MB * S::NB * S::X + 8 * (PA * S::MB + PB * S::NB) > 192 ? 2 : 1, MP = S::MB / PARTS, LAST = STEPS * PARTS - 1;
+    static_assert(STEPS % 2 == 0 && S::MB % PARTS == 0, "the first fragments of a slice are always the same registers'");
     // where both operands pass through registers, these are free for the next request as soon as they are in LDS
     static constexpr bool EARLY = HOW_A != kDirect && HOW_B != kDirect;
-    struct Fragments { u4 a[PA][S::MB], b[PB][S::NB]; };
-    typedef f16v Sums[SUMS][S::MB][S::NB];
+    struct Fragments { u4 a[2][PA][MP], b[2][PB][S::NB]; };
 
-    static __device__ __forceinline__ void read(Fragments &f, const uint8_t *lds, uint32_t k0, uint32_t wm, uint32_t wn, uint32_t lane)
+    // the fragments of part kk
+    template <int kk> static __device__ __forceinline__ void read(Fragments &f, const uint8_t *lds, uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane)
     {
-        #pragma unroll
-        for (int pl = 0; pl < PB; ++pl)
+        const uint32_t k0 = (kk / PARTS * S::WK + wk) * S::MK;
+        if constexpr (kk % PARTS == 0)
             #pragma unroll
-            for (int j = 0; j < S::NB; ++j) f.b[pl][j] = LoadB::L::fragment(lds + LoadA::bytes + pl * LoadB::L::bytes, (wn * S::NB + j) * 32, k0, lane);
+            for (int pl = 0; pl < PB; ++pl)
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j)
+                    f.b[kk / PARTS % 2][pl][j] = LoadB::L::template fragment<S::MI>(lds + LoadA::bytes + pl * LoadB::L::bytes, (wn * S::NB + j) * S::MI, k0, lane);
         #pragma unroll
         for (int pl = 0; pl < PA; ++pl)
             #pragma unroll
-            for (int i = 0; i < S::MB; ++i) f.a[pl][i] = LoadA::L::fragment(lds + pl * LoadA::L::bytes, (wm * S::MB + i) * 32, k0, lane);
+            for (int i = 0; i < MP; ++i)
+                f.a[kk % 2][pl][i] = LoadA::L::template fragment<S::MI>(lds + pl * LoadA::L::bytes, (wm * S::MB + kk % PARTS * MP + i) * S::MI, k0, lane);
     }
 
-    static __device__ __forceinline__ void multiply(const Fragments &f, Sums &acc)
+    template <int kk> static __device__ __forceinline__ void multiply(const Fragments &f, Sums &acc)
     {
+        const auto &a = f.a[kk % 2];
+        const auto &b = f.b[kk / PARTS % 2];
         #pragma unroll
-        for (int i = 0; i < S::MB; ++i)
+        for (int i = 0; i < MP; ++i)
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) {
-                acc[0][i][j] = T::mfma(f.b[0][j], f.a[0][i], acc[0][i][j]);
+                constexpr int first = kk % PARTS * MP;
+                acc[0][first + i][j] = T::mfma(b[0][j], a[0][i], acc[0][first + i][j]);
                 if constexpr (PB == 3) {
-                    f16v s = acc[1][i][j];
+                    Block s = acc[1][first + i][j];
                     if constexpr (PA == 3) {
-                        s = T::mfma(f.b[0][j], f.a[2][i], s);
-                        s = T::mfma(f.b[2][j], f.a[0][i], s);
-                        s = T::mfma(f.b[1][j], f.a[1][i], s);
-                        s = T::mfma(f.b[0][j], f.a[1][i], s);
+                        s = T::mfma(b[0][j], a[2][i], s);
+                        s = T::mfma(b[2][j], a[0][i], s);
+                        s = T::mfma(b[1][j], a[1][i], s);
+                        s = T::mfma(b[0][j], a[1][i], s);
                     } else {
-                        s = T::mfma(f.b[2][j], f.a[0][i], s);
+                        s = T::mfma(b[2][j], a[0][i], s);
                     }
-                    acc[1][i][j] = T::mfma(f.b[1][j], f.a[0][i], s);
+                    acc[1][first + i][j] = T::mfma(b[1][j], a[0][i], s);
                 }
             }
     }
 
-    // Step kk of the slice in `cur`.  (fill is cur: a name of its own tells the compiler that reads need not wait for what is requested into
+    // Part kk of the slice in `cur`.  (fill is cur: a name of its own tells the compiler that reads need not wait for what is requested into
     // it; the meeting of the waves keeps the reads of the old slice in front.)  WHOLE: the slice that is requested needs no checks.
     template <bool WHOLE, int kk = 0>
-    static __device__ __forceinline__ void steps(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
-                                                 bool more, uint32_t k_fill, Fragments (&f)[2], Sums &acc, uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
+    static __device__ __forceinline__ void parts(const uint8_t *__restrict__ cur, uint8_t *__restrict__ next, uint8_t *__restrict__ fill, LoadA &la, LoadB &lb,
+                                                 bool more, uint32_t k_fill, Fragments &f, Sums &acc, uint32_t wm, uint32_t wn, uint32_t wk, uint32_t lane,
                                                  uint32_t wave)
     {
-        if constexpr (kk < STEPS) {
-            constexpr bool LAST = kk + 1 == STEPS;
-            if constexpr (kk + 2 == STEPS) {
+        if constexpr (kk <= LAST) {
+            if constexpr (kk + 1 == LAST) {
                 la.deliver(next);
                 lb.deliver(next + LoadA::bytes);
             }
-            if constexpr (LAST) { if (WHOLE) slices_arrived<EARLY ? 63 : (ST - 2) * REQUESTS>(); else slices_arrived<EARLY ? 63 : 0>(); }
-            if constexpr (EARLY ? kk + 2 == STEPS : LAST) {
+            if constexpr (kk == LAST) { if (WHOLE) slices_arrived<EARLY ? 63 : (ST - 2) * REQUESTS>(); else slices_arrived<EARLY ? 63 : 0>(); }
+            if constexpr (kk == LAST - EARLY) {
                 if constexpr (WHOLE) {
                     la.request_whole(fill, k_fill, wave);
                     lb.request_whole(fill + LoadA::bytes, k_fill, wave);
@@ -453,12 +464,12 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
                     lb.ask(fill + LoadA::bytes, k_fill, wave);
                 }
             }
-            if (LAST) read(f[0], next, wk * 16, wm, wn, lane);
-            else      read(f[(kk + 1) % 2], cur, ((kk + 1) * S::WK + wk) * 16, wm, wn, lane);
-            multiply(f[kk % 2], acc);
-            // the reads between the first products, so that the last of them has arrived when the next step begins, the requests beside them
-            constexpr int READS = PA * S::MB * (A_KC ? 1 : 2) + PB * S::NB * (B_KC ? 1 : 2), PRODUCTS = S::MB * S::NB * (PB == 1 ? 1 : PA == 3 ? 6 : 3);
-            constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, ASKED = LoadA::N * LoadA::RAW + LoadB::N * LoadB::RAW, ASK = (EARLY ? kk + 2 == STEPS : LAST) && WHOLE ? (ASKED + PRODUCTS - 1) / PRODUCTS : 0;
+            if constexpr (kk == LAST) read<0>(f, next, wm, wn, wk, lane); else read<kk + 1>(f, cur, wm, wn, wk, lane);
+            multiply<kk>(f, acc);
+            // the reads between the first products, so that the last of them has arrived when the next part begins, the requests beside them
+            constexpr int READS = PA * MP * (A_KC ? 1 : 2) + ((kk + 1) % PARTS ? 0 : PB * S::NB * (B_KC ? 1 : 2)), PRODUCTS = MP * S::NB * (PB == 1 ? 1 : PA == 3 ? 6 : 3);
+            constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, ASKED = LoadA::N * LoadA::RAW + LoadB::N * LoadB::RAW;
+            constexpr int ASK = kk == LAST - EARLY && WHOLE ? (ASKED + PRODUCTS - 1) / PRODUCTS : 0;
             #pragma unroll
             for (int r = 0; r < PRODUCTS; ++r) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
@@ -466,7 +477,7 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
                 if constexpr (ASK > 0) if (r * ASK < ASKED) __builtin_amdgcn_sched_group_barrier(0x20, ASK, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
-            steps<WHOLE, kk + 1>(cur, next, fill, la, lb, more, k_fill, f, acc, wm, wn, wk, lane, wave);
+            parts<WHOLE, kk + 1>(cur, next, fill, la, lb, more, k_fill, f, acc, wm, wn, wk, lane, wave);
         }
     }
 };
@@ -502,14 +513,14 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         }
     }
 
-    // rows r0 + first, r0 + first + PASS, ... of 32; v: the turned tile, PITCH floats a row, its column 0 is column c0 of C
-    template <int LANES, int PITCH> __device__ __forceinline__ void rows(const ProductParams &p, const Place &at, uint32_t r0, uint32_t c0, const float *v) const
+    // rows r0 + first, r0 + first + PASS, ... of ROWS; v: the turned tile, PITCH floats a row, its column 0 is column c0 of C
+    template <int LANES, int PITCH, int ROWS> __device__ __forceinline__ void rows(const ProductParams &p, const Place &at, uint32_t r0, uint32_t c0, const float *v) const
     {
         constexpr uint32_t PASS = 64 / LANES;
         const uint32_t first = threadIdx.x % 64 / LANES, l = threadIdx.x % LANES, qa = f32 ? 4 * l : 8 * l, qb = f32 ? qa + 4 * LANES : qa + 4;
         const uint32_t ca = c0 + qa, cb = c0 + qb;
         // what belongs to a row is fetched once, by the lane of its number
-        const uint32_t lane = threadIdx.x % 64, mine = r0 + lane % 32;
+        const uint32_t lane = threadIdx.x % 64, mine = r0 + lane % ROWS;
         const uint64_t my_row = at.row0 + mine;
         float row_factor = factor;
         uint32_t row_number = 0;
@@ -520,7 +531,7 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
             if (FINISH == Finish::Store && p.out_row) row_number = p.out_row[my_row];
         }
         #pragma unroll 4
-        for (uint32_t k = 0; k < 32; k += PASS) {
+        for (uint32_t k = 0; k < ROWS; k += PASS) {
             const uint32_t r = k + first;
             const float f = by_row ? __shfl(row_factor, r, 64) : factor;
             const uint32_t number = by_row ? __shfl(row_number, r, 64) : 0;
@@ -620,13 +631,13 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
 
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wk = wave % S::WK, wn = wave / S::WK % S::WN, wm = wave / S::WK / S::WN;
-    f16v acc[P::SUMS][S::MB][S::NB];
+    typename P::Sums acc;
     #pragma unroll
     for (int s = 0; s < P::SUMS; ++s)
         #pragma unroll
         for (int i = 0; i < S::MB; ++i)
             #pragma unroll
-            for (int j = 0; j < S::NB; ++j) acc[s][i][j] = f16v{0};
+            for (int j = 0; j < S::NB; ++j) acc[s][i][j] = typename P::Block{0};
 
     // this split's slices
     uint32_t slices = (at.terms + S::BK - 1) / S::BK, slice0 = 0;
@@ -647,28 +658,28 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 la.ask(lds + i * P::stage, k0 + i * S::BK, wave);
                 lb.ask(lds + i * P::stage + P::LoadA::bytes, k0 + i * S::BK, wave);
             }
-        typename P::Fragments f[2];
         if (HOW_A == kDirect && HOW_B == kDirect && slices >= P::ST) slices_arrived<(P::ST - 1) * P::REQUESTS>(); else slices_arrived<0>();
-        P::read(f[0], lds, wk * 16, wm, wn, lane);
-        // (keeps the compiler from joining these reads with the loop's last ones at the head of the loop, where nothing hides them)
+        uint32_t t = 0, cur = 0, next = P::stage;
+        auto turn = [&] { cur = next; next = next + P::stage == P::ST * P::stage ? 0 : next + P::stage; };
+        auto whole = [&] { return la.fits && lb.fits && t + P::ST < slices && k0 + (t + P::ST + 1) * S::BK <= at.terms; };
+        // (the empty statements keep the compiler from joining the first reads with the loop's last ones at the head of the loop, where nothing hides them)
+        typename P::Fragments f;
+        P::template read<0>(f, lds, wm, wn, wk, lane);
         #pragma unroll
         for (int pl = 0; pl < P::PA; ++pl)
             #pragma unroll
-            for (int i = 0; i < S::MB; ++i) asm volatile("" : "+v"(f[0].a[pl][i]));
+            for (int i = 0; i < P::MP; ++i) asm volatile("" : "+v"(f.a[0][pl][i]));
         #pragma unroll
         for (int pl = 0; pl < P::PB; ++pl)
             #pragma unroll
-            for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f[0].b[pl][j]));
-        uint32_t t = 0, cur = 0, next = P::stage;
-        auto turn = [&] { cur = next; next = next + P::stage == P::ST * P::stage ? 0 : next + P::stage; };
-        if (la.fits && lb.fits)
-            for (; t + P::ST < slices && k0 + (t + P::ST + 1) * S::BK <= at.terms; ++t) {
-                P::template steps<true>(lds + cur, lds + next, lds + cur, la, lb, true, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
-                turn();
-            }
+            for (int j = 0; j < S::NB; ++j) asm volatile("" : "+v"(f.b[0][pl][j]));
+        for (; whole(); ++t) {
+            P::template parts<true>(lds + cur, lds + next, lds + cur, la, lb, true, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            turn();
+        }
         #pragma unroll 1
         for (; t < slices; ++t) {
-            P::template steps<false>(lds + cur, lds + next, lds + cur, la, lb, t + P::ST < slices, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
+            P::template parts<false>(lds + cur, lds + next, lds + cur, la, lb, t + P::ST < slices, k0 + (t + P::ST) * S::BK, f, acc, wm, wn, wk, lane, wave);
             turn();
         }
     }
@@ -737,7 +748,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
 
     if constexpr (S::WK > 1) {
         // the waves' sums over their terms meet in LDS, row by row, in the order of the waves
-        static_assert(S::WM == 1 && S::MB == 1, "waves share the terms of 32 rows");
+        static_assert(S::WM == 1 && S::MB == 1 && S::MI == 32, "waves share the terms of 32 rows");
         constexpr int PITCH = S::BN + 4, LANES = S::BN / 4;
         float *part = reinterpret_cast<float *>(lds);
         #pragma unroll
@@ -778,45 +789,47 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             }
         }
     } else if constexpr (FINISH == Finish::Stats || FINISH == Finish::Keep) {
-        // The maximum over the wave's columns (a lane and the one 32 further on hold a row), over the waves, and the sums of exponentials below the tile's
+        // The maximum over the wave's columns (lanes MI apart hold a row), over the waves, and the sums of exponentials below the tile's
         // maximum; kept or not, the same bits.
         constexpr bool KEEP = FINISH == Finish::Keep;
         float *tops = reinterpret_cast<float *>(lds), *sums = tops + S::WN * S::BM;        // the operand buffers are free
-        const uint32_t c0 = at.n0 + wn * S::NB * 32 + 4 * (lane / 32);
+        const uint32_t c0 = at.n0 + wn * S::NB * S::MI + 4 * (lane / S::MI);
         const bool whole = at.n0 + S::BN <= p.n;
         #pragma unroll
         for (int i = 0; i < S::MB; ++i) {
-            const uint32_t r = (wm * S::MB + i) * 32 + lane % 32;
+            const uint32_t r = (wm * S::MB + i) * S::MI + lane % S::MI;
             const int32_t target = r < at.rows ? p.target[at.row0 + r] - static_cast<int32_t>(p.v0) : -1;
             if (__ballot(target >= static_cast<int32_t>(at.n0) && target < static_cast<int32_t>(at.n0 + S::BN))) {
                 #pragma unroll
                 for (int j = 0; j < S::NB; ++j)
                     #pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        if (static_cast<int32_t>(c0 + j * 32 + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
+                    for (int x = 0; x < S::X; ++x)
+                        if (static_cast<int32_t>(c0 + j * S::MI + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
             }
             float top = -INFINITY;
             if (!whole) {
                 #pragma unroll
                 for (int j = 0; j < S::NB; ++j)
                     #pragma unroll
-                    for (int x = 0; x < 16; ++x) if (c0 + j * 32 + 8 * (x / 4) + x % 4 >= p.n) acc[0][i][j][x] = -INFINITY;
+                    for (int x = 0; x < S::X; ++x) if (c0 + j * S::MI + 8 * (x / 4) + x % 4 >= p.n) acc[0][i][j][x] = -INFINITY;
             }
             #pragma unroll
             for (int j = 0; j < S::NB; ++j)
                 #pragma unroll
-                for (int x = 0; x < 16; ++x) top = fmaxf(top, acc[0][i][j][x]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64)) * unscale;
-            if (lane < 32) tops[wn * S::BM + r] = top;
+                for (int x = 0; x < S::X; ++x) top = fmaxf(top, acc[0][i][j][x]);
+            #pragma unroll
+            for (int d = S::MI; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+            top *= unscale;
+            if (lane < S::MI) tops[wn * S::BM + r] = top;
             __builtin_amdgcn_sched_barrier(0);                 // one row block's values at a time
         }
         __syncthreads();
-        constexpr int PITCH = S::NB * 32 + 4, LANES = S::NB * 8;
-        static_assert(2 * S::WN * S::BM * 4 + S::threads / 64 * 32 * PITCH * 4 <= P::lds_bytes, "statistics and the waves' turned rows");
-        float *mine = sums + S::WN * S::BM + wave * 32 * PITCH;
+        constexpr int PITCH = S::NB * S::MI + 4, LANES = S::NB * S::MI / 4;
+        static_assert(2 * S::WN * S::BM * 4 + S::threads / 64 * S::MI * PITCH * 4 <= P::lds_bytes, "statistics and the waves' turned rows");
+        float *mine = sums + S::WN * S::BM + wave * S::MI * PITCH;
         #pragma unroll
         for (int i = 0; i < S::MB; ++i) {
-            const uint32_t r0 = (wm * S::MB + i) * 32, r = r0 + lane % 32;
+            const uint32_t r0 = (wm * S::MB + i) * S::MI, r = r0 + lane % S::MI;
             float top = -INFINITY, sum = 0.0f;
             #pragma unroll
             for (int w = 0; w < S::WN; ++w) top = fmaxf(top, tops[w * S::BM + r]);
@@ -824,24 +837,25 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) {
                 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
+                for (int g = 0; g < S::X / 4; ++g) {
                     f4 e;
                     #pragma unroll
                     for (int x = 0; x < 4; ++x) e[x] = T::exp(acc[0][i][j][4 * g + x] * unscale, base);
                     sum += (e[0] + e[1]) + (e[2] + e[3]);
-                    if (KEEP) *reinterpret_cast<f4 *>(mine + (lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) = e;
+                    if (KEEP) *reinterpret_cast<f4 *>(mine + (lane % S::MI) * PITCH + j * S::MI + 8 * g + 4 * (lane / S::MI)) = e;
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            sum += __shfl_xor(sum, 32, 64);
-            if (lane < 32) sums[wn * S::BM + r] = sum;
+            #pragma unroll
+            for (int d = S::MI; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+            if (lane < S::MI) sums[wn * S::BM + r] = sum;
             if constexpr (KEEP) {
                 __builtin_amdgcn_wave_barrier();
                 #pragma unroll 4
-                for (uint32_t k = lane / LANES; k < 32; k += 64 / LANES) {
+                for (uint32_t k = lane / LANES; k < S::MI; k += 64 / LANES) {
                     const uint32_t q = lane % LANES * 4;
                     const f4 e = *reinterpret_cast<const f4 *>(mine + k * PITCH + q);
-                    if (r0 + k < at.rows) keep_values<T>(p.out, (at.row0 + r0 + k) * p.ldc + at.n0 + wn * S::NB * 32 + q, e);
+                    if (r0 + k < at.rows) keep_values<T>(p.out, (at.row0 + r0 + k) * p.ldc + at.n0 + wn * S::NB * S::MI + q, e);
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -856,11 +870,11 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
         }
     } else {
-        // 32 rows at a time turn in the wave's own part of LDS, so that consecutive lanes take consecutive columns.  Tiles that lie
+        // A block of rows at a time turns in the wave's own part of LDS, so that consecutive lanes take consecutive columns.  Tiles that lie
         // within C with every row on 16 bytes are finished eight columns at a time, without a decision per element.
-        constexpr int PITCH = S::NB * 32 + 4, LANES = S::NB * 4, PASS = 64 / LANES;     // rows of one pass
-        float *mine = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
-        const uint32_t q = lane % LANES * 8, c = at.n0 + wn * S::NB * 32 + q;
+        constexpr int PITCH = S::NB * S::MI + 4, LANES = S::NB * S::MI / 8, PASS = 64 / LANES;     // rows of one pass
+        float *mine = reinterpret_cast<float *>(lds) + wave * S::MI * PITCH;
+        const uint32_t q = lane % LANES * 8, c = at.n0 + wn * S::NB * S::MI + q;
         const RowFinish<T, WEIGHTS, FINISH> whole(p, at, factor);
         const bool fast = at.n0 + S::BN <= p.n && whole.aligned;
         #pragma unroll
@@ -868,16 +882,16 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int j = 0; j < S::NB; ++j)
                 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f4 *>(mine + (lane % 32) * PITCH + j * 32 + 8 * g + 4 * (lane / 32)) =
+                for (int g = 0; g < S::X / 4; ++g)
+                    *reinterpret_cast<f4 *>(mine + (lane % S::MI) * PITCH + j * S::MI + 8 * g + 4 * (lane / S::MI)) =
                         f4{acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1], acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]} * unscale;
             __builtin_amdgcn_wave_barrier();
-            const uint32_t r0 = (wm * S::MB + i) * 32;
+            const uint32_t r0 = (wm * S::MB + i) * S::MI;
             if (fast) {
-                whole.template rows<LANES, PITCH>(p, at, r0, at.n0 + wn * S::NB * 32, mine);
+                whole.template rows<LANES, PITCH, S::MI>(p, at, r0, at.n0 + wn * S::NB * S::MI, mine);
             } else {
                 #pragma unroll 1
-                for (uint32_t r = lane / LANES; r < 32; r += PASS)
+                for (uint32_t r = lane / LANES; r < S::MI; r += PASS)
                     #pragma unroll
                     for (int h = 0; h < 2; ++h) finish(r0 + r, c + 4 * h, *reinterpret_cast<const f4 *>(mine + r * PITCH + q + 4 * h));
             }
@@ -897,12 +911,17 @@ hipError_t launch_one(hipStream_t stream, const ProductParams &p)
     return hipGetLastError();
 }
 
-typedef TileShape<256, 256, 64, 2, 4, 1> Large16;
+// 16x16x32 draws less power for the same products than 32x32x16: 8 groups of 8192 rows, 4096 x 4096 1765 us instead of 1890, 16 of 1024, 2048 x 2048
+// 119 instead of 128.  Codes leave no registers for its fragments beside those on their way (weight gradient of 16 groups of 1024 rows, 2048 x 2048:
+// 236 us, with 32x32x16 214), and two medium tiles on a compute unit lose by it (16 of 512, 1024 x 1024: 27 instead of 24).
+typedef TileShape<256, 256, 64, 2, 4, 1, 2, 16> Large16;
+typedef TileShape<256, 256, 64, 2, 4, 1> Large16Codes;
 typedef TileShape<128, 128, 64, 2, 2, 1> Medium16;
 // where every compute unit has one block at most: the medium tile with four slices in LDS instead of two (and room for a second block).  2048 x 2048 x
-// 2048: 25 us instead of 29, 4 groups of 1024 rows, 2048 to 512 columns: 22 instead of 26, out of memory 23 instead of 33; with 512 blocks (16 groups of 512
+// 2048: 24 us instead of 29, 4 groups of 1024 rows, 2048 to 512 columns: 22 instead of 26, out of memory 23 instead of 33 (1024 x 4096 x 4096 41 us, with
+// 32x32x16 43, input gradient 38 and 43); with 512 blocks (16 groups of 512
 // rows, 1024 x 1024) 30 instead of 24
-typedef TileShape<128, 128, 64, 2, 4, 1, 4> Deep16;
+typedef TileShape<128, 128, 64, 2, 4, 1, 4, 16> Deep16;
 typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 // short sums and few blocks: a slice more in flight (one row, 4096 x 4096: 10.1 us instead of 11.0; the other tiles lose by four slices of 32: 8 groups
 // of 8192 rows, 4096 x 4096, input gradient 1962 us instead of 1840: of a row of 64 bytes the other half of the line is fetched again)
@@ -924,7 +943,7 @@ hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
         const bool b_direct = direct_b(LAYOUT, p);
         if constexpr (WEIGHTS)
             if (!p.a) {
-                if (b_direct && tile == Tile::Large) return launch_one<T, LAYOUT, Large16, FINISH, kCodes, kDirect>(stream, p);
+                if (b_direct && tile == Tile::Large) return launch_one<T, LAYOUT, Large16Codes, FINISH, kCodes, kDirect>(stream, p);
                 if (b_direct) return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kDirect>(stream, p)
                                                          : launch_one<T, LAYOUT, Medium16, FINISH, kCodes, kDirect>(stream, p);
                 return tile == Tile::Small ? launch_one<T, LAYOUT, Small16, FINISH, kCodes, kRegs>(stream, p)
