@@ -269,8 +269,8 @@ Workspace carve(const cocod_cross_entropy_call *c)
     w.pieces = static_cast<uint32_t>((whole + w.piece - 1) / w.piece);
     const uint32_t n = static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab);
     const bool dim8 = c->dim % 8 == 0;                         // a dense table's rows then start on 16 bytes
-    w.logits = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, c->vocab, c->dim, false);
-    w.slopes = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, n, c->dim, false);             // (exponentials need the whole sum)
+    w.logits = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, c->vocab, c->dim, false, false);
+    w.slopes = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, n, c->dim, false, false);             // (exponentials need the whole sum)
     w.to_hidden = plan_product(Layout::Rows_KN, t, dim8, rows, c->groups, 0, c->dim, n, true);
     w.to_table = plan_product(Layout::Weights, t, true, rows, c->groups, n, c->dim, 0, true);
     w.index = take(rows * 4);

@@ -68,7 +68,7 @@ struct ProductParams {
 };
 
 // Tile shapes a launch can take (plan_product picks one).
-enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3 };
+enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3, Tall = 4 };
 
 // C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats, Keep or Slope), one launch, with splits one more that joins
 // them.  hipErrorInvalidConfiguration: the grid would exceed a launch's limits.
@@ -95,17 +95,18 @@ inline bool direct_b(Layout layout, const ProductParams &p)
 {
     return direct_operand(p.b, p.ldb, layout == Layout::Weights ? 0 : p.b_group, layout != Layout::Rows_NK || p.k % 8 == 0);
 }
-// The tile that a launch takes where `planned` was planned: the large and the deep one need operands that go to LDS directly (the large one
+// The tile that a launch takes where `planned` was planned: all but the medium and the small one need operands that go to LDS directly (the large one
 // also takes codes).
 inline Tile settle_tile(Dtype type, Layout layout, Tile planned, const ProductParams &p)
 {
-    if (planned == Tile::Deep && (type == Dtype::F32 || !direct_a(layout, p) || !direct_b(layout, p))) return Tile::Medium;
+    if ((planned == Tile::Deep || planned == Tile::Tall) && (type == Dtype::F32 || !direct_a(layout, p) || !direct_b(layout, p))) return Tile::Medium;
     return planned == Tile::Large && (type == Dtype::F32 || (p.a && !direct_a(layout, p)) || !direct_b(layout, p)) ? Tile::Medium : planned;
 }
 
-// Tile and splits of a product, from its sizes alone; direct: 16-bit operands are expected to go to LDS directly.
+// Tile and splits of a product, from its sizes alone; direct: 16-bit operands are expected to go to LDS directly; stored: Finish::Store.
 struct ProductPlan { Tile tile; uint32_t splits; };
-ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split);
+ProductPlan plan_product(Layout layout, Dtype type, bool direct, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t k, bool may_split,
+                         bool stored = true);
 // Bytes of ProductParams::part (0 with one split), whose rows hold part_pitch(n) floats.
 inline uint64_t part_pitch(uint32_t n) { return (static_cast<uint64_t>(n) + 3) / 4 * 4; }
 uint64_t part_bytes(const ProductPlan &plan, Layout layout, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n);

@@ -182,6 +182,30 @@ def test_every_tile(dtype, bounds, rows, k, n):
         close(dw, out, oh.product_bound(out, mag, terms, to))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("bounds, rows, wide, summed", [
+    ([3, 195, 195, 900, 1092, 1993], 2000, 2056, 520), ([1, 1999], 2000, 2056, 520),              # rows of 192
+    ([0, 1, 600, 600, 1700, 2999], 3000, 4104, 392), ([0, 100, 100, 390, 500, 700], 700, 2056, 392)])      # the large tile; four slices in flight
+@pytest.mark.parametrize("direction", ["forward", "input_grad"])
+def test_rows_in_tiles_of_several_slices(dtype, bounds, rows, wide, summed, direction):
+    """The 16-bit tiles for many rows, with sums of several slices and a part of one: groups of exactly one tile, of a part of one, of none."""
+    k, n = (summed, wide) if direction == "forward" else (wide, summed)
+    gen, t, groups = generator(len(bounds)), oh.TYPES[dtype][1], len(bounds) - 1
+    x, dy, w = oh.matrix(rows, k, 0, t, gen), oh.matrix(rows, n, 0, t, gen), oh.stack(groups, k, n, 0, 0, t, gen)
+    written = oh.inside(bounds, rows)
+    buf, got = oh.output((rows, wide), 8, t)
+    if direction == "forward":
+        oh.call("forward", oh.layer(dtype, bounds, rows, k, n, x=x, w=w, y=got, flags=P.GROUPED_RELU_OUT))
+        out, mag, terms = oh.exact_product("forward", bounds, x, w)
+        want = out.clamp(min=0)
+    else:
+        oh.call("input_grad", oh.layer(dtype, bounds, rows, k, n, x=x, dy=dy, w=w, dx=got, flags=P.GROUPED_RELU_IN))
+        out, mag, terms = oh.exact_product("input_grad", bounds, dy, w)
+        want = out * (x > 0)
+    close(got[written], want[written], oh.product_bound(out, mag, terms, t)[written])
+    assert oh.untouched(buf, got, written)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("case", [0, 1, 3, 4, 5, 7])
 def test_products_from_codes(dtype, case):
@@ -407,6 +431,12 @@ LOSSES = [
     ([1, 2999], 3000, 72, 4104, 0, 0, 0.1),
     ([0, 5990], 6000, 72, 136, 0, 0, 0.1),
     ([0, 690], 700, 73, 4101, 0, 0, 0.1),
+    # four slices in flight, all at once and by pieces; the large tile with sums of several slices, the same; pieces with odd rows
+    ([0, 100, 100, 390, 500, 700], 700, 264, 2056, 0, 0, 0.1),
+    ([2, 400, 700], 700, 264, 5000, 0, 2560, 0.2),
+    ([1, 1000, 2999], 3000, 264, 4104, 0, 0, 0.1),
+    ([0, 1100, 3000], 3000, 264, 8200, 0, 4352, 0.1),
+    ([0, 1200, 2500], 2500, 203, 4104, 0, 2304, 0.1),
 ]
 
 
