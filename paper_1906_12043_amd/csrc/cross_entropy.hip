@@ -280,7 +280,7 @@ Workspace carve(const cocod_cross_entropy_call *c)
     w.target_logit = take(rows * 4);
     w.row_scale = take(rows * 4);
     w.hidden = take(rows * w.pitch * s);
-    const uint32_t narrow = w.logits.tile == Tile::Small ? 64 : 128;         // the large tile may have to give way to the medium one
+    const uint32_t planned = tile_cols(t, w.logits.tile), narrow = planned < 128 ? planned : 128;        // the large tile may have to give way to the medium one
     w.stats = take((static_cast<uint64_t>(c->vocab) + narrow - 1) / narrow * rows * 8);
     if (grads) {
         w.slope = take(rows * w.piece * s);

@@ -68,7 +68,7 @@ struct ProductParams {
 };
 
 // Tile shapes a launch can take (plan_product picks one).
-enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3, Tall = 4 };
+enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3, Tall = 4, Square = 5 };
 
 // C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats, Keep or Slope), one launch, with splits one more that joins
 // them.  hipErrorInvalidConfiguration: the grid would exceed a launch's limits.
@@ -80,7 +80,10 @@ hipError_t launch_logits_f16(hipStream_t stream, Finish finish, Tile tile, const
 hipError_t launch_logits_f32(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p);
 
 // Columns of the tiles in which Finish::Stats forms its statistics (ProductParams::stats holds one row of them per column tile).
-inline uint32_t tile_cols(Dtype type, Tile tile) { return tile == Tile::Small ? 64 : tile == Tile::Large && type != Dtype::F32 ? 256 : 128; }
+inline uint32_t tile_cols(Dtype type, Tile tile)
+{
+    return tile == Tile::Small || tile == Tile::Square ? 64 : tile == Tile::Large && type != Dtype::F32 ? 256 : 128;
+}
 
 // 16-bit operands that start on a 16-byte address, with rows of whole 16-byte pieces, go to LDS without passing through registers.
 inline bool direct_operand(const void *base, uint64_t ld, uint64_t group, bool whole)
@@ -95,8 +98,8 @@ inline bool direct_b(Layout layout, const ProductParams &p)
 {
     return direct_operand(p.b, p.ldb, layout == Layout::Weights ? 0 : p.b_group, layout != Layout::Rows_NK || p.k % 8 == 0);
 }
-// The tile that a launch takes where `planned` was planned: all but the medium and the small one need operands that go to LDS directly (the large one
-// also takes codes).
+// The tile that a launch takes where `planned` was planned: the large, the deep and the tall one need operands that go to LDS directly (the large
+// one also takes codes).
 inline Tile settle_tile(Dtype type, Layout layout, Tile planned, const ProductParams &p)
 {
     if ((planned == Tile::Deep || planned == Tile::Tall) && (type == Dtype::F32 || !direct_a(layout, p) || !direct_b(layout, p))) return Tile::Medium;
