@@ -43,19 +43,19 @@ hipError_t launch_join(hipStream_t stream, Dtype type, Layout layout, const Prod
 }
 
 // The tile and the number of splits that are expected to take least time.  A compute unit takes ceil(blocks / 256) blocks one after the other (where it
-// holds several at a time they share it), each `per_slice` for every slice of its sum and `per_tile` once, in us; a launch costs 5, joining splits 4 and
-// their traffic at 4 TB/s.  Fitted to 111 products of 1 to 64 groups, 1 to 8192 rows and widths 300 to 32000, every tile with 1 to 16 splits (the
-// 16-bit large tile, that of four slices in LDS and the tall one to 90 products, the fp32 ones to 24): the choice costs 2 % more time than the best one in the mean.  For
-// instance, us (large / medium / small tile, best splits in brackets):
+// holds several at a time they share it), each `per_slice` for every slice of its sum (`alone` times that if the unit has no other block) and `per_tile`
+// once, in us; a launch costs 5, joining splits 4 and their traffic at 4 TB/s.  Fitted to 111 products of 1 to 64 groups, 1 to 8192 rows and widths 300
+// to 32000, every tile with 1 to 16 splits (the 16-bit large tile, that of four slices in LDS and the tall one again to 90, fp32 to 24, operands through
+// registers to 39): the choice costs 2 % more time than the best one in the mean.  For instance, us (large / medium / small tile, best splits in brackets):
 // bf16 16 groups of one row, 1024 x 1024: 16 (4) / 12 (4) / 8 (1); 4 of 64 rows, 2048 x 2048: 22 (4) / 18 (4) / 14 (1); 16 of 512 rows, 1024 x
 // 1024: 33 (1) / 26 (1) / 50 (1); 16 of 500 rows, 2048 x 1024, input gradient: 40 (1) / 47 (1) / 93 (1); 4 of 768 rows, 32000 x 1024: 239 (4) / 266 (8) /
 // 468 (4), weight gradient 283 (1) / 342 (1) / 701 (1); through registers one row, 4095 x 2047: - / 18 (8) / 14 (8), 2048 rows, 2047 x 2047: - / 46 (1) /
 // 77 (1); fp32 16 of 250 rows, 1024 x 1024: - / 56 (1) / 97 (1), 8 of 8 rows, 2048 x 2048: - / 58 (4) / 31 (2).
-struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile, alone; Tile tile; uint32_t most_turns; };      // alone: per slice so much more where a unit has one block
+struct TileCost { uint32_t bm, bn, bk; double per_slice, per_tile, alone; Tile tile; uint32_t most_turns; };
 constexpr TileCost kCostDirect[] = {{256, 256, 64, 1.05, 7.0, 1.0, Tile::Large, ~0u}, {128, 128, 64, 0.40, 1.4, 1.75, Tile::Medium, ~0u},
                                     {32, 64, 128, 0.25, 0.5, 1.0, Tile::Small, ~0u}, {128, 128, 64, 0.50, 1.6, 1.0, Tile::Deep, 1},
                                     {192, 128, 64, 0.63, 4.0, 1.0, Tile::Tall, ~0u}};
-constexpr TileCost kCostRegs[] = {{128, 128, 64, 0.81, 3.4, 1.0, Tile::Medium, ~0u}, {32, 64, 128, 0.50, 0.65, 1.0, Tile::Small, ~0u}};
+constexpr TileCost kCostRegs[] = {{128, 128, 64, 0.70, 3.4, 1.6, Tile::Medium, ~0u}, {32, 64, 128, 0.45, 0.65, 1.4, Tile::Small, ~0u}};
 constexpr TileCost kCost32[] = {{128, 128, 32, 1.25, 3.7, 1.0, Tile::Medium, ~0u}, {32, 64, 64, 0.57, 1.3, 1.4, Tile::Small, ~0u},
                                 {64, 64, 32, 0.48, 1.5, 1.75, Tile::Square, ~0u}};
 constexpr uint32_t kMaxSplits = 16;
