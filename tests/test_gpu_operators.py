@@ -187,13 +187,14 @@ def test_every_tile(dtype, bounds, rows, k, n):
     ([3, 195, 195, 900, 1092, 1993], 2000, 2056, 520), ([1, 1999], 2000, 2056, 520),              # rows of 192
     ([0, 1, 600, 600, 1700, 2999], 3000, 4104, 392), ([0, 100, 100, 390, 500, 700], 700, 2056, 392)])      # the large tile; four slices in flight
 @pytest.mark.parametrize("direction", ["forward", "input_grad"])
-def test_rows_in_tiles_of_several_slices(dtype, bounds, rows, wide, summed, direction):
+@pytest.mark.parametrize("pad", [8, 3])
+def test_rows_in_tiles_of_several_slices(dtype, bounds, rows, wide, summed, direction, pad):
     """The 16-bit tiles for many rows, with sums of several slices and a part of one: groups of exactly one tile, of a part of one, of none."""
     k, n = (summed, wide) if direction == "forward" else (wide, summed)
     gen, t, groups = generator(len(bounds)), oh.TYPES[dtype][1], len(bounds) - 1
     x, dy, w = oh.matrix(rows, k, 0, t, gen), oh.matrix(rows, n, 0, t, gen), oh.stack(groups, k, n, 0, 0, t, gen)
     written = oh.inside(bounds, rows)
-    buf, got = oh.output((rows, wide), 8, t)
+    buf, got = oh.output((rows, wide), pad, t)
     if direction == "forward":
         oh.call("forward", oh.layer(dtype, bounds, rows, k, n, x=x, w=w, y=got, flags=P.GROUPED_RELU_OUT))
         out, mag, terms = oh.exact_product("forward", bounds, x, w)
