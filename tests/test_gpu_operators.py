@@ -493,6 +493,37 @@ def test_loss_and_gradients(dtype, case, total):
     assert torch.equal(table, de)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("bounds, rows, dim, vocab", [([2, 40, 40, 60, 71], 80, 64, 130), ([0, 200], 200, 264, 1000), ([0, 1], 1, 8, 1), ([5, 20, 30], 33, 128, 2500)])
+@pytest.mark.parametrize("pad", [0, 8, 1])
+@pytest.mark.parametrize("total", [False, True])
+def test_loss_alone_of_few_rows(dtype, bounds, rows, dim, vocab, pad, total):
+    """Without gradients: rows without a target between the others, a group without any, targets beside the vocabulary and at the ends of their type."""
+    gen, t, groups = generator(rows + dim), oh.TYPES[dtype][1], len(bounds) - 1
+    h, e = oh.matrix(rows, dim, pad, t, gen), oh.stack(groups, vocab, dim, pad, pad, t, gen, std=3.0 / dim ** 0.5)
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    for i, none in enumerate((-1, vocab, vocab + 1, -2 ** 31, 2 ** 31 - 1, -100)):
+        if rows > 1:
+            target[bounds[0] + 1 + 3 * i % (bounds[1] - bounds[0])] = none
+    if groups > 1:
+        target[bounds[-2]:bounds[-1]] = -100
+    h[(target < 0) | (target >= vocab)] = float("nan")
+    want = oh.exact_loss(bounds, h, e, target, total, 1.0)
+    bound = oh.loss_bounds(want, t, dim, vocab)
+    written = oh.inside(bounds, rows)
+    lbuf, loss = oh.output((1, rows), 3, torch.float32)
+    gbuf, group_loss = oh.output((1, groups), 1, torch.float32)
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, group_loss=group_loss, loss=loss,
+                                                                       flags=P.CROSS_ENTROPY_SUM if total else 0))
+    close(loss[0][written], want["loss"][written], bound["loss"][written])
+    for g, s in oh.groups_of(bounds):
+        n = int(((target[s] >= 0) & (target[s] < vocab)).sum())
+        far = bound["loss"][s].sum() / (1 if total else max(n, 1)) + oh.STEP * want["group_loss"][g].abs()
+        assert abs(group_loss[0, g].double() - want["group_loss"][g]) <= far
+    assert lbuf[0, rows:].tolist() == [oh.SENTINEL] * 3 and bool((loss[0][~written] == oh.SENTINEL).all())
+    assert float(gbuf[0, groups]) == oh.SENTINEL
+
+
 def test_loss_gradient_against_differences():
     """(L(h + s d) - L(h - s d)) / 2 s against <dh, d>, and the same for the table.  L in fp32 is off by the bound r of each row's loss, here
     below 4e-6; at s = 2^-6 that is 2.6e-4 in the quotient; the cubic term is s^2 / 6 max |L'''| |d . e|^3, with |d . e| <= 1 and
