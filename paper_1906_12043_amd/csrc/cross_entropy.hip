@@ -122,8 +122,8 @@ template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Ro
 }
 
 // norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss, also in the place of the
-// target's logit.  ROWS rows per pass of a block, sixteen threads a row.
-constexpr int kNormThreads = 16, kNormAhead = 4;
+// target's logit.  ROWS rows per pass of a block, THREADS threads a row.
+constexpr int kNormThreads = 16, kNormAhead = 4, kFewThreads = 4;
 struct Norms {
     const uint32_t *index;
     const float2 *stats;              // [tiles][rows]
@@ -137,16 +137,16 @@ __device__ __forceinline__ void add_part(float &top, float &sum, float2 s)
     top = m;
 }
 // the loss of row r in the threads with y == 0 (others: 0); GATHERED: it comes from another row of the caller's
-template <int ROWS, bool GATHERED = true> __device__ __forceinline__ float norm_rows(const Rows &p, const Norms &n, uint64_t r, bool in, float2 (&part)[kNormThreads][ROWS])
+template <int ROWS, bool GATHERED, int THREADS> __device__ __forceinline__ float norm_rows(const Rows &p, const Norms &n, uint64_t r, bool in, float2 (&part)[THREADS][ROWS])
 {
     const uint32_t x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
     float top = -INFINITY, sum = 0.0f;
     if (in) {
-        for (uint32_t t = y; t < n.tiles; t += kNormThreads * kNormAhead) {
+        for (uint32_t t = y; t < n.tiles; t += THREADS * kNormAhead) {
             float2 s[kNormAhead];
             #pragma unroll
             for (int i = 0; i < kNormAhead; ++i) {
-                const uint32_t u = t + i * kNormThreads;
+                const uint32_t u = t + i * THREADS;
                 s[i] = u < n.tiles ? n.stats[u * p.rows + r] : make_float2(-INFINITY, 0.0f);
             }
             #pragma unroll
@@ -158,7 +158,7 @@ template <int ROWS, bool GATHERED = true> __device__ __forceinline__ float norm_
     float l = 0.0f;
     if (y == 0 && in) {
         #pragma unroll
-        for (int w = 1; w < kNormThreads; ++w) add_part(top, sum, part[w][x]);
+        for (int w = 1; w < THREADS; ++w) add_part(top, sum, part[w][x]);
         const float norm = top + logf(sum);
         n.norm[r] = norm;
         l = norm - n.target_logit[r];
@@ -174,17 +174,17 @@ __global__ __launch_bounds__(kNormRows * kNormThreads) void norm_kernel(const Ro
 {
     __shared__ float2 part[kNormThreads][kNormRows];
     const uint64_t r = static_cast<uint64_t>(blockIdx.x) * kNormRows + threadIdx.x % kNormRows;
-    norm_rows<kNormRows>(p, n, r, r >= clamped(p, 0) && r < clamped(p, p.groups) && n.index[r] != kNoRow, part);
+    norm_rows<kNormRows, true>(p, n, r, r >= clamped(p, 0) && r < clamped(p, p.groups) && n.index[r] != kNoRow, part);
 }
 
 // One block per group: the mean (or sum) of its rows' losses, summed in a fixed order in 64 bits.  NORMS: the rows' losses, too (a launch less where a
 // block has little to do).  Not GATHERED: rows without a target lie between the others.
 constexpr int kMeanThreads = 1024;
-template <bool NORMS, bool GATHERED = true> __global__ __launch_bounds__(kMeanThreads) void mean_kernel(const Rows p, const Norms n, const int64_t *ends, float *group_loss, int sum_only)
+template <bool NORMS, bool GATHERED = true, int THREADS = kNormThreads> __global__ __launch_bounds__(kMeanThreads) void mean_kernel(const Rows p, const Norms n, const int64_t *ends, float *group_loss, int sum_only)
 {
-    constexpr int ROWS = kMeanThreads / kNormThreads;
+    constexpr int ROWS = kMeanThreads / THREADS;
     __shared__ double part[kMeanThreads];
-    __shared__ float2 parts[kNormThreads][NORMS ? ROWS : 1];
+    __shared__ float2 parts[THREADS][NORMS ? ROWS : 1];
     const uint32_t g = blockIdx.x;
     const uint64_t begin = clamped(p, g), end = GATHERED ? static_cast<uint64_t>(ends[g]) : clamped(p, g + 1);
     uint64_t count = end > begin ? end - begin : 0;
@@ -202,7 +202,7 @@ template <bool NORMS, bool GATHERED = true> __global__ __launch_bounds__(kMeanTh
     } else if constexpr (NORMS) {
         for (uint64_t r0 = begin; r0 < end; r0 += ROWS) {
             const uint64_t r = r0 + threadIdx.x % ROWS;
-            s += norm_rows<ROWS>(p, n, r, r < end && n.index[r] != kNoRow, parts);         // (offsets that do not ascend may leave holes)
+            s += norm_rows<ROWS, true>(p, n, r, r < end && n.index[r] != kNoRow, parts);         // (offsets that do not ascend may leave holes)
         }
     } else {
         for (uint64_t r = begin + threadIdx.x; r < end; r += kMeanThreads) s += n.target_logit[r];
@@ -404,7 +404,8 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
     z.k = c->dim; z.splits = 1; z.target = target;
     // The loss alone of a few rows that the product can take where they are: those without a target go through it, too, and are left out of the
-    // sums (64 rows, 1000 x 256: 11 us instead of 16; 16 rows, 16000 x 1024: 17 instead of 21; half of 512 rows, 512 x 256: 33 and 35).  Not in fp32, where a row that is not finite has its whole tile formed again.
+    // sums (64 rows, 1000 x 256: 11 us instead of 16; 16 rows, 16000 x 1024: 17 instead of 21).  Not in fp32, where a row that is not finite has its whole
+    // tile formed again.
     const bool few = t != Dtype::F32 && !c->dh && !c->de && direct_a(Layout::Rows_NK, z) && c->rows * w.pitch * s <= kGatherHere * c->groups;
     if (!few) { z.a = ws + w.hidden; z.lda = w.pitch; }
     const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, z);
@@ -437,9 +438,14 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
         }
         if (!here) hipLaunchKernelGGL(norm_kernel, dim3(static_cast<uint32_t>((c->rows + kNormRows - 1) / kNormRows)), dim3(kNormRows * kNormThreads), 0, q, rows, norms);
     }
-    if (!gathered)           hipLaunchKernelGGL((mean_kernel<true, false>), dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
-    else if (here)           hipLaunchKernelGGL(mean_kernel<true>, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
-    else if (c->group_loss)  hipLaunchKernelGGL(mean_kernel<false>, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
+    if (here || c->group_loss) {
+        // a few statistics a row: more rows at a time (256 rows, 1000 x 256: 11 us instead of 22, half of 512 rows, 512 x 256: 13.5 instead of 33)
+        const bool wide = norms.tiles <= kFewThreads * kNormAhead;
+        const auto mean = !here      ? mean_kernel<false>
+                          : gathered ? (wide ? mean_kernel<true, true, kFewThreads> : mean_kernel<true, true>)
+                                     : (wide ? mean_kernel<true, false, kFewThreads> : mean_kernel<true, false>);
+        hipLaunchKernelGGL(mean, dim3(c->groups), dim3(kMeanThreads), 0, q, rows, norms, ends, c->group_loss, sum_only);
+    }
     if (int rc = launch_status(hipGetLastError(), what)) return rc;
     if (!c->dh && !c->de) return COCOD_OK;
 
