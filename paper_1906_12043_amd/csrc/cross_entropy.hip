@@ -250,8 +250,9 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Row
 }
 
 // Up to so many bytes of hidden states per group, and so many statistics per thread of a group's block, one block of 1024 threads does the small work of a group
-// together with what precedes or follows it; beyond, kernels of their own spread it over the chip.
-constexpr uint64_t kGatherHere = 256u << 10, kStatsHere = 4;
+// together with what precedes or follows it; beyond, kernels of their own spread it over the chip (with gradients, us together / apart: 64 rows of 256
+// 31 / 31, 256 rows 39 / 32, 512 rows 51 / 36).  And so many bytes up to which rows stay where they are if only their losses are wanted.
+constexpr uint64_t kGatherHere = 32u << 10, kStatsHere = 8, kLeaveHere = 1u << 20;
 
 // The caller's memory, carved up.
 struct Workspace {
@@ -404,9 +405,9 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
     z.k = c->dim; z.splits = 1; z.target = target;
     // The loss alone of a few rows that the product can take where they are: those without a target go through it, too, and are left out of the
-    // sums (64 rows, 1000 x 256: 11 us instead of 16; 16 rows, 16000 x 1024: 17 instead of 21).  Not in fp32, where a row that is not finite has its whole
-    // tile formed again.
-    const bool few = t != Dtype::F32 && !c->dh && !c->de && direct_a(Layout::Rows_NK, z) && c->rows * w.pitch * s <= kGatherHere * c->groups;
+    // sums (64 rows, 1000 x 256: 11 us instead of 16; 512 rows 14 instead of 18; 16 rows, 16000 x 1024: 17 instead of 21).  Not in fp32, where a
+    // row that is not finite has its whole tile formed again.
+    const bool few = t != Dtype::F32 && !c->dh && !c->de && direct_a(Layout::Rows_NK, z) && c->rows * w.pitch * s <= kLeaveHere * c->groups;
     if (!few) { z.a = ws + w.hidden; z.lda = w.pitch; }
     const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, z);
     const uint32_t cols = tile_cols(t, tile);
