@@ -105,7 +105,11 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, 
     if (threadIdx.x == 0) ends[g] = static_cast<int64_t>(at);
     if constexpr (GATHER) {                                    // (the barrier that ended the loop ordered the block's own writes of index)
         for (uint64_t r = begin + wave; r < end; r += kCompactThreads / 64) {
-            if (r < at) gather_row(hidden, r, index[r], lane);
+            if (r < at) {
+                // Groups whose offsets do not ascend share rows, and the block of another one may have left kNoRow in this place since.
+                const uint32_t from = index[r];
+                if (from != kNoRow) gather_row(hidden, r, from, lane);
+            }
             if (!has_target(p, r)) clear_row(hidden, r, lane);
         }
     }

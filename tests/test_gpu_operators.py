@@ -413,6 +413,29 @@ def test_offsets_that_do_not_ascend_leave_the_arrays_alone_outside():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 1000])
+@pytest.mark.parametrize("grads", [True, False])
+def test_loss_of_groups_that_share_rows(dtype, dim, grads):
+    """Offsets that do not ascend make groups share rows.  Groups of rows without a target beside long ones with most of theirs: their blocks mark
+    the shared rows as gathered from nowhere while others gather them.  Results are undefined; nothing outside the arrays is touched.  With
+    64 columns a group's block gathers its rows itself, with 1000 a launch of its own does."""
+    t, gen, rows, vocab = oh.TYPES[dtype][1], generator(19), 300, 130
+    bounds = [0, 250, 10, 12, 5, 300, 0, 300, 20, 22, 290, 3, 200, 100, 150, 40, 260, 10, 12, 0, 300]
+    groups = len(bounds) - 1
+    h, e = oh.matrix(rows, dim, 0, t, gen), oh.stack(1, vocab, dim, 0, 0, t, gen, std=dim ** -0.5).expand(groups, vocab, dim)
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    target[10:12], target[20:22], target[100:150:2], target[280:] = -100, vocab, -1, -1
+    lbuf, loss = oh.output((1, rows), 3, torch.float32)
+    hbuf, dh = oh.output((rows, dim), 8, t)
+    ebuf, de = oh.output((groups, vocab, dim), 8, t)
+    c = oh.cross_entropy_call(dtype, bounds, h, e, target, dh if grads else None, de if grads else None, None, loss)
+    for _ in range(5):
+        P.cross_entropy(torch.cuda.current_stream(), c)
+    torch.cuda.synchronize()
+    assert lbuf[0, rows:].tolist() == [oh.SENTINEL] * 3 and oh.untouched(hbuf, dh) and oh.untouched(ebuf, de)
+
+
 # ---- loss ---------------------------------------------------------------------------------------------------
 
 LOSSES = [
