@@ -419,7 +419,8 @@ enum { COCOD_GROUPED_FORWARD = 0, COCOD_GROUPED_INPUT_GRAD = 1, COCOD_GROUPED_WE
 /*
  * One linear layer of all groups, y_g = x_g w_g.  A call reads the fields it names; the others are
  * ignored.  w may lie inside the workers' models ([W][stride], w_stride = stride) and dw inside the gradient that
- * cocod_external_step or cocod_external_step_bf16 takes.
+ * cocod_external_step or cocod_external_step_bf16 takes.  The backward calls do not read COCOD_GROUPED_RELU_OUT: the gradient comes
+ * through a layer's relu where it is formed, by COCOD_GROUPED_RELU_IN of the layer that follows or by COCOD_CROSS_ENTROPY_RELU_IN of the loss.
  */
 typedef struct cocod_grouped {
     uint32_t struct_size;           /* sizeof(cocod_grouped); checked */
@@ -434,7 +435,7 @@ typedef struct cocod_grouped {
     const uint8_t *x_scales; uint64_t ld_scales;   /*   and its scales, [rows][ceil(inner / 32)] */
     const void *w;   uint64_t ldw, w_stride;       /* [groups][inner][outer]; w_stride 0: one matrix for all groups */
     void *y;         uint64_t ldy;          /* [rows][outer] */
-    const void *dy;  uint64_t lddy;         /* [rows][outer] gradient at y */
+    const void *dy;  uint64_t lddy;         /* [rows][outer] gradient at x w, in front of the relu that y may have gone through */
     void *dx;        uint64_t lddx;         /* [rows][inner] gradient at x */
     void *dw;        uint64_t lddw, dw_stride;     /* [groups][inner][outer] gradient at w, a matrix of its own for every group */
     uint32_t dw_dtype;              /* dtype, or COCOD_F32 */
@@ -452,7 +453,10 @@ int cocod_grouped_input_grad(void *stream, const cocod_grouped *g);
 /* dw_g = x_g^T dy_g (x NULL: the product takes the codes and scales as they are); zero for a group without rows. */
 int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g);
 
-enum { COCOD_CROSS_ENTROPY_SUM = 1u };      /* a group's loss is the sum of its rows' losses, not their mean */
+enum {
+    COCOD_CROSS_ENTROPY_SUM = 1u,       /* a group's loss is the sum of its rows' losses, not their mean */
+    COCOD_CROSS_ENTROPY_RELU_IN = 4u    /* h is the output of a relu: dh is taken through it (zero where h is not above zero) */
+};
 
 /*
  * Softmax cross-entropy of logits h_g e_g^T over a vocabulary, without the logits in memory, and the gradients of

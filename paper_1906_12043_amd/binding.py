@@ -16,7 +16,7 @@ FLAG_DRY_RUN = 1
 F32, BF16, F16 = 0, 1, 2
 GROUPED_RELU_OUT, GROUPED_RELU_IN = 1, 2
 GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD = 0, 1, 2
-CROSS_ENTROPY_SUM = 1
+CROSS_ENTROPY_SUM, CROSS_ENTROPY_RELU_IN = 1, 4
 
 
 class Config(C.Structure):

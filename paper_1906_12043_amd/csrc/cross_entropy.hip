@@ -318,7 +318,7 @@ int check(const cocod_cross_entropy_call *c)
     if (c->struct_size != sizeof(cocod_cross_entropy_call))
         return set_error(COCOD_ERR_INVALID, "struct_size %u does not match this library (%zu)", c->struct_size, sizeof(cocod_cross_entropy_call));
     if (int rc = check_dtype(c->dtype)) return rc;
-    if (c->flags & ~COCOD_CROSS_ENTROPY_SUM) return set_error(COCOD_ERR_INVALID, "unknown flag bits 0x%x", c->flags);
+    if (c->flags & ~(COCOD_CROSS_ENTROPY_SUM | COCOD_CROSS_ENTROPY_RELU_IN)) return set_error(COCOD_ERR_INVALID, "unknown flag bits 0x%x", c->flags);
     if (c->groups < 1 || c->groups > kMaxGroups) return set_error(COCOD_ERR_INVALID, "groups must be in 1..65535");
     if (c->rows >= kMaxLossRows) return set_error(COCOD_ERR_INVALID, "rows must be below 2^26");
     if (c->dim < 1 || c->dim > kMaxWidth || c->vocab < 1 || c->vocab > kMaxWidth) return set_error(COCOD_ERR_INVALID, "dim and vocab must be in 1..2^30");
@@ -483,6 +483,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
             d.b = e; d.ldb = c->lde; d.b_group = z.b_group;
             d.k = n; d.a_zero_padded = 1;
             d.out = c->dh; d.ldc = c->lddh; d.out_row = index; d.row_scale = row_scale;
+            if (c->flags & COCOD_CROSS_ENTROPY_RELU_IN) { d.mask = ws + w.hidden; d.ld_mask = w.pitch; }       // (rows of C are gathered ones)
             if (w.pieces > 1) { d.sum = reinterpret_cast<float *>(ws + w.sum); d.ld_sum = w.sum_pitch; d.sum_read = i > 0; d.sum_write = i + 1 < w.pieces; }
             d.splits = w.to_hidden.splits;
             if (int rc = launch_status(launch_store(q, t, Layout::Rows_KN, settle_tile(t, Layout::Rows_KN, w.to_hidden.tile, d), d), what)) return rc;

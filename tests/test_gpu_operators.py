@@ -1,5 +1,8 @@
 """Grouped products, vocabulary loss and 8-bit checkpoints on the GPU against plain 64-bit implementations; every output is checked
 element by element against a bound derived in operator_harness, and everything around the outputs has to stay as it was."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -595,7 +598,75 @@ def test_loss_with_a_shared_table_and_infinite_logits():
     assert bool(torch.isfinite(de).all()) and not bool(de[1, 50:60].any())
 
 
+# bounds, rows, dim, vocab, pad, piece: one piece and several, rows in small and large tiles, joined splits, rows off 16 bytes
+RELU_LOSSES = [([2, 40, 40, 71], 80, 64, 300, 0, 0), ([0, 200, 333], 340, 120, 700, 8, 256), ([0, 3], 3, 33, 77, 1, 0),
+               ([1, 1000, 2999], 3000, 264, 2056, 0, 1024), ([0, 600], 600, 1032, 2500, 0, 0), ([0, 2990], 3000, 1032, 700, 0, 512)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("case", range(len(RELU_LOSSES)))
+def test_loss_behind_a_relu(dtype, case):
+    """dh is zero where h is not above zero, and else has the bits that it has without the relu; nothing else changes."""
+    bounds, rows, dim, vocab, pad, piece = RELU_LOSSES[case]
+    gen, t, groups = generator(300 + case), oh.TYPES[dtype][1], len(bounds) - 1
+    h, e = oh.matrix(rows, dim, pad, t, gen), oh.stack(groups, vocab, dim, pad, pad, t, gen, std=2.0 / dim ** 0.5)
+    h.copy_(torch.relu(h))
+    h[::3, 1::7] = -0.0
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    target[1::5] = -1
+    h[1::5] = float("nan")
+    written, outs = oh.inside(bounds, rows), []
+    for flags in (0, P.CROSS_ENTROPY_RELU_IN):
+        loss = torch.zeros(rows, device="cuda")
+        (hbuf, dh), (ebuf, de) = oh.output((rows, dim), pad, t), oh.output((groups, vocab, dim), pad, t)
+        P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, dh, de, None, loss, piece=piece, flags=flags))
+        assert oh.untouched(hbuf, dh, written)
+        outs.append((loss, dh, ebuf))
+    want = oh.exact_loss(bounds, h, e, target)
+    close(outs[0][1][written], want["dh"][written], oh.loss_bounds(want, t, dim, vocab)["dh"][written])
+    through = torch.where(h > 0, outs[0][1], torch.zeros_like(h))
+    assert torch.equal(outs[1][1][written], through[written])
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][2], outs[1][2])
+
+
 # ---- together ------------------------------------------------------------------------------------------------
+
+def readme_example():
+    """The README's block of Python, as it stands there."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    blocks = re.findall(r"```python\n(.*?)```", text, re.S)
+    assert len(blocks) == 1
+    return blocks[0]
+
+
+def test_the_example_of_the_readme():
+    """Run as it stands: every result against 64 bits from the inputs it was made of, and the weights' gradient against 64 bits from the first inputs:
+    y, dz, dy and dW are rounded to bf16 once each (2^-8 of the value), y once more through the logits, dh and dE: 8 2^-8 in the norm."""
+    bounds, R, K, N, V = [0, 60, 60, 200], 200, 96, 64, 500
+    W, gen, t = len(bounds) - 1, generator(23), torch.bfloat16
+    x, w, table = oh.matrix(R, K, 0, t, gen), oh.stack(W, K, N, 0, 0, t, gen, std=K ** -0.5), oh.stack(W, V, N, 0, 0, t, gen, std=2.0 * N ** -0.5)
+    targets = torch.randint(0, V, (R,), generator=gen, device="cuda", dtype=torch.int32)
+    targets[::5] = -1
+    y, dy, dx = (torch.zeros((R, c), dtype=t, device="cuda") for c in (N, N, K))
+    names = dict(torch=torch, W=W, R=R, K=K, N=N, V=V, offsets=torch.tensor(bounds, dtype=torch.int64, device="cuda"), x=x, w=w, y=y, dy=dy, dx=dx,
+                 dw=torch.zeros((W, K, N), device="cuda"), table=table, targets=targets, loss=torch.zeros(R, device="cuda"),
+                 group_loss=torch.zeros(W, device="cuda"), dtable=torch.zeros_like(table), stream=torch.cuda.current_stream())
+    exec(compile(readme_example(), "README.md", "exec"), names)
+    out, mag, terms = oh.exact_product("forward", bounds, x, w)
+    close(y, out.clamp(min=0), oh.product_bound(out, mag, terms, t))
+    want = oh.exact_loss(bounds, y, table, targets)
+    bound = oh.loss_bounds(want, t, N, V)
+    close(names["loss"], want["loss"], bound["loss"])
+    close(names["dtable"], want["de"], bound["de"])
+    close(dy, want["dh"] * (y > 0), bound["dh"])
+    got, mag, terms = oh.exact_product("weight_grad", bounds, x, dy)
+    close(names["dw"], got, oh.product_bound(got, mag, terms, torch.float32))
+    first = oh.exact_loss(bounds, out.clamp(min=0), table, targets)
+    dw, _, _ = oh.exact_product("weight_grad", bounds, x, first["dh"] * (out > 0))
+    for g in range(W):
+        assert float((names["dw"][g].double() - dw[g]).norm()) <= 2.0 ** -5 * float(dw[g].norm()), g
+
+
 
 class Workers:
     """W workers with models of two layers and a vocabulary's table in one packed row each, trained by the framework's step with the caller's

@@ -168,3 +168,11 @@ def test_checkpoint_arguments_are_refused(args, text):
     refused(P.checkpoint_store, None, *args, text=text)
     dtype, rows, cols, x, ldx, codes, ldc, scales, lds = args
     refused(P.checkpoint_load, None, dtype, rows, cols, codes, ldc, scales, lds, x, ldx, text=text)
+
+
+def test_the_loss_knows_its_flags():
+    both = P.CROSS_ENTROPY_SUM | P.CROSS_ENTROPY_RELU_IN
+    assert P.cross_entropy_workspace(loss_call(flags=both)) == P.cross_entropy_workspace(loss_call())
+    for flags in (2, 8, both | 2, 1 << 31):
+        refused(P.cross_entropy, None, loss_call(flags=flags), text="flag")
+        refused(P.cross_entropy_workspace, loss_call(flags=flags), text="flag")
