@@ -1,7 +1,7 @@
 // Mean softmax cross-entropy of ragged batches over a large vocabulary, and its gradient, without the logits in memory.
 //
 //   z = h E_g^T,  loss_r = log sum_v exp z_rv - z_r,t(r),  L_g = sum_r loss_r / n_g,
-//   dL/dz_rv = (exp(z_rv - norm_r) - [v = t(r)]) / n_g,  dh = dz E_g,  dE_g = dz^T h
+//   dL/dz_rv = (exp z_rv / sum_u exp z_ru - [v = t(r)]) / n_g,  dh = dz E_g,  dE_g = dz^T h
 //
 // Rows without a target take no part: the others are gathered to the front of their group, so that no product sees a row that is
 // masked (whatever its values are) and masked rows cost nothing.  The vocabulary is gone through twice: once for maximum and sum
@@ -125,14 +125,18 @@ template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Ro
     if (!has_target(p, r)) clear_row(hidden, r, lane);
 }
 
-// norm[r] = logarithm of the row's sum of exponentials, from the column tiles' maxima and sums; the row's loss, also in the place of the
-// target's logit.  ROWS rows per pass of a block, THREADS threads a row.
+// What a row's slopes need, from the column tiles' maxima and sums, and its loss, also in the place of the target's logit.  The target is not among
+// those sums: with s the sum of the other exponentials, all below the larger one m of the others' maximum and the target's logit z,
+//   loss = (m - z) + log(s + exp(z - m)), log1p(s) where z = m;   slope of the target = -s / (s + exp(z - m)),
+// so that both keep their digits where the target is almost certain, however large the logits are (a logarithm of the whole sum, rounded at the
+// size of m, left none of a loss of 1e-6 at logits of 40, and the target's slope with steps of |m| 2^-24).
+// ROWS rows per pass of a block, THREADS threads a row.
 constexpr int kNormThreads = 16, kNormAhead = 4, kFewThreads = 4;
 struct Norms {
     const uint32_t *index;
     const float2 *stats;              // [tiles][rows]
     uint32_t tiles;
-    float *target_logit, *norm, *loss;
+    float *target_logit, *top, *inverse, *target_slope, *loss;
 };
 __device__ __forceinline__ void add_part(float &top, float &sum, float2 s)
 {
@@ -163,9 +167,11 @@ template <int ROWS, bool GATHERED, int THREADS> __device__ __forceinline__ float
     if (y == 0 && in) {
         #pragma unroll
         for (int w = 1; w < THREADS; ++w) add_part(top, sum, part[w][x]);
-        const float norm = top + logf(sum);
-        n.norm[r] = norm;
-        l = norm - n.target_logit[r];
+        const float z = n.target_logit[r], m = fmaxf(top, z), others = sum * expf(top - m), all = others + expf(z - m);
+        n.top[r] = m;
+        n.inverse[r] = 1.0f / all;
+        n.target_slope[r] = -others / all;
+        l = (m - z) + (z >= top ? log1pf(others) : logf(all));
         n.target_logit[r] = l;
         n.loss[GATHERED ? n.index[r] : r] = l;
     }
@@ -220,7 +226,7 @@ template <bool NORMS, bool GATHERED = true, int THREADS = kNormThreads> __global
     if (threadIdx.x == 0 && group_loss) group_loss[g] = static_cast<float>(count ? (sum_only ? part[0] : part[0] / static_cast<double>(count)) : 0.0);
 }
 
-// Slopes from kept exponentials, in their place: exp(z - top) exp(top - norm) - [v = t], top the tile's maximum.  Eight columns a thread.
+// Slopes from kept exponentials, in their place: exp(z - top) exp(top - m) / sum, top the tile's maximum; the target's is there.  Eight columns a thread.
 template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Rows p, const Norms n, const int32_t *target, void *slopes, uint64_t pitch, uint32_t v0,
                                                                        uint32_t columns, uint32_t columns_end, uint32_t tile_cols, uint32_t parts)
 {
@@ -228,7 +234,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Row
     const uint64_t r = blockIdx.x / parts;
     const uint32_t c = (blockIdx.x % parts * 256 + threadIdx.x) * 8;
     if (c >= columns_end || r < clamped(p, 0) || r >= clamped(p, p.groups) || n.index[r] == kNoRow) return;
-    const float factor = expf(n.stats[static_cast<uint64_t>(c / tile_cols) * p.rows + r].x - n.norm[r]);
+    const float factor = expf(n.stats[static_cast<uint64_t>(c / tile_cols) * p.rows + r].x - n.top[r]) * n.inverse[r];
     const uint32_t number = static_cast<uint32_t>(target[r]) - v0 - c;
     elem *at = static_cast<elem *>(slopes) + r * pitch + c;
     float v[8];
@@ -242,7 +248,7 @@ template <class T> __global__ __launch_bounds__(256) void slope_kernel(const Row
     }
     #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
-        if (number == j) v[j] -= 1.0f;
+        if (number == j) v[j] = n.target_slope[r];
         if (c + j >= columns) v[j] = 0.0f;
     }
     if constexpr (sizeof(elem) == 4) {
@@ -260,7 +266,7 @@ constexpr uint64_t kGatherHere = 32u << 10, kStatsHere = 8, kLeaveHere = 1u << 2
 
 // The caller's memory, carved up.
 struct Workspace {
-    uint64_t index, target, ends, norm, target_logit, row_scale, hidden, stats, slope, sum, part, bytes;
+    uint64_t index, target, ends, top, inverse, target_slope, target_logit, row_scale, hidden, stats, slope, sum, part, bytes;
     uint64_t pitch, piece, sum_pitch;
     uint32_t pieces;
     bool keep;                        // the last piece's exponentials stay from the first pass, as slopes to be
@@ -292,7 +298,9 @@ Workspace carve(const cocod_cross_entropy_call *c)
     w.index = take(rows * 4);
     w.target = take(rows * 4);
     w.ends = take(c->groups * 8ull);
-    w.norm = take(rows * 4);
+    w.top = take(rows * 4);
+    w.inverse = take(rows * 4);
+    w.target_slope = take(rows * 4);
     w.target_logit = take(rows * 4);
     w.row_scale = take(rows * 4);
     w.hidden = take(rows * w.pitch * s);
@@ -396,7 +404,8 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     uint8_t *ws = static_cast<uint8_t *>(c->workspace);
     uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
     int64_t *ends = reinterpret_cast<int64_t *>(ws + w.ends);
-    float *norm = reinterpret_cast<float *>(ws + w.norm), *row_scale = reinterpret_cast<float *>(ws + w.row_scale);
+    float *const top = reinterpret_cast<float *>(ws + w.top), *const inverse = reinterpret_cast<float *>(ws + w.inverse);
+    float *const target_slope = reinterpret_cast<float *>(ws + w.target_slope), *const row_scale = reinterpret_cast<float *>(ws + w.row_scale);
     int32_t *target = reinterpret_cast<int32_t *>(ws + w.target);
     const Rows rows = {c->offsets, c->groups, c->rows, c->targets, c->vocab};
     const float unslope = t == Dtype::F16 ? 0x1p-14f : 1.0f;   // fp16 slopes are kept times 2^14
@@ -415,7 +424,8 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     if (!few) { z.a = ws + w.hidden; z.lda = w.pitch; }
     const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, z);
     const uint32_t cols = tile_cols(t, tile);
-    Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), (c->vocab + cols - 1) / cols, reinterpret_cast<float *>(ws + w.target_logit), norm, c->loss};
+    Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), (c->vocab + cols - 1) / cols, reinterpret_cast<float *>(ws + w.target_logit), top, inverse,
+                   target_slope, c->loss};
     const bool here = c->rows * norms.tiles <= kStatsHere * kMeanThreads * c->groups, gathered = !(few && here && c->rows);
     if (gathered) {
         z.a = ws + w.hidden; z.lda = w.pitch;
@@ -469,7 +479,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
         } else if (c->rows) {
             ProductParams p = z;
             p.b = e; p.n = n; p.v0 = static_cast<uint32_t>(v0);
-            p.norm = norm;
+            p.top = top; p.inverse = inverse; p.target_slope = target_slope;
             p.out = ws + w.slope; p.ldc = w.piece; p.ldc_zero = (n + 7) / 8 * 8;
             if (int rc = launch_status(launch_logits(q, t, Finish::Slope, settle_tile(t, Layout::Rows_NK, w.slopes.tile, p), p), what)) return rc;
         }

@@ -21,7 +21,7 @@ enum class Layout { Rows_KN, Rows_NK, Weights };
 // What becomes of a tile of C.
 enum class Finish {
     Store,       // relu, mask, scale, running sum; store in the element type or fp32
-    Stats,       // logits: maximum and sum of exponentials of the tile's part of every row, and the target's logit
+    Stats,       // logits: maximum and sum of exponentials of the tile's part of every row but its target, and the target's logit
     Keep,        //   the same, and the exponentials stored (bf16: in fp16 times 2^14; pitch and columns to the end of the last tile are the buffer's)
     Slope        // logits: softmax minus one-hot, stored in the element type
 };
@@ -60,9 +60,10 @@ struct ProductParams {
     uint32_t splits;
     // logits
     const int32_t *target;            // [rows]
-    float2 *stats;                    // [column tiles][rows]: maximum, sum of exponentials
+    float2 *stats;                    // [column tiles][rows]: maximum, sum of exponentials, of all but the target
     float *target_logit;              // [rows]
-    const float *norm;                // [rows]: logarithm of the sum of exponentials
+    const float *top, *inverse;       // [rows]: largest logit; 1 / sum of the exponentials below it
+    const float *target_slope;        // [rows]: probability of the target, less one
     uint32_t v0;                      // vocabulary entry of column 0
     uint32_t ldc_zero;                // Slope: columns up to here are stored, those from n on as zeros
 };

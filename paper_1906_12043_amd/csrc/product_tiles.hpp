@@ -522,11 +522,11 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         // what belongs to a row is fetched once, by the lane of its number
         const uint32_t lane = threadIdx.x % 64, mine = r0 + lane % ROWS;
         const uint64_t my_row = at.row0 + mine;
-        float row_factor = factor;
+        float row_factor = factor, row_top = 0.0f;
         uint32_t row_number = 0;
         const bool by_row = !WEIGHTS && !part && (FINISH == Finish::Slope || p.row_scale || p.out_row);
         if (by_row && mine < at.rows) {
-            if (FINISH == Finish::Slope) { row_factor = p.norm[my_row]; row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
+            if (FINISH == Finish::Slope) { row_top = p.top[my_row]; row_factor = p.inverse[my_row] * slope_scale<T>(); row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
             if (FINISH == Finish::Store && p.row_scale) row_factor = p.row_scale[my_row];
             if (FINISH == Finish::Store && p.out_row) row_number = p.out_row[my_row];
         }
@@ -535,19 +535,19 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
             const uint32_t r = k + first;
             const float f = by_row ? __shfl(row_factor, r, 64) : factor;
             const uint32_t number = by_row ? __shfl(row_number, r, 64) : 0;
+            const float top = FINISH == Finish::Slope ? __shfl(row_top, r, 64) : 0.0f;
             f4 a = *reinterpret_cast<const f4 *>(v + r * PITCH + qa), b = *reinterpret_cast<const f4 *>(v + r * PITCH + qb);
             if (r0 + r >= at.rows) continue;
             const uint64_t row = at.row0 + r0 + r;
             char *at_row = to + static_cast<uint64_t>(r0 + r) * pitch;
             if constexpr (FINISH == Finish::Slope) {
                 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) { a[j] = T::exp(a[j], f); b[j] = T::exp(b[j], f); }
+                for (uint32_t j = 0; j < 4; ++j) { a[j] = T::exp(a[j], top) * f; b[j] = T::exp(b[j], top) * f; }
                 if (number - ca < 4 || number - cb < 4) {      // the target is one of these columns
+                    const float t = p.target_slope[row] * slope_scale<T>();
                     #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) { if (number - ca == j) a[j] -= 1.0f; if (number - cb == j) b[j] -= 1.0f; }
+                    for (uint32_t j = 0; j < 4; ++j) { if (number - ca == j) a[j] = t; if (number - cb == j) b[j] = t; }
                 }
-                a *= slope_scale<T>();
-                b *= slope_scale<T>();
             } else if (!part) {
                 if (!WEIGHTS) {
                     if (p.out_row) { if (number == kNoRow) continue; at_row = to + number * pitch; }
@@ -735,11 +735,11 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             }
         } else if constexpr (FINISH == Finish::Slope) {
             if (r >= at.rows || c >= p.ldc_zero) return;
-            const float norm = p.norm[at.row0 + r];
+            const float top = p.top[at.row0 + r], inverse = p.inverse[at.row0 + r] * slope_scale<T>(), slope = p.target_slope[at.row0 + r] * slope_scale<T>();
             const int32_t target = p.target[at.row0 + r];
             #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = (T::exp(v[j], norm) - (static_cast<int32_t>(p.v0 + c + j) == target ? 1.0f : 0.0f)) * slope_scale<T>();
+                v[j] = static_cast<int32_t>(p.v0 + c + j) == target ? slope : T::exp(v[j], top) * inverse;
                 if (c + j >= p.n) v[j] = 0.0f;
             }
             store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
@@ -772,7 +772,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 #pragma unroll
                 for (uint32_t j = 0; j < 4; ++j) {
                     if (c + j >= p.n) v[j] = -INFINITY;
-                    else if (static_cast<int32_t>(p.v0 + c + j) == target) p.target_logit[at.row0 + r] = v[j];
+                    else if (static_cast<int32_t>(p.v0 + c + j) == target) { p.target_logit[at.row0 + r] = v[j]; v[j] = -INFINITY; }
                     top = fmaxf(top, v[j]);
                 }
                 #pragma unroll
@@ -790,7 +790,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         }
     } else if constexpr (FINISH == Finish::Stats || FINISH == Finish::Keep) {
         // The maximum over the wave's columns (lanes MI apart hold a row), over the waves, and the sums of exponentials below the tile's
-        // maximum; kept or not, the same bits.
+        // maximum; kept or not, the same bits.  The target's logit goes apart and counts as minus infinity here.
         constexpr bool KEEP = FINISH == Finish::Keep;
         float *tops = reinterpret_cast<float *>(lds), *sums = tops + S::WN * S::BM;        // the operand buffers are free
         const uint32_t c0 = at.n0 + wn * S::NB * S::MI + 4 * (lane / S::MI);
@@ -804,7 +804,10 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 for (int j = 0; j < S::NB; ++j)
                     #pragma unroll
                     for (int x = 0; x < S::X; ++x)
-                        if (static_cast<int32_t>(c0 + j * S::MI + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
+                        if (static_cast<int32_t>(c0 + j * S::MI + 8 * (x / 4) + x % 4) == target) {
+                            p.target_logit[at.row0 + r] = acc[0][i][j][x] * unscale;
+                            acc[0][i][j][x] = -INFINITY;
+                        }
             }
             float top = -INFINITY;
             if (!whole) {

@@ -598,6 +598,69 @@ def test_loss_with_a_shared_table_and_infinite_logits():
     assert bool(torch.isfinite(de).all()) and not bool(de[1, 50:60].any())
 
 
+# rows, dim, vocab, pad, piece: few rows (waves that share the terms), rows off 16 bytes, the larger tiles, one piece and several
+CONFIDENT = [(40, 16, 700, 0, 0), (40, 16, 700, 0, 256), (41, 13, 700, 0, 256), (700, 264, 5000, 0, 0), (700, 16, 5000, 8, 2560), (2999, 72, 4104, 0, 1024)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("case", range(len(CONFIDENT)))
+def test_confident_rows_keep_their_digits(dtype, case):
+    """Rows whose target is almost certain, with logits of up to 600: loss and slopes to a relative bound that knows no size of the logits.
+
+    Every logit is a sum of two products of a few bits, exact in fp32.  x = z - (a maximum) is then exact, too; an exponential of it is off by
+    (|x| + 2) 2^-23 of itself, and what is below e^-90 of the largest of all does not count (2^-120, and the exponentials between the passes below).  Up
+    to three factors of that kind, with the 300 + vocab / 64 additions of the others' sum: a slope, the sum of the others relative to the target and with it a loss
+    below one are off by rel = (3 * 92 + 300 + vocab / 64) 2^-23, a loss above by its own roundings, too: 8 steps in all.  Slopes: half a step of a 16-bit type
+    (fp16: not below steps of 2^-38); bf16 exponentials between the passes: 2^-11, not below steps of 2^-38 of their tile's largest.  Then the products.
+    """
+    rows, dim, vocab, pad, piece = CONFIDENT[case]
+    t, gen = oh.TYPES[dtype][1], generator(400 + case)
+    u, f = oh.half_step(t), torch.float64
+    sure = torch.tensor([0, vocab // 2 + 5, vocab - 1], device="cuda")                     # entries that rows are sure of: in the first tile, within, in the last
+    h, e = oh.matrix(rows, dim, pad, t, gen), oh.stack(1, vocab, dim, pad, 0, t, gen)
+    h.zero_()
+    e.zero_()
+    e[0, :, :3] = torch.randint(-16, 17, (vocab, 3), generator=gen, device="cuda").to(t) / 8
+    e[0, sure] = 0.0
+    for i in range(3):
+        e[0, sure[i], i] = 4.0
+        e[0, sure[i], 4 + i] = 1.0                                                          # dh shows the slope of this entry by itself
+    e[0, :, 3] = 1.0                                                                        # the size of all logits; dh shows the sum of all slopes
+    e[0, :, 7] = 1.0
+    e[0, sure, 7] = 0.0                                                                     #   and of the others'
+    who = torch.arange(rows, device="cuda") % 3
+    gaps = torch.tensor([1.0, 2.0, 3.0, 5.0, 7.0, 12.0, 30.0], device="cuda")
+    h[torch.arange(rows), who] = gaps[torch.arange(rows, device="cuda") // 3 % 7].to(t)
+    h[:, 3] = torch.tensor([0.0, 40.0, -100.0, 480.0], device="cuda")[torch.arange(rows, device="cuda") // 21 % 4].to(t)
+    target = sure[who].int()
+    target[5::11] = torch.randint(0, vocab, (len(target[5::11]),), generator=gen, device="cuda", dtype=torch.int32)       # and some that are wrong
+    z = h.to(f) @ e[0].to(f).t()
+    at = torch.arange(rows, device="cuda")
+    ratio = torch.exp(z - z[at, target.long()][:, None])                                    # to the target's exponential
+    ratio[at, target.long()] = 0.0
+    others = ratio.sum(1)
+    want = torch.log1p(others)
+    dz = ratio / (1 + others)[:, None]
+    dz[at, target.long()] = -others / (1 + others)
+    rel = (3 * 92 + 300 + vocab / 64) * oh.STEP
+    scale = 1.0 if dtype == "fp16" else 1024.0                                              # (the table's gradient stays within fp16)
+    for grads in (True, False):
+        loss, (hbuf, dh), (ebuf, de) = torch.empty(rows, device="cuda"), oh.output((rows, dim), pad, t), oh.output((1, vocab, dim), pad, t)
+        mean = torch.empty(1, device="cuda")
+        P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, [0, rows], h, e, target, dh if grads else None, de if grads else None, mean,
+                                                                           loss, piece=piece, flags=P.CROSS_ENTROPY_SUM, grad_scale=scale))
+        close(loss, want, (rel + 8 * oh.STEP) * want + 2.0 ** -120)
+        assert abs(mean.double() - want.sum()) <= (rel + 9 * oh.STEP) * want.sum()
+        if grads:
+            off = dz.abs() * (rel + 8 * oh.STEP + (u if t != torch.float32 else 0.0) + (2.0 ** -11 if dtype == "bf16" else 0.0)) + 2.0 ** -120
+            off += {"bf16": 2.0 ** -39, "fp16": 2.0 ** -39, "fp32": 0.0}[dtype] * (1.0 if dtype == "fp16" else (ratio / (1 + others)[:, None]).amax(1, keepdim=True))
+            for got, left, right, terms in ((dh, (off, dz), e[0].to(f), vocab), (de[0], (off.t(), dz.t()), h.to(f), rows)):
+                out = scale * (left[1] @ right)
+                far = left[0] @ right.abs() + (terms + 8) * oh.STEP * ((left[1].abs() + left[0]) @ right.abs())
+                close(got, out, scale * far * (1 + u) + (u + 4 * oh.STEP) * out.abs() + torch.finfo(t).smallest_normal * torch.finfo(t).eps)
+            assert oh.untouched(hbuf, dh) and oh.untouched(ebuf, de)
+
+
 # bounds, rows, dim, vocab, pad, piece: one piece and several, rows in small and large tiles, joined splits, rows off 16 bytes
 RELU_LOSSES = [([2, 40, 40, 71], 80, 64, 300, 0, 0), ([0, 200, 333], 340, 120, 700, 8, 256), ([0, 3], 3, 33, 77, 1, 0),
                ([1, 1000, 2999], 3000, 264, 2056, 0, 1024), ([0, 600], 600, 1032, 2500, 0, 0), ([0, 2990], 3000, 1032, 700, 0, 512)]
