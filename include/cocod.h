@@ -462,7 +462,9 @@ enum {
  * Softmax cross-entropy of logits h_g e_g^T over a vocabulary, without the logits in memory, and the gradients of
  * grad_scale * (loss of the group).  A row whose target is not in 0 .. vocab - 1 has none: its loss and its
  * row of dh are zero, it does not count in the mean, and nothing of its h is used.  A group without
- * targets has loss 0 and gradient 0.  16-bit types: the slopes at the logits are rounded to the type before the products.
+ * targets has loss 0 and gradient 0.  16-bit types: the slopes at the logits are rounded to the type before the products (bf16: by up to
+ * 2^-8 + 2^-11 of themselves, fp16: 2^-11, not below steps of 2^-38), so an entry of dh or de is off by up to that part of the sum of its
+ * products' magnitudes, beside its own rounding; near a minimum, where they cancel, that may be much of the entry.  COCOD_F32 keeps the slopes in fp32.
  */
 typedef struct cocod_cross_entropy_call {
     uint32_t struct_size;           /* sizeof(cocod_cross_entropy_call); checked */

@@ -661,6 +661,38 @@ def test_confident_rows_keep_their_digits(dtype, case):
             assert oh.untouched(hbuf, dh) and oh.untouched(ebuf, de)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("steps, piece", [(60, 0), (400, 0), (400, 256)])
+def test_gradients_near_a_minimum(dtype, steps, piece):
+    """A trained table, whose gradient is a small difference of large sums.  What the header says of 16 bits: every slope is off by half a step of the type
+    (bf16: and 2^-11) of itself, so dE by that part of the sum of magnitudes and its own rounding; what fp32 adds is in loss_bounds, element by element."""
+    t, gen, rows, vocab, dim, f = oh.TYPES[dtype][1], generator(21), 4096, 400, 64, torch.float64
+    h = torch.randn(rows, dim, generator=gen, device="cuda").to(torch.bfloat16)
+    true = torch.randn(vocab, dim, generator=gen, device="cuda", dtype=f) * 0.3
+    target = torch.multinomial(torch.softmax(h.to(f) @ true.t(), 1), 1, generator=gen)[:, 0].int()
+    e, m, v = (torch.zeros(vocab, dim, dtype=f, device="cuda") for _ in range(3))
+    for step in range(1, steps + 1):
+        dz = torch.softmax(h.to(f) @ e.t(), 1)
+        dz[torch.arange(rows), target.long()] -= 1
+        g = dz.t() @ h.to(f) / rows
+        m, v = 0.9 * m + 0.1 * g, 0.999 * v + 0.001 * g * g
+        e = e - 0.02 * (m / (1 - 0.9 ** step)) / ((v / (1 - 0.999 ** step)).sqrt() + 1e-12)
+    h, e = h.to(t), e[None].to(t)
+    want = oh.exact_loss([0, rows], h, e, target)
+    bound = oh.loss_bounds(want, t, dim, vocab)
+    loss, dh, de = torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(e)
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, [0, rows], h, e, target, dh, de, None, loss, piece=piece))
+    close(loss, want["loss"], bound["loss"])
+    close(dh, want["dh"], bound["dh"])
+    close(de, want["de"], bound["de"])
+    dz = want["parts"][0][7]
+    magnitude, u = (dz.abs().t() @ h.to(f).abs()) / rows, oh.half_step(t)
+    # fp16: slopes are not below steps of 2^-38; fp32: the sums' (rows + 8) 2^-23 stand for everything
+    part = {"bf16": u + 2.0 ** -11, "fp16": u, "fp32": 0.0}[dtype] + (rows + 8 + 400) * oh.STEP
+    floor = (2.0 ** -39 * h.to(f).abs().mean(0) if dtype != "fp32" else 0.0) + torch.finfo(t).smallest_normal * torch.finfo(t).eps
+    close(de[0], want["de"][0], part * (1 + u) * magnitude + u * want["de"][0].abs() + floor)
+
+
 # bounds, rows, dim, vocab, pad, piece: one piece and several, rows in small and large tiles, joined splits, rows off 16 bytes
 RELU_LOSSES = [([2, 40, 40, 71], 80, 64, 300, 0, 0), ([0, 200, 333], 340, 120, 700, 8, 256), ([0, 3], 3, 33, 77, 1, 0),
                ([1, 1000, 2999], 3000, 264, 2056, 0, 1024), ([0, 600], 600, 1032, 2500, 0, 0), ([0, 2990], 3000, 1032, 700, 0, 512)]
