@@ -506,6 +506,18 @@ int cocod_checkpoint_store(void *stream, int dtype, uint64_t rows, uint64_t cols
 int cocod_checkpoint_load(void *stream, int dtype, uint64_t rows, uint64_t cols, const uint8_t *codes, uint64_t ld_codes,
                           const uint8_t *scales, uint64_t ld_scales, void *x, uint64_t ldx);
 
+/*
+ * For tests: how the products of a call would run.  Makes no GPU call and reads no memory that the description points to.  Of the loss: the logits'
+ * statistics, the slopes, the gradients of the hidden states and of the table (splits 0: no such product).
+ */
+typedef struct cocod_product_plan {
+    uint32_t tile;                  /* of the result: 0 256x256, 1 128x128, 2 32x64, 3 128x128 with four slices in flight, 4 192x128, 5 64x64 */
+    uint32_t splits;                /* of the sums */
+    uint32_t operands;              /* 0: both go to LDS directly, 1: through registers, 2: the first one is codes */
+} cocod_product_plan;
+int cocod_debug_grouped_plan(const cocod_grouped *g, int direction, cocod_product_plan *out);
+int cocod_debug_cross_entropy_plan(const cocod_cross_entropy_call *c, cocod_product_plan out[4], uint32_t *pieces);
+
 /* Last error text of ctx, or of the last failed cocod_create / context-free call when ctx is NULL.
    Never NULL; owned by the library; valid until the next call on the same context / thread. */
 const char *cocod_last_error(const cocod_ctx *ctx);

@@ -80,6 +80,11 @@ class CrossEntropy(_Call):
         super().__init__(**{"grad_scale": 1.0, **fields})
 
 
+class ProductPlan(C.Structure):
+    """Mirror of struct cocod_product_plan."""
+    _fields_ = [("tile", C.c_uint32), ("splits", C.c_uint32), ("operands", C.c_uint32)]
+
+
 class CocodError(RuntimeError):
     def __init__(self, status, message):
         super().__init__("cocod status %d: %s" % (status, message))
@@ -138,6 +143,8 @@ def lib():
             "cocod_grouped_weight_grad": ([vp, P(Grouped)], i32),
             "cocod_cross_entropy_workspace": ([P(CrossEntropy), P(u64)], i32),
             "cocod_cross_entropy": ([vp, P(CrossEntropy)], i32),
+            "cocod_debug_grouped_plan": ([P(Grouped), i32, P(ProductPlan)], i32),
+            "cocod_debug_cross_entropy_plan": ([P(CrossEntropy), P(ProductPlan), P(u32)], i32),
             "cocod_checkpoint_store": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_checkpoint_load": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_debug_copy": ([vp, vp, vp, u64], i32),
@@ -217,6 +224,20 @@ def cross_entropy_workspace(call):
 
 def cross_entropy(stream, call):
     return _check(lib().cocod_cross_entropy(_addr(stream), C.byref(call)))
+
+
+def debug_grouped_plan(layer, direction):
+    """(tile, splits, operands) with which this direction of the layer runs."""
+    out = ProductPlan()
+    _check(lib().cocod_debug_grouped_plan(C.byref(layer), direction, C.byref(out)))
+    return out.tile, out.splits, out.operands
+
+
+def debug_cross_entropy_plan(call):
+    """[(tile, splits, operands)] of logits, slopes, gradient of the hidden states and of the table, and the number of pieces."""
+    out, pieces = (ProductPlan * 4)(), C.c_uint32()
+    _check(lib().cocod_debug_cross_entropy_plan(C.byref(call), out, C.byref(pieces)))
+    return [(p.tile, p.splits, p.operands) for p in out], pieces.value
 
 
 def checkpoint_store(stream, dtype, rows, cols, x, ldx, codes, ld_codes, scales, ld_scales):

@@ -355,6 +355,32 @@ template <class E> hipError_t launch_gather(hipStream_t s, const Rows &rows, con
     return hipGetLastError();
 }
 
+// The operands of the call's products (the rest of the parameters is the call's): logits of the gathered rows, and of a piece that begins at entry v0 the
+// gradients of the hidden states and of the table.
+ProductParams logits_operands(const cocod_cross_entropy_call *c, const Workspace &w, const uint8_t *ws)
+{
+    ProductParams p{};
+    p.a = ws + w.hidden; p.lda = w.pitch;
+    p.b = c->e; p.ldb = c->lde; p.b_group = c->groups > 1 ? c->e_stride : 0;
+    p.k = c->dim;
+    return p;
+}
+ProductParams hidden_operands(const cocod_cross_entropy_call *c, const Workspace &w, const uint8_t *ws, uint64_t v0, uint32_t n)
+{
+    ProductParams p{};
+    p.a = ws + w.slope; p.lda = w.piece; p.a_zero_padded = 1;
+    p.b = static_cast<const uint8_t *>(c->e) + v0 * c->lde * dtype_bytes(kTypes[c->dtype]); p.ldb = c->lde; p.b_group = c->groups > 1 ? c->e_stride : 0;
+    p.k = n;
+    return p;
+}
+ProductParams table_operands(const Workspace &w, const uint8_t *ws)
+{
+    ProductParams p{};
+    p.a = ws + w.slope; p.lda = w.piece;
+    p.b = ws + w.hidden; p.ldb = w.pitch;
+    return p;
+}
+
 }  // namespace
 }  // namespace cocod
 
@@ -416,23 +442,23 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     const int sum_only = (c->flags & COCOD_CROSS_ENTROPY_SUM) != 0;
 
     const float scale = c->grad_scale * unslope;
-    ProductParams z{};
+    const ProductParams gathered_rows = logits_operands(c, w, ws);
+    ProductParams z = gathered_rows;
     z.a = c->h; z.lda = c->ldh;
-    z.b = c->e; z.ldb = c->lde; z.b_group = c->groups > 1 ? c->e_stride : 0;
     z.offsets = c->offsets; z.ends = ends; z.groups = c->groups; z.rows = c->rows;
-    z.k = c->dim; z.splits = 1; z.target = target;
+    z.splits = 1; z.target = target;
     // The loss alone of a few rows that the product can take where they are: those without a target go through it, too, and are left out of the
     // sums (64 rows, 1000 x 256: 11 us instead of 16; 512 rows 14 instead of 18; 16 rows, 16000 x 1024: 17 instead of 21).  Not in fp32, where a
     // row that is not finite has its whole tile formed again.
     const bool few = t != Dtype::F32 && !c->dh && !c->de && direct_a(Layout::Rows_NK, z) && c->rows * w.pitch * s <= kLeaveHere * c->groups;
-    if (!few) { z.a = ws + w.hidden; z.lda = w.pitch; }
+    if (!few) { z.a = gathered_rows.a; z.lda = gathered_rows.lda; }
     const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, z);
     const uint32_t cols = tile_cols(t, tile);
     Norms norms = {index, reinterpret_cast<const float2 *>(ws + w.stats), (c->vocab + cols - 1) / cols, reinterpret_cast<float *>(ws + w.target_logit), top, inverse,
                    target_slope, c->loss};
     const bool here = c->rows * norms.tiles <= kStatsHere * kMeanThreads * c->groups, gathered = !(few && here && c->rows);
     if (gathered) {
-        z.a = ws + w.hidden; z.lda = w.pitch;
+        z.a = gathered_rows.a; z.lda = gathered_rows.lda;
         if (int rc = launch_status(t == Dtype::F32 ? launch_gather<float>(q, rows, c, w, ws, scale) : launch_gather<uint16_t>(q, rows, c, w, ws, scale), what)) return rc;
     } else {
         z.ends = nullptr; z.target = c->targets;
@@ -487,15 +513,14 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
             p.out = ws + w.slope; p.ldc = w.piece; p.ldc_zero = (n + 7) / 8 * 8;
             if (int rc = launch_status(launch_logits(q, t, Finish::Slope, settle_tile(t, Layout::Rows_NK, w.slopes.tile, p), p), what)) return rc;
         }
-        ProductParams p{};
-        p.offsets = c->offsets; p.ends = ends; p.groups = c->groups; p.rows = c->rows;
-        p.a = ws + w.slope; p.lda = w.piece;
-        p.n = c->dim;
-        p.part = reinterpret_cast<float *>(ws + w.part); p.ld_part = part_pitch(c->dim);
+        auto common = [&](ProductParams &d) {
+            d.offsets = c->offsets; d.ends = ends; d.groups = c->groups; d.rows = c->rows;
+            d.n = c->dim;
+            d.part = reinterpret_cast<float *>(ws + w.part); d.ld_part = part_pitch(c->dim);
+        };
         if (c->dh && c->rows) {
-            ProductParams d = p;
-            d.b = e; d.ldb = c->lde; d.b_group = z.b_group;
-            d.k = n; d.a_zero_padded = 1;
+            ProductParams d = hidden_operands(c, w, ws, v0, n);
+            common(d);
             d.out = c->dh; d.ldc = c->lddh; d.out_row = index; d.row_scale = row_scale;
             if (c->flags & COCOD_CROSS_ENTROPY_RELU_IN) { d.mask = ws + w.hidden; d.ld_mask = w.pitch; }       // (rows of C are gathered ones)
             if (w.pieces > 1) { d.sum = reinterpret_cast<float *>(ws + w.sum); d.ld_sum = w.sum_pitch; d.sum_read = i > 0; d.sum_write = i + 1 < w.pieces; }
@@ -503,8 +528,8 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
             if (int rc = launch_status(launch_store(q, t, Layout::Rows_KN, settle_tile(t, Layout::Rows_KN, w.to_hidden.tile, d), d), what)) return rc;
         }
         if (c->de) {
-            ProductParams d = p;
-            d.b = ws + w.hidden; d.ldb = w.pitch;
+            ProductParams d = table_operands(w, ws);
+            common(d);
             d.m = n;
             d.out = static_cast<uint8_t *>(c->de) + v0 * c->ldde * s; d.ldc = c->ldde; d.out_group = c->de_stride;
             d.scale = scale; d.mean = !sum_only;
@@ -512,6 +537,27 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
             if (int rc = launch_status(launch_store(q, t, Layout::Weights, settle_tile(t, Layout::Weights, w.to_table.tile, d), d), what)) return rc;
         }
     }
+    return COCOD_OK;
+}
+
+int cocod_debug_cross_entropy_plan(const cocod_cross_entropy_call *c, cocod_product_plan out[4], uint32_t *pieces)
+{
+    if (!out || !pieces) return set_error(COCOD_ERR_INVALID, "out or pieces is NULL");
+    if (int rc = check(c)) return rc;
+    const Dtype t = kTypes[c->dtype];
+    const Workspace w = carve(c);
+    const uint8_t *ws = static_cast<const uint8_t *>(c->workspace);
+    const ProductParams z = logits_operands(c, w, ws), h = hidden_operands(c, w, ws, 0, static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab)),
+                        e = table_operands(w, ws);
+    auto plan = [&](Layout layout, const ProductPlan &planned, const ProductParams &p) {
+        return plan_as_run(t, layout, settle_tile(t, layout, planned.tile, p), planned.splits, p);
+    };
+    const cocod_product_plan none = {0, 0, 0};
+    out[0] = plan(Layout::Rows_NK, w.logits, z);
+    out[1] = (c->dh || c->de) && (w.pieces > 1 || !w.keep) ? plan(Layout::Rows_NK, w.slopes, z) : none;
+    out[2] = c->dh ? plan(Layout::Rows_KN, w.to_hidden, h) : none;
+    out[3] = c->de ? plan(Layout::Weights, w.to_table, e) : none;
+    *pieces = w.pieces;
     return COCOD_OK;
 }
 

@@ -156,60 +156,29 @@ int start(const cocod_grouped *g, Layout layout, ProductParams &p, ProductPlan &
     return COCOD_OK;
 }
 
-int run(void *stream, const cocod_grouped *g, Layout layout, const ProductParams &p, const ProductPlan &plan, const char *what)
+int prepare_forward(const cocod_grouped *g, ProductParams &p, ProductPlan &plan)
 {
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    const OnStreamDevice device(s);
-    if (device.status() != hipSuccess) return launch_status(device.status(), what);
-    return launch_status(launch_store(s, kTypes[g->dtype], layout, plan.tile, p), what);
-}
-
-}  // namespace
-}  // namespace cocod
-
-using namespace cocod;
-
-extern "C" {
-
-int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *bytes)
-{
-    if (!bytes) return set_error(COCOD_ERR_INVALID, "bytes is NULL");
-    if (int rc = check_shape(g)) return rc;
-    if (direction < COCOD_GROUPED_FORWARD || direction > COCOD_GROUPED_WEIGHT_GRAD) return set_error(COCOD_ERR_INVALID, "unknown direction %d", direction);
-    const Layout layout = direction == COCOD_GROUPED_FORWARD ? Layout::Rows_KN : direction == COCOD_GROUPED_INPUT_GRAD ? Layout::Rows_NK : Layout::Weights;
-    *bytes = workspace_of(g, layout, plan_of(g, layout, true));
-    return COCOD_OK;
-}
-
-int cocod_grouped_forward(void *stream, const cocod_grouped *g)
-{
-    if (int rc = check_shape(g)) return rc;
     const uint64_t s = dtype_bytes(kTypes[g->dtype]);
     if (int rc = check_matrix("x", g->x, g->inner, g->ldx, s, g->rows)) return rc;
     if (int rc = check_matrix("w", g->w, g->outer, g->ldw, s)) return rc;
     if (int rc = check_stride("w", g->w_stride, g->groups, g->inner, g->outer, g->ldw, true)) return rc;
     if (int rc = check_matrix("y", g->y, g->outer, g->ldy, s, g->rows)) return rc;
-    ProductParams p{};
     p.a = g->x; p.lda = g->ldx;
     p.b = g->w; p.ldb = g->ldw; p.b_group = g->groups > 1 ? g->w_stride : 0;
     p.n = g->outer; p.k = g->inner;
     p.out = g->y; p.ldc = g->ldy;
     p.relu = (g->flags & COCOD_GROUPED_RELU_OUT) != 0;
     const Extent in[] = {{"x", g->x, matrix_bytes(g->rows, g->inner, g->ldx, s)}, {"w", g->w, stack_bytes(g->groups, g->w_stride, g->inner, g->outer, g->ldw, s)}};
-    ProductPlan plan;
-    if (int rc = start(g, Layout::Rows_KN, p, plan, {"y", g->y, matrix_bytes(g->rows, g->outer, g->ldy, s)}, in, 2)) return rc;
-    return g->rows ? run(stream, g, Layout::Rows_KN, p, plan, "cocod_grouped_forward") : COCOD_OK;
+    return start(g, Layout::Rows_KN, p, plan, {"y", g->y, matrix_bytes(g->rows, g->outer, g->ldy, s)}, in, 2);
 }
 
-int cocod_grouped_input_grad(void *stream, const cocod_grouped *g)
+int prepare_input_grad(const cocod_grouped *g, ProductParams &p, ProductPlan &plan)
 {
-    if (int rc = check_shape(g)) return rc;
     const uint64_t s = dtype_bytes(kTypes[g->dtype]);
     if (int rc = check_matrix("dy", g->dy, g->outer, g->lddy, s, g->rows)) return rc;
     if (int rc = check_matrix("w", g->w, g->outer, g->ldw, s)) return rc;
     if (int rc = check_stride("w", g->w_stride, g->groups, g->inner, g->outer, g->ldw, true)) return rc;
     if (int rc = check_matrix("dx", g->dx, g->inner, g->lddx, s, g->rows)) return rc;
-    ProductParams p{};
     p.a = g->dy; p.lda = g->lddy;
     p.b = g->w; p.ldb = g->ldw; p.b_group = g->groups > 1 ? g->w_stride : 0;
     p.n = g->inner; p.k = g->outer;
@@ -226,18 +195,14 @@ int cocod_grouped_input_grad(void *stream, const cocod_grouped *g)
             in[2] = {"x_codes", g->x_codes, matrix_bytes(g->rows, g->inner, g->ld_codes, 1)};
         }
     }
-    ProductPlan plan;
-    if (int rc = start(g, Layout::Rows_NK, p, plan, {"dx", g->dx, matrix_bytes(g->rows, g->inner, g->lddx, s)}, in, 3)) return rc;
-    return g->rows ? run(stream, g, Layout::Rows_NK, p, plan, "cocod_grouped_input_grad") : COCOD_OK;
+    return start(g, Layout::Rows_NK, p, plan, {"dx", g->dx, matrix_bytes(g->rows, g->inner, g->lddx, s)}, in, 3);
 }
 
-int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g)
+int prepare_weight_grad(const cocod_grouped *g, ProductParams &p, ProductPlan &plan)
 {
-    if (int rc = check_shape(g)) return rc;
     const uint64_t s = dtype_bytes(kTypes[g->dtype]);
     if (g->dw_dtype != g->dtype && g->dw_dtype != COCOD_F32) return set_error(COCOD_ERR_INVALID, "dw_dtype must be the element type or COCOD_F32");
     const uint64_t so = dtype_bytes(kTypes[g->dw_dtype]);
-    ProductParams p{};
     Extent in[3];
     int n_in = 1;
     if (g->x) {
@@ -260,9 +225,66 @@ int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g)
     p.m = g->inner; p.n = g->outer;
     p.out = g->dw; p.ldc = g->lddw; p.out_group = g->dw_stride;
     p.out_f32 = g->dw_dtype == COCOD_F32;
+    return start(g, Layout::Weights, p, plan, {"dw", g->dw, stack_bytes(g->groups, g->dw_stride, g->inner, g->outer, g->lddw, so)}, in, n_in);
+}
+
+// Checks of a direction's arguments, its parameters and plan.
+int prepare(const cocod_grouped *g, Layout layout, ProductParams &p, ProductPlan &plan)
+{
+    if (int rc = check_shape(g)) return rc;
+    return layout == Layout::Rows_KN ? prepare_forward(g, p, plan) : layout == Layout::Rows_NK ? prepare_input_grad(g, p, plan) : prepare_weight_grad(g, p, plan);
+}
+
+int run(void *stream, const cocod_grouped *g, Layout layout, const char *what)
+{
+    ProductParams p{};
     ProductPlan plan;
-    if (int rc = start(g, Layout::Weights, p, plan, {"dw", g->dw, stack_bytes(g->groups, g->dw_stride, g->inner, g->outer, g->lddw, so)}, in, n_in)) return rc;
-    return run(stream, g, Layout::Weights, p, plan, "cocod_grouped_weight_grad");
+    if (int rc = prepare(g, layout, p, plan)) return rc;
+    if (!g->rows && layout != Layout::Weights) return COCOD_OK;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const OnStreamDevice device(s);
+    if (device.status() != hipSuccess) return launch_status(device.status(), what);
+    return launch_status(launch_store(s, kTypes[g->dtype], layout, plan.tile, p), what);
+}
+
+int layout_of(int direction, Layout &layout)
+{
+    if (direction < COCOD_GROUPED_FORWARD || direction > COCOD_GROUPED_WEIGHT_GRAD) return set_error(COCOD_ERR_INVALID, "unknown direction %d", direction);
+    layout = direction == COCOD_GROUPED_FORWARD ? Layout::Rows_KN : direction == COCOD_GROUPED_INPUT_GRAD ? Layout::Rows_NK : Layout::Weights;
+    return COCOD_OK;
+}
+
+}  // namespace
+}  // namespace cocod
+
+using namespace cocod;
+
+extern "C" {
+
+int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *bytes)
+{
+    if (!bytes) return set_error(COCOD_ERR_INVALID, "bytes is NULL");
+    if (int rc = check_shape(g)) return rc;
+    Layout layout;
+    if (int rc = layout_of(direction, layout)) return rc;
+    *bytes = workspace_of(g, layout, plan_of(g, layout, true));
+    return COCOD_OK;
+}
+
+int cocod_grouped_forward(void *stream, const cocod_grouped *g) { return run(stream, g, Layout::Rows_KN, "cocod_grouped_forward"); }
+int cocod_grouped_input_grad(void *stream, const cocod_grouped *g) { return run(stream, g, Layout::Rows_NK, "cocod_grouped_input_grad"); }
+int cocod_grouped_weight_grad(void *stream, const cocod_grouped *g) { return run(stream, g, Layout::Weights, "cocod_grouped_weight_grad"); }
+
+int cocod_debug_grouped_plan(const cocod_grouped *g, int direction, cocod_product_plan *out)
+{
+    if (!out) return set_error(COCOD_ERR_INVALID, "out is NULL");
+    Layout layout;
+    if (int rc = layout_of(direction, layout)) return rc;
+    ProductParams p{};
+    ProductPlan plan;
+    if (int rc = prepare(g, layout, p, plan)) return rc;
+    *out = plan_as_run(kTypes[g->dtype], layout, plan.tile, plan.splits, p);
+    return COCOD_OK;
 }
 
 }  // extern "C"

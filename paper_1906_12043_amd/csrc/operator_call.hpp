@@ -73,6 +73,13 @@ inline int check_dtype(uint32_t dtype)
     return dtype <= COCOD_F16 ? COCOD_OK : set_error(COCOD_ERR_INVALID, "unknown element type %u", dtype);
 }
 
+// What cocod_debug_*_plan says of a product that runs with these parameters.
+inline cocod_product_plan plan_as_run(Dtype type, Layout layout, Tile tile, uint32_t splits, const ProductParams &p)
+{
+    const bool direct_b_too = type != Dtype::F32 && direct_b(layout, p);
+    return {static_cast<uint32_t>(tile), splits, !p.a ? 2u : direct_b_too && direct_a(layout, p) ? 0u : 1u};
+}
+
 inline int launch_status(hipError_t e, const char *what)
 {
     if (e == hipSuccess) return COCOD_OK;
