@@ -119,14 +119,16 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const Rows p, 
     }
 }
 
-// The gathered rows by a launch of their own, a wave a row.
+// The gathered rows by a launch of their own, a wave a row (a block's waves take further rows where that would be more threads than a launch holds).
+constexpr uint32_t kMostGatherBlocks = 1u << 23;
 template <class E> __global__ __launch_bounds__(256) void gather_kernel(const Rows p, const uint32_t *index, const Hidden<E> hidden)
 {
-    const uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
     const uint32_t lane = threadIdx.x % 64;
-    if (r < clamped(p, 0) || r >= clamped(p, p.groups)) return;
-    if (index[r] != kNoRow) gather_row(hidden, r, index[r], lane);
-    if (!has_target(p, r)) clear_row(hidden, r, lane);
+    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64; r < p.rows; r += static_cast<uint64_t>(gridDim.x) * 4) {
+        if (r < clamped(p, 0) || r >= clamped(p, p.groups)) continue;
+        if (index[r] != kNoRow) gather_row(hidden, r, index[r], lane);
+        if (!has_target(p, r)) clear_row(hidden, r, lane);
+    }
 }
 
 // What a row's slopes need, from the column tiles' maxima and sums, and its loss, also in the place of the target's logit.  The target is not among
@@ -350,7 +352,8 @@ template <class E> hipError_t launch_gather(hipStream_t s, const Rows &rows, con
         hipLaunchKernelGGL((compact_kernel<E, true>), dim3(c->groups), dim3(kCompactThreads), 0, s, rows, index, target, ends, sum_only, scale, row_scale, hidden);
     } else {
         hipLaunchKernelGGL((compact_kernel<E, false>), dim3(c->groups), dim3(kCompactThreads), 0, s, rows, index, target, ends, sum_only, scale, row_scale, hidden);
-        hipLaunchKernelGGL(gather_kernel<E>, dim3(static_cast<uint32_t>((rows.rows + 3) / 4)), dim3(256), 0, s, rows, index, hidden);
+        const uint32_t blocks = static_cast<uint32_t>((rows.rows + 3) / 4);
+        hipLaunchKernelGGL(gather_kernel<E>, dim3(blocks < kMostGatherBlocks ? blocks : kMostGatherBlocks), dim3(256), 0, s, rows, index, hidden);
     }
     return hipGetLastError();
 }

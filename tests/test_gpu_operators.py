@@ -550,6 +550,29 @@ def test_loss_alone_of_few_rows(dtype, bounds, rows, dim, vocab, pad, total):
     assert float(gbuf[0, groups]) == oh.SENTINEL
 
 
+def test_loss_of_as_many_rows_as_are_allowed():
+    """2^26 - 1 rows: a wave a row would be 2^32 threads.  Two logits a row, exact in fp32: the loss is log1p(e^-x) of their difference x, below 8, to
+    the exponential's (x + 2) steps, one of the logarithm, and one of each rounding: 16 steps of the loss."""
+    rows, gen = (1 << 26) - 1, generator(31)
+    h = torch.zeros((rows, 8), dtype=torch.bfloat16, device="cuda")
+    h[:, 0] = (torch.randint(-64, 65, (rows,), generator=gen, device="cuda", dtype=torch.int32) / 16).to(torch.bfloat16)
+    e = torch.zeros((1, 2, 8), dtype=torch.bfloat16, device="cuda")
+    e[0, 0, 0], e[0, 1, 0] = 1.0, -1.0
+    target = torch.arange(rows, device="cuda", dtype=torch.int32) % 5 - 1            # -1, 0, 1 and two beside the vocabulary
+    loss, mean = torch.full((rows,), oh.SENTINEL, device="cuda"), torch.empty(1, device="cuda")
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call("bf16", [1, rows - 1], h, e, target, group_loss=mean, loss=loss))
+    assert float(loss[0]) == oh.SENTINEL and float(loss[-1]) == oh.SENTINEL
+    total, count = 0.0, 0
+    for part in torch.arange(1, rows - 1, device="cuda").split(1 << 23):
+        x = 2 * h[part, 0].double() * torch.where(target[part] == 0, 1.0, -1.0)
+        want = torch.log1p(torch.exp(-x.abs())) + torch.clamp(-x, min=0)
+        has = (target[part] == 0) | (target[part] == 1)
+        want = torch.where(has, want, torch.zeros_like(want))
+        close(loss[part], want, 16 * oh.STEP * want)
+        total, count = total + want.sum().item(), count + int(has.sum())
+    assert abs(mean.item() - total / count) <= 17 * oh.STEP * total / count
+
+
 def test_loss_gradient_against_differences():
     """(L(h + s d) - L(h - s d)) / 2 s against <dh, d>, and the same for the table.  L in fp32 is off by the bound r of each row's loss, here
     below 4e-6; at s = 2^-6 that is 2.6e-4 in the quotient; the cubic term is s^2 / 6 max |L'''| |d . e|^3, with |d . e| <= 1 and
