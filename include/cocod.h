@@ -401,7 +401,9 @@ int cocod_debug_copy(void *stream, const float *src, float *dst, uint64_t n);
  * pitch work.  16-bit operands that start on 16 bytes, with pitches, group strides and a summed axis that
  * are multiples of 8, are the fast ones; of such a row the whole 16-byte piece that holds its last
  * element is read.  Row-wise arrays may be NULL where rows is 0.  COCOD_ERR_UNSUPPORTED: the result has more tiles than one
- * launch holds (2^32 threads: 2^24 tiles of 128 x 128, or of 32 x 64 where groups have few rows, a tile begun per group counted).  Outputs must not overlap other arguments.  Sums are kept in fp32 (fp32 operands are multiplied
+ * launch holds (2^32 threads: 2^23 tiles of 128 x 128 or larger, 2^24 of 64 x 64 or of 32 x 64 where groups have few rows, a tile begun per
+ * group counted); a loss is then refused in the middle, with some of its outputs written.  Outputs must not overlap other arguments: arrays
+ * count from their first to their last element, so that one which lies in the gaps of another is refused, too.  Sums are kept in fp32 (fp32 operands are multiplied
  * at fp32 accuracy) and rounded once.
  */
 typedef enum cocod_dtype {
@@ -444,7 +446,7 @@ typedef struct cocod_grouped {
     uint64_t workspace_bytes;
 } cocod_grouped;
 
-/* Bytes of workspace with which the call of this direction splits its sums (0: it would not); reads the sizes only. */
+/* Bytes of workspace with which the call of this direction splits its sums (0: it would not); reads the sizes and checks the address of offsets, no other. */
 int cocod_grouped_workspace(const cocod_grouped *g, int direction, uint64_t *bytes);
 /* y_g = x_g w_g, through a relu with COCOD_GROUPED_RELU_OUT (a NaN stays one). */
 int cocod_grouped_forward(void *stream, const cocod_grouped *g);
