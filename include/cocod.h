@@ -402,7 +402,7 @@ int cocod_debug_copy(void *stream, const float *src, float *dst, uint64_t n);
  * are multiples of 8, are the fast ones; of such a row the whole 16-byte piece that holds its last
  * element is read.  Row-wise arrays may be NULL where rows is 0.  COCOD_ERR_UNSUPPORTED: the result has more tiles than one
  * launch holds (2^32 threads: 2^23 tiles of 128 x 128 or larger, 2^24 of 64 x 64 or of 32 x 64 where groups have few rows, a tile begun per
- * group counted); a loss is then refused in the middle, with some of its outputs written.  Outputs must not overlap other arguments: arrays
+ * group counted); nothing is then begun.  Outputs must not overlap other arguments: arrays
  * count from their first to their last element, so that one which lies in the gaps of another is refused, too.  Sums are kept in fp32 (fp32 operands are multiplied
  * at fp32 accuracy) and rounded once.
  */

@@ -384,6 +384,22 @@ ProductParams table_operands(const Workspace &w, const uint8_t *ws)
     return p;
 }
 
+// Every launch of the call holds its product, or nothing is begun.
+int check_launches(const cocod_cross_entropy_call *c, const Workspace &w, const uint8_t *ws, const char *what)
+{
+    const Dtype t = kTypes[c->dtype];
+    const uint32_t n = static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab);
+    auto fits = [&](Layout layout, const ProductPlan &plan, const ProductParams &p, uint32_t m, uint32_t cols, uint32_t splits) {
+        const TileSize size = tile_size(t, settle_tile(t, layout, plan.tile, p));
+        return fits_a_launch(size, blocks_of(size, layout == Layout::Weights, c->rows, c->groups, m, cols, splits));
+    };
+    const ProductParams z = logits_operands(c, w, ws);
+    const bool all = fits(Layout::Rows_NK, w.logits, z, 0, c->vocab, 1) && (!(c->dh || c->de) || fits(Layout::Rows_NK, w.slopes, z, 0, n, 1)) &&
+                     (!c->dh || fits(Layout::Rows_KN, w.to_hidden, hidden_operands(c, w, ws, 0, n), 0, c->dim, w.to_hidden.splits)) &&
+                     (!c->de || fits(Layout::Weights, w.to_table, table_operands(w, ws), n, c->dim, w.to_table.splits));
+    return all ? COCOD_OK : launch_status(hipErrorInvalidConfiguration, what);
+}
+
 }  // namespace
 }  // namespace cocod
 
@@ -435,6 +451,7 @@ int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c)
     const char *const what = "cocod_cross_entropy";
     if (device.status() != hipSuccess) return launch_status(device.status(), what);
     uint8_t *ws = static_cast<uint8_t *>(c->workspace);
+    if (int rc = check_launches(c, w, ws, what)) return rc;
     uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
     int64_t *ends = reinterpret_cast<int64_t *>(ws + w.ends);
     float *const top = reinterpret_cast<float *>(ws + w.top), *const inverse = reinterpret_cast<float *>(ws + w.inverse);

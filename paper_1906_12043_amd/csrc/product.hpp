@@ -80,10 +80,25 @@ hipError_t launch_logits_bf16(hipStream_t stream, Finish finish, Tile tile, cons
 hipError_t launch_logits_f16(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p);
 hipError_t launch_logits_f32(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p);
 
+// Rows, columns and threads of a tile as it runs (product_tiles.hpp asserts them), and whether a launch holds all tiles of a product.
+struct TileSize { uint32_t bm, bn, threads; };
+constexpr TileSize tile_size(Dtype type, Tile tile)
+{
+    return tile == Tile::Small ? TileSize{32, 64, 256} : tile == Tile::Square ? TileSize{64, 64, 256} : type == Dtype::F32 ? TileSize{128, 128, 512}
+           : tile == Tile::Large ? TileSize{256, 256, 512} : tile == Tile::Tall ? TileSize{192, 128, 512} : TileSize{128, 128, tile == Tile::Deep ? 512u : 256u};
+}
+inline uint64_t blocks_of(const TileSize &t, bool weights, uint64_t rows, uint32_t groups, uint32_t m, uint32_t n, uint32_t splits)
+{
+    // of the rows, a tile begun per group
+    const uint64_t row_tiles = weights ? static_cast<uint64_t>(groups) * ((m + t.bm - 1) / t.bm) : rows / t.bm + groups;
+    return row_tiles * ((n + t.bn - 1) / t.bn) * splits;
+}
+inline bool fits_a_launch(const TileSize &t, uint64_t blocks) { return blocks * t.threads < (1ull << 32); }
+
 // Columns of the tiles in which Finish::Stats forms its statistics (ProductParams::stats holds one row of them per column tile).
 inline uint32_t tile_cols(Dtype type, Tile tile)
 {
-    return tile == Tile::Small || tile == Tile::Square ? 64 : tile == Tile::Large && type != Dtype::F32 ? 256 : 128;
+    return tile_size(type, tile).bn;
 }
 
 // 16-bit operands that start on a 16-byte address, with rows of whole 16-byte pieces, go to LDS without passing through registers.

@@ -906,10 +906,9 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
 template <class T, Layout LAYOUT, class S, Finish FINISH, int HOW_A, int HOW_B>
 hipError_t launch_one(hipStream_t stream, const ProductParams &p)
 {
-    const uint64_t col_tiles = (p.n + S::BN - 1) / S::BN;
-    const uint64_t row_tiles = LAYOUT == Layout::Weights ? static_cast<uint64_t>(p.groups) * ((p.m + S::BM - 1) / S::BM) : p.rows / S::BM + p.groups;
-    const uint64_t blocks = row_tiles * col_tiles * p.splits;
-    if (blocks * S::threads >= (1ull << 32)) return hipErrorInvalidConfiguration;
+    constexpr TileSize size = {S::BM, S::BN, S::threads};
+    const uint64_t blocks = blocks_of(size, LAYOUT == Layout::Weights, p.rows, p.groups, p.m, p.n, p.splits);
+    if (!fits_a_launch(size, blocks)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((product_kernel<T, LAYOUT, S, FINISH, HOW_A, HOW_B>), dim3(static_cast<uint32_t>(blocks)), dim3(S::threads), 0, stream, p);
     return hipGetLastError();
 }
@@ -938,6 +937,16 @@ typedef TileShape<32, 64, 64, 1, 2, 2> Small32;
 // between these, three blocks on a compute unit: weight gradient of 4 groups of 250 rows, 512 x 768 13.7 us instead of 15.3 (medium) and 17.4 (small), of 2 of
 // 254, 512 x 5003 38 instead of 45 and 49; 2048 x 2048 x 2048 132 against 101 and 180
 typedef TileShape<64, 64, 32, 2, 2, 1> Square32;
+
+template <class S> constexpr bool is_size(Dtype type, Tile tile)
+{
+    const TileSize t = tile_size(type, tile);
+    return t.bm == S::BM && t.bn == S::BN && t.threads == S::threads;
+}
+static_assert(is_size<Large16>(Dtype::BF16, Tile::Large) && is_size<Large16Codes>(Dtype::BF16, Tile::Large) && is_size<Medium16>(Dtype::BF16, Tile::Medium) &&
+              is_size<Deep16>(Dtype::BF16, Tile::Deep) && is_size<Tall16>(Dtype::BF16, Tile::Tall) && is_size<Small16>(Dtype::BF16, Tile::Small) &&
+              is_size<Small16Direct>(Dtype::BF16, Tile::Small) && is_size<Medium32>(Dtype::F32, Tile::Medium) && is_size<Small32>(Dtype::F32, Tile::Small) &&
+              is_size<Square32>(Dtype::F32, Tile::Square), "tile_size");
 
 template <class T, Layout LAYOUT, Finish FINISH>
 hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)

@@ -176,3 +176,12 @@ def test_the_loss_knows_its_flags():
     for flags in (2, 8, both | 2, 1 << 31):
         refused(P.cross_entropy, None, loss_call(flags=flags), text="flag")
         refused(P.cross_entropy_workspace, loss_call(flags=flags), text="flag")
+
+
+@pytest.mark.parametrize("dtype, rows, vocab, more", [
+    (P.BF16, 1 << 22, 1 << 18, {}),                                       # 2^14 by 2^10 tiles of 256 x 256 for the logits
+    (P.F32, 1 << 20, 1 << 18, dict(dh=None, de=None)),                    # 2^13 by 2^11 tiles of 128 x 128
+    (P.BF16, 100, 1 << 30, dict(groups=16, de_stride=1 << 36, e_stride=0, dh=None, piece=1 << 30))])      # 2^24 row tiles of a table for each of 16 groups
+def test_losses_of_more_tiles_than_a_launch_are_refused_before_anything_is_begun(dtype, rows, vocab, more):
+    far = dict(e=1 << 44, targets=1 << 54, loss=1 << 55, h=1 << 56, dh=1 << 57, de=1 << 58, e_stride=0, groups=1, workspace=1 << 60, workspace_bytes=1 << 59)
+    refused(P.cross_entropy, None, loss_call(dtype=dtype, rows=rows, vocab=vocab, **{**far, **more}), status=P.ERR_UNSUPPORTED, text="tiles")
