@@ -8,7 +8,7 @@
 //
 // Bound by memory: s + 1 + 1/32 bytes per value in either direction; a thread takes eight values, four threads a scale.
 #include "operator_call.hpp"
-#include "product_tiles.hpp"
+#include "product_finish.hpp"
 
 namespace cocod {
 namespace {
@@ -24,8 +24,7 @@ struct CheckpointParams {
     uint64_t ldx;
     uint8_t *codes, *scales;
     uint64_t ld_codes, ld_scales;
-    uint64_t threads;                 // of the whole launch: a thread's chunks lie this far apart
-    uint64_t step_rows;               //   which is so many rows
+    uint64_t step_rows;               // a thread's chunks lie as far apart as the launch has threads, which is so many rows
     uint32_t step_chunks;             //   and so many chunks
 };
 
@@ -237,9 +236,9 @@ template <class T> hipError_t launch(hipStream_t stream, CheckpointParams p, boo
     const uint64_t chunks = p.rows * p.per_row, blocks = (chunks + kCheckpointThreads - 1) / kCheckpointThreads;
     constexpr uint64_t kMostBlocks = 1u << 20;
     const uint32_t grid = static_cast<uint32_t>(blocks < kMostBlocks ? blocks : kMostBlocks);
-    p.threads = static_cast<uint64_t>(grid) * kCheckpointThreads;
-    p.step_rows = p.threads / p.per_row;
-    p.step_chunks = static_cast<uint32_t>(p.threads % p.per_row);
+    const uint64_t threads = static_cast<uint64_t>(grid) * kCheckpointThreads;
+    p.step_rows = threads / p.per_row;
+    p.step_chunks = static_cast<uint32_t>(threads % p.per_row);
     if (load) hipLaunchKernelGGL(load_kernel<T>, dim3(grid), dim3(kCheckpointThreads), 0, stream, p);
     else      hipLaunchKernelGGL(store_kernel<T>, dim3(grid), dim3(kCheckpointThreads), 0, stream, p);
     return hipGetLastError();
