@@ -49,6 +49,8 @@ class _Call(C.Structure):
             if name not in types:
                 raise TypeError("%s has no field %s" % (type(self).__name__, name))
             setattr(self, name, _addr(value) if types[name] is C.c_void_p else value)
+            if types[name] in (C.c_uint32, C.c_uint64) and getattr(self, name) != value:
+                raise ValueError("%s.%s = %r does not fit the field" % (type(self).__name__, name, value))      # (the field would hold another number)
 
 
 class Grouped(_Call):

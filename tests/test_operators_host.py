@@ -185,3 +185,14 @@ def test_the_loss_knows_its_flags():
 def test_losses_of_more_tiles_than_a_launch_are_refused_before_anything_is_begun(dtype, rows, vocab, more):
     far = dict(e=1 << 44, targets=1 << 54, loss=1 << 55, h=1 << 56, dh=1 << 57, de=1 << 58, e_stride=0, groups=1, workspace=1 << 60, workspace_bytes=1 << 59)
     refused(P.cross_entropy, None, loss_call(dtype=dtype, rows=rows, vocab=vocab, **{**far, **more}), status=P.ERR_UNSUPPORTED, text="tiles")
+
+
+def test_numbers_that_a_field_cannot_hold_are_refused():
+    for field, value in (("inner", (1 << 32) + 64), ("outer", -1), ("groups", 1 << 32), ("rows", -1), ("rows", 1 << 64), ("ldx", (1 << 64) + 64)):
+        with pytest.raises(ValueError, match=field):
+            grouped(**{field: value})
+        with pytest.raises(ValueError, match=field):
+            grouped().set(**{field: value})
+    with pytest.raises(ValueError, match="vocab"):
+        loss_call(vocab=(1 << 32) + 1000)
+    assert grouped(rows=(1 << 64) - 1).rows == (1 << 64) - 1 and loss_call(grad_scale=0.1).grad_scale == pytest.approx(0.1)
