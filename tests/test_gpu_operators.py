@@ -747,6 +747,57 @@ def test_loss_behind_a_relu(dtype, case):
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][2], outs[1][2])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("each, dim, vocab, piece", [(9, 16, 600, 0), (9, 16, 600, 256), (10, 13, 600, 0), (160, 72, 2600, 0), (160, 72, 2600, 1024)])
+def test_logits_that_are_not_finite(dtype, each, dim, vocab, piece):
+    """Infinities and NaN in a group's table, at the target and beside it, alone and everywhere: loss and gradients are infinite or NaN where 64-bit
+    arithmetic by the definition has them so, and finite where it does not; a group without them keeps its values."""
+    inf, t, gen, f = float("inf"), oh.TYPES[dtype][1], generator(dim), torch.float64
+    tables = [{}, {5: inf}, {7: -inf, vocab - 1: -inf}, "all but 2", "all", {vocab - 2: float("nan")}, {}]
+    groups, rows = len(tables), len(tables) * each
+    bounds = [g * each for g in range(groups + 1)]
+    h, e = oh.matrix(rows, dim, 0, t, gen), oh.stack(groups, vocab, dim, 0, 0, t, gen, std=2.0 / dim ** 0.5)
+    h[:, 0], e[:, :, 0] = 1.0, 0.0
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    for g, special in enumerate(tables):
+        first = target[g * each:(g + 1) * each]
+        if special == "all but 2":
+            e[g, :, 0], e[g, 2, 0], first[0], first[1:] = -inf, 0.0, 2, 4
+            first[2:5] = 2
+        elif special == "all":
+            e[g, :, 0] = -inf
+        else:
+            for v, x in special.items():
+                e[g, v, 0] = x
+            first[:4] = torch.tensor([5, 7, vocab - 1, vocab - 2], dtype=torch.int32)
+    z = torch.cat([h[s].to(f) @ e[g].to(f).t() for g, s in oh.groups_of(bounds)])
+    at = torch.arange(rows, device="cuda")
+    want = -torch.log_softmax(z, 1)[at, target.long()]
+    dz = torch.softmax(z, 1)
+    dz[at, target.long()] -= 1
+    loss, dh, de = torch.empty(rows, device="cuda"), torch.empty_like(h), torch.empty_like(e)
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, dh, de, None, loss, piece=piece))
+    only = torch.empty(rows, device="cuda")
+    P.cross_entropy(torch.cuda.current_stream(), oh.cross_entropy_call(dtype, bounds, h, e, target, loss=only))
+    assert torch.equal(torch.isnan(loss), torch.isnan(want)) and torch.equal(torch.isposinf(loss), torch.isposinf(want)) and not bool(torch.isneginf(loss).any())
+    fine = torch.isfinite(want)
+    assert torch.equal(only[fine], loss[fine]) and torch.equal(torch.isnan(only), torch.isnan(want)) and torch.equal(torch.isposinf(only), torch.isposinf(want))
+    sure = 3 * each + torch.tensor([0, 2, 3, 4], device="cuda")
+    assert not bool(loss[sure].any()) and bool(torch.isposinf(loss[3 * each + 1]))          # the only possible entry: loss 0; an impossible one: infinite
+    magnitude = torch.cat([h[s].to(f).abs() @ torch.nan_to_num(e[g], nan=0.0, posinf=0.0, neginf=0.0).to(f).abs().t() for g, s in oh.groups_of(bounds)]).amax(1)
+    bound = 2 * ((dim + 8) * oh.STEP * magnitude + (300 + vocab / 64) * oh.STEP) + 2 * oh.STEP * want.abs()
+    close(loss[fine], want[fine], bound[fine])
+    for g, s in oh.groups_of(bounds):
+        for got, out in ((dh[s], dz[s] @ e[g].to(f)), (de[g], dz[s].t() @ h[s].to(f))):
+            got = got.to(f)
+            assert torch.equal(torch.isnan(got), torch.isnan(out)) and torch.equal(torch.isinf(got), torch.isinf(out)), g
+            assert torch.equal(got[torch.isinf(got)], out[torch.isinf(out)]), g
+    calm = oh.exact_loss(bounds[:2], h[:each], e[:1], target[:each])
+    near = oh.loss_bounds(calm, t, dim, vocab)
+    close(dh[:each], calm["dh"], near["dh"])
+    close(de[:1], calm["de"], near["de"])
+
+
 # ---- together ------------------------------------------------------------------------------------------------
 
 def readme_example():
