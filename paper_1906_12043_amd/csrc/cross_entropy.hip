@@ -384,7 +384,7 @@ ProductParams table_operands(const Workspace &w, const uint8_t *ws)
     return p;
 }
 
-// Every launch of the call holds its product, or nothing is begun.
+// Every launch that the call makes holds its product, or nothing is begun.
 int check_launches(const cocod_cross_entropy_call *c, const Workspace &w, const uint8_t *ws, const char *what)
 {
     const Dtype t = kTypes[c->dtype];
@@ -394,8 +394,11 @@ int check_launches(const cocod_cross_entropy_call *c, const Workspace &w, const 
         return fits_a_launch(size, blocks_of(size, layout == Layout::Weights, c->rows, c->groups, m, cols, splits));
     };
     const ProductParams z = logits_operands(c, w, ws);
-    const bool all = fits(Layout::Rows_NK, w.logits, z, 0, c->vocab, 1) && (!(c->dh || c->de) || fits(Layout::Rows_NK, w.slopes, z, 0, n, 1)) &&
-                     (!c->dh || fits(Layout::Rows_KN, w.to_hidden, hidden_operands(c, w, ws, 0, n), 0, c->dim, w.to_hidden.splits)) &&
+    const bool rows = c->rows != 0, formed_again = (c->dh || c->de) && (w.pieces > 1 || !w.keep);
+    const uint32_t kept = w.keep ? static_cast<uint32_t>(c->vocab - (w.pieces - 1) * w.piece) : 0;      // columns of a launch of their own
+    const bool all = (!rows || (fits(Layout::Rows_NK, w.logits, z, 0, c->vocab - kept, 1) && fits(Layout::Rows_NK, w.logits, z, 0, kept, 1))) &&
+                     (!rows || !formed_again || fits(Layout::Rows_NK, w.slopes, z, 0, n, 1)) &&
+                     (!rows || !c->dh || fits(Layout::Rows_KN, w.to_hidden, hidden_operands(c, w, ws, 0, n), 0, c->dim, w.to_hidden.splits)) &&
                      (!c->de || fits(Layout::Weights, w.to_table, table_operands(w, ws), n, c->dim, w.to_table.splits));
     return all ? COCOD_OK : launch_status(hipErrorInvalidConfiguration, what);
 }

@@ -573,6 +573,19 @@ def test_loss_of_as_many_rows_as_are_allowed():
     assert abs(mean.item() - total / count) <= 17 * oh.STEP * total / count
 
 
+def test_loss_without_rows_of_groups_whose_tiles_no_launch_would_hold():
+    """65535 groups by 200000 entries would be 2^27 tiles at the least, a tile begun per group; without rows there is no such product."""
+    groups, vocab, dim = 65535, 200000, 8
+    e = torch.zeros((1, vocab, dim), dtype=torch.bfloat16, device="cuda").expand(groups, vocab, dim)
+    mean = torch.full((groups,), oh.SENTINEL, device="cuda")
+    empty = torch.empty((0, dim), dtype=torch.bfloat16, device="cuda")
+    call = oh.cross_entropy_call("bf16", [0] * (groups + 1), empty, e, torch.empty(0, dtype=torch.int32, device="cuda"), group_loss=mean, loss=torch.empty(0, device="cuda"))
+    P.cross_entropy(torch.cuda.current_stream(), call)
+    call.set(dh=torch.empty(16, dtype=torch.bfloat16, device="cuda"), lddh=dim)
+    P.cross_entropy(torch.cuda.current_stream(), call)
+    assert not bool(mean.any())
+
+
 def test_loss_gradient_against_differences():
     """(L(h + s d) - L(h - s d)) / 2 s against <dh, d>, and the same for the table.  L in fp32 is off by the bound r of each row's loss, here
     below 4e-6; at s = 2^-6 that is 2.6e-4 in the quotient; the cubic term is s^2 / 6 max |L'''| |d . e|^3, with |d . e| <= 1 and
