@@ -509,6 +509,118 @@ int cocod_checkpoint_load(void *stream, int dtype, uint64_t rows, uint64_t cols,
                           const uint8_t *scales, uint64_t ld_scales, void *x, uint64_t ldx);
 
 /*
+ * Tokens (rows of x) to the rows of the groups that own them, the ragged batches of the calls above, and back.  Every token has `choices`
+ * choices of a group; pair (t, j) is token t's j-th.  cocod_route_sort gives every pair a row: pairs in the order of group, token and choice.
+ * A pair whose choice is not in 0 .. groups - 1 has no row, nor has one that finds `capacity` pairs of its group in front of it: place is
+ * -1, the pair takes no part, nothing of its weight is used and its dweights is 0.  A token may choose a group more than once.  The other
+ * calls read place (entries outside 0 .. tokens * choices - 1 count as -1) and so also serve a caller who sorts by other means; rows that
+ * no pair has are neither read nor written.  Two pairs with one row: no access leaves the arrays, but the results are undefined.
+ * Sums are kept in fp32, over the choices in their order, and rounded once.
+ */
+typedef struct cocod_route {
+    uint32_t struct_size;           /* sizeof(cocod_route); checked */
+    uint32_t dtype;                 /* cocod_dtype of x, xs, ys, y, dy, dys, dxs, dx (cocod_route_sort does not read it) */
+    uint32_t groups;                /* 1 .. 65535 */
+    uint32_t choices;               /* 1 .. 64 */
+    uint64_t tokens;                /* tokens * choices < 2^31; 0 is legal */
+    uint64_t capacity;              /* rows that a group takes at most; 0: as many as come (the calls but cocod_route_sort do not read it) */
+    uint32_t width;                 /* columns of the rows, 1 .. 2^30 (cocod_route_sort does not read it) */
+    uint32_t flags;                 /* 0 */
+    const int32_t *experts; uint64_t ld_experts;   /* [tokens][choices] groups chosen */
+    int32_t *place;  uint64_t ld_place;     /* [tokens][choices] written by cocod_route_sort, read by the others */
+    int64_t *offsets;               /* [groups + 1], 8-byte aligned, written by cocod_route_sort */
+    const float *weights; uint64_t ld_weights;     /* [tokens][choices]; NULL: 1 */
+    const void *x;   uint64_t ldx;          /* [tokens][width] */
+    void *xs;        uint64_t ldxs;         /* [tokens * choices][width], as the other row-wise arrays of the groups: ys, dys, dxs */
+    const void *ys;  uint64_t ldys;
+    void *y;         uint64_t ldy;          /* [tokens][width] */
+    const void *dy;  uint64_t lddy;         /* [tokens][width] gradient at y */
+    void *dys;       uint64_t lddys;        /* gradient at ys; NULL: not wanted */
+    float *dweights; uint64_t ld_dweights;  /* [tokens][choices] gradient at weights; NULL: not wanted, ys is not read */
+    const void *dxs; uint64_t lddxs;        /* gradient at xs */
+    void *dx;        uint64_t lddx;         /* [tokens][width] gradient at x */
+    void *workspace;                /* cocod_route_sort: device, 16-byte aligned; may be NULL where none is needed */
+    uint64_t workspace_bytes;
+} cocod_route;
+
+/* Bytes of workspace that cocod_route_sort needs (0 for small batches); reads tokens, choices and groups. */
+int cocod_route_workspace(const cocod_route *r, uint64_t *bytes);
+/* place and offsets from experts. */
+int cocod_route_sort(void *stream, const cocod_route *r);
+/* xs[place[t][j]] = x[t] */
+int cocod_route_dispatch(void *stream, const cocod_route *r);
+/* dx[t] = sum over j of dxs[place[t][j]] */
+int cocod_route_dispatch_grad(void *stream, const cocod_route *r);
+/* y[t] = sum over j of weights[t][j] * ys[place[t][j]] */
+int cocod_route_combine(void *stream, const cocod_route *r);
+/* dys[place[t][j]] = weights[t][j] * dy[t],  dweights[t][j] = <dy[t], ys[place[t][j]]> */
+int cocod_route_combine_grad(void *stream, const cocod_route *r);
+
+enum {
+    COCOD_ADAMW_STATE_F32 = 0,      /* m and v as fp32 */
+    COCOD_ADAMW_STATE_8BIT = 1      /* m and the square root of v as 8-bit codes with a scale for every 32 */
+};
+
+/* What changes from step to step. */
+typedef struct cocod_adamw_now {
+    float lr, grad_scale;
+    float bias1, bias2;             /* 1 - beta1^step, 1 - beta2^step */
+    uint32_t seed;
+    uint32_t skip;                  /* not 0: the step leaves everything as it is (gradients that overflowed) */
+    uint32_t reserved[2];
+} cocod_adamw_now;
+
+/*
+ * A tensor of worker 0; worker i's arrays lie i * stride elements behind (scales: i * stride / 32).  8-bit states: 32 consecutive elements
+ * of the tensor share a scale, its last ones may be fewer; m_scales and v_scales hold ceil(n / 32).  All zero codes and scales are zero states.
+ */
+typedef struct cocod_adamw_tensor {
+    uint64_t n;                     /* elements, up to 2^40; 0: nothing is done */
+    void *p;                        /* parameters, in place */
+    const void *g;                  /* gradient */
+    void *m, *v;                    /* states, in place: float, or uint8_t codes */
+    uint8_t *m_scales, *v_scales;
+    void *copy;                     /* NULL, or the new parameters once more, rounded to copy_dtype (dtype COCOD_F32 only) */
+    float weight_decay;
+    float lr_scale;                 /* the tensor's learning rate is lr * lr_scale */
+} cocod_adamw_tensor;
+
+/*
+ * One AdamW step of all workers:  g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ * p = p (1 - lr weight_decay) - lr (m / bias1) / (sqrt(v / bias2) + eps).  p, m and v go through fp32; p (and copy) are rounded to nearest.
+ * It stands in the place of cocod_external_step for callers whose local step is AdamW: on the live model of an idle context, with
+ * cocod_average_apply_fused after k of them.
+ *
+ * 8-bit states are kept as cocod_checkpoint_store keeps activations (cocod_checkpoint_load with one row of n columns, fp32, reads m, and the root of v; the
+ * smallest scale is 2^-117 for m, 2^-51 for the root), but rounded up or down by chance, so that the stored m and the square of
+ * the stored root are the new m and v in the mean: by 16 random bits each that depend on (seed, number of the tensor, worker,
+ * element) alone.  The caller gives every step another seed.  A root that is not zero is not stored as zero.  The new p comes from
+ * m and v before they are rounded.  A state that is not finite is stored as NaN and does not count for the scale.
+ * Arrays may begin at any element.  The arrays of a call must not overlap each other; within a tensor and a worker that is checked.
+ */
+typedef struct cocod_adamw_call {
+    uint32_t struct_size;           /* sizeof(cocod_adamw_call); checked */
+    uint32_t dtype, grad_dtype, copy_dtype;       /* cocod_dtype of p, g, copy */
+    uint32_t state;                 /* COCOD_ADAMW_STATE_* */
+    uint32_t flags;                 /* 0 */
+    uint32_t workers;               /* 1 .. 65535 */
+    uint32_t seed;
+    uint64_t stride;                /* elements from worker to worker, of all arrays; a multiple of 32 for 8-bit states; not read with one worker */
+    const cocod_adamw_tensor *tensors;            /* HOST memory, read during the call (a captured call keeps what it says) */
+    uint64_t count;                 /* of tensors, up to 2^20 */
+    float lr, beta1, beta2, eps;    /* betas in 0 .. 1, 1 excluded; eps >= 0 */
+    float grad_scale;               /* gradients are multiplied by it */
+    uint32_t reserved;
+    uint64_t step;                  /* the number of this step, from 1 */
+    const cocod_adamw_now *now;     /* device, 4-byte aligned; not NULL: read by the kernels in place of lr, grad_scale, step and seed, for steps
+                                       that are replayed from a graph or decided on the device */
+} cocod_adamw_call;
+
+/* Fills *now (host memory) from lr, grad_scale, betas, step and seed of the call. */
+int cocod_adamw_now_of(const cocod_adamw_call *c, cocod_adamw_now *now);
+int cocod_adamw(void *stream, const cocod_adamw_call *c);
+
+/*
  * For tests: how the products of a call would run.  Makes no GPU call and reads no memory that the description points to.  Of the loss: the logits'
  * statistics, the slopes, the gradients of the hidden states and of the table (splits 0: no such product).
  */

@@ -8,6 +8,8 @@ from .binding import (  # noqa: F401
     cocod_create, cocod_destroy, cocod_local_steps, cocod_average_begin, cocod_average_end_apply,
     Grouped, CrossEntropy, grouped_workspace, grouped_forward, grouped_input_grad, grouped_weight_grad,
     cross_entropy_workspace, cross_entropy, checkpoint_store, checkpoint_load,
+    Route, route_workspace, route_sort, route_dispatch, route_dispatch_grad, route_combine, route_combine_grad,
+    AdamW, AdamWTensor, AdamWNow, adamw_now, adamw, ADAMW_STATE_F32, ADAMW_STATE_8BIT,
     debug_grouped_plan, debug_cross_entropy_plan,
     F32, BF16, F16, GROUPED_RELU_OUT, GROUPED_RELU_IN, GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD, CROSS_ENTROPY_SUM, CROSS_ENTROPY_RELU_IN,
     GRAD_QUADRATIC, GRAD_MLP, GRAD_EXTERNAL, SCHED_OVERLAP, SCHED_SERIAL, SCHED_FUSED, SCHED_HEAD, FLAG_DRY_RUN,

@@ -17,6 +17,7 @@ F32, BF16, F16 = 0, 1, 2
 GROUPED_RELU_OUT, GROUPED_RELU_IN = 1, 2
 GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD = 0, 1, 2
 CROSS_ENTROPY_SUM, CROSS_ENTROPY_RELU_IN = 1, 4
+ADAMW_STATE_F32, ADAMW_STATE_8BIT = 0, 1
 
 
 class Config(C.Structure):
@@ -80,6 +81,61 @@ class CrossEntropy(_Call):
 
     def __init__(self, **fields):
         super().__init__(**{"grad_scale": 1.0, **fields})
+
+
+class Route(_Call):
+    """Mirror of struct cocod_route.  It holds addresses only: the tensors are the caller's to keep."""
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("groups", C.c_uint32), ("choices", C.c_uint32),
+        ("tokens", C.c_uint64), ("capacity", C.c_uint64), ("width", C.c_uint32), ("flags", C.c_uint32),
+        ("experts", C.c_void_p), ("ld_experts", C.c_uint64), ("place", C.c_void_p), ("ld_place", C.c_uint64), ("offsets", C.c_void_p),
+        ("weights", C.c_void_p), ("ld_weights", C.c_uint64), ("x", C.c_void_p), ("ldx", C.c_uint64), ("xs", C.c_void_p), ("ldxs", C.c_uint64),
+        ("ys", C.c_void_p), ("ldys", C.c_uint64), ("y", C.c_void_p), ("ldy", C.c_uint64), ("dy", C.c_void_p), ("lddy", C.c_uint64),
+        ("dys", C.c_void_p), ("lddys", C.c_uint64), ("dweights", C.c_void_p), ("ld_dweights", C.c_uint64),
+        ("dxs", C.c_void_p), ("lddxs", C.c_uint64), ("dx", C.c_void_p), ("lddx", C.c_uint64),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class AdamWNow(C.Structure):
+    """Mirror of struct cocod_adamw_now."""
+    _fields_ = [("lr", C.c_float), ("grad_scale", C.c_float), ("bias1", C.c_float), ("bias2", C.c_float), ("seed", C.c_uint32), ("skip", C.c_uint32),
+                ("reserved", C.c_uint32 * 2)]
+
+
+class AdamWTensor(C.Structure):
+    """Mirror of struct cocod_adamw_tensor."""
+    _fields_ = [("n", C.c_uint64), ("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scales", C.c_void_p),
+                ("v_scales", C.c_void_p), ("copy", C.c_void_p), ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
+
+
+class AdamW(_Call):
+    """Mirror of struct cocod_adamw_call (grad_scale 1 and one worker unless given).  `tensors`: a sequence of dicts with the fields of
+    AdamWTensor (lr_scale 1 and weight_decay 0 unless given); it holds their addresses only, in an array of its own."""
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("copy_dtype", C.c_uint32),
+        ("state", C.c_uint32), ("flags", C.c_uint32), ("workers", C.c_uint32), ("seed", C.c_uint32), ("stride", C.c_uint64),
+        ("tensors", C.POINTER(AdamWTensor)), ("count", C.c_uint64),
+        ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("grad_scale", C.c_float), ("reserved", C.c_uint32),
+        ("step", C.c_uint64), ("now", C.c_void_p),
+    ]
+
+    def __init__(self, tensors=(), **fields):
+        super().__init__(**{"grad_scale": 1.0, "workers": 1, **fields})
+        self.set_tensors(tensors)
+
+    def set_tensors(self, tensors):
+        tensors = list(tensors)
+        array = (AdamWTensor * max(1, len(tensors)))()
+        types = dict(AdamWTensor._fields_)
+        for one, fields in zip(array, tensors):
+            for name, value in {"weight_decay": 0.0, "lr_scale": 1.0, **fields}.items():
+                if name not in types:
+                    raise TypeError("AdamWTensor has no field %s" % name)
+                setattr(one, name, _addr(value) if types[name] is C.c_void_p else value)
+                if types[name] is C.c_uint64 and getattr(one, name) != value:
+                    raise ValueError("AdamWTensor.%s = %r does not fit the field" % (name, value))
+        self.tensors, self.count = array, len(tensors)
 
 
 class ProductPlan(C.Structure):
@@ -149,6 +205,14 @@ def lib():
             "cocod_debug_cross_entropy_plan": ([P(CrossEntropy), P(ProductPlan), P(u32)], i32),
             "cocod_checkpoint_store": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_checkpoint_load": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
+            "cocod_route_workspace": ([P(Route), P(u64)], i32),
+            "cocod_route_sort": ([vp, P(Route)], i32),
+            "cocod_route_dispatch": ([vp, P(Route)], i32),
+            "cocod_route_dispatch_grad": ([vp, P(Route)], i32),
+            "cocod_route_combine": ([vp, P(Route)], i32),
+            "cocod_route_combine_grad": ([vp, P(Route)], i32),
+            "cocod_adamw_now_of": ([P(AdamW), P(AdamWNow)], i32),
+            "cocod_adamw": ([vp, P(AdamW)], i32),
             "cocod_debug_copy": ([vp, vp, vp, u64], i32),
             "cocod_debug_normals": ([vp, u64, u32, u32, u32, u64, u64, i32, vp], i32),
         }
@@ -248,6 +312,44 @@ def checkpoint_store(stream, dtype, rows, cols, x, ldx, codes, ld_codes, scales,
 
 def checkpoint_load(stream, dtype, rows, cols, codes, ld_codes, scales, ld_scales, x, ldx):
     return _check(lib().cocod_checkpoint_load(_addr(stream), dtype, rows, cols, _addr(codes), ld_codes, _addr(scales), ld_scales, _addr(x), ldx))
+
+
+def route_workspace(call):
+    """Bytes of workspace that route_sort(stream, call) needs."""
+    out = C.c_uint64()
+    _check(lib().cocod_route_workspace(C.byref(call), C.byref(out)))
+    return out.value
+
+
+def route_sort(stream, call):
+    return _check(lib().cocod_route_sort(_addr(stream), C.byref(call)))
+
+
+def route_dispatch(stream, call):
+    return _check(lib().cocod_route_dispatch(_addr(stream), C.byref(call)))
+
+
+def route_dispatch_grad(stream, call):
+    return _check(lib().cocod_route_dispatch_grad(_addr(stream), C.byref(call)))
+
+
+def route_combine(stream, call):
+    return _check(lib().cocod_route_combine(_addr(stream), C.byref(call)))
+
+
+def route_combine_grad(stream, call):
+    return _check(lib().cocod_route_combine_grad(_addr(stream), C.byref(call)))
+
+
+def adamw_now(call):
+    """AdamWNow of the call's lr, grad_scale, betas, step and seed: the bytes that `now` points to on the device."""
+    out = AdamWNow()
+    _check(lib().cocod_adamw_now_of(C.byref(call), C.byref(out)))
+    return out
+
+
+def adamw(stream, call):
+    return _check(lib().cocod_adamw(_addr(stream), C.byref(call)))
 
 
 # ---- the five entry points of the round, by their C names -----------------------------------
