@@ -494,6 +494,58 @@ typedef struct cocod_cross_entropy_call {
 int cocod_cross_entropy_workspace(const cocod_cross_entropy_call *c, uint64_t *bytes);
 int cocod_cross_entropy(void *stream, const cocod_cross_entropy_call *c);
 
+enum {
+    COCOD_TOKEN_SCORES_RELU_IN = 1u         /* h is the output of a relu: dh is taken through it (zero where h is not above zero) */
+};
+enum { COCOD_TOKEN_SCORES_FORWARD = 0, COCOD_TOKEN_SCORES_GRAD = 1 };
+
+/*
+ * Log probabilities of given tokens, entropies and the most probable alternatives, with logits z = scale * h_g e_g^T over a vocabulary that are not kept:
+ *   logp[r] = log softmax(z_r)[targets[r]],  entropy[r] = - sum over v of p_rv log p_rv  (an entry with p = 0 counts as 0),
+ *   top_ids[r][j], top_logp[r][j]: the entry with the j-th largest logit (of equal ones the lowest index first) and its log probability; -1 and minus
+ *   infinity behind the last entry of a vocabulary with fewer.
+ * targets NULL: every row takes part, without logp.  Otherwise a row whose target is not in 0 .. vocab - 1 takes no part: its logp and entropy
+ * are 0, its alternatives -1 and minus infinity, its row of dh is 0, and nothing of its h is used.  Entries whose logits differ by less than the roundings of their
+ * sums may change places, and the log probability of an alternative may differ from logp of the same entry by as much.  A NaN logit counts as minus
+ * infinity among the alternatives, and makes the log probabilities and the entropy of its row NaN.
+ *
+ * The gradient is that of sum over r of d_logp[r] logp[r] + d_entropy[r] entropy[r]; the call reads norms as the forward call of the same h, e, scale and targets left
+ * them (and offsets, h, e, targets, scale).  A row where both slopes are 0 takes no part.  16-bit types: the slopes at the logits are rounded to the type before the products
+ * (bf16: by up to 2^-8 of themselves, fp16: 2^-11, not below 2^-38 of the group's largest |d_logp| + 32 |d_entropy|), so an entry of dh or de is off by
+ * up to that part of the sum of its products' magnitudes, beside its own rounding.  COCOD_F32 keeps them in fp32.  A group without rows that take part has gradient 0.
+ */
+typedef struct cocod_token_scores_call {
+    uint32_t struct_size;           /* sizeof(cocod_token_scores_call); checked */
+    uint32_t dtype;                 /* cocod_dtype of h, e, dh, de */
+    uint32_t groups;                /* 1 .. 65535 */
+    uint32_t flags;                 /* COCOD_TOKEN_SCORES_* */
+    uint64_t rows;                  /* < 2^26; 0 is legal */
+    uint32_t dim, vocab;            /* 1 .. 2^30 */
+    const int64_t *offsets;         /* device, [groups + 1], 8-byte aligned */
+    const void *h;   uint64_t ldh;              /* [rows][dim] hidden states */
+    const void *e;   uint64_t lde, e_stride;    /* [groups][vocab][dim]; e_stride 0: one table for all groups */
+    const int32_t *targets;         /* device, [rows]; may be NULL */
+    float scale;                    /* of the logits (1 / temperature), finite, > 0 */
+    uint32_t top;                   /* alternatives of a row, 0 .. 32 */
+    float *logp, *entropy;          /* device, [rows]; NULL: not wanted */
+    int32_t *top_ids;               /* device, [rows][top] */
+    float *top_logp;                /* device, [rows][top] */
+    uint64_t ld_top;                /* of both */
+    float *norms;                   /* device, [rows][4], 16-byte aligned: written forward (NULL: not wanted), read by the gradient */
+    const float *d_logp, *d_entropy;            /* device, [rows]; NULL: 0 */
+    void *dh;        uint64_t lddh;             /* [rows][dim]; NULL: not wanted */
+    void *de;        uint64_t ldde, de_stride;  /* [groups][vocab][dim], a table of its own for every group; NULL: not wanted */
+    uint32_t piece;                 /* gradient: vocabulary entries whose slopes are in memory at a time, as in cocod_cross_entropy_call */
+    uint32_t reserved;
+    void *workspace;                /* device, 256-byte aligned */
+    uint64_t workspace_bytes;
+} cocod_token_scores_call;
+
+/* Bytes of workspace that the call of this direction needs (with alternatives: rows * vocab bytes, and a little); reads the sizes, top, piece, and whether dh and de are NULL. */
+int cocod_token_scores_workspace(const cocod_token_scores_call *c, int direction, uint64_t *bytes);
+int cocod_token_scores(void *stream, const cocod_token_scores_call *c);
+int cocod_token_scores_grad(void *stream, const cocod_token_scores_call *c);
+
 /*
  * Activations in 8 bits from the forward to the backward pass.  32 consecutive values of a row (the last ones of a
  * row may be fewer) share a scale 2^e, stored as e + 127: the smallest power of two, not below 2^-117 (COCOD_F16: 2^-15), for

@@ -8,6 +8,7 @@ from .binding import (  # noqa: F401
     cocod_create, cocod_destroy, cocod_local_steps, cocod_average_begin, cocod_average_end_apply,
     Grouped, CrossEntropy, grouped_workspace, grouped_forward, grouped_input_grad, grouped_weight_grad,
     cross_entropy_workspace, cross_entropy, checkpoint_store, checkpoint_load,
+    TokenScores, token_scores_workspace, token_scores, token_scores_grad, TOKEN_SCORES_RELU_IN, TOKEN_SCORES_FORWARD, TOKEN_SCORES_GRAD,
     Route, route_workspace, route_sort, route_dispatch, route_dispatch_grad, route_combine, route_combine_grad,
     AdamW, AdamWTensor, AdamWNow, adamw_now, adamw, ADAMW_STATE_F32, ADAMW_STATE_8BIT,
     debug_grouped_plan, debug_cross_entropy_plan,

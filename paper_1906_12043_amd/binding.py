@@ -17,6 +17,8 @@ F32, BF16, F16 = 0, 1, 2
 GROUPED_RELU_OUT, GROUPED_RELU_IN = 1, 2
 GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD = 0, 1, 2
 CROSS_ENTROPY_SUM, CROSS_ENTROPY_RELU_IN = 1, 4
+TOKEN_SCORES_RELU_IN = 1
+TOKEN_SCORES_FORWARD, TOKEN_SCORES_GRAD = 0, 1
 ADAMW_STATE_F32, ADAMW_STATE_8BIT = 0, 1
 
 
@@ -81,6 +83,22 @@ class CrossEntropy(_Call):
 
     def __init__(self, **fields):
         super().__init__(**{"grad_scale": 1.0, **fields})
+
+
+class TokenScores(_Call):
+    """Mirror of struct cocod_token_scores_call (scale 1 unless given)."""
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("groups", C.c_uint32), ("flags", C.c_uint32),
+        ("rows", C.c_uint64), ("dim", C.c_uint32), ("vocab", C.c_uint32), ("offsets", C.c_void_p),
+        ("h", C.c_void_p), ("ldh", C.c_uint64), ("e", C.c_void_p), ("lde", C.c_uint64), ("e_stride", C.c_uint64), ("targets", C.c_void_p),
+        ("scale", C.c_float), ("top", C.c_uint32), ("logp", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p), ("top_logp", C.c_void_p),
+        ("ld_top", C.c_uint64), ("norms", C.c_void_p), ("d_logp", C.c_void_p), ("d_entropy", C.c_void_p),
+        ("dh", C.c_void_p), ("lddh", C.c_uint64), ("de", C.c_void_p), ("ldde", C.c_uint64), ("de_stride", C.c_uint64),
+        ("piece", C.c_uint32), ("reserved", C.c_uint32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+    def __init__(self, **fields):
+        super().__init__(**{"scale": 1.0, **fields})
 
 
 class Route(_Call):
@@ -205,6 +223,9 @@ def lib():
             "cocod_debug_cross_entropy_plan": ([P(CrossEntropy), P(ProductPlan), P(u32)], i32),
             "cocod_checkpoint_store": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_checkpoint_load": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
+            "cocod_token_scores_workspace": ([P(TokenScores), i32, P(u64)], i32),
+            "cocod_token_scores": ([vp, P(TokenScores)], i32),
+            "cocod_token_scores_grad": ([vp, P(TokenScores)], i32),
             "cocod_route_workspace": ([P(Route), P(u64)], i32),
             "cocod_route_sort": ([vp, P(Route)], i32),
             "cocod_route_dispatch": ([vp, P(Route)], i32),
@@ -312,6 +333,21 @@ def checkpoint_store(stream, dtype, rows, cols, x, ldx, codes, ld_codes, scales,
 
 def checkpoint_load(stream, dtype, rows, cols, codes, ld_codes, scales, ld_scales, x, ldx):
     return _check(lib().cocod_checkpoint_load(_addr(stream), dtype, rows, cols, _addr(codes), ld_codes, _addr(scales), ld_scales, _addr(x), ldx))
+
+
+def token_scores_workspace(call, direction):
+    """Bytes of workspace that token_scores or token_scores_grad (direction) needs."""
+    out = C.c_uint64()
+    _check(lib().cocod_token_scores_workspace(C.byref(call), direction, C.byref(out)))
+    return out.value
+
+
+def token_scores(stream, call):
+    return _check(lib().cocod_token_scores(_addr(stream), C.byref(call)))
+
+
+def token_scores_grad(stream, call):
+    return _check(lib().cocod_token_scores_grad(_addr(stream), C.byref(call)))
 
 
 def route_workspace(call):

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcocod.so")
 SOURCES = ["api.hip", "local_step.hip", "averaging.hip", "fill.hip", "mlp.hip", "grouped.hip", "cross_entropy.hip", "checkpoint.hip",
-           "route.hip", "adamw.hip",
+           "route.hip", "token_scores.hip", "adamw.hip",
            "product_bf16.hip", "product_f16.hip", "product_f32.hip", "logits_bf16.hip", "logits_f16.hip", "logits_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for all device code (scalar fp32 only)

@@ -15,36 +15,14 @@
 // that part of its sum of MAGNITUDES, beside its own last rounding.  Far from a minimum that is hidden by the last rounding; where the slopes cancel it is
 // not: 8192 rows, 256 entries, 64 columns in bf16, relative error of dE 1.6e-3 with a table of zeros (its last rounding alone: as much), 2.5e-3 / 7.6e-3
 // after 20 / 60 optimiser steps (magnitudes 13 / 45 times the entries), 0.2 after 400 (1200 times); 2^-12.5 of the magnitudes in all three.
-#include "operator_call.hpp"
-#include "product_finish.hpp"
+#include "vocabulary.hpp"
 
 #include <cmath>
 
 namespace cocod {
 namespace {
 
-const Dtype kTypes[] = {Dtype::F32, Dtype::BF16, Dtype::F16};
-constexpr uint32_t kPieceUnit = 256;
 constexpr uint64_t kMaxLossRows = 1ull << 26;        // a wave a row in one launch
-constexpr uint64_t kPieceElements = 1ull << 28;      // of dz in memory at a time, unless the caller says otherwise
-
-struct Rows {
-    const int64_t *offsets;
-    uint32_t groups;
-    uint64_t rows;
-    const int32_t *target;
-    uint32_t vocab;
-};
-
-__device__ __forceinline__ uint64_t clamped(const Rows &p, uint32_t i)
-{
-    const int64_t v = p.offsets[i];
-    return v < 0 ? 0 : static_cast<uint64_t>(v) > p.rows ? p.rows : static_cast<uint64_t>(v);
-}
-__device__ __forceinline__ bool has_target(const Rows &p, uint64_t r)
-{
-    return static_cast<uint32_t>(p.target[r]) < p.vocab;          // negative ones are large
-}
 
 // A row's gathered copy (pitch a multiple of 8, zeros behind dim) by the lanes of a wave.
 template <class E> struct Hidden {
@@ -59,15 +37,7 @@ template <class E> struct Hidden {
 };
 template <class E> __device__ __forceinline__ void gather_row(const Hidden<E> &p, uint64_t r, uint32_t from, uint32_t lane)
 {
-    const E *src = p.h + from * p.ldh;
-    E *dst = p.out + r * p.pitch;
-    constexpr uint32_t V = 16 / sizeof(E);
-    if ((reinterpret_cast<uintptr_t>(src) & 15) == 0 && p.dim % V == 0) {
-        for (uint32_t j = lane * V; j < p.dim; j += 64 * V) *reinterpret_cast<float4 *>(dst + j) = *reinterpret_cast<const float4 *>(src + j);
-        for (uint32_t j = p.dim + lane; j < p.pitch; j += 64) dst[j] = 0;
-    } else {
-        for (uint32_t j = lane; j < p.pitch; j += 64) dst[j] = j < p.dim ? src[j] : E(0);
-    }
+    copy_row(p.h + from * p.ldh, p.dim, p.out + r * p.pitch, p.pitch, lane);
 }
 // A row without a target: loss 0, gradient 0.
 template <class E> __device__ __forceinline__ void clear_row(const Hidden<E> &p, uint64_t r, uint32_t lane)
@@ -288,13 +258,9 @@ Workspace carve(const cocod_cross_entropy_call *c)
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) / 256 * 256; return o; };
     w.pitch = (static_cast<uint64_t>(c->dim) + 7) / 8 * 8;
-    uint64_t piece = c->piece ? c->piece : kPieceElements / (rows ? rows : 1);
-    const uint64_t whole = (static_cast<uint64_t>(c->vocab) + kPieceUnit - 1) / kPieceUnit * kPieceUnit;
-    piece = (piece < kPieceUnit ? kPieceUnit : piece) / kPieceUnit * kPieceUnit;
-    if (piece > whole) piece = whole;
-    w.pieces = static_cast<uint32_t>((whole + piece - 1) / piece);
-    w.piece = c->piece ? piece : (whole / kPieceUnit + w.pieces - 1) / w.pieces * kPieceUnit;      // of equal size
-    w.pieces = static_cast<uint32_t>((whole + w.piece - 1) / w.piece);
+    const Pieces pieces = pieces_of(c->piece, rows, c->vocab);
+    w.piece = pieces.size;
+    w.pieces = pieces.count;
     const uint32_t n = static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab);
     const bool dim8 = c->dim % 8 == 0;                         // a dense table's rows then start on 16 bytes
     w.logits = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, c->vocab, c->dim, false, false);

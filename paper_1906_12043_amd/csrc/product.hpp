@@ -23,7 +23,10 @@ enum class Finish {
     Store,       // relu, mask, scale, running sum; store in the element type or fp32
     Stats,       // logits: maximum and sum of exponentials of the tile's part of every row but its target, and the target's logit
     Keep,        //   the same, and the exponentials stored (bf16: in fp16 times 2^14; pitch and columns to the end of the last tile are the buffer's)
-    Slope        // logits: softmax minus one-hot, stored in the element type
+    Slope,       // logits: softmax minus one-hot, stored in the element type
+    Moments,     // logits: of the tile's part of every row the maximum, the sum of exponentials without one of the largest, and that of distances times
+                 //   exponentials; the target's logit; where asked, the largest of every four columns
+    Score        // logits: slopes of log probability and entropy, stored in the element type
 };
 
 struct ProductParams {
@@ -65,13 +68,21 @@ struct ProductParams {
     const float *top, *inverse;       // [rows]: largest logit; 1 / sum of the exponentials below it
     const float *target_slope;        // [rows]: probability of the target, less one
     uint32_t v0;                      // vocabulary entry of column 0
+    // token scores
+    float logit_scale;                // logits are multiplied by it, > 0
+    float4 *moments;                  // [rows][column tiles]: maximum, sum, sum of distances (target may be null then)
+    uint32_t moment_tiles;
+    float *quads;                     // non-null: [rows][ld_quads], see quad_place
+    uint64_t ld_quads;                // a multiple of 64
+    const float *slope_one;           // [rows]: slope of an entry d below the largest is e^d (inverse + slope_one d)
+    const float *group_scale;         // Weights, non-null: C of a group is multiplied by this instead of scale
     uint32_t ldc_zero;                // Slope: columns up to here are stored, those from n on as zeros
 };
 
 // Tile shapes a launch can take (plan_product picks one).
 enum class Tile : uint32_t { Large = 0, Medium = 1, Small = 2, Deep = 3, Tall = 4, Square = 5 };
 
-// C = A B, stored (Finish::Store) or as logits (Rows_NK with Finish::Stats, Keep or Slope), one launch, with splits one more that joins
+// C = A B, stored (Finish::Store) or as logits (Rows_NK with one of the other finishes), one launch, with splits one more that joins
 // them.  hipErrorInvalidConfiguration: the grid would exceed a launch's limits.
 hipError_t launch_store_bf16(hipStream_t stream, Layout layout, Tile tile, const ProductParams &p);
 hipError_t launch_store_f16(hipStream_t stream, Layout layout, Tile tile, const ProductParams &p);
@@ -94,6 +105,15 @@ inline uint64_t blocks_of(const TileSize &t, bool weights, uint64_t rows, uint32
     return row_tiles * ((n + t.bn - 1) / t.bn) * splits;
 }
 inline bool fits_a_launch(const TileSize &t, uint64_t blocks) { return blocks * t.threads < (1ull << 32); }
+
+// Finish::Moments leaves the largest of four consecutive columns, a quad, in the order in which a wave's lanes hold them: a wave has `width` quads of a row, `each`
+// of them in a lane; lane k's i-th is the wave's quad i * width / each + k, and stands at k * each + i.
+struct QuadOrder { uint32_t width, each; };
+constexpr QuadOrder quad_order(Dtype type, Tile tile)
+{
+    return tile == Tile::Small ? QuadOrder{16, 16} : type == Dtype::F32 ? QuadOrder{8, 4}
+           : tile == Tile::Large ? QuadOrder{16, 4} : tile == Tile::Deep ? QuadOrder{8, 2} : QuadOrder{16, 8};
+}
 
 // Columns of the tiles in which Finish::Stats forms its statistics (ProductParams::stats holds one row of them per column tile).
 inline uint32_t tile_cols(Dtype type, Tile tile)

@@ -78,6 +78,15 @@ struct F32 : Bf16 {
     static __device__ __forceinline__ float exp(float x, float base) { return expf(x - base); }
 };
 
+// Slope of an entry whose logit lies d below the row's largest, from the row's two factors (Finish::Score).  Below -200 the exponential is zero, and so is
+// the slope, also where d is minus infinity.
+constexpr float kFarBelow = -200.0f;
+template <class T> __device__ __forceinline__ float score_slope(float d, float none, float one)
+{
+    d = fmaxf(d, kFarBelow);
+    return T::exp(d, 0.0f) * fmaf(one, d, none);
+}
+
 __device__ __forceinline__ uint64_t bound_at(const ProductParams &p, uint32_t i)
 {
     const int64_t v = p.offsets[i];
@@ -155,6 +164,7 @@ __device__ __forceinline__ void finish_quad(const ProductParams &p, uint32_t gro
 
 __device__ __forceinline__ float group_factor(const ProductParams &p, uint32_t group)
 {
+    if (p.group_scale) return p.group_scale[group];
     if (!p.mean) return p.scale;
     const uint64_t len = length_at(p, group);
     return len ? p.scale / static_cast<float>(len) : 0.0f;

@@ -522,10 +522,12 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
         // what belongs to a row is fetched once, by the lane of its number
         const uint32_t lane = threadIdx.x % 64, mine = r0 + lane % ROWS;
         const uint64_t my_row = at.row0 + mine;
-        float row_factor = factor, row_top = 0.0f;
+        float row_factor = factor, row_top = 0.0f, row_one = 0.0f;
         uint32_t row_number = 0;
-        const bool by_row = !WEIGHTS && !part && (FINISH == Finish::Slope || p.row_scale || p.out_row);
+        constexpr bool SLOPE = FINISH == Finish::Slope || FINISH == Finish::Score;
+        const bool by_row = !WEIGHTS && !part && (SLOPE || p.row_scale || p.out_row);
         if (by_row && mine < at.rows) {
+            if (FINISH == Finish::Score) { row_top = p.top[my_row]; row_factor = p.inverse[my_row]; row_one = p.slope_one[my_row]; row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
             if (FINISH == Finish::Slope) { row_top = p.top[my_row]; row_factor = p.inverse[my_row] * slope_scale<T>(); row_number = static_cast<uint32_t>(p.target[my_row]) - p.v0; }
             if (FINISH == Finish::Store && p.row_scale) row_factor = p.row_scale[my_row];
             if (FINISH == Finish::Store && p.out_row) row_number = p.out_row[my_row];
@@ -535,7 +537,8 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
             const uint32_t r = k + first;
             const float f = by_row ? __shfl(row_factor, r, 64) : factor;
             const uint32_t number = by_row ? __shfl(row_number, r, 64) : 0;
-            const float top = FINISH == Finish::Slope ? __shfl(row_top, r, 64) : 0.0f;
+            const float top = SLOPE ? __shfl(row_top, r, 64) : 0.0f;
+            const float one = FINISH == Finish::Score ? __shfl(row_one, r, 64) : 0.0f;
             f4 a = *reinterpret_cast<const f4 *>(v + r * PITCH + qa), b = *reinterpret_cast<const f4 *>(v + r * PITCH + qb);
             if (r0 + r >= at.rows) continue;
             const uint64_t row = at.row0 + r0 + r;
@@ -545,6 +548,14 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
                 for (uint32_t j = 0; j < 4; ++j) { a[j] = T::exp(a[j], top) * f; b[j] = T::exp(b[j], top) * f; }
                 if (number - ca < 4 || number - cb < 4) {      // the target is one of these columns
                     const float t = p.target_slope[row] * slope_scale<T>();
+                    #pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) { if (number - ca == j) a[j] = t; if (number - cb == j) b[j] = t; }
+                }
+            } else if constexpr (FINISH == Finish::Score) {
+                #pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) { a[j] = score_slope<T>(a[j] * p.logit_scale - top, f, one); b[j] = score_slope<T>(b[j] * p.logit_scale - top, f, one); }
+                if (number - ca < 4 || number - cb < 4) {
+                    const float t = p.target_slope[row];
                     #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) { if (number - ca == j) a[j] = t; if (number - cb == j) b[j] = t; }
                 }
@@ -602,6 +613,26 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
             }
         }
     }
+};
+
+// Sums over entries of a row below its largest logit `top`: exponentials of those below it, number of those equal to it, distances times exponentials.
+// The sum of the exponentials is 1 + rest, rest = below + largest - 1: the 1 stays apart, so that log(1 + rest) keeps its digits where the row is sure.
+template <class T> struct Moment {
+    float below = 0.0f, largest = 0.0f, far = 0.0f;
+    __device__ __forceinline__ void add(float z, float top)
+    {
+        const float d = z - (top == -INFINITY ? 0.0f : top), e = T::exp(d, 0.0f);       // (what is not finite stays so in `below`)
+        below += d == 0.0f ? 0.0f : e;
+        largest += d == 0.0f ? 1.0f : 0.0f;
+        far = fmaf(e, fmaxf(d, kFarBelow), far);
+    }
+    __device__ __forceinline__ void add_lane(int d)
+    {
+        below += __shfl_xor(below, d, 64);
+        largest += __shfl_xor(largest, d, 64);
+        far += __shfl_xor(far, d, 64);
+    }
+    __device__ __forceinline__ float4 result(float top) const { return make_float4(top, below + (largest - 1.0f), far, 0.0f); }
 };
 
 template <class T, Layout LAYOUT, class S, Finish FINISH, int HOW_A, int HOW_B>
@@ -743,8 +774,19 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 if (c + j >= p.n) v[j] = 0.0f;
             }
             store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
+        } else if constexpr (FINISH == Finish::Score) {
+            if (r >= at.rows || c >= p.ldc_zero) return;
+            const float top = p.top[at.row0 + r], none = p.inverse[at.row0 + r], one = p.slope_one[at.row0 + r], slope = p.target_slope[at.row0 + r];
+            const int32_t target = p.target[at.row0 + r];
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = static_cast<int32_t>(p.v0 + c + j) == target ? slope : score_slope<T>(v[j] * p.logit_scale - top, none, one);
+                if (c + j >= p.n) v[j] = 0.0f;
+            }
+            store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);
         }
     };
+    const bool find_target = FINISH != Finish::Moments || p.target;
 
     if constexpr (S::WK > 1) {
         // the waves' sums over their terms meet in LDS, row by row, in the order of the waves
@@ -784,6 +826,27 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
                 #pragma unroll
                 for (int d = 1; d < LANES; d <<= 1) sum += __shfl_xor(sum, d, 64);
                 if (q == 0 && r < at.rows) p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
+            } else if constexpr (FINISH == Finish::Moments) {
+                static_assert(LANES <= 64 && 64 % LANES == 0 && LANES == quad_order(T::dtype, Tile::Small).width, "a row within a wave, a quad a lane");
+                const int32_t target = find_target && r < at.rows ? p.target[at.row0 + r] : -1;
+                float most = -INFINITY;
+                #pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    v[j] *= p.logit_scale;
+                    if (c + j >= p.n) v[j] = -INFINITY;
+                    else if (static_cast<int32_t>(c + j) == target) p.target_logit[at.row0 + r] = v[j];
+                    most = fmaxf(most, v[j]);
+                }
+                if (p.quads && r < at.rows) p.quads[(at.row0 + r) * p.ld_quads + c / 4] = most;
+                float top = most;
+                #pragma unroll
+                for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+                Moment<T> sum;
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) sum.add(v[j], top);
+                #pragma unroll
+                for (int d = 1; d < LANES; d <<= 1) sum.add_lane(d);
+                if (q == 0 && r < at.rows) p.moments[(at.row0 + r) * p.moment_tiles + at.n0 / S::BN] = sum.result(top);
             } else {
                 finish(r, c, v);
             }
@@ -871,6 +934,86 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             #pragma unroll
             for (int w = 0; w < S::WN; ++w) sum += sums[w * S::BM + r];
             p.stats[static_cast<uint64_t>(at.n0 / S::BN) * p.rows + at.row0 + r] = make_float2(top, sum);
+        }
+    } else if constexpr (FINISH == Finish::Moments) {
+        // As above: the tile's maximum, then the sums below it.  The target is among them; it is one of the largest that is left out.
+        float *tops = reinterpret_cast<float *>(lds), *sums = tops + S::WN * S::BM, *ones = sums + S::WN * S::BM, *far = ones + S::WN * S::BM;
+        static_assert(4 * S::WN * S::BM * 4 <= P::lds_bytes, "the waves' sums");
+        const uint32_t c0 = at.n0 + wn * S::NB * S::MI + 4 * (lane / S::MI);
+        const bool whole = at.n0 + S::BN <= p.n;
+        const float scale = unscale * p.logit_scale;
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i) {
+            const uint32_t r = (wm * S::MB + i) * S::MI + lane % S::MI;
+            const int32_t target = find_target && r < at.rows ? p.target[at.row0 + r] : -1;
+            if (__ballot(target >= static_cast<int32_t>(at.n0) && target < static_cast<int32_t>(at.n0 + S::BN))) {
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j)
+                    #pragma unroll
+                    for (int x = 0; x < S::X; ++x)
+                        if (static_cast<int32_t>(c0 + j * S::MI + 8 * (x / 4) + x % 4) == target) p.target_logit[at.row0 + r] = acc[0][i][j][x] * scale;
+            }
+            if (!whole) {
+                #pragma unroll
+                for (int j = 0; j < S::NB; ++j)
+                    #pragma unroll
+                    for (int x = 0; x < S::X; ++x) if (c0 + j * S::MI + 8 * (x / 4) + x % 4 >= p.n) acc[0][i][j][x] = -INFINITY;
+            }
+            constexpr int EACH = S::NB * S::X / 4;
+            constexpr QuadOrder order = quad_order(T::dtype, S::BN == 256 ? Tile::Large : S::threads == 512 ? Tile::Deep : S::BN == 64 ? Tile::Square : Tile::Medium);
+            static_assert(order.width == S::NB * S::MI / 4 && order.each == EACH, "quad_order");
+            float quad[EACH], top = -INFINITY;
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j)
+                #pragma unroll
+                for (int g = 0; g < S::X / 4; ++g) {
+                    const auto &v = acc[0][i][j];
+                    const float most = fmaxf(fmaxf(v[4 * g], v[4 * g + 1]), fmaxf(v[4 * g + 2], v[4 * g + 3]));
+                    quad[j * (S::X / 4) + g] = most * scale;
+                    top = fmaxf(top, most);
+                }
+            if (p.quads && r < at.rows) {
+                float *to = p.quads + (at.row0 + r) * p.ld_quads + (at.n0 + wn * S::NB * S::MI) / 4 + lane / S::MI * EACH;
+                if constexpr (EACH == 2) *reinterpret_cast<float2 *>(to) = make_float2(quad[0], quad[1]);
+                else
+                    #pragma unroll
+                    for (int e = 0; e < EACH; e += 4) *reinterpret_cast<f4 *>(to + e) = f4{quad[e], quad[e + 1], quad[e + 2], quad[e + 3]};
+            }
+            #pragma unroll
+            for (int d = S::MI; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+            if (lane < S::MI) tops[wn * S::BM + r] = top * scale;
+            __builtin_amdgcn_sched_barrier(0);                 // one row block's values at a time
+        }
+        __syncthreads();
+        #pragma unroll
+        for (int i = 0; i < S::MB; ++i) {
+            const uint32_t r = (wm * S::MB + i) * S::MI + lane % S::MI;
+            float top = -INFINITY;
+            #pragma unroll
+            for (int w = 0; w < S::WN; ++w) top = fmaxf(top, tops[w * S::BM + r]);
+            Moment<T> sum;
+            #pragma unroll
+            for (int j = 0; j < S::NB; ++j) {
+                #pragma unroll
+                for (int x = 0; x < S::X; ++x) sum.add(acc[0][i][j][x] * scale, top);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            #pragma unroll
+            for (int d = S::MI; d < 64; d <<= 1) sum.add_lane(d);
+            if (lane < S::MI) { sums[wn * S::BM + r] = sum.below; ones[wn * S::BM + r] = sum.largest; far[wn * S::BM + r] = sum.far; }
+        }
+        __syncthreads();
+        for (uint32_t r = threadIdx.x; r < at.rows; r += S::threads) {
+            float top = -INFINITY;
+            Moment<T> sum;
+            #pragma unroll
+            for (int w = 0; w < S::WN; ++w) {
+                top = fmaxf(top, tops[w * S::BM + r]);
+                sum.below += sums[w * S::BM + r];
+                sum.largest += ones[w * S::BM + r];
+                sum.far += far[w * S::BM + r];
+            }
+            p.moments[(at.row0 + r) * p.moment_tiles + at.n0 / S::BN] = sum.result(top);
         }
     } else {
         // A block of rows at a time turns in the wave's own part of LDS, so that consecutive lanes take consecutive columns.  Tiles that lie
@@ -993,6 +1136,8 @@ template <class T> hipError_t launch_store(hipStream_t stream, Layout layout, Ti
 template <class T> hipError_t launch_logits(hipStream_t stream, Finish finish, Tile tile, const ProductParams &p)
 {
     if (finish == Finish::Stats) return launch_layout<T, Layout::Rows_NK, Finish::Stats>(stream, tile, p);
+    if (finish == Finish::Moments) return launch_layout<T, Layout::Rows_NK, Finish::Moments>(stream, tile, p);
+    if (finish == Finish::Score) return launch_layout<T, Layout::Rows_NK, Finish::Score>(stream, tile, p);
     if constexpr (!std::is_same<T, F16>::value)                // (its slopes would be rounded twice to the same eleven bits)
         if (finish == Finish::Keep) return launch_layout<T, Layout::Rows_NK, Finish::Keep>(stream, tile, p);
     return finish == Finish::Slope ? launch_layout<T, Layout::Rows_NK, Finish::Slope>(stream, tile, p) : hipErrorInvalidValue;
