@@ -15,8 +15,12 @@
 // differ from the product's in the order of their sums.  No atomics: results do not depend on the order of blocks.
 //
 // Backward: the logits are formed again, piece by piece, as slopes in the element type, for the two products that follow, as the loss does; in 16 bits a
-// slope is off by half a step of itself, fp16 slopes are taken times a power of two per group that brings their bound below to 2^14:
-// p |d - D| is below 22 for any vocabulary up to 2^30, so |a| + 32 |b| bounds a slope.  Rows whose slopes a and b are both zero take no part.
+// slope is off by half a step of itself.  The largest slope of most rows is the target's, and its rounding would be that of the row's whole gradient; so the mantissa
+// of the target's slope is taken out of the row's slopes, which leaves a power of two there: dh is multiplied by it in fp32, and the product for dE
+// takes rows of h times it (a row whose entry no other row has for its target is then rounded once, as its last rounding would; 4096 rows, 32003 entries of 1024,
+// error of dh and dE against 64 bits: 1.02 times that of a plain form in fp32, 1.41 times without).  fp16 slopes are also taken times a power of two per
+// group that brings their bound below 2^14: p |d - D| is below 22 for any vocabulary up to 2^30, so |a| + 32 |b| bounds a slope.  Rows whose slopes a and
+// b are both zero take no part.
 #include "vocabulary.hpp"
 #include "row_access.hpp"
 
@@ -26,7 +30,7 @@ namespace cocod {
 namespace {
 
 constexpr uint64_t kMaxScoreRows = 1ull << 26;
-constexpr uint32_t kMostTop = 32;
+constexpr uint32_t kMostTop = 32, kFewRows = 256;
 constexpr float kEntropyBound = 32.0f, kSlopeScale16 = 0x1p14f;
 // Up to so many bytes of hidden states per group rows stay where they are, those without a target among them.
 constexpr uint64_t kLeaveHere = 1u << 20;
@@ -100,31 +104,58 @@ template <class E> struct Gather {
     uint32_t dim;
     E *out;
     uint64_t pitch;
+    E *scaled;                        // non-null: rows times the mantissa of their target's slope
     // gradient
     E *dh;                            // may be null
     uint64_t lddh;
     const float4 *norms;
     float scale;
-    const float *row_scale;           // may be null: 1
+    int normal;                       // row_scale holds the group's factor
+    float *row_scale;                 // may be null (fp32: nothing is taken out)
     float *top, *none, *one, *target_slope;
 };
 constexpr uint32_t kMostRowBlocks = 1u << 23;
-template <class E> __global__ __launch_bounds__(256) void scores_gather_kernel(const Taking p, const Gather<E> q)
+// A row times a factor of at most 1, rounded to the type.
+template <class T> __device__ __forceinline__ void scaled_row(const typename T::elem *src, uint32_t dim, typename T::elem *dst, uint64_t pitch, float factor, uint32_t lane)
 {
+    typedef Piece<T> V;
+    for (uint32_t j = lane * V::N; j < pitch; j += 64 * V::N) {
+        const u4 raw = j < dim ? V::load(src + j, dim - j) : u4{0, 0, 0, 0};
+        float v[V::N];
+        #pragma unroll
+        for (uint32_t i = 0; i < V::N; ++i) v[i] = V::value(raw, i) * factor;
+        V::store(dst + j, V::pack(v));
+    }
+}
+template <class T> __global__ __launch_bounds__(256) void scores_gather_kernel(const Taking p, const Gather<typename T::elem> q)
+{
+    typedef typename T::elem E;
     const uint32_t lane = threadIdx.x % 64;
     for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64; r < p.rows.rows; r += static_cast<uint64_t>(gridDim.x) * 4) {
         if (!in_groups(p.rows, r)) continue;
         const uint32_t from = q.index[r];
         if (from != kNoRow) {
-            copy_row(q.h + from * q.ldh, q.dim, q.out + r * q.pitch, q.pitch, lane);
-            if (p.grad && lane == 0) {
+            const E *h = q.h + from * q.ldh;
+            copy_row(h, q.dim, q.out + r * q.pitch, q.pitch, lane);
+            if (p.grad) {
                 const float4 n = q.norms[from];                // top, rest, D, distance of the target
                 const float a = slope_of_logp(p, from), b = slope_of_entropy(p, from), inverse = 1.0f / (1.0f + n.y);
-                const float k = q.row_scale ? q.scale / q.row_scale[r] : q.scale, pt = expf(n.w) * inverse, others = n.w == 0.0f ? n.y * inverse : 1.0f - pt;
-                q.top[r] = n.x;
-                q.none[r] = (b * n.z - a) * inverse * k;
-                q.one[r] = -b * inverse * k;
-                q.target_slope[r] = (a * others + b * pt * (n.z - n.w)) * k;
+                const float back = q.normal ? q.row_scale[r] : 1.0f, k = q.scale / back;
+                const float pt = expf(n.w) * inverse, others = n.w == 0.0f ? n.y * inverse : 1.0f - pt;
+                float target = (a * others + b * pt * (n.z - n.w)) * k, mantissa = 1.0f;
+                if (q.row_scale && p.rows.target && fabsf(target) > 0x1p-126f && fabsf(target) < 0x1p126f) {
+                    mantissa = __builtin_amdgcn_frexp_mantf(fabsf(target));       // in 1/2 .. 1
+                    target = copysignf(ldexpf(1.0f, __builtin_amdgcn_frexp_expf(target)), target);
+                }
+                if (q.scaled) scaled_row<T>(h, q.dim, q.scaled + r * q.pitch, q.pitch, mantissa, lane);
+                if (lane == 0) {
+                    const float even = inverse * k / mantissa;
+                    q.top[r] = n.x;
+                    q.none[r] = (b * n.z - a) * even;
+                    q.one[r] = -b * even;
+                    q.target_slope[r] = target;
+                    if (q.row_scale) q.row_scale[r] = back * mantissa;
+                }
             }
         }
         if (p.grad && q.dh && !takes_part(p, r))
@@ -156,21 +187,65 @@ __device__ __forceinline__ float value_of(unsigned long long rank)
     const uint32_t u = static_cast<uint32_t>(rank >> 32);
     return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
 }
-// The k largest of the ranks rank(0) .. rank(n - 1), in order, by one wave; 0 behind them.
-template <class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, unsigned long long *out, uint32_t lane)
+// The largest of the lanes' numbers, by lane moves within rows of 16 and broadcasts of their last lanes.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t larger_moved(uint32_t v)
 {
-    unsigned long long best = 0;
-    for (uint32_t i = lane; i < n; i += 64) { const unsigned long long v = rank(i); best = v > best ? v : best; }
-    for (uint32_t j = 0; j < k; ++j) {
-        unsigned long long all = best;
-        #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) { const unsigned long long v = __shfl_xor(all, d, 64); all = v > all ? v : all; }
-        if (lane == 0) out[j] = all;
-        if (best == all && all != 0) {                         // (ranks differ) this lane's next one
-            best = 0;
-            for (uint32_t i = lane; i < n; i += 64) { const unsigned long long v = rank(i); best = v < all && v > best ? v : best; }
+    const uint32_t u = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(v), static_cast<int>(v), CTRL, ROWS, 0xf, false));
+    return u > v ? u : v;
+}
+__device__ __forceinline__ uint32_t wave_largest(uint32_t v)
+{
+    v = larger_moved<0x111, 0xf>(v);                           // from 1, 2, 4 and 8 lanes below
+    v = larger_moved<0x112, 0xf>(v);
+    v = larger_moved<0x114, 0xf>(v);
+    v = larger_moved<0x118, 0xf>(v);
+    v = larger_moved<0x142, 0xa>(v);                           // rows 1 and 3 from the last lane of the row below
+    v = larger_moved<0x143, 0xc>(v);                           // rows 2 and 3 from lane 31
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The k largest of the ranks rank(0) .. rank(n - 1), in order, to list[0 .. k - 1]; 0 behind them.  The block's threads fetch kRanks of them at a time into LDS behind the
+// list so far, one wave finds the largest of them (a lane keeps the best two of every 64th and looks for more when both are taken).
+constexpr uint32_t kRanks = 2048;
+template <class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, unsigned long long *list)
+{
+    const uint32_t lane = threadIdx.x % 64;
+    if (threadIdx.x < k) list[threadIdx.x] = 0;
+    for (uint32_t base = 0; base < n; base += kRanks) {
+        const uint32_t count = n - base < kRanks ? n - base : kRanks, all = k + count;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) list[k + i] = rank(base + i);
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            unsigned long long best = 0, next = 0, mine = 0;
+            bool known = true;                                 // `next` is the lane's second best
+            const auto look = [&](unsigned long long below) {
+                best = next = 0;
+                known = true;
+                #pragma unroll 4
+                for (uint32_t i = lane; i < all; i += 64) {
+                    const unsigned long long v = list[i] < below ? list[i] : 0;
+                    next = v > best ? best : v > next ? v : next;
+                    best = v > best ? v : best;
+                }
+            };
+            look(~0ull);
+            for (uint32_t j = 0; j < k; ++j) {
+                const uint32_t high = wave_largest(static_cast<uint32_t>(best >> 32));
+                const uint32_t low = wave_largest(static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0);
+                const unsigned long long taken = static_cast<unsigned long long>(high) << 32 | low;
+                if (lane == j) mine = taken;
+                if (taken == 0) break;
+                if (best == taken) {                           // (ranks differ)
+                    if (known) { best = next; known = false; }
+                    else       look(taken);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (lane < k) list[lane] = mine;
         }
     }
+    __syncthreads();
 }
 
 struct Scores {
@@ -196,18 +271,20 @@ struct Scores {
     float scale;
 };
 
-// WAVES waves a row: one where no alternatives are wanted, four where they are.
-template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kernel(const Scores p)
+// WAVES waves a row: one where no alternatives are wanted; four where they are, sixteen if rows are fewer than compute units (4 rows, 131072 entries:
+// FEW us instead of 34).
+template <class T, int WAVES> __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void scores_kernel(const Scores p)
 {
     typedef Piece<T> V;
     typedef typename T::elem elem;
     constexpr bool TOP = WAVES > 1;
-    __shared__ Joined parts[4];
-    __shared__ unsigned long long tile_rank[TOP ? kMostTop : 1], quad_rank[TOP ? kMostTop : 1], entry_rank[TOP ? 4 * kMostTop : 1];
+    constexpr int ROWS = WAVES > 4 ? 1 : 4 / WAVES;            // of a block
+    __shared__ Joined parts[WAVES];
+    __shared__ unsigned long long tile_rank[TOP ? kMostTop : 1], quad_rank[TOP ? kMostTop : 1], entry_rank[TOP ? 4 * kMostTop : 1], list[TOP ? kMostTop + kRanks : 1];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tid = threadIdx.x % (64 * WAVES);
     const Rows &rows = p.taking.rows;
     // (all threads of a row leave a turn together)
-    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * (4 / WAVES) + threadIdx.x / (64 * WAVES); r < rows.rows; r += static_cast<uint64_t>(gridDim.x) * (4 / WAVES)) {
+    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * ROWS + threadIdx.x / (64 * WAVES); r < rows.rows; r += static_cast<uint64_t>(gridDim.x) * ROWS) {
         if (!in_groups(rows, r)) continue;
         if (!takes_part(p.taking, r)) {
             if (tid == 0) {
@@ -223,7 +300,14 @@ template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kern
 
         Joined sum = {-INFINITY, -1.0f, 0.0f};
         const float4 *moments = p.moments + r * p.tiles;
-        for (uint32_t t = tid; t < p.tiles; t += 64 * WAVES) { const float4 m = moments[t]; sum = join(sum, {m.x, m.y, m.z}); }
+        constexpr int AHEAD = 4;
+        for (uint32_t t = tid; t < p.tiles; t += 64 * WAVES * AHEAD) {
+            float4 m[AHEAD];
+            #pragma unroll
+            for (int a = 0; a < AHEAD; ++a) m[a] = t + a * 64 * WAVES < p.tiles ? moments[t + a * 64 * WAVES] : make_float4(-INFINITY, -1.0f, 0.0f, 0.0f);
+            #pragma unroll
+            for (int a = 0; a < AHEAD; ++a) sum = join(sum, {m[a].x, m[a].y, m[a].z});
+        }
         #pragma unroll
         for (int d = 1; d < 64; d <<= 1) sum = join_lane(sum, d);
         if constexpr (TOP) {
@@ -242,18 +326,18 @@ template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kern
         if constexpr (TOP) {
             // the tiles, the quads in them
             const float *quads = p.quads + r * p.ld_quads;
-            if (wave == 0) {
-                largest(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, tile_rank, lane);
-                __builtin_amdgcn_wave_barrier();
-                const uint32_t others = p.order.width / p.order.each, all = (rows.vocab + 3) / 4;
-                largest(p.top * p.tile_quads, p.top, [&](uint32_t i) -> unsigned long long {
-                    const unsigned long long tile = tile_rank[i / p.tile_quads];
-                    if (!tile) return 0;
-                    const uint32_t at = place_of(tile) * p.tile_quads + i % p.tile_quads, in = at % p.order.width;
-                    const uint32_t quad = at - in + in % p.order.each * others + in / p.order.each;
-                    return quad < all ? rank_of(quads[at], quad) : 0;
-                }, quad_rank, lane);
-            }
+            largest(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, list);
+            if (tid < p.top) tile_rank[tid] = list[tid];
+            __syncthreads();
+            const uint32_t others = p.order.width / p.order.each, all = (rows.vocab + 3) / 4;
+            largest(p.top * p.tile_quads, p.top, [&](uint32_t i) -> unsigned long long {
+                const unsigned long long tile = tile_rank[i / p.tile_quads];
+                if (!tile) return 0;
+                const uint32_t at = place_of(tile) * p.tile_quads + i % p.tile_quads, in = at % p.order.width;
+                const uint32_t quad = at - in + in % p.order.each * others + in / p.order.each;
+                return quad < all ? rank_of(quads[at], quad) : 0;
+            }, list);
+            if (tid < p.top) quad_rank[tid] = list[tid];
             __syncthreads();
             // their logits, a quad a wave at a time
             uint32_t g = 0;
@@ -272,15 +356,23 @@ template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kern
                 const elem *row[4];
                 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) row[k] = e + static_cast<uint64_t>(v0 + (k < count ? k : 0)) * p.lde;
+                uint32_t c = lane * V::N;
                 #pragma unroll 2
-                for (uint32_t c = lane * V::N; c < p.dim; c += 64 * V::N) {
-                    const u4 a = V::load(h + c, p.dim - c);
+                for (; c + V::N <= p.dim; c += 64 * V::N) {
+                    const u4 a = V::load(h + c);
+                    u4 b[4];
                     #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        const u4 b = V::load(row[k] + c, p.dim - c);
+                    for (uint32_t k = 0; k < 4; ++k) b[k] = V::load(row[k] + c);
+                    #pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k)
                         #pragma unroll
-                        for (uint32_t i = 0; i < V::N; ++i) dot[k] = fmaf(V::value(a, i), V::value(b, i), dot[k]);
-                    }
+                        for (uint32_t i = 0; i < V::N; ++i) dot[k] = fmaf(V::value(a, i), V::value(b[k], i), dot[k]);
+                }
+                #pragma unroll 1
+                for (; c < p.dim; ++c) {                       // the last columns of one lane
+                    const float a = widen<T>(h[c]);
+                    #pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) dot[k] = fmaf(a, widen<T>(row[k][c]), dot[k]);
                 }
                 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1)
@@ -302,14 +394,11 @@ template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kern
                 }
             }
             __syncthreads();
-            if (wave == 0) {
-                largest(4 * p.top, p.top, [&](uint32_t i) { return entry_rank[i]; }, quad_rank, lane);
-                __builtin_amdgcn_wave_barrier();
-                if (lane < p.top) {
-                    const unsigned long long rank = quad_rank[lane];
-                    p.top_ids[to * p.ld_top + lane] = rank ? static_cast<int32_t>(place_of(rank)) : -1;
-                    p.top_logp[to * p.ld_top + lane] = rank ? (value_of(rank) - sum.top) - norm : -INFINITY;
-                }
+            largest(4 * p.top, p.top, [&](uint32_t i) { return entry_rank[i]; }, list);
+            if (tid < p.top) {
+                const unsigned long long rank = list[tid];
+                p.top_ids[to * p.ld_top + tid] = rank ? static_cast<int32_t>(place_of(rank)) : -1;
+                p.top_logp[to * p.ld_top + tid] = rank ? (value_of(rank) - sum.top) - norm : -INFINITY;
             }
             __syncthreads();                                   // the next row's
         }
@@ -320,7 +409,7 @@ template <class T, int WAVES> __global__ __launch_bounds__(256) void scores_kern
 
 struct Workspace {
     uint64_t index, target, ends, hidden, target_logit, moments, quads, ld_quads;
-    uint64_t row_scale, group_scale, top, none, one, target_slope, slope, sum, part;
+    uint64_t scaled, row_scale, group_scale, top, none, one, target_slope, slope, sum, part;
     uint64_t pitch, piece, sum_pitch, bytes;
     uint32_t pieces;
     ProductPlan logits, to_hidden, to_table;
@@ -354,6 +443,7 @@ Workspace carve(const cocod_token_scores_call *c, bool grad)
         w.logits = plan_product(Layout::Rows_NK, t, dim8, rows, c->groups, 0, n, c->dim, false, false);
         w.to_hidden = plan_product(Layout::Rows_KN, t, dim8, rows, c->groups, 0, c->dim, n, true);
         w.to_table = plan_product(Layout::Weights, t, true, rows, c->groups, n, c->dim, 0, true);
+        w.scaled = c->de && t != Dtype::F32 ? take(rows * w.pitch * s) : w.hidden;
         w.row_scale = take(rows * 4);
         w.group_scale = take(c->groups * 4ull);
         w.top = take(rows * 4);
@@ -423,7 +513,7 @@ ProductParams table_operands(const Workspace &w, const uint8_t *ws)
 {
     ProductParams p{};
     p.a = ws + w.slope; p.lda = w.piece;
-    p.b = ws + w.hidden; p.ldb = w.pitch;
+    p.b = ws + w.scaled; p.ldb = w.pitch;
     return p;
 }
 bool fits(const cocod_token_scores_call *c, Layout layout, const ProductPlan &plan, const ProductParams &p, uint32_t m, uint32_t n, uint32_t splits)
@@ -433,8 +523,9 @@ bool fits(const cocod_token_scores_call *c, Layout layout, const ProductPlan &pl
     return fits_a_launch(size, blocks_of(size, layout == Layout::Weights, c->rows, c->groups, m, n, splits));
 }
 
-template <class E> hipError_t launch_gather(hipStream_t q, const Taking &taking, const cocod_token_scores_call *c, const Workspace &w, uint8_t *ws)
+template <class T> hipError_t launch_gather(hipStream_t q, const Taking &taking, const cocod_token_scores_call *c, const Workspace &w, uint8_t *ws)
 {
+    typedef typename T::elem E;
     const bool normal = taking.grad && kTypes[c->dtype] == Dtype::F16;
     uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
     float *row_scale = reinterpret_cast<float *>(ws + w.row_scale);
@@ -450,12 +541,14 @@ template <class E> hipError_t launch_gather(hipStream_t q, const Taking &taking,
         g.dh = static_cast<E *>(c->dh); g.lddh = c->lddh;
         g.norms = reinterpret_cast<const float4 *>(c->norms);
         g.scale = c->scale;
-        g.row_scale = normal ? row_scale : nullptr;
+        g.normal = normal;
+        g.row_scale = sizeof(E) == 2 ? row_scale : nullptr;
+        g.scaled = w.scaled != w.hidden ? reinterpret_cast<E *>(ws + w.scaled) : nullptr;
         g.top = reinterpret_cast<float *>(ws + w.top); g.none = reinterpret_cast<float *>(ws + w.none);
         g.one = reinterpret_cast<float *>(ws + w.one); g.target_slope = reinterpret_cast<float *>(ws + w.target_slope);
     }
     const uint64_t blocks = (c->rows + 3) / 4;
-    hipLaunchKernelGGL(scores_gather_kernel<E>, dim3(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks)), dim3(256), 0, q, taking, g);
+    hipLaunchKernelGGL(scores_gather_kernel<T>, dim3(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks)), dim3(256), 0, q, taking, g);
     return hipGetLastError();
 }
 
@@ -463,7 +556,8 @@ template <class T> hipError_t launch_scores(hipStream_t q, const Scores &p)
 {
     const uint64_t blocks = p.top ? p.taking.rows.rows : (p.taking.rows.rows + 3) / 4;
     const dim3 grid(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks));
-    if (p.top) hipLaunchKernelGGL((scores_kernel<T, 4>), grid, dim3(256), 0, q, p);
+    if (p.top && blocks <= kFewRows) hipLaunchKernelGGL((scores_kernel<T, 16>), grid, dim3(1024), 0, q, p);
+    else if (p.top) hipLaunchKernelGGL((scores_kernel<T, 4>), grid, dim3(256), 0, q, p);
     else       hipLaunchKernelGGL((scores_kernel<T, 1>), grid, dim3(256), 0, q, p);
     return hipGetLastError();
 }
@@ -522,7 +616,7 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     if (gathered) z = logits_operands(c, w, ws, true);
     if (!fits(c, Layout::Rows_NK, w.logits, z, 0, c->vocab, 1)) return launch_status(hipErrorInvalidConfiguration, what);
     if (gathered)
-        if (int rc = launch_status(t == Dtype::F32 ? launch_gather<float>(q, taking, c, w, ws) : launch_gather<uint16_t>(q, taking, c, w, ws), what)) return rc;
+        if (int rc = launch_status(t == Dtype::F32 ? launch_gather<F32>(q, taking, c, w, ws) : t == Dtype::BF16 ? launch_gather<Bf16>(q, taking, c, w, ws) : launch_gather<F16>(q, taking, c, w, ws), what)) return rc;
     const Tile tile = settle_tile(t, Layout::Rows_NK, w.logits.tile, z);
     const uint32_t cols = tile_cols(t, tile);
     z.offsets = c->offsets; z.ends = gathered ? reinterpret_cast<const int64_t *>(ws + w.ends) : nullptr; z.groups = c->groups; z.rows = c->rows;
@@ -592,10 +686,10 @@ int cocod_token_scores_grad(void *stream, const cocod_token_scores_call *c)
     taking.rows = {c->offsets, c->groups, c->rows, c->targets, c->vocab};
     taking.grad = 1;
     taking.d_logp = c->d_logp; taking.d_entropy = c->d_entropy;
-    if (int rc = launch_status(t == Dtype::F32 ? launch_gather<float>(q, taking, c, w, ws) : launch_gather<uint16_t>(q, taking, c, w, ws), what)) return rc;
+    if (int rc = launch_status(t == Dtype::F32 ? launch_gather<F32>(q, taking, c, w, ws) : t == Dtype::BF16 ? launch_gather<Bf16>(q, taking, c, w, ws) : launch_gather<F16>(q, taking, c, w, ws), what)) return rc;
     const uint32_t *index = reinterpret_cast<const uint32_t *>(ws + w.index);
     const int64_t *ends = reinterpret_cast<const int64_t *>(ws + w.ends);
-    const float *row_scale = t == Dtype::F16 ? reinterpret_cast<const float *>(ws + w.row_scale) : nullptr;
+    const float *row_scale = t != Dtype::F32 ? reinterpret_cast<const float *>(ws + w.row_scale) : nullptr;
     for (uint32_t i = 0; i < w.pieces; ++i) {
         const uint64_t v0 = i * w.piece;
         const uint32_t n = static_cast<uint32_t>(c->vocab - v0 < w.piece ? c->vocab - v0 : w.piece);

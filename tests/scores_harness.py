@@ -5,7 +5,8 @@ with the error d, that of an exponential (|x| + 2 steps at a distance x) and of 
 r = d + (300 + vocab / 64) 2^-23 + 2^-23 D of itself, with D = sum p |distance|; log(1 + rest) by at most r log(1 + rest), as rest / (1 + rest) <= log(1 + rest).
 D is off by d-changes of p (sum p |x - D| d <= 2 D d), by d itself and by roundings, (300 + vocab / 64) 2^-23 D + 2^-22 sum p x^2.  H changes by at most 2 H d, and both roundings.
 A probability is off by the factor q = r + 2 d + 80 steps + 2^-23 max |x| (x where it still counts: 104), so a slope a ([t] - p) - b p (x - D) by |a| p q + |b| p (|x - D| q + d + far D); then it is
-rounded by half a step of the type (fp16: not below half of 2^-38 of the group's largest |a| + 32 |b|, times 2, as a power of two is taken).  The products add what products add.
+rounded by half a step of the type (fp16: not below half of 2^-38 of the group's largest |a| + 32 |b|, times 2, as a power of two is taken), after a division by a number in 1/2 .. 1 by which
+the result is multiplied again (two steps of 2^-23; twice the fp16 floor), for de by way of h, which is rounded to the type as well.  The products add what products add.
 """
 import torch
 
@@ -63,9 +64,13 @@ def exact_scores(bounds, h, e, target, scale=1.0, d_logp=None, d_entropy=None):
         off = off + (u if t != torch.float32 else 4 * STEP) * (dz.abs() + off)
         if t == torch.float16:
             off = off + 2.0 ** -38 * scale * (a.abs() + 32 * b.abs()).max()
+        if t != torch.float32:
+            off = off + 2 * STEP * (dz.abs() + off)
         tiny = torch.finfo(t).smallest_normal * torch.finfo(t).eps
         for key, where, left, right, terms in (("dh", ids, (off, dz), ee, vocab), ("de", g, (off.t(), dz.t()), hh, len(ids))):
             out[key][where] = left[1] @ right
+            if key == "de" and t != torch.float32:
+                left = (left[0] + u * (left[0] + left[1].abs()), left[1])
             total = left[0] @ right.abs() + (terms + 8) * STEP * ((left[1].abs() + left[0]) @ right.abs())
             far[key][where] = total * (1 + u) + (u + 4 * STEP) * out[key][where].abs() + tiny
     out["part"] = part
