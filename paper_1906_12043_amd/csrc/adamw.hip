@@ -10,8 +10,12 @@
 // a function of (seed, tensor, worker, element): a multiply-and-shift mixer of 32 bits, three multiplications an element, where a
 // ten-round counter generator would cost more time than the memory leaves.  p' comes from m' and v' before they are rounded.
 //
-// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element, with 8-bit states 16.1.  A thread takes eight elements, four threads a
-// scale.  Tensors travel in the kernel's arguments, a launch for every kMostTensors of them, so nothing has to be laid out on the device and a captured
+// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 852-903 us, 5.6-5.9 TB/s), with 8-bit states 16.1 (138 M: 413 us, 5.4
+// TB/s; four streams read and five written, a copy reaches 6.6).  A thread takes four elements, eight lanes a scale.  What it took: four elements side by side instead of eight
+// in a thread, tiles within a tensor without a decision between their loads (a wait stood behind each: 8-bit 513 us), 8-bit states that find out once a wave whether
+// every code is a normal one and every number finite, past the caches where the states are larger than those.  Half the tile or twice and four times its elements, 512 or
+// 1024 threads, runs of tiles per die: no better.
+// Tensors travel in the kernel's arguments, a launch for every kMostTensors of them, so nothing has to be laid out on the device and a captured
 // launch holds all it needs.
 #include "operator_call.hpp"
 #include "row_access.hpp"
@@ -23,11 +27,14 @@ namespace {
 
 constexpr uint32_t kStateBlock = 32;                 // elements that share a scale
 constexpr int kThreads = 256;
-constexpr uint32_t kEach = 8;                        // elements of a thread
-constexpr uint32_t kTile = kThreads * kEach;         // of a block
+constexpr uint32_t kSpan = kThreads * 4;             // elements of a block's threads side by side, four each
+constexpr uint32_t kSpans = 1;                       // of them a tile has
+constexpr uint32_t kTile = kSpan * kSpans;
 constexpr uint32_t kMostTensors = 40;                // of a launch: its arguments stay below 4 KiB
 constexpr uint32_t kMostBlocks = 1u << 20;
 constexpr uint64_t kMostElements = 1ull << 40;       // of a tensor
+// More than the last-level cache holds goes past the caches (16 workers of 11.2 M, fp32: 852 us instead of 1001; 3 M in 16 and 8 bits: 17.1 instead of 16.1).
+constexpr uint64_t kLastLevelCache = 256ull << 20;
 
 struct Tensor {
     void *p;
@@ -51,199 +58,287 @@ struct AdamWParams {
 };
 static_assert(sizeof(AdamWParams) <= 4096, "arguments of a kernel");
 
-__device__ __forceinline__ float power(int e) { return __uint_as_float(static_cast<unsigned>(e + 127) << 23); }      // 2^e, e in -126 .. 127
-__device__ __forceinline__ float larger_of_block(float v)      // over the four threads of a block of 32
+template <bool STREAM, class V> __device__ __forceinline__ V fetch(const V *from)
 {
-    v = fmaxf(v, __shfl_xor(v, 1, 64));
-    return fmaxf(v, __shfl_xor(v, 2, 64));
+    if constexpr (STREAM) return __builtin_nontemporal_load(from); else return *from;
 }
-// Smallest e, not below low, for which the block's largest finite magnitude is at most 448 2^e.
-__device__ __forceinline__ int block_scale(float most, int low)
+template <bool STREAM, class V, class W> __device__ __forceinline__ void put(V *to, W v)
 {
-    if (!(most > 0.0f)) return low;
-    const int exp = __builtin_amdgcn_frexp_expf(most);
-    const int e = exp - (__builtin_amdgcn_frexp_mantf(most) <= 0.875f ? 9 : 8);
+    if constexpr (STREAM) __builtin_nontemporal_store(v, to); else *to = v;
+}
+
+// Four consecutive elements in fp32, and back; count < 4 at a tensor's end.
+// STREAM: past the caches.
+template <class T, bool STREAM> struct Four {
+    typedef typename T::elem elem;
+    typedef f4 __attribute__((aligned(4))) f4_any;
+    typedef u2 __attribute__((aligned(2))) u2_elems;
+    static __device__ __forceinline__ f4 load(const void *base, uint64_t at, uint32_t count)
+    {
+        const elem *from = static_cast<const elem *>(base) + at;
+        f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (count >= 4) {
+            if constexpr (sizeof(elem) == 4) return fetch<STREAM>(reinterpret_cast<const f4_any *>(from));
+            else {
+                const u2 w = fetch<STREAM>(reinterpret_cast<const u2_elems *>(from));
+                #pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = widen<T>(static_cast<elem>(w[j / 2] >> (16 * (j % 2))));
+                return v;
+            }
+        }
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) if (j < count) v[j] = widen<T>(from[j]);
+        return v;
+    }
+    static __device__ __forceinline__ void store(void *base, uint64_t at, uint32_t count, f4 v)
+    {
+        elem *to = static_cast<elem *>(base) + at;
+        if constexpr (sizeof(elem) == 4) {
+            if (count >= 4) { put<STREAM>(reinterpret_cast<f4_any *>(to), v); return; }
+            #pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = v[j];
+        } else {
+            const u2 w = {T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+            if (count >= 4) { put<STREAM>(reinterpret_cast<u2_elems *>(to), w); return; }
+            #pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = static_cast<elem>(w[j / 2] >> (16 * (j % 2)));
+        }
+    }
+};
+template <bool STREAM> __device__ __forceinline__ uint32_t load_codes(const void *base, uint64_t at, uint32_t count)
+{
+    typedef uint32_t __attribute__((aligned(1))) word_any;
+    const uint8_t *from = static_cast<const uint8_t *>(base) + at;
+    if (count >= 4) return fetch<STREAM>(reinterpret_cast<const word_any *>(from));
+    uint32_t w = 0;
+    #pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) if (j < count) w |= static_cast<uint32_t>(from[j]) << (8 * j);
+    return w;
+}
+template <bool STREAM> __device__ __forceinline__ void store_codes(void *base, uint64_t at, uint32_t count, uint32_t w)
+{
+    typedef uint32_t __attribute__((aligned(1))) word_any;
+    uint8_t *to = static_cast<uint8_t *>(base) + at;
+    if (count >= 4) { put<STREAM>(reinterpret_cast<word_any *>(to), w); return; }
+    #pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = static_cast<uint8_t>(w >> (8 * j));
+}
+
+// ---- states of 8 bits: a block of 32 lies in eight neighbouring lanes, four elements each --------------------------------
+
+__device__ __forceinline__ float power(int e) { return __uint_as_float(static_cast<unsigned>(e + 127) << 23); }      // 2^e, e in -126 .. 127
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int CTRL> __device__ __forceinline__ uint32_t larger_moved(uint32_t v)
+{
+    return larger(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ uint32_t larger_of_block(uint32_t v)
+{
+    return larger_moved<0x141>(larger_moved<0x4e>(larger_moved<0xb1>(v)));      // lanes 1 and 2 apart, eight lanes mirrored
+}
+// Smallest e, not below `low`, for which the magnitude with these bits is at most 448 2^e (448 = 1.75 * 2^8).
+__device__ __forceinline__ int block_scale(uint32_t bits, int low)
+{
+    const int e = static_cast<int>((bits + 0x1fffffu) >> 23) - 135;
     return e > low ? e : low;
 }
-
-// y >= 0 in units of the smallest code.  The code not above y, what it stands for and the step to the next one.
-struct Below { uint32_t code; float low, step; };
-__device__ __forceinline__ Below code_below(float y)
+__device__ __forceinline__ void decode(uint32_t codes, uint8_t scale, f4 &v)
 {
-    const uint32_t bits = __float_as_uint(y);
-    Below b;
-    if (y < 8.0f) {
-        b.code = static_cast<uint32_t>(y);
-        b.low = static_cast<float>(b.code);
-        b.step = 1.0f;
-    } else {
-        b.code = (bits >> 20) - (130u << 3) + 8;
-        b.low = __uint_as_float(bits & 0xfff00000u);
-        b.step = __uint_as_float((bits & 0x7f800000u) - (3u << 23));
-    }
-    return b;
-}
-// What a code stands for, times `unit` (the smallest code's value).
-__device__ __forceinline__ float value_of(uint32_t code, float unit)
-{
-    const uint32_t mag = code & 0x7f;
-    if (mag == 0x7f) return __uint_as_float(0x7fc00000u);
-    const float v = mag < 8 ? static_cast<float>(mag) : __uint_as_float((mag - 8 + (130u << 3)) << 20);
-    return (code & 0x80 ? -v : v) * unit;
-}
-__device__ __forceinline__ float unit_of(uint8_t scale)        // 2^(scale - 127 - 9), split where it leaves the normal range
-{
-    const int e = static_cast<int>(scale) - 136;
-    return power(e / 2) * power(e - e / 2);
+    const float unit = __uint_as_float(static_cast<unsigned>(scale) << 23);
+    const v2 low = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, unit, false), high = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, unit, true);
+    v = f4{low.x, low.y, high.x, high.y};
 }
 
-__device__ __forceinline__ uint32_t random_bits(uint64_t at, uint32_t stream)
+// Random bits of element `at` of a tensor; those of the elements behind it follow by adding kNextElement to x.
+constexpr uint32_t kNextElement = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t random_seed(uint64_t at, uint32_t stream) { return static_cast<uint32_t>(at) * kNextElement + static_cast<uint32_t>(at >> 32) * 0x85EBCA6Bu + stream; }
+__device__ __forceinline__ uint32_t mixed(uint32_t x)
 {
-    uint32_t x = static_cast<uint32_t>(at) * 0x9E3779B1u + static_cast<uint32_t>(at >> 32) * 0x85EBCA6Bu + stream;
     x = (x ^ (x >> 16)) * 0x7FEB352Du;
     x = (x ^ (x >> 15)) * 0x846CA68Bu;
     return x ^ (x >> 16);
 }
 
-// Eight consecutive elements in fp32, and back; count < 8 at a tensor's end.
-template <class T> __device__ __forceinline__ void load_eight(const void *base, uint64_t at, uint32_t count, float (&v)[kEach])
+// y in units of the smallest code.  A code is its neighbour below, plus one where the way from there to y, in 65536ths of the step, is above the random number.
+// Normal codes (y >= 8) are the upper bits of y's: adding 2^20 - 1 - 16 * random to the lower twenty carries where they are above 16 * random.
+constexpr uint32_t kCodeOfBits = 1032;               // y's upper bits less its code: 8 is code 8
+__device__ __forceinline__ uint32_t normal_code(float y, uint32_t random_up) { return (__float_as_uint(y) + (0xfffffu - 16u * random_up - (kCodeOfBits << 20))) >> 20; }
+__device__ __forceinline__ uint32_t any_code(float y, uint32_t random_up)
 {
-    typedef Piece<T> V;
-    const typename T::elem *from = static_cast<const typename T::elem *>(base) + at;
-    #pragma unroll
-    for (uint32_t h = 0; h < kEach; h += V::N) {
-        const u4 raw = count > h ? V::load(from + h, count - h) : u4{0, 0, 0, 0};
-        #pragma unroll
-        for (uint32_t j = 0; j < V::N; ++j) v[h + j] = V::value(raw, j);
-    }
+    if (y >= 8.0f) return normal_code(y, random_up);
+    const uint32_t code = static_cast<uint32_t>(y);
+    return code + ((y - static_cast<float>(code)) * 65536.0f > static_cast<float>(random_up) ? 1u : 0u);
 }
-template <class T> __device__ __forceinline__ void store_eight(void *base, uint64_t at, uint32_t count, const float (&v)[kEach])
+// The same for the root y of w, by the way of the squares; what is not zero gets a code that is not.
+__device__ __forceinline__ uint32_t normal_root(float y, float w, uint32_t random_up)
 {
-    typedef Piece<T> V;
-    typename T::elem *to = static_cast<typename T::elem *>(base) + at;
-    #pragma unroll
-    for (uint32_t h = 0; h < kEach; h += V::N) {
-        float part[V::N];
-        #pragma unroll
-        for (uint32_t j = 0; j < V::N; ++j) part[j] = v[h + j];
-        if (count > h) V::store(to + h, V::pack(part), count - h);
-    }
+    const uint32_t bits = __float_as_uint(y) & 0xfff00000u;
+    const float low = __uint_as_float(bits), high = __uint_as_float(bits + 0x100000u), low2 = low * low, way = w - low2;
+    return (bits >> 20) - kCodeOfBits + (way * 65536.0f > static_cast<float>(random_up) * fmaf(high, high, -low2) ? 1u : 0u);
 }
-__device__ __forceinline__ u2 load_codes(const void *base, uint64_t at, uint32_t count)
+__device__ __forceinline__ uint32_t any_root(float y, float w, uint32_t random_up, bool some)
 {
-    const uint8_t *from = static_cast<const uint8_t *>(base) + at;
-    if (count >= kEach) return *reinterpret_cast<const u2_any *>(from);
-    u2 w = {0, 0};
-    #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) if (j < count) w[j / 4] |= static_cast<unsigned>(from[j]) << (8 * (j % 4));
-    return w;
-}
-__device__ __forceinline__ void store_codes(void *base, uint64_t at, uint32_t count, u2 w)
-{
-    uint8_t *to = static_cast<uint8_t *>(base) + at;
-    if (count >= kEach) { *reinterpret_cast<u2_any *>(to) = w; return; }
-    #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) if (j < count) to[j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
+    if (y >= 8.0f) return normal_root(y, w, random_up);
+    const float low = floorf(y), high = low + 1.0f;
+    const uint32_t code = static_cast<uint32_t>(low) + ((w - low * low) * 65536.0f > static_cast<float>(random_up) * (high * high - low * low) ? 1u : 0u);
+    return code == 0 && some ? 1u : code;
 }
 
-template <class TP, class TG, bool EIGHT> __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWParams s)
+// Codes of four elements and the scales of their block.  Where every element of a wave is finite and has a normal code, nothing else is looked at.
+struct Stored { uint32_t m, v; uint8_t m_scale, v_scale; };
+__device__ __forceinline__ Stored store_states(const f4 &m, const f4 &v, const f4 &root, uint32_t x)
 {
     #pragma clang fp contract(off)
-    const cocod_adamw_now now = s.now_device ? *s.now_device : s.now;
-    if (now.skip) return;
-    const float root_bias2 = 1.0f / sqrtf(now.bias2);
-    for (uint64_t tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
-        const uint32_t per_worker = s.first_tile[s.count];
-        const uint32_t worker = static_cast<uint32_t>(tile / per_worker), in = static_cast<uint32_t>(tile - static_cast<uint64_t>(worker) * per_worker);
-        uint32_t lo = 0, hi = s.count;                         // first_tile[lo] <= in < first_tile[hi]
-        while (hi - lo > 1) { const uint32_t mid = (lo + hi) / 2; if (s.first_tile[mid] <= in) lo = mid; else hi = mid; }
-        const Tensor &t = s.tensor[lo];
-        const uint64_t at = static_cast<uint64_t>(in - s.first_tile[lo]) * kTile + threadIdx.x * kEach;       // of the tensor
-        const uint64_t base = worker * s.stride + at;
-        const uint32_t count = at >= t.n ? 0 : t.n - at < kEach ? static_cast<uint32_t>(t.n - at) : kEach;
-        const float lr = now.lr * t.lr_scale, keep = 1.0f - lr * t.weight_decay, step = lr / now.bias1;
-
-        float p[kEach], g[kEach], m[kEach], v[kEach];
-        load_eight<TP>(t.p, base, count, p);
-        load_eight<TG>(t.g, base, count, g);
-        uint64_t scale_at = 0;
-        if constexpr (EIGHT) {
-            const u2 cm = load_codes(t.m, base, count), cv = load_codes(t.v, base, count);
-            scale_at = worker * (s.stride / kStateBlock) + at / kStateBlock;
-            const float um = count ? unit_of(t.m_scales[scale_at]) : 0.0f, uv = count ? unit_of(t.v_scales[scale_at]) : 0.0f;
-            #pragma unroll
-            for (uint32_t j = 0; j < kEach; ++j) {
-                m[j] = value_of(cm[j / 4] >> (8 * (j % 4)), um);
-                const float root = value_of(cv[j / 4] >> (8 * (j % 4)), uv);
-                v[j] = root * root;
-            }
-        } else {
-            load_eight<F32>(t.m, base, count, m);
-            load_eight<F32>(t.v, base, count, v);
-        }
+    constexpr uint32_t kInfinity = 0x7f800000u;
+    uint32_t bm[4], bv[4], most_m = 0, most_v = 0;
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        bm[j] = __float_as_uint(m[j]) & 0x7fffffffu;
+        bv[j] = __float_as_uint(v[j]);                         // (never negative; a NaN's sign is left out)
+        most_m = larger(most_m, bm[j]);
+        most_v = larger(most_v, bv[j] & 0x7fffffffu);
+    }
+    most_m = larger_of_block(most_m);
+    most_v = larger_of_block(most_v);
+    bool plain = most_m < kInfinity && most_v < kInfinity;
+    if (!plain) {                                              // what is not finite does not count
+        most_m = most_v = 0;
         #pragma unroll
-        for (uint32_t j = 0; j < kEach; ++j) {
-            const float d = g[j] * now.grad_scale;
-            m[j] = m[j] * s.beta1 + d * s.rest1;
-            v[j] = v[j] * s.beta2 + (d * s.rest2) * d;
-            g[j] = sqrtf(v[j]);
-            p[j] = p[j] * keep - step * (m[j] * __builtin_amdgcn_rcpf(g[j] * root_bias2 + s.eps));
+        for (int j = 0; j < 4; ++j) {
+            if (bm[j] < kInfinity) most_m = larger(most_m, bm[j]);
+            if ((bv[j] & 0x7fffffffu) < kInfinity) most_v = larger(most_v, bv[j]);
         }
-        store_eight<TP>(t.p, base, count, p);
+        most_m = larger_of_block(most_m);
+        most_v = larger_of_block(most_v);
+    }
+    const int em = block_scale(most_m, -117), er = block_scale(__float_as_uint(sqrtf(__uint_as_float(most_v))), -51);
+    const float um = power(9 - em), ur = power(9 - er), ur2 = ur * ur;
+    float ym[4], yr[4], w[4];
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        ym[j] = fabsf(m[j]) * um;
+        yr[j] = root[j] * ur;
+        w[j] = v[j] * ur2;
+        plain = plain && ym[j] >= 8.0f && yr[j] >= 8.0f;
+    }
+    Stored out = {0, 0, static_cast<uint8_t>(em + 127), static_cast<uint8_t>(er + 127)};
+    if (__all(plain)) {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t random = mixed(x + j * kNextElement);
+            out.m |= (normal_code(ym[j], random >> 16) | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * j);
+            out.v |= normal_root(yr[j], w[j], random & 0xffffu) << (8 * j);
+        }
+    } else {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t random = mixed(x + j * kNextElement);
+            const bool fine_m = bm[j] < kInfinity, fine_v = (bv[j] & 0x7fffffffu) < kInfinity;
+            out.m |= ((fine_m ? any_code(ym[j], random >> 16) : 0x7fu) | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * j);
+            out.v |= (fine_v ? any_root(yr[j], w[j], random & 0xffffu, bv[j] != 0) : 0x7fu) << (8 * j);
+        }
+    }
+    return out;
+}
+
+// A tile of a tensor.  WHOLE: it lies within the tensor, so that nothing is decided between the loads, which are then all on their way at a time.
+struct Terms { float grad_scale, keep, step, root_bias2; uint32_t stream; };
+template <class TP, class TG, bool EIGHT, bool STREAM, bool WHOLE>
+__device__ __forceinline__ void update(const AdamWParams &s, const Tensor &t, const Terms &now, uint32_t worker, uint64_t first)
+{
+    #pragma clang fp contract(off)
+    f4 p[kSpans], g[kSpans], m[kSpans], v[kSpans];
+    uint32_t codes_m[kSpans], codes_v[kSpans], count[kSpans];
+    uint8_t scale_m[kSpans], scale_v[kSpans];
+    #pragma unroll
+    for (uint32_t u = 0; u < kSpans; ++u) {
+        const uint64_t at = first + u * kSpan, base = worker * s.stride + at;
+        count[u] = WHOLE ? 4 : at >= t.n ? 0 : t.n - at < 4 ? static_cast<uint32_t>(t.n - at) : 4;
+        p[u] = Four<TP, STREAM>::load(t.p, base, count[u]);
+        g[u] = Four<TG, STREAM>::load(t.g, base, count[u]);
+        if constexpr (EIGHT) {
+            const uint64_t scale_at = worker * (s.stride / kStateBlock) + at / kStateBlock;
+            codes_m[u] = load_codes<STREAM>(t.m, base, count[u]);
+            codes_v[u] = load_codes<STREAM>(t.v, base, count[u]);
+            scale_m[u] = count[u] ? t.m_scales[scale_at] : 0;
+            scale_v[u] = count[u] ? t.v_scales[scale_at] : 0;
+        } else {
+            m[u] = Four<F32, STREAM>::load(t.m, base, count[u]);
+            v[u] = Four<F32, STREAM>::load(t.v, base, count[u]);
+        }
+    }
+    #pragma unroll
+    for (uint32_t u = 0; u < kSpans; ++u) {
+        const uint64_t at = first + u * kSpan, base = worker * s.stride + at;
+        if constexpr (EIGHT) {
+            decode(codes_m[u], scale_m[u], m[u]);
+            decode(codes_v[u], scale_v[u], v[u]);
+            v[u] *= v[u];
+        }
+        f4 root;
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const float d = g[u][j] * now.grad_scale;
+            m[u][j] = m[u][j] * s.beta1 + d * s.rest1;
+            v[u][j] = v[u][j] * s.beta2 + (d * s.rest2) * d;
+            // (a code hangs on the last bit of the root only through its block's largest, of which store_states takes an exact one)
+            root[j] = EIGHT ? __builtin_amdgcn_sqrtf(v[u][j]) : sqrtf(v[u][j]);
+            p[u][j] = fmaf(-now.step, m[u][j] * __builtin_amdgcn_rcpf(fmaf(root[j], now.root_bias2, s.eps)), p[u][j] * now.keep);
+        }
+        Four<TP, STREAM>::store(t.p, base, count[u], p[u]);
         if constexpr (sizeof(typename TP::elem) == 4) {
-            if (t.copy && s.copy_dtype == COCOD_BF16) store_eight<Bf16>(t.copy, base, count, p);
-            else if (t.copy)                          store_eight<F16>(t.copy, base, count, p);
+            if (t.copy && s.copy_dtype == COCOD_BF16) Four<Bf16, STREAM>::store(t.copy, base, count[u], p[u]);
+            else if (t.copy)                          Four<F16, STREAM>::store(t.copy, base, count[u], p[u]);
         }
         if constexpr (!EIGHT) {
-            store_eight<F32>(t.m, base, count, m);
-            store_eight<F32>(t.v, base, count, v);
+            Four<F32, STREAM>::store(t.m, base, count[u], m[u]);
+            Four<F32, STREAM>::store(t.v, base, count[u], v[u]);
         } else {
-            float most_m = 0.0f, most_r = 0.0f;
             #pragma unroll
-            for (uint32_t j = 0; j < kEach; ++j) {
-                if (j >= count) { m[j] = 0.0f; v[j] = 0.0f; g[j] = 0.0f; }
-                if (__builtin_isfinite(m[j])) most_m = fmaxf(most_m, fabsf(m[j]));
-                if (__builtin_isfinite(g[j])) most_r = fmaxf(most_r, g[j]);
-            }
-            const int em = block_scale(larger_of_block(most_m), -117), er = block_scale(larger_of_block(most_r), -51);
-            const float um1 = power((9 - em) / 2), um2 = power((9 - em) - (9 - em) / 2), ur = power(9 - er);
-            const uint32_t stream = now.seed + (s.number + lo) * 0x632BE5ABu + worker * 0x85157AF5u;
-            u2 cm = {0, 0}, cv = {0, 0};
-            #pragma unroll
-            for (uint32_t j = 0; j < kEach; ++j) {
-                const uint32_t bits = random_bits(at + j, stream);
-                const bool fine_m = __builtin_isfinite(m[j]), fine_r = __builtin_isfinite(g[j]);
-                const float y = fine_m ? fabsf(m[j]) * um1 * um2 : 0.0f;
-                const Below a = code_below(y);
-                uint32_t code = a.code + (y - a.low > static_cast<float>(bits >> 16) * 0x1p-16f * a.step ? 1u : 0u);
-                code = (fine_m ? code : 0x7fu) | (__float_as_uint(m[j]) >> 31 << 7);
-                cm[j / 4] |= code << (8 * (j % 4));
-                const float r = fine_r ? g[j] * ur : 0.0f, w = fine_r ? v[j] * ur * ur : 0.0f;
-                const Below b = code_below(r);
-                code = b.code + (w - b.low * b.low > static_cast<float>(bits & 0xffffu) * 0x1p-16f * (b.step * (2.0f * b.low + b.step)) ? 1u : 0u);
-                if (code == 0 && g[j] > 0.0f) code = 1;
-                cv[j / 4] |= (fine_r ? code : 0x7fu) << (8 * (j % 4));
-            }
-            store_codes(t.m, base, count, cm);
-            store_codes(t.v, base, count, cv);
-            if (count && threadIdx.x % 4 == 0) {
-                t.m_scales[scale_at] = static_cast<uint8_t>(em + 127);
-                t.v_scales[scale_at] = static_cast<uint8_t>(er + 127);
+            for (uint32_t j = 0; j < 4; ++j) if (j >= count[u]) { m[u][j] = 0.0f; v[u][j] = 0.0f; root[j] = 0.0f; }
+            const Stored stored = store_states(m[u], v[u], root, random_seed(at, now.stream));
+            store_codes<STREAM>(t.m, base, count[u], stored.m);
+            store_codes<STREAM>(t.v, base, count[u], stored.v);
+            if (count[u] && threadIdx.x % 8 == 0) {
+                const uint64_t scale_at = worker * (s.stride / kStateBlock) + at / kStateBlock;
+                t.m_scales[scale_at] = stored.m_scale;
+                t.v_scales[scale_at] = stored.v_scale;
             }
         }
     }
 }
 
-template <class TP, class TG> void launch(hipStream_t q, bool eight, uint32_t grid, const AdamWParams &s)
+template <class TP, class TG, bool EIGHT, bool STREAM> __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWParams s)
 {
-    if (eight) hipLaunchKernelGGL((adamw_kernel<TP, TG, true>), dim3(grid), dim3(kThreads), 0, q, s);
-    else       hipLaunchKernelGGL((adamw_kernel<TP, TG, false>), dim3(grid), dim3(kThreads), 0, q, s);
+    const cocod_adamw_now now = s.now_device ? *s.now_device : s.now;
+    if (now.skip) return;
+    const uint32_t lane = threadIdx.x % 64, per_worker = s.first_tile[s.count];
+    const uint32_t mine = lane < s.count ? s.first_tile[lane] : ~0u;       // (a tile's number is below that)
+    static_assert(kMostTensors <= 64, "a lane a tensor");
+    for (uint64_t tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
+        const uint32_t worker = s.workers == 1 ? 0 : static_cast<uint32_t>(tile / per_worker), in = static_cast<uint32_t>(tile - static_cast<uint64_t>(worker) * per_worker);
+        const uint32_t which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(mine <= in)) - 1);
+        const Tensor &t = s.tensor[which];
+        const uint64_t begin = static_cast<uint64_t>(in - s.first_tile[which]) * kTile, first = begin + threadIdx.x * 4;
+        const float lr = now.lr * t.lr_scale;
+        const Terms terms = {now.grad_scale, 1.0f - lr * t.weight_decay, lr / now.bias1, 1.0f / sqrtf(now.bias2),
+                             now.seed + (s.number + which) * 0x632BE5ABu + worker * 0x85157AF5u};
+        if (t.n - begin >= kTile) update<TP, TG, EIGHT, STREAM, true>(s, t, terms, worker, first);
+        else                      update<TP, TG, EIGHT, STREAM, false>(s, t, terms, worker, first);
+    }
 }
-template <class TP> void launch(hipStream_t q, uint32_t grad, bool eight, uint32_t grid, const AdamWParams &s)
+
+template <class TP, class TG> void launch(hipStream_t q, bool eight, bool stream, uint32_t grid, const AdamWParams &s)
 {
-    if (grad == COCOD_F32)       launch<TP, F32>(q, eight, grid, s);
-    else if (grad == COCOD_BF16) launch<TP, Bf16>(q, eight, grid, s);
-    else                         launch<TP, F16>(q, eight, grid, s);
+    const auto kernel = eight ? (stream ? adamw_kernel<TP, TG, true, true> : adamw_kernel<TP, TG, true, false>)
+                              : (stream ? adamw_kernel<TP, TG, false, true> : adamw_kernel<TP, TG, false, false>);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, q, s);
+}
+template <class TP> void launch(hipStream_t q, uint32_t grad, bool eight, bool stream, uint32_t grid, const AdamWParams &s)
+{
+    if (grad == COCOD_F32)       launch<TP, F32>(q, eight, stream, grid, s);
+    else if (grad == COCOD_BF16) launch<TP, Bf16>(q, eight, stream, grid, s);
+    else                         launch<TP, F16>(q, eight, stream, grid, s);
 }
 
 bool finite_in(float v, float low, float high) { return std::isfinite(v) && v >= low && v < high; }
@@ -351,6 +446,11 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c)
     s.rest2 = static_cast<float>(1.0 - static_cast<double>(c->beta2));
     s.now_device = c->now;
     if (!c->now) s.now = {c->lr, c->grad_scale, bias(c->beta1, c->step), bias(c->beta2, c->step), c->seed, 0, {0, 0}};
+    const bool eight = c->state == COCOD_ADAMW_STATE_8BIT;
+    uint64_t elements = 0;
+    for (uint64_t i = 0; i < c->count; ++i) elements += c->tensors[i].n;
+    const uint64_t each = dtype_bytes(static_cast<Dtype>(c->dtype)) + dtype_bytes(static_cast<Dtype>(c->grad_dtype)) + (eight ? 2 : 8);
+    const bool stream_past = elements * each * c->workers > kLastLevelCache;
     const OnStreamDevice device(q);
     bool begun = false;
     auto flush = [&]() -> int {
@@ -359,10 +459,9 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c)
         begun = true;
         s.tiles = static_cast<uint64_t>(s.first_tile[s.count]) * s.workers;
         const uint32_t grid = static_cast<uint32_t>(s.tiles < kMostBlocks ? s.tiles : kMostBlocks);
-        const bool eight = c->state == COCOD_ADAMW_STATE_8BIT;
-        if (c->dtype == COCOD_F32)       launch<F32>(q, c->grad_dtype, eight, grid, s);
-        else if (c->dtype == COCOD_BF16) launch<Bf16>(q, c->grad_dtype, eight, grid, s);
-        else                             launch<F16>(q, c->grad_dtype, eight, grid, s);
+        if (c->dtype == COCOD_F32)       launch<F32>(q, c->grad_dtype, eight, stream_past, grid, s);
+        else if (c->dtype == COCOD_BF16) launch<Bf16>(q, c->grad_dtype, eight, stream_past, grid, s);
+        else                             launch<F16>(q, c->grad_dtype, eight, stream_past, grid, s);
         s.count = 0;
         return launch_status(hipGetLastError(), what);
     };

@@ -273,7 +273,7 @@ def test_states_of_8_bits(types, sizes, workers):
     assert np.array_equal(after[0][mark], before[0][mark]) and np.array_equal(after[1][mark], before[1][mark]) and x.p.rest_untouched()
 
 
-@pytest.mark.parametrize("magnitude", [0.0, 1e-42, 1e-30, 1e-12, 1.0, 1e12, 1e18, 3e38])
+@pytest.mark.parametrize("magnitude", [0.0, 1e-42, 1e-30, 3e-23, 1e-20, 1e-18, 1e-12, 1.0, 1e12, 1e18, 3e38])
 def test_states_of_8_bits_over_the_range(magnitude):
     x = Eight([4096], 1, 3)
     x.g.part(0).mul_(magnitude)
