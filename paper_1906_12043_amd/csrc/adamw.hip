@@ -33,8 +33,6 @@ constexpr uint32_t kTile = kSpan * kSpans;
 constexpr uint32_t kMostTensors = 40;                // of a launch: its arguments stay below 4 KiB
 constexpr uint32_t kMostBlocks = 1u << 20;
 constexpr uint64_t kMostElements = 1ull << 40;       // of a tensor
-// More than the last-level cache holds goes past the caches (16 workers of 11.2 M, fp32: 852 us instead of 1001; 3 M in 16 and 8 bits: 17.1 instead of 16.1).
-constexpr uint64_t kLastLevelCache = 256ull << 20;
 
 struct Tensor {
     void *p;
@@ -58,29 +56,18 @@ struct AdamWParams {
 };
 static_assert(sizeof(AdamWParams) <= 4096, "arguments of a kernel");
 
-template <bool STREAM, class V> __device__ __forceinline__ V fetch(const V *from)
-{
-    if constexpr (STREAM) return __builtin_nontemporal_load(from); else return *from;
-}
-template <bool STREAM, class V, class W> __device__ __forceinline__ void put(V *to, W v)
-{
-    if constexpr (STREAM) __builtin_nontemporal_store(v, to); else *to = v;
-}
-
 // Four consecutive elements in fp32, and back; count < 4 at a tensor's end.
 // STREAM: past the caches.
 template <class T, bool STREAM> struct Four {
     typedef typename T::elem elem;
-    typedef f4 __attribute__((aligned(4))) f4_any;
-    typedef u2 __attribute__((aligned(2))) u2_elems;
     static __device__ __forceinline__ f4 load(const void *base, uint64_t at, uint32_t count)
     {
         const elem *from = static_cast<const elem *>(base) + at;
         f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         if (count >= 4) {
-            if constexpr (sizeof(elem) == 4) return fetch<STREAM>(reinterpret_cast<const f4_any *>(from));
+            if constexpr (sizeof(elem) == 4) return __builtin_bit_cast(f4, fetch16<STREAM>(from));
             else {
-                const u2 w = fetch<STREAM>(reinterpret_cast<const u2_elems *>(from));
+                const u2 w = fetch8<STREAM>(from);
                 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = widen<T>(static_cast<elem>(w[j / 2] >> (16 * (j % 2))));
                 return v;
@@ -94,12 +81,12 @@ template <class T, bool STREAM> struct Four {
     {
         elem *to = static_cast<elem *>(base) + at;
         if constexpr (sizeof(elem) == 4) {
-            if (count >= 4) { put<STREAM>(reinterpret_cast<f4_any *>(to), v); return; }
+            if (count >= 4) { put16<STREAM>(to, __builtin_bit_cast(u4, v)); return; }
             #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = v[j];
         } else {
             const u2 w = {T::pack(v[0], v[1]), T::pack(v[2], v[3])};
-            if (count >= 4) { put<STREAM>(reinterpret_cast<u2_elems *>(to), w); return; }
+            if (count >= 4) { put8<STREAM>(to, w); return; }
             #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = static_cast<elem>(w[j / 2] >> (16 * (j % 2)));
         }
@@ -107,9 +94,8 @@ template <class T, bool STREAM> struct Four {
 };
 template <bool STREAM> __device__ __forceinline__ uint32_t load_codes(const void *base, uint64_t at, uint32_t count)
 {
-    typedef uint32_t __attribute__((aligned(1))) word_any;
     const uint8_t *from = static_cast<const uint8_t *>(base) + at;
-    if (count >= 4) return fetch<STREAM>(reinterpret_cast<const word_any *>(from));
+    if (count >= 4) return fetch4<STREAM>(from);
     uint32_t w = 0;
     #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) if (j < count) w |= static_cast<uint32_t>(from[j]) << (8 * j);
@@ -117,9 +103,8 @@ template <bool STREAM> __device__ __forceinline__ uint32_t load_codes(const void
 }
 template <bool STREAM> __device__ __forceinline__ void store_codes(void *base, uint64_t at, uint32_t count, uint32_t w)
 {
-    typedef uint32_t __attribute__((aligned(1))) word_any;
     uint8_t *to = static_cast<uint8_t *>(base) + at;
-    if (count >= 4) { put<STREAM>(reinterpret_cast<word_any *>(to), w); return; }
+    if (count >= 4) { put4<STREAM>(to, w); return; }
     #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) if (j < count) to[j] = static_cast<uint8_t>(w >> (8 * j));
 }
@@ -450,6 +435,7 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c)
     uint64_t elements = 0;
     for (uint64_t i = 0; i < c->count; ++i) elements += c->tensors[i].n;
     const uint64_t each = dtype_bytes(static_cast<Dtype>(c->dtype)) + dtype_bytes(static_cast<Dtype>(c->grad_dtype)) + (eight ? 2 : 8);
+    // (16 workers of 11.2 M, fp32: 852 us instead of 1001; 3 M in 16 and 8 bits: 17.1 instead of 16.1)
     const bool stream_past = elements * each * c->workers > kLastLevelCache;
     const OnStreamDevice device(q);
     bool begun = false;

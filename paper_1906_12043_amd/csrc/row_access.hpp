@@ -5,6 +5,38 @@
 namespace cocod {
 namespace {
 
+// What a launch moves beyond this goes past the caches (STREAM below): it would only displace itself.
+constexpr uint64_t kLastLevelCache = 256ull << 20;
+
+// 16, 8 or 4 bytes at any address.  (An alignment is lost where a template deduces a type, so these name theirs.)
+typedef u4 __attribute__((aligned(1))) u4_at;
+typedef u2 __attribute__((aligned(1))) u2_at;
+typedef uint32_t __attribute__((aligned(1))) u1_at;
+template <bool STREAM> __device__ __forceinline__ u4 fetch16(const void *from)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const u4_at *>(from)); else return *static_cast<const u4_at *>(from);
+}
+template <bool STREAM> __device__ __forceinline__ u2 fetch8(const void *from)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const u2_at *>(from)); else return *static_cast<const u2_at *>(from);
+}
+template <bool STREAM> __device__ __forceinline__ uint32_t fetch4(const void *from)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const u1_at *>(from)); else return *static_cast<const u1_at *>(from);
+}
+template <bool STREAM> __device__ __forceinline__ void put16(void *to, u4 v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u4_at *>(to)); else *static_cast<u4_at *>(to) = v;
+}
+template <bool STREAM> __device__ __forceinline__ void put8(void *to, u2 v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u2_at *>(to)); else *static_cast<u2_at *>(to) = v;
+}
+template <bool STREAM> __device__ __forceinline__ void put4(void *to, uint32_t v)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<u1_at *>(to)); else *static_cast<u1_at *>(to) = v;
+}
+
 template <class T> __device__ __forceinline__ float widen(typename T::elem v)
 {
     if constexpr (sizeof(v) == 4) return v;
@@ -17,13 +49,13 @@ template <class T> struct Piece {
     typedef typename T::elem elem;
     static constexpr uint32_t N = 16 / sizeof(elem);
 
-    static __device__ __forceinline__ u4 load(const elem *from) { return *reinterpret_cast<const u4_any *>(from); }
-    static __device__ __forceinline__ void store(elem *to, u4 raw) { *reinterpret_cast<u4_any *>(to) = raw; }
+    template <bool STREAM = false> static __device__ __forceinline__ u4 load(const elem *from) { return fetch16<STREAM>(from); }
+    template <bool STREAM = false> static __device__ __forceinline__ void store(elem *to, u4 raw) { put16<STREAM>(to, raw); }
 
     // the first `count` of them (all where count >= N); the others are zeros
-    static __device__ __forceinline__ u4 load(const elem *from, uint32_t count)
+    template <bool STREAM = false> static __device__ __forceinline__ u4 load(const elem *from, uint32_t count)
     {
-        if (count >= N) return load(from);
+        if (count >= N) return load<STREAM>(from);
         u4 raw = {0, 0, 0, 0};
         #pragma unroll
         for (uint32_t j = 0; j < N; ++j)
@@ -33,9 +65,9 @@ template <class T> struct Piece {
             }
         return raw;
     }
-    static __device__ __forceinline__ void store(elem *to, u4 raw, uint32_t count)
+    template <bool STREAM = false> static __device__ __forceinline__ void store(elem *to, u4 raw, uint32_t count)
     {
-        if (count >= N) { store(to, raw); return; }
+        if (count >= N) { store<STREAM>(to, raw); return; }
         #pragma unroll
         for (uint32_t j = 0; j < N; ++j)
             if (j < count) {
