@@ -1,0 +1,149 @@
+"""The operators as they are used together: a training step of a model whose tokens go to two of five experts of two layers each, with the log probabilities and entropies of the tokens as
+its objective and AdamW as its step - against the same step in 64 bits by automatic differentiation, eager and replayed.
+
+Bound.  A product of K terms in fp32 is off by at most (K + 8) 2^-23 times the sum of magnitudes, which for K terms of random signs is below sqrt(K) times the result, in the 2-norm: with
+K <= 72, 80 * 2^-23 * 8.5 = 8.1e-5 of the result.  The longest path (router's rows, two layers, weighted sum, logits, slopes, and the same backwards) has five products and
+four sums of few terms: below 5e-4, in the 2-norm.  A step from m = 0 and v = 0.04 everywhere moves a parameter by lr (0.1 g) / (sqrt(0.98 * 0.04 + 0.02 g^2 ...) + eps): a smooth function, whose
+relative error in the 2-norm is at most that of g plus 14 roundings.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_1906_12043_amd as P
+
+pytestmark = pytest.mark.gpu
+T, K, G, C, F, V = 300, 2, 5, 64, 72, 413            # tokens, choices, experts, columns, hidden columns, entries
+BOUND = 5e-4
+LR, B1, B2, EPS = 1e-2, 0.9, 0.98, 1e-8
+
+
+class Step:
+    """Buffers and descriptions, as a program keeps them."""
+
+    def __init__(self, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *s, std=1.0: torch.randn(*s, generator=gen, device="cuda") * std          # noqa: E731
+        new = lambda *s: torch.zeros(s, device="cuda")                                          # noqa: E731
+        self.x, self.w1, self.w2, self.e = rand(T, C), rand(G, C, F, std=C ** -0.5), rand(G, F, C, std=F ** -0.5), rand(V, C, std=2 * C ** -0.5)
+        self.experts = torch.zeros((T, K), dtype=torch.int32, device="cuda")
+        self.weights, self.targets = new(T, K), torch.zeros(T, dtype=torch.int32, device="cuda")
+        self.d_logp, self.d_entropy = new(T), new(T)
+        self.place, self.offsets = torch.zeros_like(self.experts), torch.zeros(G + 1, dtype=torch.int64, device="cuda")
+        self.one_group = torch.tensor([0, T], device="cuda")
+        R = T * K
+        self.xs, self.hidden, self.ys, self.y = new(R, C), new(R, F), new(R, C), new(T, C)
+        self.logp, self.entropy, self.norms, self.dy = new(T), new(T), new(T, 4), new(T, C)
+        self.dys, self.dhidden, self.dxs, self.dx, self.dweights = new(R, C), new(R, F), new(R, C), new(T, C), new(T, K)
+        self.dw1, self.dw2, self.de = torch.zeros_like(self.w1), torch.zeros_like(self.w2), torch.zeros_like(self.e)
+        self.route = P.Route(dtype=P.F32, groups=G, choices=K, tokens=T, width=C, experts=self.experts, ld_experts=K, place=self.place, ld_place=K, offsets=self.offsets,
+                             weights=self.weights, ld_weights=K, x=self.x, ldx=C, xs=self.xs, ldxs=C, ys=self.ys, ldys=C, y=self.y, ldy=C, dy=self.dy, lddy=C, dys=self.dys, lddys=C,
+                             dweights=self.dweights, ld_dweights=K, dxs=self.dxs, lddxs=C, dx=self.dx, lddx=C)
+        layer = dict(dtype=P.F32, groups=G, rows=R, offsets=self.offsets, dw_dtype=P.F32)
+        self.first = P.Grouped(inner=C, outer=F, x=self.xs, ldx=C, w=self.w1, ldw=F, w_stride=C * F, y=self.hidden, ldy=F, dy=self.dhidden, lddy=F, dx=self.dxs, lddx=C, dw=self.dw1,
+                               lddw=F, dw_stride=C * F, flags=P.GROUPED_RELU_OUT, **layer)
+        self.second = P.Grouped(inner=F, outer=C, x=self.hidden, ldx=F, w=self.w2, ldw=C, w_stride=C * F, y=self.ys, ldy=C, dy=self.dys, lddy=C, dx=self.dhidden, lddx=F, dw=self.dw2,
+                                lddw=C, dw_stride=C * F, flags=P.GROUPED_RELU_IN, **layer)
+        self.head = P.TokenScores(dtype=P.F32, groups=1, rows=T, dim=C, vocab=V, offsets=self.one_group, h=self.y, ldh=C, e=self.e, lde=C, e_stride=V * C, targets=self.targets, scale=0.9,
+                                  logp=self.logp, entropy=self.entropy, norms=self.norms, d_logp=self.d_logp, d_entropy=self.d_entropy, dh=self.dy, lddh=C, de=self.de, ldde=C,
+                                  de_stride=V * C)
+        need = max(P.route_workspace(self.route), P.token_scores_workspace(self.head, P.TOKEN_SCORES_FORWARD), P.token_scores_workspace(self.head, P.TOKEN_SCORES_GRAD), 256)
+        self.ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        self.route.set(workspace=self.ws, workspace_bytes=need)
+        self.head.set(workspace=self.ws, workspace_bytes=need)
+        self.params = [(self.w1, self.dw1), (self.w2, self.dw2), (self.e, self.de)]
+        self.states = [(torch.zeros_like(p), torch.full_like(p, 0.04)) for p, _ in self.params]
+        self.adamw = P.AdamW(tensors=[dict(n=p.numel(), p=p, g=g, m=m, v=v, weight_decay=0.05) for (p, g), (m, v) in zip(self.params, self.states)], dtype=P.F32, grad_dtype=P.F32,
+                             lr=LR, beta1=B1, beta2=B2, eps=EPS, step=100)
+
+    def batch(self, seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.x.copy_(torch.randn(T, C, generator=gen, device="cuda"))
+        score = torch.rand(T, G, generator=gen, device="cuda")
+        best, which = torch.topk(score, K, dim=1)
+        self.experts.copy_(which)
+        self.experts[::17] = -1                               # padded tokens
+        self.weights.copy_(torch.softmax(best, 1))
+        self.targets.copy_(torch.randint(-1, V, (T,), generator=gen, device="cuda"))
+        self.d_logp.copy_(torch.randn(T, generator=gen, device="cuda"))
+        self.d_entropy.fill_(0.1)
+
+    def run(self, stream):
+        P.route_sort(stream, self.route)
+        P.route_dispatch(stream, self.route)
+        P.grouped_forward(stream, self.first)
+        P.grouped_forward(stream, self.second)
+        P.route_combine(stream, self.route)
+        P.token_scores(stream, self.head)
+        P.token_scores_grad(stream, self.head)
+        P.route_combine_grad(stream, self.route)
+        P.grouped_weight_grad(stream, self.second)
+        P.grouped_input_grad(stream, self.second)
+        P.grouped_weight_grad(stream, self.first)
+        P.grouped_input_grad(stream, self.first)
+        P.route_dispatch_grad(stream, self.route)
+        P.adamw(stream, self.adamw)
+
+    def outputs(self):
+        return dict(y=self.y, logp=self.logp, entropy=self.entropy, dx=self.dx, dweights=self.dweights, dw1=self.dw1, dw2=self.dw2, de=self.de, w1=self.w1, w2=self.w2, e=self.e)
+
+
+def plain(s):
+    """The same step in 64 bits, from the step's present parameters, states and batch."""
+    d = torch.float64
+    x, w, w1, w2, e = (t.to(d).clone().requires_grad_() for t in (s.x, s.weights, s.w1, s.w2, s.e))
+    rows = []
+    for t in range(T):
+        y = torch.zeros(C, dtype=d, device="cuda")
+        for j in range(K):
+            g = int(s.experts[t, j])
+            if g >= 0:
+                y = y + w[t, j] * (torch.relu(x[t] @ w1[g]) @ w2[g])
+        rows.append(y)
+    y = torch.stack(rows)
+    lp = torch.log_softmax(float(torch.tensor(0.9)) * (y @ e.t()), 1)
+    keep = (s.targets >= 0).to(d)
+    logp = lp.gather(1, s.targets.clamp(min=0).long()[:, None])[:, 0] * keep
+    entropy = -(lp.exp() * lp).sum(1) * keep
+    (logp * s.d_logp.to(d) + entropy * s.d_entropy.to(d)).sum().backward()
+    out = dict(y=y, logp=logp, entropy=entropy, dx=x.grad, dweights=w.grad, dw1=w1.grad, dw2=w2.grad, de=e.grad)
+    for name, p, (m, v) in zip(("w1", "w2", "e"), (w1, w2, e), s.states):
+        m_new, v_new = B1 * m.to(d) + (1 - B1) * p.grad, B2 * v.to(d) + (1 - B2) * p.grad ** 2
+        out[name] = p.detach() * (1 - LR * 0.05) - LR * (m_new / (1 - B1 ** 100)) / (torch.sqrt(v_new / (1 - B2 ** 100)) + EPS)
+    return {k: v.detach() for k, v in out.items()}
+
+
+def far(a, b):
+    return float(torch.linalg.norm(a.double() - b) / torch.linalg.norm(b))
+
+
+def test_a_training_step():
+    s = Step()
+    s.batch(1)
+    want = plain(s)
+    s.run(torch.cuda.current_stream())
+    for k, got in s.outputs().items():
+        assert far(got, want[k]) <= BOUND, (k, far(got, want[k]))
+    assert bool((s.dx[::17] == 0).all()) and bool((s.dweights[::17] == 0).all())
+
+
+def test_the_same_steps_replayed():
+    a, b = Step(), Step()
+    side = torch.cuda.Stream()
+    a.batch(5)
+    b.batch(5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.run(side)
+    for k in range(4):
+        a.batch(10 + k)
+        b.batch(10 + k)
+        a.run(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for (name, x), y in zip(a.outputs().items(), b.outputs().values()):
+            assert torch.equal(x, y), (k, name)
+    assert math.isfinite(float(a.e.sum()))
