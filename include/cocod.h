@@ -541,7 +541,7 @@ typedef struct cocod_token_scores_call {
     uint64_t workspace_bytes;
 } cocod_token_scores_call;
 
-/* Bytes of workspace that the call of this direction needs (with alternatives: rows * vocab bytes, and a little); reads the sizes, top, piece, and whether dh and de are NULL. */
+/* Bytes of workspace that the call of this direction needs (with alternatives: rows * (vocab + 8 top) bytes, and a little); reads the sizes, top, piece, and whether dh and de are NULL. */
 int cocod_token_scores_workspace(const cocod_token_scores_call *c, int direction, uint64_t *bytes);
 int cocod_token_scores(void *stream, const cocod_token_scores_call *c);
 int cocod_token_scores_grad(void *stream, const cocod_token_scores_call *c);

@@ -9,8 +9,8 @@
 // sure of its token; elsewhere p_t is at most one half.  D comes from distances, so nothing cancels in H (both parts are positive) nor in d_v - D.
 //
 // Forward: one product, whose epilogue leaves m, rest and sum d exp d of every row and column tile and, where alternatives are wanted, the largest of every
-// four columns (1/4 of the logits: 1 GiB at 8192 x 131072).  Then a block per row joins them, finds the tiles with the `top` largest maxima, in these the
-// quads (any of the `top` largest entries lies in one of them, and of equal ones those in front), forms the quads' logits again, four dot
+// four columns (1/4 of the logits: 1 GiB at 8192 x 131072).  Then a wave per row joins them and finds the tiles with the `top` largest maxima, and in these the
+// quads (any of the `top` largest entries lies in one of them, and of equal ones those in front); a block per row forms the quads' logits again, four dot
 // products each, and sorts.  A quad's largest entry keeps the product's bits, so that the alternatives agree with log p_t; the others may
 // differ from the product's in the order of their sums.  No atomics: results do not depend on the order of blocks.
 //
@@ -30,10 +30,15 @@ namespace cocod {
 namespace {
 
 constexpr uint64_t kMaxScoreRows = 1ull << 26;
-constexpr uint32_t kMostTop = 32, kFewRows = 256;
+constexpr uint32_t kMostTop = 32;
+// Up to so many rows four waves take a row's statistics instead of one (32000 entries: 300 rows with 20 alternatives 23 us instead of 37, 2000 with 8 23 against 16), and sixteen
+// its alternatives instead of four (300 rows with 20: 31 against 26).
+constexpr uint32_t kFewRows = 512, kVeryFewRows = 64;
 constexpr float kEntropyBound = 32.0f, kSlopeScale16 = 0x1p14f;
 // Up to so many bytes of hidden states per group rows stay where they are, those without a target among them.
 constexpr uint64_t kLeaveHere = 1u << 20;
+// Up to so many bytes per group the block that finds the rows also copies them (9 rows of 1728 in fp16: 5 us instead of 10).
+constexpr uint64_t kGatherHere = 32u << 10;
 
 // Which rows take part, and with what slopes.
 struct Taking {
@@ -50,11 +55,74 @@ __device__ __forceinline__ bool takes_part(const Taking &p, uint64_t r)
 }
 __device__ __forceinline__ bool in_groups(const Rows &p, uint64_t r) { return r >= clamped(p, 0) && r < clamped(p, p.groups); }
 
+// Copies of the rows that take part, and what their slopes are made of.
+template <class E> struct Gather {
+    const uint32_t *index;
+    const E *h;
+    uint64_t ldh;
+    uint32_t dim;
+    E *out;
+    uint64_t pitch;
+    E *scaled;                        // non-null: rows times the mantissa of their target's slope
+    // gradient
+    E *dh;                            // may be null
+    uint64_t lddh;
+    const float4 *norms;
+    float scale;
+    int normal;                       // row_scale holds the group's factor
+    float *row_scale;                 // may be null (fp32: nothing is taken out)
+    float *top, *none, *one, *target_slope;
+};
+// A row times a factor of at most 1, rounded to the type.
+template <class T> __device__ __forceinline__ void scaled_row(const typename T::elem *src, uint32_t dim, typename T::elem *dst, uint64_t pitch, float factor, uint32_t lane)
+{
+    typedef Piece<T> V;
+    for (uint32_t j = lane * V::N; j < pitch; j += 64 * V::N) {
+        const u4 raw = j < dim ? V::load(src + j, dim - j) : u4{0, 0, 0, 0};
+        float v[V::N];
+        #pragma unroll
+        for (uint32_t i = 0; i < V::N; ++i) v[i] = V::value(raw, i) * factor;
+        V::store(dst + j, V::pack(v));
+    }
+}
+// Row r of the copies, from row `from` of the caller's, by a wave.
+template <class T> __device__ __forceinline__ void gather_row(const Taking &p, const Gather<typename T::elem> &q, uint64_t r, uint32_t from, uint32_t lane)
+{
+    const typename T::elem *h = q.h + from * q.ldh;
+    copy_row(h, q.dim, q.out + r * q.pitch, q.pitch, lane);
+    if (!p.grad) return;
+    const float4 n = q.norms[from];                            // top, rest, D, distance of the target
+    const float a = slope_of_logp(p, from), b = slope_of_entropy(p, from), inverse = 1.0f / (1.0f + n.y);
+    const float back = q.normal ? q.row_scale[r] : 1.0f, k = q.scale / back;
+    const float pt = expf(n.w) * inverse, others = n.w == 0.0f ? n.y * inverse : 1.0f - pt;
+    float target = (a * others + b * pt * (n.z - n.w)) * k, mantissa = 1.0f;
+    if (q.row_scale && p.rows.target && fabsf(target) > 0x1p-126f && fabsf(target) < 0x1p126f) {
+        mantissa = __builtin_amdgcn_frexp_mantf(fabsf(target));       // in 1/2 .. 1
+        target = copysignf(ldexpf(1.0f, __builtin_amdgcn_frexp_expf(target)), target);
+    }
+    if (q.scaled) scaled_row<T>(h, q.dim, q.scaled + r * q.pitch, q.pitch, mantissa, lane);
+    if (lane == 0) {
+        const float even = inverse * k / mantissa;
+        q.top[r] = n.x;
+        q.none[r] = (b * n.z - a) * even;
+        q.one[r] = -b * even;
+        q.target_slope[r] = target;
+        if (q.row_scale) q.row_scale[r] = back * mantissa;
+    }
+}
+// Row r of the caller's: no gradient where it takes no part.
+template <class T> __device__ __forceinline__ void clear_row(const Taking &p, const Gather<typename T::elem> &q, uint64_t r, uint32_t lane)
+{
+    if (p.grad && q.dh && !takes_part(p, r))
+        for (uint32_t j = lane; j < q.dim; j += 64) q.dh[r * q.lddh + j] = 0;
+}
+
 // One block per group: the rows that take part, in order, to the front of the group's part of `index`; kNoRow behind them.  NORMAL: the group's power of
-// two, for the table's gradient and row by row.
+// two, for the table's gradient and row by row.  HERE: the copies as well (a launch less where there is little to copy).
 constexpr int kTakeThreads = 1024;
-template <bool NORMAL> __global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, float scale, uint32_t *index, int32_t *target, int64_t *ends, float *group_scale,
-                                                                                   float *row_scale)
+template <class T, bool NORMAL, bool HERE>
+__global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, float scale, uint32_t *index, int32_t *target, int64_t *ends, float *group_scale, float *row_scale,
+                                                            const Gather<typename T::elem> gather)
 {
     __shared__ uint32_t counts[kTakeThreads / 64];
     __shared__ float most[kTakeThreads / 64];
@@ -94,72 +162,29 @@ template <bool NORMAL> __global__ __launch_bounds__(kTakeThreads) void take_kern
         if (threadIdx.x == 0) group_scale[g] = back;
         for (uint64_t r = begin + threadIdx.x; r < at; r += kTakeThreads) row_scale[r] = back;
     }
-}
-
-// Gathered copies of the rows, a wave a row, and what a row's slopes are made of.
-template <class E> struct Gather {
-    const uint32_t *index;
-    const E *h;
-    uint64_t ldh;
-    uint32_t dim;
-    E *out;
-    uint64_t pitch;
-    E *scaled;                        // non-null: rows times the mantissa of their target's slope
-    // gradient
-    E *dh;                            // may be null
-    uint64_t lddh;
-    const float4 *norms;
-    float scale;
-    int normal;                       // row_scale holds the group's factor
-    float *row_scale;                 // may be null (fp32: nothing is taken out)
-    float *top, *none, *one, *target_slope;
-};
-constexpr uint32_t kMostRowBlocks = 1u << 23;
-// A row times a factor of at most 1, rounded to the type.
-template <class T> __device__ __forceinline__ void scaled_row(const typename T::elem *src, uint32_t dim, typename T::elem *dst, uint64_t pitch, float factor, uint32_t lane)
-{
-    typedef Piece<T> V;
-    for (uint32_t j = lane * V::N; j < pitch; j += 64 * V::N) {
-        const u4 raw = j < dim ? V::load(src + j, dim - j) : u4{0, 0, 0, 0};
-        float v[V::N];
-        #pragma unroll
-        for (uint32_t i = 0; i < V::N; ++i) v[i] = V::value(raw, i) * factor;
-        V::store(dst + j, V::pack(v));
+    if constexpr (HERE) {
+        __syncthreads();                                       // (also the block's writes of index and row_scale)
+        for (uint64_t r = begin + wave; r < end; r += kTakeThreads / 64) {
+            if (r < at) {
+                // Groups whose offsets do not ascend share rows, and the block of another one may have left kNoRow in this place since.
+                const uint32_t from = index[r];
+                if (from != kNoRow) gather_row<T>(p, gather, r, from, lane);
+            }
+            clear_row<T>(p, gather, r, lane);
+        }
     }
 }
+
+// The copies by a launch of their own, a wave a row.
+constexpr uint32_t kMostRowBlocks = 1u << 23, kMostAlternativeBlocks = 1u << 21;
 template <class T> __global__ __launch_bounds__(256) void scores_gather_kernel(const Taking p, const Gather<typename T::elem> q)
 {
-    typedef typename T::elem E;
     const uint32_t lane = threadIdx.x % 64;
     for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64; r < p.rows.rows; r += static_cast<uint64_t>(gridDim.x) * 4) {
         if (!in_groups(p.rows, r)) continue;
         const uint32_t from = q.index[r];
-        if (from != kNoRow) {
-            const E *h = q.h + from * q.ldh;
-            copy_row(h, q.dim, q.out + r * q.pitch, q.pitch, lane);
-            if (p.grad) {
-                const float4 n = q.norms[from];                // top, rest, D, distance of the target
-                const float a = slope_of_logp(p, from), b = slope_of_entropy(p, from), inverse = 1.0f / (1.0f + n.y);
-                const float back = q.normal ? q.row_scale[r] : 1.0f, k = q.scale / back;
-                const float pt = expf(n.w) * inverse, others = n.w == 0.0f ? n.y * inverse : 1.0f - pt;
-                float target = (a * others + b * pt * (n.z - n.w)) * k, mantissa = 1.0f;
-                if (q.row_scale && p.rows.target && fabsf(target) > 0x1p-126f && fabsf(target) < 0x1p126f) {
-                    mantissa = __builtin_amdgcn_frexp_mantf(fabsf(target));       // in 1/2 .. 1
-                    target = copysignf(ldexpf(1.0f, __builtin_amdgcn_frexp_expf(target)), target);
-                }
-                if (q.scaled) scaled_row<T>(h, q.dim, q.scaled + r * q.pitch, q.pitch, mantissa, lane);
-                if (lane == 0) {
-                    const float even = inverse * k / mantissa;
-                    q.top[r] = n.x;
-                    q.none[r] = (b * n.z - a) * even;
-                    q.one[r] = -b * even;
-                    q.target_slope[r] = target;
-                    if (q.row_scale) q.row_scale[r] = back * mantissa;
-                }
-            }
-        }
-        if (p.grad && q.dh && !takes_part(p, r))
-            for (uint32_t j = lane; j < q.dim; j += 64) q.dh[r * q.lddh + j] = 0;
+        if (from != kNoRow) gather_row<T>(p, q, r, from, lane);
+        clear_row<T>(p, q, r, lane);
     }
 }
 
@@ -204,48 +229,65 @@ __device__ __forceinline__ uint32_t wave_largest(uint32_t v)
     return __builtin_amdgcn_readlane(v, 63);
 }
 
-// The k largest of the ranks rank(0) .. rank(n - 1), in order, to list[0 .. k - 1]; 0 behind them.  The block's threads fetch kRanks of them at a time into LDS behind the
-// list so far, one wave finds the largest of them (a lane keeps the best two of every 64th and looks for more when both are taken).
-constexpr uint32_t kRanks = 2048;
-template <class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, unsigned long long *list)
+// All threads that work on a row: a wave, or a block.
+template <int THREADS> __device__ __forceinline__ void together()
 {
-    const uint32_t lane = threadIdx.x % 64;
-    if (threadIdx.x < k) list[threadIdx.x] = 0;
-    for (uint32_t base = 0; base < n; base += kRanks) {
-        const uint32_t count = n - base < kRanks ? n - base : kRanks, all = k + count;
+    if constexpr (THREADS == 64) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) list[k + i] = rank(base + i);
-        __syncthreads();
-        if (threadIdx.x < 64) {
-            unsigned long long best = 0, next = 0, mine = 0;
-            bool known = true;                                 // `next` is the lane's second best
-            const auto look = [&](unsigned long long below) {
-                best = next = 0;
-                known = true;
-                #pragma unroll 4
-                for (uint32_t i = lane; i < all; i += 64) {
-                    const unsigned long long v = list[i] < below ? list[i] : 0;
-                    next = v > best ? best : v > next ? v : next;
-                    best = v > best ? v : best;
-                }
-            };
-            look(~0ull);
-            for (uint32_t j = 0; j < k; ++j) {
-                const uint32_t high = wave_largest(static_cast<uint32_t>(best >> 32));
-                const uint32_t low = wave_largest(static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0);
-                const unsigned long long taken = static_cast<unsigned long long>(high) << 32 | low;
-                if (lane == j) mine = taken;
-                if (taken == 0) break;
-                if (best == taken) {                           // (ranks differ)
-                    if (known) { best = next; known = false; }
-                    else       look(taken);
-                }
-            }
-            __builtin_amdgcn_wave_barrier();
-            if (lane < k) list[lane] = mine;
+    }
+}
+
+// The k largest of the `all` ranks in `list` (all different, but for 0), in order, by one wave: lane j returns the j-th, 0 where there are fewer.  A lane keeps the best two of every
+// 64th and looks for more when both are taken.
+__device__ __forceinline__ unsigned long long pick(const unsigned long long *list, uint32_t all, uint32_t k, uint32_t lane)
+{
+    unsigned long long best = 0, next = 0, mine = 0;
+    bool known = true;                                         // `next` is the lane's second best
+    const auto look = [&](unsigned long long below) {
+        best = next = 0;
+        known = true;
+        #pragma unroll 2
+        for (uint32_t i = lane; i < all; i += 64) {
+            const unsigned long long v = list[i] < below ? list[i] : 0;
+            next = v > best ? best : v > next ? v : next;
+            best = v > best ? v : best;
+        }
+    };
+    look(~0ull);
+    for (uint32_t j = 0; j < k; ++j) {
+        const uint32_t high = wave_largest(static_cast<uint32_t>(best >> 32));
+        const uint32_t low = wave_largest(static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0);
+        const unsigned long long taken = static_cast<unsigned long long>(high) << 32 | low;
+        if (lane == j) mine = taken;
+        if (taken == 0) break;
+        if (best == taken) {
+            if (known) { best = next; known = false; }
+            else       look(taken);
         }
     }
-    __syncthreads();
+    return mine;
+}
+
+// The k largest of rank(0) .. rank(n - 1), in order, to list[0 .. k - 1]; 0 behind them.  THREADS threads fetch `kRanks` of them at a time into LDS, behind the list so far.
+template <int THREADS> constexpr uint32_t kRanks = THREADS == 64 ? 512 : 2048;
+template <int THREADS, class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, unsigned long long *list, uint32_t tid)
+{
+    if (tid < k) list[tid] = 0;
+    for (uint32_t base = 0; base < n; base += kRanks<THREADS>) {
+        const uint32_t count = n - base < kRanks<THREADS> ? n - base : kRanks<THREADS>;
+        #pragma unroll 4
+        for (uint32_t i = tid; i < count; i += THREADS) list[k + i] = rank(base + i);
+        together<THREADS>();
+        if (tid < 64) {
+            const unsigned long long mine = pick(list, k + count, k, tid);
+            together<64>();
+            if (tid < k) list[tid] = mine;
+        }
+        together<THREADS>();
+    }
 }
 
 struct Scores {
@@ -264,6 +306,8 @@ struct Scores {
     const float *quads;
     uint64_t ld_quads;
     QuadOrder order;
+    unsigned long long *quad_rank;    // [rows][top]
+    float2 *row_norm;                 // [rows]: largest logit, log(1 + rest)
     const int32_t *target;            // by row of the product; null: none
     const void *h, *e;                // h: rows of the product
     uint64_t ldh, lde, e_stride;
@@ -271,20 +315,16 @@ struct Scores {
     float scale;
 };
 
-// WAVES waves a row: one where no alternatives are wanted; four where they are, sixteen if rows are fewer than compute units (4 rows, 131072 entries:
-// FEW us instead of 34).
-template <class T, int WAVES> __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void scores_kernel(const Scores p)
+// Log probability and entropy of a row, and the quads of its alternatives.  WAVES waves a row: four where rows are few and have alternatives.
+template <int WAVES, bool TOP> __global__ __launch_bounds__(256) void scores_kernel(const Scores p)
 {
-    typedef Piece<T> V;
-    typedef typename T::elem elem;
-    constexpr bool TOP = WAVES > 1;
-    constexpr int ROWS = WAVES > 4 ? 1 : 4 / WAVES;            // of a block
+    constexpr int ROWS = 4 / WAVES, THREADS = 64 * WAVES;
     __shared__ Joined parts[WAVES];
-    __shared__ unsigned long long tile_rank[TOP ? kMostTop : 1], quad_rank[TOP ? kMostTop : 1], entry_rank[TOP ? 4 * kMostTop : 1], list[TOP ? kMostTop + kRanks : 1];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tid = threadIdx.x % (64 * WAVES);
+    __shared__ unsigned long long tile_rank[ROWS][TOP ? kMostTop : 1], lists[ROWS][TOP ? kMostTop + kRanks<THREADS> : 1];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tid = threadIdx.x % THREADS, mine = threadIdx.x / THREADS;
     const Rows &rows = p.taking.rows;
     // (all threads of a row leave a turn together)
-    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * ROWS + threadIdx.x / (64 * WAVES); r < rows.rows; r += static_cast<uint64_t>(gridDim.x) * ROWS) {
+    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * ROWS + mine; r < rows.rows; r += static_cast<uint64_t>(gridDim.x) * ROWS) {
         if (!in_groups(rows, r)) continue;
         if (!takes_part(p.taking, r)) {
             if (tid == 0) {
@@ -292,7 +332,7 @@ template <class T, int WAVES> __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVE
                 if (p.entropy) p.entropy[r] = 0.0f;
                 if (p.norms) p.norms[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
-            for (uint32_t j = tid; j < p.top; j += 64 * WAVES) { p.top_ids[r * p.ld_top + j] = -1; p.top_logp[r * p.ld_top + j] = -INFINITY; }
+            if (TOP && tid < p.top) { p.top_ids[r * p.ld_top + tid] = -1; p.top_logp[r * p.ld_top + tid] = -INFINITY; }
             if (!p.index) continue;
         }
         const uint32_t to = p.index ? p.index[r] : static_cast<uint32_t>(r);
@@ -301,114 +341,132 @@ template <class T, int WAVES> __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVE
         Joined sum = {-INFINITY, -1.0f, 0.0f};
         const float4 *moments = p.moments + r * p.tiles;
         constexpr int AHEAD = 4;
-        for (uint32_t t = tid; t < p.tiles; t += 64 * WAVES * AHEAD) {
+        for (uint32_t t = tid; t < p.tiles; t += THREADS * AHEAD) {
             float4 m[AHEAD];
             #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) m[a] = t + a * 64 * WAVES < p.tiles ? moments[t + a * 64 * WAVES] : make_float4(-INFINITY, -1.0f, 0.0f, 0.0f);
+            for (int a = 0; a < AHEAD; ++a) m[a] = t + a * THREADS < p.tiles ? moments[t + a * THREADS] : make_float4(-INFINITY, -1.0f, 0.0f, 0.0f);
             #pragma unroll
             for (int a = 0; a < AHEAD; ++a) sum = join(sum, {m[a].x, m[a].y, m[a].z});
         }
         #pragma unroll
         for (int d = 1; d < 64; d <<= 1) sum = join_lane(sum, d);
-        if constexpr (TOP) {
+        if constexpr (WAVES > 1) {
             if (lane == 0) parts[wave] = sum;
             __syncthreads();
             sum = parts[0];
             #pragma unroll
             for (int w = 1; w < WAVES; ++w) sum = join(sum, parts[w]);
         }
-        const float norm = log1pf(sum.rest), far = sum.far / (1.0f + sum.rest), target_logit = p.target_logit ? p.target_logit[r] : sum.top, distance = target_logit - sum.top;
         if (tid == 0) {
+            const float norm = log1pf(sum.rest), far = sum.far / (1.0f + sum.rest), distance = p.target_logit ? p.target_logit[r] - sum.top : 0.0f;
             if (p.logp) p.logp[to] = distance - norm;
             if (p.entropy) p.entropy[to] = norm - far;
             if (p.norms) p.norms[to] = make_float4(sum.top, sum.rest, far, distance);
+            if (TOP) p.row_norm[r] = make_float2(sum.top, norm);
         }
         if constexpr (TOP) {
             // the tiles, the quads in them
+            unsigned long long *list = lists[mine], *tiles = tile_rank[mine];
             const float *quads = p.quads + r * p.ld_quads;
-            largest(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, list);
-            if (tid < p.top) tile_rank[tid] = list[tid];
-            __syncthreads();
+            largest<THREADS>(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, list, tid);
+            if (tid < p.top) tiles[tid] = list[tid];
+            together<THREADS>();
             const uint32_t others = p.order.width / p.order.each, all = (rows.vocab + 3) / 4;
-            largest(p.top * p.tile_quads, p.top, [&](uint32_t i) -> unsigned long long {
-                const unsigned long long tile = tile_rank[i / p.tile_quads];
+            largest<THREADS>(p.top * p.tile_quads, p.top, [&](uint32_t i) -> unsigned long long {
+                const unsigned long long tile = tiles[i / p.tile_quads];
                 if (!tile) return 0;
                 const uint32_t at = place_of(tile) * p.tile_quads + i % p.tile_quads, in = at % p.order.width;
                 const uint32_t quad = at - in + in % p.order.each * others + in / p.order.each;
                 return quad < all ? rank_of(quads[at], quad) : 0;
-            }, list);
-            if (tid < p.top) quad_rank[tid] = list[tid];
-            __syncthreads();
-            // their logits, a quad a wave at a time
-            uint32_t g = 0;
-            for (uint32_t lo = 0, hi = rows.groups; hi - lo > 1;) {      // group of the row: the last one that begins at it or in front, if it is not empty
-                const uint32_t mid = (lo + hi) / 2;
-                if (clamped(rows, mid) <= r) lo = mid; else hi = mid;
-                g = lo;
-            }
-            const elem *h = static_cast<const elem *>(p.h) + r * p.ldh, *e = static_cast<const elem *>(p.e) + g * p.e_stride;
-            const uint32_t target = p.target ? static_cast<uint32_t>(p.target[r]) : ~0u;
-            for (uint32_t j = wave; j < p.top; j += WAVES) {
-                const unsigned long long rank = quad_rank[j];
-                if (!rank) { if (lane < 4) entry_rank[4 * j + lane] = 0; continue; }
-                const uint32_t v0 = place_of(rank) * 4, count = rows.vocab - v0 < 4 ? rows.vocab - v0 : 4;
-                float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const elem *row[4];
-                #pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) row[k] = e + static_cast<uint64_t>(v0 + (k < count ? k : 0)) * p.lde;
-                uint32_t c = lane * V::N;
-                #pragma unroll 2
-                for (; c + V::N <= p.dim; c += 64 * V::N) {
-                    const u4 a = V::load(h + c);
-                    u4 b[4];
-                    #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) b[k] = V::load(row[k] + c);
-                    #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k)
-                        #pragma unroll
-                        for (uint32_t i = 0; i < V::N; ++i) dot[k] = fmaf(V::value(a, i), V::value(b[k], i), dot[k]);
-                }
-                #pragma unroll 1
-                for (; c < p.dim; ++c) {                       // the last columns of one lane
-                    const float a = widen<T>(h[c]);
-                    #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) dot[k] = fmaf(a, widen<T>(row[k][c]), dot[k]);
-                }
-                #pragma unroll
-                for (int d = 1; d < 64; d <<= 1)
-                    #pragma unroll
-                    for (int k = 0; k < 4; ++k) dot[k] += __shfl_xor(dot[k], d, 64);
-                const float most = value_of(rank);
-                uint32_t first = 0;
-                #pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) {
-                    dot[k] = k < count ? dot[k] * p.scale : -INFINITY;
-                    if (dot[k] != dot[k]) dot[k] = -INFINITY;
-                    if (k > 0 && dot[k] > dot[first]) first = k;
-                }
-                if (lane < 4) {
-                    float v = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
-                    v = lane == first ? most : fminf(v, most);
-                    if (v0 + lane == target) v = target_logit;
-                    entry_rank[4 * j + lane] = lane < count ? rank_of(v, v0 + lane) : 0;
-                }
-            }
-            __syncthreads();
-            largest(4 * p.top, p.top, [&](uint32_t i) { return entry_rank[i]; }, list);
-            if (tid < p.top) {
-                const unsigned long long rank = list[tid];
-                p.top_ids[to * p.ld_top + tid] = rank ? static_cast<int32_t>(place_of(rank)) : -1;
-                p.top_logp[to * p.ld_top + tid] = rank ? (value_of(rank) - sum.top) - norm : -INFINITY;
-            }
-            __syncthreads();                                   // the next row's
+            }, list, tid);
+            if (tid < p.top) p.quad_rank[r * p.top + tid] = list[tid];
+            together<THREADS>();                               // the next row's
         }
+    }
+}
+
+// A row's alternatives from its quads: their logits, a quad a wave at a time, and the largest of these.  A block a row.
+template <class T> __global__ __launch_bounds__(1024) void alternatives_kernel(const Scores p)
+{
+    typedef Piece<T> V;
+    typedef typename T::elem elem;
+    __shared__ unsigned long long entries[4 * kMostTop];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    const Rows &rows = p.taking.rows;
+    for (uint64_t r = blockIdx.x; r < rows.rows; r += gridDim.x) {
+        if (!in_groups(rows, r) || (!p.index && !takes_part(p.taking, r))) continue;
+        const uint32_t to = p.index ? p.index[r] : static_cast<uint32_t>(r);
+        if (to == kNoRow) continue;
+        uint32_t g = 0;
+        for (uint32_t lo = 0, hi = rows.groups; hi - lo > 1;) {      // group of the row: the last one that begins at it or in front, if it is not empty
+            const uint32_t mid = (lo + hi) / 2;
+            if (clamped(rows, mid) <= r) lo = mid; else hi = mid;
+            g = lo;
+        }
+        const elem *h = static_cast<const elem *>(p.h) + r * p.ldh, *e = static_cast<const elem *>(p.e) + g * p.e_stride;
+        const uint32_t target = p.target ? static_cast<uint32_t>(p.target[r]) : ~0u;
+        for (uint32_t j = wave; j < p.top; j += waves) {
+            const unsigned long long rank = p.quad_rank[r * p.top + j];
+            if (!rank) { if (lane < 4) entries[4 * j + lane] = 0; continue; }
+            const uint32_t v0 = __builtin_amdgcn_readfirstlane(place_of(rank)) * 4, count = rows.vocab - v0 < 4 ? rows.vocab - v0 : 4;
+            float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const elem *row[4];
+            #pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) row[k] = e + static_cast<uint64_t>(v0 + (k < count ? k : 0)) * p.lde;
+            uint32_t c = lane * V::N;
+            #pragma unroll 2
+            for (; c + V::N <= p.dim; c += 64 * V::N) {
+                const u4 a = V::load(h + c);
+                u4 b[4];
+                #pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) b[k] = V::load(row[k] + c);
+                #pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                    #pragma unroll
+                    for (uint32_t i = 0; i < V::N; ++i) dot[k] = fmaf(V::value(a, i), V::value(b[k], i), dot[k]);
+            }
+            #pragma unroll 1
+            for (; c < p.dim; ++c) {                           // the last columns of one lane
+                const float a = widen<T>(h[c]);
+                #pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) dot[k] = fmaf(a, widen<T>(row[k][c]), dot[k]);
+            }
+            #pragma unroll
+            for (int d = 1; d < 64; d <<= 1)
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) dot[k] += __shfl_xor(dot[k], d, 64);
+            const float most = value_of(rank);
+            uint32_t first = 0;
+            #pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                dot[k] = k < count ? dot[k] * p.scale : -INFINITY;
+                if (dot[k] != dot[k]) dot[k] = -INFINITY;
+                if (k > 0 && dot[k] > dot[first]) first = k;
+            }
+            if (lane < 4) {
+                float v = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
+                v = lane == first ? most : fminf(v, most);
+                if (v0 + lane == target) v = p.target_logit[r];
+                entries[4 * j + lane] = lane < count ? rank_of(v, v0 + lane) : 0;
+            }
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const unsigned long long rank = pick(entries, 4 * p.top, p.top, lane);
+            const float2 norm = p.row_norm[r];
+            if (lane < p.top) {
+                p.top_ids[to * p.ld_top + lane] = rank ? static_cast<int32_t>(place_of(rank)) : -1;
+                p.top_logp[to * p.ld_top + lane] = rank ? (value_of(rank) - norm.x) - norm.y : -INFINITY;
+            }
+        }
+        __syncthreads();                                       // the next row's
     }
 }
 
 // ---- the calls -------------------------------------------------------------------------------------------
 
 struct Workspace {
-    uint64_t index, target, ends, hidden, target_logit, moments, quads, ld_quads;
+    uint64_t index, target, ends, hidden, target_logit, moments, quads, ld_quads, quad_rank, row_norm;
     uint64_t scaled, row_scale, group_scale, top, none, one, target_slope, slope, sum, part;
     uint64_t pitch, piece, sum_pitch, bytes;
     uint32_t pieces;
@@ -434,7 +492,11 @@ Workspace carve(const cocod_token_scores_call *c, bool grad)
         const uint32_t planned = tile_cols(t, w.logits.tile), narrow = planned < 128 ? planned : 128;        // the large tile may have to give way to the medium one
         w.moments = take((static_cast<uint64_t>(c->vocab) + narrow - 1) / narrow * rows * 16);
         w.ld_quads = (static_cast<uint64_t>(c->vocab) + 255) / 256 * 64;
-        if (c->top) w.quads = take(rows * w.ld_quads * 4);
+        if (c->top) {
+            w.quads = take(rows * w.ld_quads * 4);
+            w.quad_rank = take(rows * c->top * 8);
+            w.row_norm = take(rows * 8);
+        }
     } else {
         const Pieces pieces = pieces_of(c->piece, rows, c->vocab);
         w.piece = pieces.size;
@@ -529,10 +591,6 @@ template <class T> hipError_t launch_gather(hipStream_t q, const Taking &taking,
     const bool normal = taking.grad && kTypes[c->dtype] == Dtype::F16;
     uint32_t *index = reinterpret_cast<uint32_t *>(ws + w.index);
     float *row_scale = reinterpret_cast<float *>(ws + w.row_scale);
-    const auto take = normal ? take_kernel<true> : take_kernel<false>;
-    hipLaunchKernelGGL(take, dim3(c->groups), dim3(kTakeThreads), 0, q, taking, c->scale, index, reinterpret_cast<int32_t *>(ws + w.target), reinterpret_cast<int64_t *>(ws + w.ends),
-                       reinterpret_cast<float *>(ws + w.group_scale), row_scale);
-    if (!c->rows) return hipGetLastError();
     Gather<E> g{};
     g.index = index;
     g.h = static_cast<const E *>(c->h); g.ldh = c->ldh; g.dim = c->dim;
@@ -547,18 +605,32 @@ template <class T> hipError_t launch_gather(hipStream_t q, const Taking &taking,
         g.top = reinterpret_cast<float *>(ws + w.top); g.none = reinterpret_cast<float *>(ws + w.none);
         g.one = reinterpret_cast<float *>(ws + w.one); g.target_slope = reinterpret_cast<float *>(ws + w.target_slope);
     }
+    const bool here = c->rows * w.pitch * sizeof(E) <= kGatherHere * c->groups;
+    const auto take = normal ? (here ? take_kernel<T, true, true> : take_kernel<T, true, false>) : (here ? take_kernel<T, false, true> : take_kernel<T, false, false>);
+    hipLaunchKernelGGL(take, dim3(c->groups), dim3(kTakeThreads), 0, q, taking, c->scale, index, reinterpret_cast<int32_t *>(ws + w.target), reinterpret_cast<int64_t *>(ws + w.ends),
+                       reinterpret_cast<float *>(ws + w.group_scale), row_scale, g);
+    if (here) return hipGetLastError();
     const uint64_t blocks = (c->rows + 3) / 4;
     hipLaunchKernelGGL(scores_gather_kernel<T>, dim3(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks)), dim3(256), 0, q, taking, g);
     return hipGetLastError();
 }
 
+void launch_scores(hipStream_t q, const Scores &p)
+{
+    const bool few = p.top && p.taking.rows.rows <= kFewRows;
+    const uint64_t blocks = few ? p.taking.rows.rows : (p.taking.rows.rows + 3) / 4;
+    const dim3 grid(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks));
+    if (few)        hipLaunchKernelGGL((scores_kernel<4, true>), grid, dim3(256), 0, q, p);
+    else if (p.top) hipLaunchKernelGGL((scores_kernel<1, true>), grid, dim3(256), 0, q, p);
+    else            hipLaunchKernelGGL((scores_kernel<1, false>), grid, dim3(256), 0, q, p);
+}
 template <class T> hipError_t launch_scores(hipStream_t q, const Scores &p)
 {
-    const uint64_t blocks = p.top ? p.taking.rows.rows : (p.taking.rows.rows + 3) / 4;
-    const dim3 grid(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks));
-    if (p.top && blocks <= kFewRows) hipLaunchKernelGGL((scores_kernel<T, 16>), grid, dim3(1024), 0, q, p);
-    else if (p.top) hipLaunchKernelGGL((scores_kernel<T, 4>), grid, dim3(256), 0, q, p);
-    else       hipLaunchKernelGGL((scores_kernel<T, 1>), grid, dim3(256), 0, q, p);
+    launch_scores(q, p);
+    if (!p.top) return hipGetLastError();
+    const uint64_t rows = p.taking.rows.rows;
+    const uint32_t most = rows <= kVeryFewRows ? 16 : 4, waves = p.top < most ? p.top : most;
+    hipLaunchKernelGGL(alternatives_kernel<T>, dim3(static_cast<uint32_t>(rows < kMostAlternativeBlocks ? rows : kMostAlternativeBlocks)), dim3(64 * waves), 0, q, p);
     return hipGetLastError();
 }
 
@@ -639,6 +711,7 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     p.logp = c->logp; p.entropy = c->entropy; p.norms = reinterpret_cast<float4 *>(c->norms);
     p.top = c->top; p.top_ids = c->top_ids; p.top_logp = c->top_logp; p.ld_top = c->ld_top;
     p.quads = z.quads; p.ld_quads = z.ld_quads; p.order = quad_order(t, tile);
+    p.quad_rank = reinterpret_cast<unsigned long long *>(ws + w.quad_rank); p.row_norm = reinterpret_cast<float2 *>(ws + w.row_norm);
     p.target = z.target;
     p.h = z.a; p.ldh = z.lda; p.e = c->e; p.lde = c->lde; p.e_stride = z.b_group;
     p.dim = c->dim; p.scale = c->scale;

@@ -88,7 +88,9 @@ def test_no_rows_need_no_gpu():
 
 def test_workspace_follows_what_is_asked_for():
     small = P.token_scores_workspace(scores(top=0), P.TOKEN_SCORES_FORWARD)
-    assert P.token_scores_workspace(scores(top=1), P.TOKEN_SCORES_FORWARD) == small + 100 * 256 == P.token_scores_workspace(scores(top=32), P.TOKEN_SCORES_FORWARD)
+    for top in (1, 32):
+        need = P.token_scores_workspace(scores(top=top), P.TOKEN_SCORES_FORWARD)
+        assert small + 100 * (256 + 8 * top + 8) <= need <= small + 100 * (256 + 8 * top + 8) + 3 * 256
     wide = dict(rows=8192, vocab=131072, dim=2048, groups=1)
     assert P.token_scores_workspace(scores(**wide), P.TOKEN_SCORES_GRAD) >= 2 ** 28 * 2
     assert P.token_scores_workspace(scores(piece=1024, **wide), P.TOKEN_SCORES_GRAD) < 2 ** 28
