@@ -240,51 +240,109 @@ template <int THREADS> __device__ __forceinline__ void together()
     }
 }
 
-// The k largest of the `all` ranks in `list` (all different, but for 0), in order, by one wave: lane j returns the j-th, 0 where there are fewer.  A lane keeps the best two of every
-// 64th and looks for more when both are taken.
-__device__ __forceinline__ unsigned long long pick(const unsigned long long *list, uint32_t all, uint32_t k, uint32_t lane)
+// How many of the wave's first `count` ranks are above this lane's.
+__device__ __forceinline__ uint32_t above(unsigned long long mine, uint32_t count, unsigned long long *scratch, uint32_t lane)
 {
-    unsigned long long best = 0, next = 0, mine = 0;
-    bool known = true;                                         // `next` is the lane's second best
-    const auto look = [&](unsigned long long below) {
-        best = next = 0;
-        known = true;
-        #pragma unroll 2
-        for (uint32_t i = lane; i < all; i += 64) {
-            const unsigned long long v = list[i] < below ? list[i] : 0;
-            next = v > best ? best : v > next ? v : next;
-            best = v > best ? v : best;
+    together<64>();
+    scratch[lane] = mine;
+    together<64>();
+    uint32_t n = 0;
+    for (uint32_t i = 0; i < count; i += 4) {
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) n += scratch[i + j] > mine ? 1 : 0;       // (behind `count` there are zeros)
+    }
+    return n;
+}
+
+// The k largest of the `all` ranks in `list` (all different, but for 0), in order, by one wave: lane j returns the j-th, 0 where there are fewer.  A lane's best is the best of every
+// 64th; what is not below the k-th of the lanes' bests, k ranks and hardly more, is put together and each one's place counted.  (Where that is
+// more than a wave, one after the other: a lane keeps its best two and looks for more when both are taken.  20 of 320: 1 us instead of 6.)
+__device__ __forceinline__ unsigned long long pick(const unsigned long long *list, uint32_t all, uint32_t k, unsigned long long *scratch, uint32_t lane)
+{
+    unsigned long long best = 0, next = 0;
+    #pragma unroll 2
+    for (uint32_t i = lane; i < all; i += 64) {
+        const unsigned long long v = list[i];
+        next = v > best ? best : v > next ? v : next;
+        best = v > best ? v : best;
+    }
+    unsigned long long candidate = best;
+    uint32_t count = 64;
+    if (all > 64) {
+        const unsigned long long last = __ballot(above(best, 64, scratch, lane) == k - 1 && best != 0);
+        unsigned long long least = 1;                          // fewer lanes than k hold any: every rank is a candidate
+        if (last) {
+            const int who = __ffsll(last) - 1;
+            least = static_cast<unsigned long long>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(best >> 32), who))) << 32 |
+                    static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(best), who));
         }
-    };
-    look(~0ull);
-    for (uint32_t j = 0; j < k; ++j) {
-        const uint32_t high = wave_largest(static_cast<uint32_t>(best >> 32));
-        const uint32_t low = wave_largest(static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0);
-        const unsigned long long taken = static_cast<unsigned long long>(high) << 32 | low;
-        if (lane == j) mine = taken;
-        if (taken == 0) break;
-        if (best == taken) {
-            if (known) { best = next; known = false; }
-            else       look(taken);
+        count = 0;
+        unsigned long long kept = 0;
+        together<64>();
+        scratch[lane] = 0;
+        together<64>();
+        for (uint32_t i0 = 0; i0 < all; i0 += 64) {
+            const unsigned long long v = i0 + lane < all ? list[i0 + lane] : 0;
+            const bool in = v >= least;
+            const unsigned long long votes = __ballot(in);
+            const uint32_t at = count + __popcll(votes & ((1ull << lane) - 1));
+            if (in && at < 64) scratch[at] = v;
+            count += __popcll(votes);
+        }
+        together<64>();
+        kept = scratch[lane];
+        candidate = kept;
+        if (count > 64) {
+            unsigned long long mine = 0;
+            bool known = true;                                 // `next` is the lane's second best
+            for (uint32_t j = 0; j < k; ++j) {
+                const uint32_t high = wave_largest(static_cast<uint32_t>(best >> 32));
+                const uint32_t low = wave_largest(static_cast<uint32_t>(best >> 32) == high ? static_cast<uint32_t>(best) : 0);
+                const unsigned long long taken = static_cast<unsigned long long>(high) << 32 | low;
+                if (lane == j) mine = taken;
+                if (taken == 0) break;
+                if (best == taken) {
+                    if (known) {
+                        best = next;
+                        known = false;
+                    } else {
+                        best = next = 0;
+                        known = true;
+                        for (uint32_t i = lane; i < all; i += 64) {
+                            const unsigned long long v = list[i] < taken ? list[i] : 0;
+                            next = v > best ? best : v > next ? v : next;
+                            best = v > best ? v : best;
+                        }
+                    }
+                }
+            }
+            return mine;
         }
     }
-    return mine;
+    const uint32_t place = above(candidate, count, scratch, lane);
+    together<64>();
+    scratch[lane] = 0;
+    together<64>();
+    if (candidate != 0 && place < k) scratch[place] = candidate;
+    together<64>();
+    return lane < k ? scratch[lane] : 0;
 }
 
 // The k largest of rank(0) .. rank(n - 1), in order, to list[0 .. k - 1]; 0 behind them.  THREADS threads fetch `kRanks` of them at a time into LDS, behind the list so far.
 template <int THREADS> constexpr uint32_t kRanks = THREADS == 64 ? 512 : 2048;
-template <int THREADS, class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, unsigned long long *list, uint32_t tid)
+template <int THREADS> struct Picking { unsigned long long list[kMostTop + kRanks<THREADS>], scratch[64]; };
+template <int THREADS, class Rank> __device__ __forceinline__ void largest(uint32_t n, uint32_t k, const Rank &rank, Picking<THREADS> &p, uint32_t tid)
 {
-    if (tid < k) list[tid] = 0;
+    if (tid < k) p.list[tid] = 0;
     for (uint32_t base = 0; base < n; base += kRanks<THREADS>) {
         const uint32_t count = n - base < kRanks<THREADS> ? n - base : kRanks<THREADS>;
         #pragma unroll 4
-        for (uint32_t i = tid; i < count; i += THREADS) list[k + i] = rank(base + i);
+        for (uint32_t i = tid; i < count; i += THREADS) p.list[k + i] = rank(base + i);
         together<THREADS>();
         if (tid < 64) {
-            const unsigned long long mine = pick(list, k + count, k, tid);
+            const unsigned long long mine = pick(p.list, k + count, k, p.scratch, tid);
             together<64>();
-            if (tid < k) list[tid] = mine;
+            if (tid < k) p.list[tid] = mine;
         }
         together<THREADS>();
     }
@@ -320,7 +378,8 @@ template <int WAVES, bool TOP> __global__ __launch_bounds__(256) void scores_ker
 {
     constexpr int ROWS = 4 / WAVES, THREADS = 64 * WAVES;
     __shared__ Joined parts[WAVES];
-    __shared__ unsigned long long tile_rank[ROWS][TOP ? kMostTop : 1], lists[ROWS][TOP ? kMostTop + kRanks<THREADS> : 1];
+    __shared__ unsigned long long tile_rank[ROWS][TOP ? kMostTop : 1];
+    __shared__ typename std::conditional<TOP, Picking<THREADS>, char>::type picking[ROWS];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tid = threadIdx.x % THREADS, mine = threadIdx.x / THREADS;
     const Rows &rows = p.taking.rows;
     // (all threads of a row leave a turn together)
@@ -366,9 +425,9 @@ template <int WAVES, bool TOP> __global__ __launch_bounds__(256) void scores_ker
         }
         if constexpr (TOP) {
             // the tiles, the quads in them
-            unsigned long long *list = lists[mine], *tiles = tile_rank[mine];
+            unsigned long long *const list = picking[mine].list, *const tiles = tile_rank[mine];
             const float *quads = p.quads + r * p.ld_quads;
-            largest<THREADS>(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, list, tid);
+            largest<THREADS>(p.tiles, p.top, [&](uint32_t t) { return rank_of(moments[t].x, t); }, picking[mine], tid);
             if (tid < p.top) tiles[tid] = list[tid];
             together<THREADS>();
             const uint32_t others = p.order.width / p.order.each, all = (rows.vocab + 3) / 4;
@@ -378,7 +437,7 @@ template <int WAVES, bool TOP> __global__ __launch_bounds__(256) void scores_ker
                 const uint32_t at = place_of(tile) * p.tile_quads + i % p.tile_quads, in = at % p.order.width;
                 const uint32_t quad = at - in + in % p.order.each * others + in / p.order.each;
                 return quad < all ? rank_of(quads[at], quad) : 0;
-            }, list, tid);
+            }, picking[mine], tid);
             if (tid < p.top) p.quad_rank[r * p.top + tid] = list[tid];
             together<THREADS>();                               // the next row's
         }
@@ -390,7 +449,7 @@ template <class T> __global__ __launch_bounds__(1024) void alternatives_kernel(c
 {
     typedef Piece<T> V;
     typedef typename T::elem elem;
-    __shared__ unsigned long long entries[4 * kMostTop];
+    __shared__ unsigned long long entries[4 * kMostTop], scratch[64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     const Rows &rows = p.taking.rows;
     for (uint64_t r = blockIdx.x; r < rows.rows; r += gridDim.x) {
@@ -452,7 +511,7 @@ template <class T> __global__ __launch_bounds__(1024) void alternatives_kernel(c
         }
         __syncthreads();
         if (wave == 0) {
-            const unsigned long long rank = pick(entries, 4 * p.top, p.top, lane);
+            const unsigned long long rank = pick(entries, 4 * p.top, p.top, scratch, lane);
             const float2 norm = p.row_norm[r];
             if (lane < p.top) {
                 p.top_ids[to * p.ld_top + lane] = rank ? static_cast<int32_t>(place_of(rank)) : -1;
