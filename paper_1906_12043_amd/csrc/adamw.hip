@@ -10,13 +10,13 @@
 // a function of (seed, tensor, worker, element): a multiply-and-shift mixer of 32 bits, three multiplications an element, where a
 // ten-round counter generator would cost more time than the memory leaves.  p' comes from m' and v' before they are rounded.
 //
-// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 852-903 us, 5.6-5.9 TB/s), with 8-bit states 16.1 (138 M: 413 us, 5.4
-// TB/s; four streams read and five written, a copy reaches 6.6).  A thread takes four elements, eight lanes a scale.  What it took: four elements side by side instead of eight
-// in a thread, tiles within a tensor without a decision between their loads (a wait stood behind each: 8-bit 513 us), 8-bit states that find out once a wave whether
-// every code is a normal one and every number finite, past the caches where the states are larger than those.  Half the tile or twice and four times its elements, 512 or
-// 1024 threads, runs of tiles per die: no better.
-// Tensors travel in the kernel's arguments, a launch for every kMostTensors of them, so nothing has to be laid out on the device and a captured
-// launch holds all it needs.
+// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 852-907 us by card, 5.5-5.9 TB/s), with 8-bit states 16.1 (138 M: 404 us,
+// 5.5 TB/s; four streams read and five written, a copy reaches 6.6).  A thread takes four elements, eight lanes a scale.  What it took, us for these two: four elements side by
+// side instead of eight in a thread, past the caches where the states are larger than those (1000 -> 903 / 501 -> 480), tiles within a tensor without a decision between their
+// loads, a wait behind each, and 8-bit states that find out once a wave whether every code is a normal one and every number finite (480 -> 413), seven waves a SIMD instead of six (413
+// -> 404).  Twice and four times the tile, 512 or 1024 threads, runs of tiles per die, blocks that stay for several tiles: no better.
+// Tensors travel in the kernel's arguments, 4 KiB, a launch for 55 to 64 of them, so nothing has to be laid out on the device and a captured
+// launch holds all it needs (61 000 parameters in 150 tensors: 14 us, 22 M in 400 with 8-bit states 107).
 #include "operator_call.hpp"
 #include "row_access.hpp"
 
@@ -30,29 +30,33 @@ constexpr int kThreads = 256;
 constexpr uint32_t kSpan = kThreads * 4;             // elements of a block's threads side by side, four each
 constexpr uint32_t kSpans = 1;                       // of them a tile has
 constexpr uint32_t kTile = kSpan * kSpans;
-constexpr uint32_t kMostTensors = 40;                // of a launch: its arguments stay below 4 KiB
 constexpr uint32_t kMostBlocks = 1u << 20;
 constexpr uint64_t kMostElements = 1ull << 40;       // of a tensor
 
-struct Tensor {
-    void *p;
-    const void *g;
-    void *m, *v;
-    uint8_t *m_scales, *v_scales;
-    void *copy;
-    uint64_t n;
-    float weight_decay, lr_scale;
-};
+// A tensor in the kernel's arguments: p, g, m, v, the scales where states have 8 bits, the copy where there is one, and the elements with the number of its pair of
+// weight decay and factor of the learning rate above them.
+constexpr uint32_t kMostTensors = 64, kMostPairs = 16, kWords = 440, kPairShift = 48;
+struct Pair { float weight_decay, lr_scale; };
 struct AdamWParams {
-    Tensor tensor[kMostTensors];
+    uint64_t words[kWords];
+    Pair pairs[kMostPairs];
     uint32_t first_tile[kMostTensors + 1];           // of every tensor, in tiles of a worker
     uint32_t count, number;                          // tensors of this launch; number of the first one in the call
+    uint32_t words_each;
     uint64_t tiles;                                  // of all workers
-    uint32_t workers, copy_dtype;
+    uint32_t workers, copy_dtype;                    // copy_dtype: COCOD_F32 where there is none
     uint64_t stride;
     float beta1, beta2, rest1, rest2, eps;
     cocod_adamw_now now;
     const cocod_adamw_now *now_device;
+};
+struct Tensor {
+    char *p;
+    const char *g;
+    char *m, *v;
+    uint8_t *m_scales, *v_scales;
+    char *copy;
+    uint64_t n;
 };
 static_assert(sizeof(AdamWParams) <= 4096, "arguments of a kernel");
 
@@ -226,6 +230,9 @@ __device__ __forceinline__ Stored store_states(const f4 &m, const f4 &v, const f
     return out;
 }
 
+// An address in device memory from its number (said so, as accesses that might also go to LDS wait for it).
+__device__ __forceinline__ char *in_memory(uint64_t address) { return (char *)(__attribute__((address_space(1))) char *)address; }
+
 // A tile of a tensor.  WHOLE: it lies within the tensor, so that nothing is decided between the loads, which are then all on their way at a time.
 struct Terms { float grad_scale, keep, step, root_bias2; uint32_t stream; };
 template <class TP, class TG, bool EIGHT, bool STREAM, bool WHOLE>
@@ -293,20 +300,30 @@ __device__ __forceinline__ void update(const AdamWParams &s, const Tensor &t, co
     }
 }
 
-template <class TP, class TG, bool EIGHT, bool STREAM> __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWParams s)
+template <class TP, class TG, bool EIGHT, bool STREAM> __global__ __launch_bounds__(kThreads, EIGHT ? 7 : 8) void adamw_kernel(const AdamWParams s)
 {
-    const cocod_adamw_now now = s.now_device ? *s.now_device : s.now;
-    if (now.skip) return;
+    cocod_adamw_now now = s.now;
+    if (s.now_device) {
+        now = *s.now_device;
+        if (now.skip) return;
+    }
     const uint32_t lane = threadIdx.x % 64, per_worker = s.first_tile[s.count];
     const uint32_t mine = lane < s.count ? s.first_tile[lane] : ~0u;       // (a tile's number is below that)
     static_assert(kMostTensors <= 64, "a lane a tensor");
     for (uint64_t tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
         const uint32_t worker = s.workers == 1 ? 0 : static_cast<uint32_t>(tile / per_worker), in = static_cast<uint32_t>(tile - static_cast<uint64_t>(worker) * per_worker);
         const uint32_t which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(mine <= in)) - 1);
-        const Tensor &t = s.tensor[which];
+        const uint64_t *const w = s.words + which * s.words_each;
+        Tensor t = {in_memory(w[0]), in_memory(w[1]), in_memory(w[2]), in_memory(w[3]), nullptr, nullptr, nullptr, 0};
+        uint32_t at = 4;
+        if constexpr (EIGHT) { t.m_scales = reinterpret_cast<uint8_t *>(in_memory(w[4])); t.v_scales = reinterpret_cast<uint8_t *>(in_memory(w[5])); at = 6; }
+        if (sizeof(typename TP::elem) == 4 && s.copy_dtype != COCOD_F32) t.copy = in_memory(w[at++]);
+        const uint64_t last = w[at];
+        t.n = last & ((1ull << kPairShift) - 1);
+        const Pair pair = s.pairs[last >> kPairShift];
         const uint64_t begin = static_cast<uint64_t>(in - s.first_tile[which]) * kTile, first = begin + threadIdx.x * 4;
-        const float lr = now.lr * t.lr_scale;
-        const Terms terms = {now.grad_scale, 1.0f - lr * t.weight_decay, lr / now.bias1, 1.0f / sqrtf(now.bias2),
+        const float lr = now.lr * pair.lr_scale;
+        const Terms terms = {now.grad_scale, 1.0f - lr * pair.weight_decay, lr / now.bias1, 1.0f / sqrtf(now.bias2),
                              now.seed + (s.number + which) * 0x632BE5ABu + worker * 0x85157AF5u};
         if (t.n - begin >= kTile) update<TP, TG, EIGHT, STREAM, true>(s, t, terms, worker, first);
         else                      update<TP, TG, EIGHT, STREAM, false>(s, t, terms, worker, first);
@@ -425,7 +442,6 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c)
     AdamWParams s{};
     s.workers = c->workers;
     s.stride = c->workers > 1 ? c->stride : 0;
-    s.copy_dtype = c->copy_dtype;
     s.beta1 = c->beta1; s.beta2 = c->beta2; s.eps = c->eps;
     s.rest1 = static_cast<float>(1.0 - static_cast<double>(c->beta1));
     s.rest2 = static_cast<float>(1.0 - static_cast<double>(c->beta2));
@@ -451,15 +467,34 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c)
         s.count = 0;
         return launch_status(hipGetLastError(), what);
     };
+    bool copies = false;
+    for (uint64_t i = 0; i < c->count; ++i) copies = copies || (c->tensors[i].n && c->tensors[i].copy);
+    s.copy_dtype = copies ? c->copy_dtype : COCOD_F32;
+    s.words_each = 5 + (eight ? 2 : 0) + (copies ? 1 : 0);
+    const uint32_t most = kWords / s.words_each < kMostTensors ? kWords / s.words_each : kMostTensors;
+    uint32_t pairs = 0;
     for (uint64_t i = 0; i < c->count; ++i) {
         const cocod_adamw_tensor &t = c->tensors[i];
         const uint64_t tiles = (t.n + kTile - 1) / kTile;
         if (!tiles) continue;
+        const auto pair_of = [&] {
+            uint32_t k = 0;
+            while (k < pairs && (s.pairs[k].weight_decay != t.weight_decay || s.pairs[k].lr_scale != t.lr_scale)) ++k;
+            return k;
+        };
+        uint32_t pair = pair_of();
         // (the tensors of a launch have consecutive numbers)
-        if (s.count && (s.count == kMostTensors || s.number + s.count != i || s.first_tile[s.count] + tiles > ~0u))
+        if (s.count && (s.count == most || s.number + s.count != i || s.first_tile[s.count] + tiles > ~0u || pair == kMostPairs)) {
             if (int rc = flush()) return rc;
+            pairs = pair = 0;
+        }
+        if (pair == pairs) s.pairs[pairs++] = {t.weight_decay, t.lr_scale};
         if (!s.count) s.number = static_cast<uint32_t>(i);
-        s.tensor[s.count] = {t.p, t.g, t.m, t.v, t.m_scales, t.v_scales, t.copy, t.n, t.weight_decay, t.lr_scale};
+        uint64_t *w = s.words + s.count * s.words_each;
+        for (const void *array : {static_cast<const void *>(t.p), t.g, static_cast<const void *>(t.m), static_cast<const void *>(t.v)}) *w++ = reinterpret_cast<uintptr_t>(array);
+        if (eight) { *w++ = reinterpret_cast<uintptr_t>(t.m_scales); *w++ = reinterpret_cast<uintptr_t>(t.v_scales); }
+        if (copies) *w++ = reinterpret_cast<uintptr_t>(t.copy);
+        *w = t.n | static_cast<uint64_t>(pair) << kPairShift;
         s.first_tile[s.count + 1] = s.first_tile[s.count] + static_cast<uint32_t>(tiles);
         ++s.count;
     }

@@ -280,6 +280,10 @@ struct Task {
 };
 __device__ __forceinline__ uint64_t quotient(uint64_t a, uint32_t b) { return a >> 32 ? a / b : static_cast<uint32_t>(a) / b; }
 
+// Where a piece that begins at column c < width is taken: the last one of a row as far back as it has to be to be whole, so that some columns are taken twice, with the same values
+// (rows shorter than a piece are taken element by element).  5768 tokens with 4 rows of 2815 columns each back: 36 us instead of 49.
+template <uint32_t N> __device__ __forceinline__ uint32_t whole_piece(uint32_t c, uint32_t width) { return c + N > width && width >= N ? width - N : c; }
+
 template <class T, int U, bool STREAM> __global__ __launch_bounds__(256) void dispatch_kernel(const RowsParams p)
 {
     typedef Piece<T> V;
@@ -291,13 +295,13 @@ template <class T, int U, bool STREAM> __global__ __launch_bounds__(256) void di
         const elem *x = static_cast<const elem *>(p.from) + token * p.ld_from;
         u4 raw[U];
         #pragma unroll
-        for (int u = 0; u < U; ++u) { const uint32_t c = c0 + u * span; if (c < p.width) raw[u] = V::load(x + c, p.width - c); }
+        for (int u = 0; u < U; ++u) if (c0 + u * span < p.width) { const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width); raw[u] = V::load(x + c, p.width - c); }
         for (uint32_t j = 0; j < p.choices; ++j) {
             const uint32_t row = static_cast<uint32_t>(p.place[token * p.ld_place + j]);
             if (row >= p.rows) continue;
             elem *to = static_cast<elem *>(p.to) + row * p.ld_to;
             #pragma unroll
-            for (int u = 0; u < U; ++u) { const uint32_t c = c0 + u * span; if (c < p.width) V::template store<STREAM>(to + c, raw[u], p.width - c); }
+            for (int u = 0; u < U; ++u) if (c0 + u * span < p.width) { const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width); V::template store<STREAM>(to + c, raw[u], p.width - c); }
         }
     }
 }
@@ -328,7 +332,8 @@ template <class T, int U, bool STREAM> __global__ __launch_bounds__(256) void co
                 weight[a] = has[a] && p.weights ? p.weights[token * p.ld_weights + j] : 1.0f;
                 const elem *from = static_cast<const elem *>(p.from) + row * p.ld_from;
                 #pragma unroll
-                for (int u = 0; u < U; ++u) { const uint32_t c = c0 + u * span; if (has[a] && c < p.width) raw[a][u] = V::template load<STREAM>(from + c, p.width - c); }
+                for (int u = 0; u < U; ++u)
+                    if (has[a] && c0 + u * span < p.width) { const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width); raw[a][u] = V::template load<STREAM>(from + c, p.width - c); }
             }
             #pragma unroll
             for (int a = 0; a < AHEAD; ++a)
@@ -340,7 +345,7 @@ template <class T, int U, bool STREAM> __global__ __launch_bounds__(256) void co
         }
         elem *y = static_cast<elem *>(p.to) + token * p.ld_to;
         #pragma unroll
-        for (int u = 0; u < U; ++u) { const uint32_t c = c0 + u * span; if (c < p.width) V::store(y + c, V::pack(sum[u]), p.width - c); }
+        for (int u = 0; u < U; ++u) if (c0 + u * span < p.width) { const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width); V::store(y + c, V::pack(sum[u]), p.width - c); }
     }
 }
 
@@ -364,21 +369,21 @@ template <class T, int U, bool STREAM> __global__ __launch_bounds__(256) void co
                 u4 g[U], v[U];
                 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const uint32_t c = c0 + u * span;
-                    if (c >= p.width) continue;
+                    if (c0 + u * span >= p.width) continue;
+                    const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width);
                     g[u] = V::load(dy + c, p.width - c);
                     if (p.dweights) v[u] = V::template load<STREAM>(ys + c, p.width - c);
                 }
                 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const uint32_t c = c0 + u * span;
-                    if (c >= p.width) continue;
+                    if (c0 + u * span >= p.width) continue;
+                    const uint32_t c = whole_piece<V::N>(c0 + u * span, p.width), again = c0 + u * span - c;       // columns that another lane has as well
                     float out[V::N];
                     #pragma unroll
                     for (uint32_t e = 0; e < V::N; ++e) {
                         const float d = V::value(g[u], e);
                         out[e] = weight * d;
-                        if (p.dweights) dot = fmaf(d, V::value(v[u], e), dot);
+                        if (p.dweights && e >= again) dot = fmaf(d, V::value(v[u], e), dot);
                     }
                     if (p.to) V::template store<STREAM>(dys + c, V::pack(out), p.width - c);
                 }

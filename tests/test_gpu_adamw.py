@@ -125,6 +125,26 @@ def test_fp32_states(kind, which, workers, shift):
         assert x.rest_untouched() and bool((x.buf[:shift] == SENTINEL).all())
 
 
+def test_many_pairs_of_decay_and_rate_and_copies_of_some():
+    """More pairs than a launch holds, tensors of no elements and tensors without a copy between the others."""
+    sizes = [40 + 7 * (i % 9) if i % 11 else 0 for i in range(90)]
+    _, tensors, p, g, m, v, copy = state_call(("fp32", "bf16", "bf16"), sizes, 2, 9, 0)
+    old = [Flat(sizes, 2, x.all.dtype, None) for x in (p, g, m, v)]
+    for o, x in zip(old, (p, g, m, v)):
+        o.buf.copy_(x.buf)
+    for i, one in enumerate(tensors):
+        one["weight_decay"], one["lr_scale"] = 0.01 * (i % 37), 1.0 + 0.25 * (i % 5)
+        if i % 4 == 1:
+            one["copy"] = None
+    P.adamw(torch.cuda.current_stream(), P.AdamW(tensors=tensors, dtype=P.F32, grad_dtype=P.BF16, copy_dtype=P.BF16, workers=2, stride=p.stride, **HYPER))
+    for i, one in enumerate(tensors):
+        for w in range(2):
+            want, far = formula(*(o.part(i, w) for o in old), one["weight_decay"], one["lr_scale"], HYPER)
+            for got, x, f in zip((p, m, v), want, far):
+                assert bool(((got.part(i, w).double() - x).abs() <= f).all()), (i, w)
+            assert torch.equal(copy.part(i, w), p.part(i, w).to(torch.bfloat16) if i % 4 != 1 else torch.full_like(copy.part(i, w), SENTINEL))
+
+
 def test_gradients_that_are_not_finite_stay_with_their_element():
     call, tensors, p, g, m, v, _ = state_call(("fp32", "fp32", None), [4096], 1, 5, 0)
     g.part(0)[100], g.part(0)[200], g.part(0)[300] = float("nan"), float("inf"), float("-inf")
