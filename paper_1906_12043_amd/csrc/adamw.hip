@@ -10,11 +10,12 @@
 // a function of (seed, tensor, worker, element): a multiply-and-shift mixer of 32 bits, three multiplications an element, where a
 // ten-round counter generator would cost more time than the memory leaves.  p' comes from m' and v' before they are rounded.
 //
-// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 852-907 us by card, 5.5-5.9 TB/s), with 8-bit states 16.1 (138 M: 404 us,
+// Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 842 us, 6.0 TB/s), with 8-bit states 16.1 (138 M: 404 us,
 // 5.5 TB/s; four streams read and five written, a copy reaches 6.6).  A thread takes four elements, eight lanes a scale.  What it took, us for these two: four elements side by
 // side instead of eight in a thread, past the caches where the states are larger than those (1000 -> 903 / 501 -> 480), tiles within a tensor without a decision between their
 // loads, a wait behind each, and 8-bit states that find out once a wave whether every code is a normal one and every number finite (480 -> 413), seven waves a SIMD instead of six (413
-// -> 404).  Twice and four times the tile, 512 or 1024 threads, runs of tiles per die, blocks that stay for several tiles: no better.
+// -> 404), four for fp32 states
+// out of memory (907 -> 842).  Twice and four times the tile, 512 or 1024 threads, runs of tiles per die, blocks that stay for several tiles: no better.
 // Tensors travel in the kernel's arguments, 4 KiB, a launch for 55 to 64 of them, so nothing has to be laid out on the device and a captured
 // launch holds all it needs (61 000 parameters in 150 tensors: 14 us, 22 M in 400 with 8-bit states 107).
 #include "operator_call.hpp"
@@ -300,7 +301,11 @@ __device__ __forceinline__ void update(const AdamWParams &s, const Tensor &t, co
     }
 }
 
-template <class TP, class TG, bool EIGHT, bool STREAM> __global__ __launch_bounds__(kThreads, EIGHT ? 7 : 8) void adamw_kernel(const AdamWParams s)
+// Waves of a SIMD: 8-bit states take the most there are registers for; fp32 states out of memory stream faster with four, whose requests lie closer together (16 workers of 11.2 M, us
+// with 8 / 5 / 4 / 3 / 2 waves: 907 / 878 / 842 / 830 / 976; 400 tensors of 80 000 for 16 workers 161 / - / 167 / 185 / -; 138 M with 8-bit states 405 with 7, 416 / 435 / 485 with 6 / 5 / 4).
+constexpr int waves_of(bool eight, bool stream) { return eight ? 7 : stream ? 4 : 8; }
+template <class TP, class TG, bool EIGHT, bool STREAM>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_of(EIGHT, STREAM), waves_of(EIGHT, STREAM)))) void adamw_kernel(const AdamWParams s)
 {
     cocod_adamw_now now = s.now;
     if (s.now_device) {
