@@ -17,11 +17,11 @@ namespace cocod {
 namespace {
 
 constexpr uint32_t kMostChoices = 64;
-constexpr uint32_t kRunPairs = 512;                  // pairs of a run at least
+constexpr uint32_t kRunPairs = 256;                  // pairs of a run at least (16384 x 8 to 128 groups: 12.5 us, with 512 13.7, 1024 19.4)
 constexpr uint32_t kMostRuns = 1024;
 constexpr uint32_t kCountRange = 8192, kPlaceRange = 4096;       // groups that a block counts / places (32 KiB of LDS each)
 constexpr uint32_t kOffsetsHere = 512;               // groups up to which every run sums up the groups in front for itself
-// One block does it all up to so many pairs and groups (us: 32 pairs, 8 groups 3 instead of 8).
+// One block does it all up to so many pairs and groups (us, one block / three launches: 2048 pairs to 8 groups 4.4 / 8.1, 8192 8.4 / 9.3, to 512 groups 11.8 / 13.9).
 constexpr uint32_t kSmallPairs = 8192, kSmallGroups = 512, kSmallWaves = 16;
 
 struct SortParams {
