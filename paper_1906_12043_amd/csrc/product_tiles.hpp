@@ -24,7 +24,8 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 // Largest factor of softmax minus one-hot kept in the element type: fp16 would lose probabilities below 2^-24.
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2, int MI_ = 32> struct TileShape {
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2, int MI_ = 32, bool ONCE_ = false> struct TileShape {
+    static constexpr bool ONCE = ONCE_;              // no other block reads what this one reads of B: past the caches
     static constexpr int STAGES = STAGES_;           // slices in LDS
     static constexpr int MI = MI_, MK = MI == 32 ? 16 : 32, X = MI * MI / 64;        // the matrix instruction: MI x MI x MK, X values a lane
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;
@@ -65,7 +66,7 @@ __device__ __forceinline__ u4 zero4() { return u4{0, 0, 0, 0}; }
 enum { kDirect = 0, kRegs = 1, kCodes = 2 };
 __device__ __attribute__((aligned(16))) const unsigned int kZeroChunk[4] = {0, 0, 0, 0};
 
-template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader {
+template <class T, int HOW, bool KC, int BX, int BK, int THREADS, bool PAST = false> struct Loader {
     typedef LdsTile<KC, BX, BK> L;
     typedef typename T::elem elem;
     static constexpr int planes = HOW == kCodes ? 1 : T::planes;
@@ -138,7 +139,7 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
                 const uint32_t row = row_of(i), c = chunk_of(i);
                 const char *from = k0 + (KC ? c * 8 : row) < k_end ? base + off[i] : reinterpret_cast<const char *>(kZeroChunk);
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, PAST ? 2 : 0);
             }
         } else {
             moved = false;
@@ -185,7 +186,7 @@ template <class T, int HOW, bool KC, int BX, int BK, int THREADS> struct Loader 
             #pragma unroll
             for (int i = 0; i < N; ++i)
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[i]),
-                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+                                                 (__attribute__((address_space(3))) void *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, PAST ? 2 : 0);
         } else {
             const uint64_t r = KC ? x0 : k0, q = KC ? k0 : x0;
             #pragma unroll
@@ -377,7 +378,7 @@ template <class T, Layout LAYOUT, class S, int HOW_A, int HOW_B> struct Product 
     static constexpr bool WEIGHTS = LAYOUT == Layout::Weights;
     static constexpr bool A_KC = !WEIGHTS, B_KC = LAYOUT == Layout::Rows_NK;
     typedef Loader<T, HOW_A, A_KC, S::BM, S::BK, S::threads> LoadA;
-    typedef Loader<T, HOW_B, B_KC, S::BN, S::BK, S::threads> LoadB;
+    typedef Loader<T, HOW_B, B_KC, S::BN, S::BK, S::threads, S::ONCE> LoadB;
     static constexpr int PA = LoadA::planes, PB = LoadB::planes, SUMS = PB == 1 ? 1 : 2;
     static constexpr int stage = LoadA::bytes + LoadB::bytes;
     static constexpr int join_bytes = S::WK > 1 ? S::WK * S::BM * (S::BN + 4) * 4 : S::threads / 64 * S::MI * (S::NB * S::MI + 4) * 4;
@@ -1075,6 +1076,8 @@ typedef TileShape<32, 64, 128, 1, 1, 4> Small16;
 // short sums and few blocks: a slice more in flight (one row, 4096 x 4096: 10.1 us instead of 11.0; the other tiles lose by four slices of 32: 8 groups
 // of 8192 rows, 4096 x 4096, input gradient 1962 us instead of 1840: of a row of 64 bytes the other half of the line is fetched again)
 typedef TileShape<32, 64, 128, 1, 1, 4, 3> Small16Direct;
+// a large table that a few rows read once, past the caches: 4 rows, 131072 entries of 2048 105 us -> 90 (6.0 TB/s); two or four slices in flight 120
+typedef TileShape<32, 64, 128, 1, 1, 4, 3, 32, true> Small16Once;
 typedef TileShape<128, 128, 32, 2, 4, 1> Medium32;
 typedef TileShape<32, 64, 64, 1, 2, 2> Small32;
 // between these, three blocks on a compute unit: weight gradient of 4 groups of 250 rows, 512 x 768 13.7 us instead of 15.3 (medium) and 17.4 (small), of 2 of
@@ -1118,6 +1121,8 @@ hipError_t launch_layout(hipStream_t stream, Tile tile, const ProductParams &p)
             if (tile == Tile::Deep) return launch_one<T, LAYOUT, Deep16, FINISH, kDirect, kDirect>(stream, p);
             if constexpr (FINISH == Finish::Store && !WEIGHTS)
                 if (tile == Tile::Tall) return launch_one<T, LAYOUT, Tall16, FINISH, kDirect, kDirect>(stream, p);
+            if constexpr (FINISH == Finish::Moments)
+                if (tile == Tile::Small && p.b_once) return launch_one<T, LAYOUT, Small16Once, FINISH, kDirect, kDirect>(stream, p);
             return tile == Tile::Small ? launch_one<T, LAYOUT, Small16Direct, FINISH, kDirect, kDirect>(stream, p)
                                        : launch_one<T, LAYOUT, Medium16, FINISH, kDirect, kDirect>(stream, p);
         }

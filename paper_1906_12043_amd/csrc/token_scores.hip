@@ -756,6 +756,7 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     z.target = !c->targets ? nullptr : gathered ? reinterpret_cast<const int32_t *>(ws + w.target) : c->targets;
     z.target_logit = reinterpret_cast<float *>(ws + w.target_logit);
     z.logit_scale = c->scale;
+    z.b_once = c->rows <= tile_size(t, Tile::Small).bm && static_cast<uint64_t>(c->groups) * c->vocab * c->dim * s > kLastLevelCache;
     z.moments = reinterpret_cast<float4 *>(ws + w.moments);
     z.moment_tiles = (c->vocab + cols - 1) / cols;
     z.quads = c->top ? reinterpret_cast<float *>(ws + w.quads) : nullptr;

@@ -317,6 +317,18 @@ def test_the_loss_is_minus_the_log_probability():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("bounds", [[0, 5], [0, 20, 32]])
+def test_a_table_larger_than_the_caches_and_few_rows(dtype, bounds):
+    rows, groups, dim, vocab = bounds[-1], len(bounds) - 1, 520, 300_001 // (len(bounds) - 1)
+    gen, h, e, target = inputs(dtype, bounds, rows, vocab, dim, 0, 50, lattice=True)
+    c, out = scores_call(dtype, bounds, h, e, target, top=5)
+    P.token_scores(torch.cuda.current_stream(), c)
+    want, far = exact_scores(bounds, h, e, target)
+    check_scores(out, want, far, bounds, rows, target)
+    check_top(out, want, 5, vocab, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_the_large_tile(dtype):
     bounds, rows, vocab, dim = LARGE
     gen, h, e, target = inputs(dtype, bounds, rows, vocab, dim, 0, 40, lattice=True)
