@@ -131,6 +131,20 @@ def test_only_one_gradient_is_wanted():
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+def test_gradients_where_no_row_takes_part(dtype):
+    """No slopes at all, slopes of zero, no row with a target, no rows: every gradient is zero."""
+    t = TYPES[dtype][1]
+    gen, h, e, target = inputs(dtype, [0, 20, 50], 50, 300, 40, 0, 3)
+    h[:] = float("nan")
+    for rows, a, targets in ((50, None, target), (50, torch.zeros(50, device="cuda"), target), (50, torch.ones(50, device="cuda"), torch.full_like(target, -1)), (0, None, None)):
+        dh, de = torch.full((50, 40), 5.0, dtype=t, device="cuda"), torch.full((2, 300, 40), 5.0, dtype=t, device="cuda")
+        c, out = scores_call(dtype, [0, 20, 50] if rows else [0, 0, 0], h, e, targets, grad=True, d_logp=a, dh=dh, de=de, rows=rows)
+        out["norms"].zero_()
+        P.token_scores_grad(torch.cuda.current_stream(), c)
+        assert bool((de == 0).all()) and bool((dh == (0 if rows else 5.0)).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 def test_one_table_for_all_groups(dtype):
     bounds = [0, 30, 30, 77]
     gen, h, e, target = inputs(dtype, bounds, 77, 900, 80, 0, 2, shared=True)
@@ -283,6 +297,33 @@ def test_replays_follow_their_inputs(rows, vocab):
         want, far = exact_scores(offsets.tolist(), h, e, target, 1.0, a, b)
         assert bool(((got["logp"].double() - want["logp"]).abs() <= far["logp"])[:rows - k].all())
         assert bool(((got["de"].double() - want["de"]).abs() <= far["de"]).all())
+
+
+def test_two_graphs_with_a_workspace_each_at_once():
+    graphs = []
+    for k in range(2):
+        gen, h, e, target = inputs("bf16", [0, 400, 900], 900, 3000, 64, 0, 60 + k, lattice=True)
+        a = torch.randn(900, generator=gen, device="cuda")
+        dh, de = torch.zeros_like(h), torch.zeros_like(e)
+        c, out = scores_call("bf16", [0, 400, 900], h, e, target, grad=True, top=6, d_logp=a, dh=dh, de=de)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            P.token_scores(side, c)
+            P.token_scores_grad(side, c)
+        graphs.append((graph, side, c, out, h, e, target, a, dh, de))
+    for _ in range(3):
+        for graph, side, *_ in graphs:
+            with torch.cuda.stream(side):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, _, c, out, h, e, target, a, dh, de in graphs:
+        want, far = exact_scores([0, 400, 900], h, e, target, 1.0, a)
+        check_scores(out, want, far, [0, 400, 900], 900, target)
+        check_top(out, want, 6, 3000, True)
+        for k, got in (("dh", dh), ("de", de)):
+            assert bool(((got.double() - want[k]).abs() <= far[k]).all())
 
 
 def test_two_streams_with_a_workspace_each():
