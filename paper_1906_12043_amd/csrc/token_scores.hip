@@ -35,7 +35,7 @@ constexpr uint32_t kMostTop = 32;
 // its alternatives instead of four (300 rows with 20: 31 against 26).
 constexpr uint32_t kFewRows = 512, kVeryFewRows = 64;
 constexpr float kEntropyBound = 32.0f, kSlopeScale16 = 0x1p14f;
-// Up to so many bytes of hidden states per group rows stay where they are, those without a target among them.
+// Up to so many bytes of hidden states per group rows stay where they are, those without a target among them (509 rows of 512 in fp32, forward and backward: 143 us instead of 149).
 constexpr uint64_t kLeaveHere = 1u << 20;
 // Up to so many bytes per group the block that finds the rows also copies them (9 rows of 1728 in fp16: 5 us instead of 10).
 constexpr uint64_t kGatherHere = 32u << 10;
@@ -743,7 +743,7 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     taking.rows = {c->offsets, c->groups, c->rows, c->targets, c->vocab};
     // Rows stay where they are if all of them take part or they are few, and the product can take them there.
     ProductParams z = logits_operands(c, w, ws, false);
-    const bool gathered = (c->targets && (t == Dtype::F32 || c->rows * w.pitch * s > kLeaveHere * c->groups)) || (t != Dtype::F32 && direct_b(Layout::Rows_NK, z) && !direct_a(Layout::Rows_NK, z));
+    const bool gathered = (c->targets && c->rows * w.pitch * s > kLeaveHere * c->groups) || (t != Dtype::F32 && direct_b(Layout::Rows_NK, z) && !direct_a(Layout::Rows_NK, z));
     if (gathered) z = logits_operands(c, w, ws, true);
     if (!fits(c, Layout::Rows_NK, w.logits, z, 0, c->vocab, 1)) return launch_status(hipErrorInvalidConfiguration, what);
     if (gathered)
