@@ -17,7 +17,7 @@
 // -> 404), four for fp32 states
 // out of memory (907 -> 842).  Twice and four times the tile, 512 or 1024 threads, runs of tiles per die, blocks that stay for several tiles: no better.
 // Tensors travel in the kernel's arguments, 4 KiB, a launch for 55 to 64 of them, so nothing has to be laid out on the device and a captured
-// launch holds all it needs (61 000 parameters in 150 tensors: 14 us, 22 M in 400 with 8-bit states 107).
+// launch holds all it needs (61 000 parameters in 150 tensors: 18 us, 22 M in 400 with 8-bit states 130).
 #include "operator_call.hpp"
 #include "row_access.hpp"
 

@@ -18,7 +18,7 @@
 // slope is off by half a step of itself.  The largest slope of most rows is the target's, and its rounding would be that of the row's whole gradient; so the mantissa
 // of the target's slope is taken out of the row's slopes, which leaves a power of two there: dh is multiplied by it in fp32, and the product for dE
 // takes rows of h times it (a row whose entry no other row has for its target is then rounded once, as its last rounding would; 4096 rows, 32003 entries of 1024,
-// error of dh and dE against 64 bits: 1.02 times that of a plain form in fp32, 1.41 times without).  fp16 slopes are also taken times a power of two per
+// error against 64 bits: dh 1.00 and dE 1.23 times that of a plain form in fp32, both 1.41 times without).  fp16 slopes are also taken times a power of two per
 // group that brings their bound below 2^14: p |d - D| is below 22 for any vocabulary up to 2^30, so |a| + 32 |b| bounds a slope.  Rows whose slopes a and
 // b are both zero take no part.
 #include "vocabulary.hpp"
@@ -31,13 +31,13 @@ namespace {
 
 constexpr uint64_t kMaxScoreRows = 1ull << 26;
 constexpr uint32_t kMostTop = 32;
-// Up to so many rows four waves take a row's statistics instead of one (32000 entries: 300 rows with 20 alternatives 23 us instead of 37, 2000 with 8 23 against 16), and sixteen
-// its alternatives instead of four (300 rows with 20: 31 against 26).
+// Up to so many rows four waves take a row's statistics instead of one (32000 entries: 300 rows with 20 alternatives 11.8 us instead of 17.6, 2000 with 8 20 against
+// 14.5), and sixteen its alternatives instead of four (16 rows with 20 of 512: 7.5 us instead of 12.1, 300 rows 14.2 against 12.8).
 constexpr uint32_t kFewRows = 512, kVeryFewRows = 64;
 constexpr float kEntropyBound = 32.0f, kSlopeScale16 = 0x1p14f;
 // Up to so many bytes of hidden states per group rows stay where they are, those without a target among them (509 rows of 512 in fp32, forward and backward: 143 us instead of 149).
 constexpr uint64_t kLeaveHere = 1u << 20;
-// Up to so many bytes per group the block that finds the rows also copies them (9 rows of 1728 in fp16: 5 us instead of 10).
+// Up to so many bytes per group the block that finds the rows also copies them (9 rows of 1728 in fp16, gradient: 6 us instead of 3 and 5 in two launches).
 constexpr uint64_t kGatherHere = 32u << 10;
 
 // Which rows take part, and with what slopes.
@@ -256,7 +256,7 @@ __device__ __forceinline__ uint32_t above(unsigned long long mine, uint32_t coun
 
 // The k largest of the `all` ranks in `list` (all different, but for 0), in order, by one wave: lane j returns the j-th, 0 where there are fewer.  A lane's best is the best of every
 // 64th; what is not below the k-th of the lanes' bests, k ranks and hardly more, is put together and each one's place counted.  (Where that is
-// more than a wave, one after the other: a lane keeps its best two and looks for more when both are taken.  20 of 320: 1 us instead of 6.)
+// more than a wave, one after the other: a lane keeps its best two and looks for more when both are taken.  300 rows, 20 of 32000 entries: the kernel takes 15 us instead of 23.)
 __device__ __forceinline__ unsigned long long pick(const unsigned long long *list, uint32_t all, uint32_t k, unsigned long long *scratch, uint32_t lane)
 {
     unsigned long long best = 0, next = 0;
