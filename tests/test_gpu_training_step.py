@@ -7,11 +7,14 @@ four sums of few terms: below 5e-4, in the 2-norm.  A step from m = 0 and v = 0.
 relative error in the 2-norm is at most that of g plus 14 roundings.
 """
 import math
+import os
+import re
 
 import pytest
 import torch
 
 import paper_1906_12043_amd as P
+from tests.scores_harness import exact_scores
 
 pytestmark = pytest.mark.gpu
 T, K, G, C, F, V = 300, 2, 5, 64, 72, 413            # tokens, choices, experts, columns, hidden columns, entries
@@ -147,3 +150,42 @@ def test_the_same_steps_replayed():
         for (name, x), y in zip(a.outputs().items(), b.outputs().values()):
             assert torch.equal(x, y), (k, name)
     assert math.isfinite(float(a.e.sum()))
+
+
+def test_the_second_example_of_the_readme():
+    """Run as it stands, in bf16.  Places and rows are whole; a token's sum of two products is off by three roundings of 2^-24 of the magnitudes and one of half a step of bf16.  From states of
+    zero a step moves every parameter by lr g / (|g| + eps), as m / c1 = g and v / c2 = g^2: within sixteen roundings of 2^-24, and 2^-24 (0.9 / 0.1 + 0.95 / 0.05 / 2) < 1.1e-6
+    where 1 - beta and c are made from beta in different precisions."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    example, = re.findall(r"```py\n(.*?)```", text, re.S)
+    W, T, K, N, V, n = 4, 50, 64, 72, 100, 1000                                        # noqa: N806
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)          # noqa: E731
+    new = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device="cuda")            # noqa: E731
+    tokens, rows_out, table = rand(T, K), rand(2 * T, N), rand(V, N)
+    chosen = torch.randint(0, W, (T, 2), generator=gen, device="cuda", dtype=torch.int32)
+    given = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    weights = torch.rand(T, 2, generator=gen, device="cuda")
+    place, offsets, x, tokens_out = new(T, 2, dtype=torch.int32), new(W + 1, dtype=torch.int64), new(2 * T, K, dtype=torch.bfloat16), new(T, N, dtype=torch.bfloat16)
+    logp, entropy, norms, ids, logps = new(T), new(T), new(T, 4), new(T, 8, dtype=torch.int32), new(T, 8)
+    g = rand(n)
+    p = new(n)
+    model = [(p, g, new(n, dtype=torch.uint8), new(n, dtype=torch.uint8), new(32, dtype=torch.uint8), new(32, dtype=torch.uint8))]
+    names = dict(P=P, torch=torch, W=W, T=T, K=K, N=N, V=V, chosen=chosen, place=place, offsets=offsets, weights=weights, tokens=tokens, x=x, rows_out=rows_out, tokens_out=tokens_out,
+                 one_group=torch.tensor([0, T], device="cuda"), table=table, given=given, temperature=2.0, logp=logp, entropy=entropy, norms=norms, ids=ids, logps=logps, model=model, t=1,
+                 stream=torch.cuda.current_stream())
+    exec(compile(example, "README.md", "exec"), names)
+    flat = chosen.reshape(-1).long()
+    order = torch.sort(flat, stable=True).indices
+    want = torch.empty_like(order)
+    want[order] = torch.arange(2 * T, device="cuda")
+    assert torch.equal(place.reshape(-1).long(), want) and offsets.tolist() == [int((flat < k).sum()) for k in range(W + 1)]
+    assert torch.equal(x[want], tokens.repeat_interleave(2, 0))
+    parts = rows_out[want].double().reshape(T, 2, N) * weights.double()[:, :, None]
+    assert bool(((tokens_out.double() - parts.sum(1)).abs() <= 2.0 ** -8 * parts.sum(1).abs() + 3 * 2.0 ** -24 * 1.01 * parts.abs().sum(1)).all())
+    exact, far_off = exact_scores([0, T], tokens_out, table[None], given, 0.5)
+    assert bool(((logp.double() - exact["logp"]).abs() <= far_off["logp"]).all()) and bool(((entropy.double() - exact["entropy"]).abs() <= far_off["entropy"]).all())
+    best = exact["all"].topk(8).values
+    assert bool(((logps.double() - best).abs() <= 2 * exact["far_all"][:, None] + 2.0 ** -20 * best.abs()).all())
+    step = -3e-4 * g.double() / (g.double().abs() + 1e-8)
+    assert bool(((p.double() - step).abs() <= 3e-4 * (16 * 2.0 ** -24 + 1.1e-6)).all())
