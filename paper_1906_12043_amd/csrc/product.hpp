@@ -69,7 +69,7 @@ struct ProductParams {
     const float *target_slope;        // [rows]: probability of the target, less one
     uint32_t v0;                      // vocabulary entry of column 0
     // token scores
-    uint32_t b_once;                  // no tile of B is read twice, and B is larger than the caches
+    uint32_t b_once;                  // a group reads no tile of B twice, and B is larger than the caches
     float logit_scale;                // logits are multiplied by it, > 0
     float4 *moments;                  // [rows][column tiles]: maximum, sum, sum of distances (target may be null then)
     uint32_t moment_tiles;

@@ -25,7 +25,7 @@ constexpr uint32_t kBandTiles = 8;                   // row tiles that take turn
 template <class T> constexpr float slope_scale() { return std::is_same<T, F16>::value ? 0x1p14f : 1.0f; }
 
 template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int STAGES_ = 2, int MI_ = 32, bool ONCE_ = false> struct TileShape {
-    static constexpr bool ONCE = ONCE_;              // no other block reads what this one reads of B: past the caches
+    static constexpr bool ONCE = ONCE_;              // what a block reads of B is not read again soon: past the caches
     static constexpr int STAGES = STAGES_;           // slices in LDS
     static constexpr int MI = MI_, MK = MI == 32 ? 16 : 32, X = MI * MI / 64;        // the matrix instruction: MI x MI x MK, X values a lane
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WK = WK_;

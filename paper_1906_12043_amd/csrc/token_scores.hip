@@ -756,7 +756,8 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     z.target = !c->targets ? nullptr : gathered ? reinterpret_cast<const int32_t *>(ws + w.target) : c->targets;
     z.target_logit = reinterpret_cast<float *>(ws + w.target_logit);
     z.logit_scale = c->scale;
-    z.b_once = c->rows <= tile_size(t, Tile::Small).bm && static_cast<uint64_t>(c->groups) * c->vocab * c->dim * s > kLastLevelCache;
+    // (one table for 16 groups of a row, 32000 entries of 1024: 113 us instead of 128 past the caches; 4 groups of two rows, 131072 of 2048: 213 against 209)
+    z.b_once = c->rows <= tile_size(t, Tile::Small).bm && static_cast<uint64_t>(z.b_group ? c->groups : 1) * c->vocab * c->dim * s > kLastLevelCache;
     z.moments = reinterpret_cast<float4 *>(ws + w.moments);
     z.moment_tiles = (c->vocab + cols - 1) / cols;
     z.quads = c->top ? reinterpret_cast<float *>(ws + w.quads) : nullptr;
