@@ -95,7 +95,8 @@ template <class T> __device__ __forceinline__ void gather_row(const Taking &p, c
     const float a = slope_of_logp(p, from), b = slope_of_entropy(p, from), inverse = 1.0f / (1.0f + n.y);
     const float back = q.normal ? q.row_scale[r] : 1.0f, k = q.scale / back;
     const float pt = expf(n.w) * inverse, others = n.w == 0.0f ? n.y * inverse : 1.0f - pt;
-    float target = (a * others + b * pt * (n.z - n.w)) * k, mantissa = 1.0f;
+    // (a target at minus infinity has no part in the entropy's slope; a NaN is in pt as well)
+    float target = (a * others + b * pt * (n.z - fmaxf(n.w, kFarBelow))) * k, mantissa = 1.0f;
     if (q.row_scale && p.rows.target && fabsf(target) > 0x1p-126f && fabsf(target) < 0x1p126f) {
         mantissa = __builtin_amdgcn_frexp_mantf(fabsf(target));       // in 1/2 .. 1
         target = copysignf(ldexpf(1.0f, __builtin_amdgcn_frexp_expf(target)), target);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_1906_12043_amd as P
-from tests.operator_harness import STEP, TYPES, matrix, output, stack, untouched
+from tests.operator_harness import STEP, TYPES, half_step, matrix, output, stack, untouched
 from tests.scores_harness import exact_scores, scores_call
 
 pytestmark = pytest.mark.gpu
@@ -383,3 +383,48 @@ def test_the_large_tile(dtype):
     check_top(out, want, 8, e.shape[1], True)
     for k, got in (("dh", dh), ("de", de)):
         assert bool(((got.double() - want[k]).abs() <= far[k]).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows", [6, 300])
+@pytest.mark.parametrize("slopes", ["logp", "entropy", "both"])
+def test_gradients_where_the_target_has_no_probability(dtype, rows, slopes):
+    """Entry 10 has the logit minus infinity in every other row, and is the target of some of these: log p is minus infinity, its slope a (1 - 0), that of the entropy 0.
+    The other logits are sums of multiples of 1/8, exact.  A probability is then off by less than 500 steps of 2^-23 and D by 3e-4 (scores_harness), so a slope by 1e-3 (|dz| + |b| p), its
+    rounding and, in fp16, two halves of 2^-38 (|a| + 32 |b|); for de h is rounded once more."""
+    vocab, dim, t = 700, 64, TYPES[dtype][1]
+    u = half_step(t) if t != torch.float32 else 0.0
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    h = torch.randint(-1, 2, (rows, dim), generator=gen, device="cuda").to(t)
+    e = (torch.randint(-4, 5, (1, vocab, dim), generator=gen, device="cuda") / 8).to(t)
+    h[:, 0], e[0, :, 0] = 0.0, 0.0
+    h[1::2, 0], e[0, 10, 0], scale = (2.0, -3e38, 1.0) if dtype != "fp16" else (2.0 ** 14, -2.0 ** 14, 2.0 ** 101)
+    if dtype == "fp16":                                                                # (a scale that brings 2^28 to infinity: the others are zero)
+        e[0, :, 1:] = 0.0
+    target = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    target[1::4], target[2::4] = 10, 10
+    a, b = (torch.empty(rows, device="cuda").uniform_(0.2, 0.4, generator=gen) / scale for _ in range(2))
+    one, two = a if slopes != "entropy" else None, b if slopes != "logp" else None
+    dh, de = torch.empty_like(h), torch.empty_like(e)
+    c, out = scores_call(dtype, [0, rows], h, e, target, grad=True, scale=scale, d_logp=one, d_entropy=two, dh=dh, de=de)
+    P.token_scores(torch.cuda.current_stream(), c)
+    P.token_scores_grad(torch.cuda.current_stream(), c)
+    assert bool((out["logp"][1::4] == -math.inf).all()) and bool(torch.isfinite(out["entropy"]).all())
+    f = torch.float64
+    hh, ee = h.to(f), e[0].to(f)
+    z = scale * (hh @ ee.t())                                                          # (there is more room above here: p is 0, log p finite)
+    p, x = torch.softmax(z, 1), z - z.amax(1, keepdim=True)
+    off_mean = torch.where(p > 0, x - (p * x).sum(1, keepdim=True), 0.0)
+    hot = torch.zeros_like(p)
+    hot.scatter_(1, target.long()[:, None], 1.0)
+    a64, b64 = (v.to(f)[:, None] * scale if v is not None else torch.zeros(rows, 1, dtype=f, device="cuda") for v in (one, two))
+    dz = a64 * (hot - p) - b64 * p * off_mean
+    off = 1e-3 * (dz.abs() + b64 * p)
+    off = off + u * (dz.abs() + off) + (2.0 ** -38 * (a64 + 32 * b64).max() if t == torch.float16 else 0.0)
+    for got, left, far, right, again in ((dh, dz, off, ee, 0.0), (de[0], dz.t(), off.t(), hh, u)):
+        want, magnitude = left @ right, left.abs() @ right.abs()
+        bound = (far @ right.abs() + again * magnitude + (max(vocab, rows) + 8) * STEP * magnitude) * (1 + 2 * u) + (half_step(t) + STEP) * want.abs()
+        bound += torch.finfo(t).smallest_normal * torch.finfo(t).eps
+        # (what lies beyond the type's largest number and half a step is infinite: 150 rows of 0.3 x 2^14 in fp16, above 65520)
+        over = want.abs() - bound >= torch.finfo(t).max * (1 + torch.finfo(t).eps / 4)
+        assert bool(torch.where(over, got.to(f) == torch.sign(want) * math.inf, (got.to(f) - want).abs() <= bound).all())
