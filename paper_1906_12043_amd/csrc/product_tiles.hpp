@@ -722,13 +722,20 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
         unscale = P::PA == 3 ? kPlaneUnscale : 1.0f / kPlaneScale;
         bool fine = true;
         #pragma unroll
-        for (int i = 0; i < S::MB; ++i)
+        for (int i = 0; i < S::MB; ++i) {
+            // (a row without a target takes no part, so it has no say in how the others' sums are formed, nor have its repeats behind the last row)
+            bool counts = true;
+            if constexpr (FINISH == Finish::Moments) {
+                const uint32_t r = (wm * S::MB + i) * S::MI + lane % S::MI;
+                counts = r < at.rows && (!p.target || static_cast<uint32_t>(p.target[at.row0 + r]) < p.n);
+            }
             #pragma unroll
             for (int j = 0; j < S::NB; ++j) {
                 acc[0][i][j] += acc[P::SUMS - 1][i][j];
                 #pragma unroll
-                for (int r = 0; r < 16; ++r) fine = fine && __builtin_isfinite(acc[0][i][j][r]);
+                for (int r = 0; r < 16; ++r) fine = fine && (!counts || __builtin_isfinite(acc[0][i][j][r]));
             }
+        }
         if (__syncthreads_or(!fine)) {
             // the same sums with fp32 products: what is not finite then is so by fp32 arithmetic
             unscale = 1.0f;

@@ -428,3 +428,22 @@ def test_gradients_where_the_target_has_no_probability(dtype, rows, slopes):
         # (what lies beyond the type's largest number and half a step is infinite: 150 rows of 0.3 x 2^14 in fp16, above 65520)
         over = want.abs() - bound >= torch.finfo(t).max * (1 + torch.finfo(t).eps / 4)
         assert bool(torch.where(over, got.to(f) == torch.sign(want) * math.inf, (got.to(f) - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("which", range(len(SHAPES)))
+def test_rows_without_a_target_change_no_bit_of_the_others(dtype, which):
+    """Whatever such a row holds, NaN, infinities or numbers whose products overflow: the results of all others are the same."""
+    bounds, rows, vocab, dim = SHAPES[which]
+    gen, h, e, target = inputs(dtype, bounds, rows, vocab, dim, 0, 500 + which)
+    target[::3] = torch.where(torch.arange(len(target[::3]), device="cuda") % 2 == 0, -1, vocab).to(torch.int32)
+    gone = (target < 0) | (target >= vocab)
+    seen = []
+    for fill in (0.0, float("nan"), math.inf, torch.finfo(h.dtype).max):
+        h[gone] = fill
+        c, out = scores_call(dtype, bounds, h, e, target, top=4, scale=0.7)
+        P.token_scores(torch.cuda.current_stream(), c)
+        seen.append(out)
+    for out in seen[1:]:
+        for k in seen[0]:
+            assert torch.equal(torch.nan_to_num(out[k].float(), 7.0), torch.nan_to_num(seen[0][k].float(), 7.0)), k
