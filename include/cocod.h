@@ -511,8 +511,9 @@ enum { COCOD_TOKEN_SCORES_FORWARD = 0, COCOD_TOKEN_SCORES_GRAD = 1 };
  *
  * The gradient is that of sum over r of d_logp[r] logp[r] + d_entropy[r] entropy[r]; the call reads norms as the forward call of the same h, e, scale and targets left
  * them (and offsets, h, e, targets, scale).  A row where both slopes are 0 takes no part.  16-bit types: the slopes at the logits are rounded to the type before the products
- * (bf16: by up to 2^-8 of themselves, fp16: 2^-11, not below 2^-38 of the group's largest |d_logp| + 32 |d_entropy|), so an entry of dh or de is off by
- * up to that part of the sum of its products' magnitudes, beside its own rounding.  COCOD_F32 keeps them in fp32.  A group without rows that take part has gradient 0.
+ * (bf16: by up to 2^-8 of themselves, fp16: 2^-11, not below 2^-38 of the group's largest |d_logp| + 32 |d_entropy|), so an entry of dh is off by up to that part of the sum
+ * of its products' magnitudes, beside its own rounding.  For de a row of h is taken times a number of its own and rounded as well (fp16: not below 2^-39 of the largest finite
+ * |h| in the group's rows that take part), so an entry of de is off by up to twice that part.  COCOD_F32 keeps both in fp32.  A group without rows that take part has gradient 0.
  */
 typedef struct cocod_token_scores_call {
     uint32_t struct_size;           /* sizeof(cocod_token_scores_call); checked */

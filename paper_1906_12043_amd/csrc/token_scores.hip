@@ -64,6 +64,7 @@ template <class E> struct Gather {
     E *out;
     uint64_t pitch;
     E *scaled;                        // non-null: rows times the mantissa of their target's slope
+    float *lift;                      // non-null (fp16, with scaled): [rows] power of two that the rows of `scaled` are taken times
     // gradient
     E *dh;                            // may be null
     uint64_t lddh;
@@ -73,7 +74,7 @@ template <class E> struct Gather {
     float *row_scale;                 // may be null (fp32: nothing is taken out)
     float *top, *none, *one, *target_slope;
 };
-// A row times a factor of at most 1, rounded to the type.
+// A row times a factor, rounded to the type.
 template <class T> __device__ __forceinline__ void scaled_row(const typename T::elem *src, uint32_t dim, typename T::elem *dst, uint64_t pitch, float factor, uint32_t lane)
 {
     typedef Piece<T> V;
@@ -84,6 +85,23 @@ template <class T> __device__ __forceinline__ void scaled_row(const typename T::
         for (uint32_t i = 0; i < V::N; ++i) v[i] = V::value(raw, i) * factor;
         V::store(dst + j, V::pack(v));
     }
+}
+// The largest magnitude of a row that is finite, in all lanes of a wave.
+template <class T> __device__ __forceinline__ float largest_of_row(const typename T::elem *src, uint32_t dim, uint32_t lane)
+{
+    typedef Piece<T> V;
+    float most = 0.0f;
+    for (uint32_t j = lane * V::N; j < dim; j += 64 * V::N) {
+        const u4 raw = V::load(src + j, dim - j);
+        #pragma unroll
+        for (uint32_t i = 0; i < V::N; ++i) {
+            const float v = fabsf(V::value(raw, i));
+            if (v < INFINITY) most = fmaxf(most, v);
+        }
+    }
+    #pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    return most;
 }
 // Row r of the copies, from row `from` of the caller's, by a wave.
 template <class T> __device__ __forceinline__ void gather_row(const Taking &p, const Gather<typename T::elem> &q, uint64_t r, uint32_t from, uint32_t lane)
@@ -101,7 +119,7 @@ template <class T> __device__ __forceinline__ void gather_row(const Taking &p, c
         mantissa = __builtin_amdgcn_frexp_mantf(fabsf(target));       // in 1/2 .. 1
         target = copysignf(ldexpf(1.0f, __builtin_amdgcn_frexp_expf(target)), target);
     }
-    if (q.scaled) scaled_row<T>(h, q.dim, q.scaled + r * q.pitch, q.pitch, mantissa, lane);
+    if (q.scaled) scaled_row<T>(h, q.dim, q.scaled + r * q.pitch, q.pitch, q.lift ? mantissa * q.lift[r] : mantissa, lane);
     if (lane == 0) {
         const float even = inverse * k / mantissa;
         q.top[r] = n.x;
@@ -118,19 +136,32 @@ template <class T> __device__ __forceinline__ void clear_row(const Taking &p, co
         for (uint32_t j = lane; j < q.dim; j += 64) q.dh[r * q.lddh + j] = 0;
 }
 
+// By row of the caller's that takes part, its largest magnitude; a wave a row.
+constexpr uint32_t kMostRowBlocks = 1u << 23, kMostAlternativeBlocks = 1u << 21;
+template <class T> __global__ __launch_bounds__(256) void scores_reach_kernel(const Taking p, const Gather<typename T::elem> q)
+{
+    const uint32_t lane = threadIdx.x % 64;
+    for (uint64_t r = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / 64; r < p.rows.rows; r += static_cast<uint64_t>(gridDim.x) * 4) {
+        if (!in_groups(p.rows, r) || !takes_part(p, r)) continue;
+        const float most = largest_of_row<T>(q.h + r * q.ldh, q.dim, lane);
+        if (lane == 0) q.lift[r] = most;
+    }
+}
+
 // One block per group: the rows that take part, in order, to the front of the group's part of `index`; kNoRow behind them.  NORMAL: the group's power of
-// two, for the table's gradient and row by row.  HERE: the copies as well (a launch less where there is little to copy).
+// two, for the table's gradient and row by row, and where h gets a second copy the power of two that brings the largest magnitude of the group's rows to 2^14 .. 2^15 there: 16-bit
+// floats below 2^-14 have fewer digits, and h times a mantissa would be rounded by up to a third of itself.  HERE: the copies as well (a launch less where there is little to copy).
 constexpr int kTakeThreads = 1024;
 template <class T, bool NORMAL, bool HERE>
 __global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, float scale, uint32_t *index, int32_t *target, int64_t *ends, float *group_scale, float *row_scale,
                                                             const Gather<typename T::elem> gather)
 {
     __shared__ uint32_t counts[kTakeThreads / 64];
-    __shared__ float most[kTakeThreads / 64];
+    __shared__ float most[kTakeThreads / 64], furthest[kTakeThreads / 64];
     const uint32_t g = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint64_t begin = clamped(p.rows, g), next = clamped(p.rows, g + 1), end = next > begin ? next : begin;
     uint64_t at = begin;
-    float bound = 0.0f;
+    float bound = 0.0f, reach = 0.0f;
     for (uint64_t r0 = begin; r0 < end; r0 += kTakeThreads) {
         const uint64_t r = r0 + threadIdx.x;
         const bool in = r < end && takes_part(p, r);
@@ -144,6 +175,7 @@ __global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, floa
             index[to] = static_cast<uint32_t>(r);
             target[to] = p.rows.target ? p.rows.target[r] : -1;
             if (NORMAL) bound = fmaxf(bound, fabsf(slope_of_logp(p, r)) + kEntropyBound * fabsf(slope_of_entropy(p, r)));
+            if (NORMAL && !HERE && gather.lift) reach = fmaxf(reach, gather.lift[r]);
         }
         at += all;
         __syncthreads();
@@ -151,17 +183,25 @@ __global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, floa
     for (uint64_t r = at + threadIdx.x; r < end; r += kTakeThreads) index[r] = kNoRow;
     if (threadIdx.x == 0) ends[g] = static_cast<int64_t>(at);
     if constexpr (NORMAL) {
+        if (HERE && gather.lift) {
+            for (uint64_t r = begin + wave; r < end; r += kTakeThreads / 64)
+                if (takes_part(p, r)) reach = fmaxf(reach, largest_of_row<T>(gather.h + r * gather.ldh, gather.dim, lane));
+        }
         #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) bound = fmaxf(bound, __shfl_xor(bound, d, 64));
-        if (lane == 0) most[wave] = bound;
+        for (int d = 1; d < 64; d <<= 1) { bound = fmaxf(bound, __shfl_xor(bound, d, 64)); reach = fmaxf(reach, __shfl_xor(reach, d, 64)); }
+        if (lane == 0) { most[wave] = bound; furthest[wave] = reach; }
         __syncthreads();
-        for (int w = 0; w < kTakeThreads / 64; ++w) bound = fmaxf(bound, most[w]);
+        for (int w = 0; w < kTakeThreads / 64; ++w) { bound = fmaxf(bound, most[w]); reach = fmaxf(reach, furthest[w]); }
         bound *= scale;
         int e = bound > 0.0f && bound < INFINITY ? __builtin_amdgcn_frexp_expf(bound) : 0;
         e = e < -100 ? -100 : e > 100 ? 100 : e;
         const float back = ldexpf(1.0f / kSlopeScale16, e);    // what the products are multiplied by
-        if (threadIdx.x == 0) group_scale[g] = back;
-        for (uint64_t r = begin + threadIdx.x; r < at; r += kTakeThreads) row_scale[r] = back;
+        const float lift = reach > 0.0f && reach < 0x1p14f ? ldexpf(1.0f, 15 - __builtin_amdgcn_frexp_expf(reach)) : 1.0f;       // (no row to lift: 1)
+        if (threadIdx.x == 0) group_scale[g] = back / lift;
+        for (uint64_t r = begin + threadIdx.x; r < at; r += kTakeThreads) {
+            row_scale[r] = back;
+            if (gather.lift) gather.lift[r] = lift;            // (from here on by gathered row)
+        }
     }
     if constexpr (HERE) {
         __syncthreads();                                       // (also the block's writes of index and row_scale)
@@ -177,7 +217,6 @@ __global__ __launch_bounds__(kTakeThreads) void take_kernel(const Taking p, floa
 }
 
 // The copies by a launch of their own, a wave a row.
-constexpr uint32_t kMostRowBlocks = 1u << 23, kMostAlternativeBlocks = 1u << 21;
 template <class T> __global__ __launch_bounds__(256) void scores_gather_kernel(const Taking p, const Gather<typename T::elem> q)
 {
     const uint32_t lane = threadIdx.x % 64;
@@ -527,7 +566,7 @@ template <class T> __global__ __launch_bounds__(1024) void alternatives_kernel(c
 
 struct Workspace {
     uint64_t index, target, ends, hidden, target_logit, moments, quads, ld_quads, quad_rank, row_norm;
-    uint64_t scaled, row_scale, group_scale, top, none, one, target_slope, slope, sum, part;
+    uint64_t scaled, lift, row_scale, group_scale, top, none, one, target_slope, slope, sum, part;
     uint64_t pitch, piece, sum_pitch, bytes;
     uint32_t pieces;
     ProductPlan logits, to_hidden, to_table;
@@ -566,6 +605,7 @@ Workspace carve(const cocod_token_scores_call *c, bool grad)
         w.to_hidden = plan_product(Layout::Rows_KN, t, dim8, rows, c->groups, 0, c->dim, n, true);
         w.to_table = plan_product(Layout::Weights, t, true, rows, c->groups, n, c->dim, 0, true);
         w.scaled = c->de && t != Dtype::F32 ? take(rows * w.pitch * s) : w.hidden;
+        w.lift = c->de && t == Dtype::F16 ? take(rows * 4) : 0;
         w.row_scale = take(rows * 4);
         w.group_scale = take(c->groups * 4ull);
         w.top = take(rows * 4);
@@ -662,16 +702,19 @@ template <class T> hipError_t launch_gather(hipStream_t q, const Taking &taking,
         g.normal = normal;
         g.row_scale = sizeof(E) == 2 ? row_scale : nullptr;
         g.scaled = w.scaled != w.hidden ? reinterpret_cast<E *>(ws + w.scaled) : nullptr;
+        g.lift = g.scaled && normal ? reinterpret_cast<float *>(ws + w.lift) : nullptr;
         g.top = reinterpret_cast<float *>(ws + w.top); g.none = reinterpret_cast<float *>(ws + w.none);
         g.one = reinterpret_cast<float *>(ws + w.one); g.target_slope = reinterpret_cast<float *>(ws + w.target_slope);
     }
     const bool here = c->rows * w.pitch * sizeof(E) <= kGatherHere * c->groups;
+    const uint64_t blocks = (c->rows + 3) / 4;
+    const dim3 by_rows(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks));
+    if (g.lift && !here) hipLaunchKernelGGL(scores_reach_kernel<T>, by_rows, dim3(256), 0, q, taking, g);
     const auto take = normal ? (here ? take_kernel<T, true, true> : take_kernel<T, true, false>) : (here ? take_kernel<T, false, true> : take_kernel<T, false, false>);
     hipLaunchKernelGGL(take, dim3(c->groups), dim3(kTakeThreads), 0, q, taking, c->scale, index, reinterpret_cast<int32_t *>(ws + w.target), reinterpret_cast<int64_t *>(ws + w.ends),
                        reinterpret_cast<float *>(ws + w.group_scale), row_scale, g);
     if (here) return hipGetLastError();
-    const uint64_t blocks = (c->rows + 3) / 4;
-    hipLaunchKernelGGL(scores_gather_kernel<T>, dim3(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks)), dim3(256), 0, q, taking, g);
+    hipLaunchKernelGGL(scores_gather_kernel<T>, by_rows, dim3(256), 0, q, taking, g);
     return hipGetLastError();
 }
 

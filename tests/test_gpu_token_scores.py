@@ -447,3 +447,35 @@ def test_rows_without_a_target_change_no_bit_of_the_others(dtype, which):
     for out in seen[1:]:
         for k in seen[0]:
             assert torch.equal(torch.nan_to_num(out[k].float(), 7.0), torch.nan_to_num(seen[0][k].float(), 7.0)), k
+
+
+@pytest.mark.parametrize("bounds, rows, vocab, dim", [([0, 9], 9, 40, 128), ([0, 40, 40, 300], 310, 500, 64), ([0, 3000, 4000], 4000, 60, 40), ([0, 700, 1500], 1500, 4100, 64)])
+@pytest.mark.parametrize("small", [1e-6, 1e-5, 1e-3])
+def test_small_hidden_states_in_fp16(bounds, rows, vocab, dim, small):
+    """Hidden states near the least numbers of the type, in whole groups (the first) or in single columns beside large ones (the last).  The factor that a row of h gets for de is rounded
+    relative to the product (scores_harness) down to half of 2^-38 of the largest |h| of the group's rows that take part, which is added here.  Rows that take none hold the largest number."""
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    h = torch.randn(rows, dim, generator=gen, device="cuda") * small
+    h[bounds[-2]:, ::4] /= small
+    h = h.half()
+    e = torch.randn(len(bounds) - 1, vocab, dim, generator=gen, device="cuda").half()
+    target = torch.randint(-1, max(2, vocab // 20), (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    a, b = torch.randn(rows, generator=gen, device="cuda") * 300, torch.randn(rows, generator=gen, device="cuda") * 100
+    a[::6], b[::6] = 0.0, 0.0
+    h[::6] = 65504.0
+    h[target < 0] = 65504.0
+    dh, de = torch.empty_like(h), torch.empty_like(e)
+    part = (target >= 0) & ((a != 0) | (b != 0))
+    for piece, one, two in ((0, a, None), (256, a, b)):
+        c, out = scores_call("fp16", bounds, h, e, target, grad=True, scale=0.5, d_logp=one, d_entropy=two, dh=dh, de=de, piece=piece)
+        P.token_scores(torch.cuda.current_stream(), c)
+        P.token_scores_grad(torch.cuda.current_stream(), c)
+        clean = torch.where(part[:, None], h, 0.0).half()
+        want, far = exact_scores(bounds, clean, e, target, 0.5, one, two)
+        for g, (lo, hi) in enumerate(zip(bounds, bounds[1:])):
+            if hi > lo:
+                slopes = 0.5 * (one[lo:hi].abs().double() * 2 + (two[lo:hi].abs().double() * 32 if two is not None else 0.0))       # |dz| of a row in all is less
+                far["de"][g] += 2.0 ** -39 * clean[lo:hi].abs().max() * slopes[part[lo:hi]].sum()
+        inside = slice(bounds[0], bounds[-1])
+        for k, got, x, f in (("dh", dh[inside], want["dh"][inside], far["dh"][inside]), ("de", de, want["de"], far["de"])):
+            assert bool(((got.double() - x).abs() <= f).all()), (k, piece, float(((got.double() - x).abs() / f.clamp(min=1e-300)).max()))
