@@ -37,8 +37,11 @@ constexpr uint32_t kFewRows = 512, kVeryFewRows = 64;
 constexpr float kEntropyBound = 32.0f, kSlopeScale16 = 0x1p14f;
 // Up to so many bytes of hidden states per group rows stay where they are, those without a target among them (509 rows of 512 in fp32, forward and backward: 143 us instead of 149).
 constexpr uint64_t kLeaveHere = 1u << 20;
-// Up to so many bytes per group the block that finds the rows also copies them (9 rows of 1728 in fp16, gradient: 6 us instead of 3 and 5 in two launches).
+// Up to so many bytes per group, and of so many groups in all, the block that finds the rows also copies them (9 rows of 1728 in fp16, gradient: 6 us instead of 3 and 5 in two launches;
+// 16 groups of 16 rows of 1024 in bf16 would take 24 instead of 27).  All rows may lie in one group, whose block then copies alone: gradients of 8000 rows of 1024 in one of 512 groups
+// 270 us instead of 1690 without the second bound, 256 rows in one of 16 27 instead of 57.
 constexpr uint64_t kGatherHere = 32u << 10;
+constexpr uint32_t kGatherGroups = 4;
 
 // Which rows take part, and with what slopes.
 struct Taking {
@@ -706,7 +709,7 @@ template <class T> hipError_t launch_gather(hipStream_t q, const Taking &taking,
         g.top = reinterpret_cast<float *>(ws + w.top); g.none = reinterpret_cast<float *>(ws + w.none);
         g.one = reinterpret_cast<float *>(ws + w.one); g.target_slope = reinterpret_cast<float *>(ws + w.target_slope);
     }
-    const bool here = c->rows * w.pitch * sizeof(E) <= kGatherHere * c->groups;
+    const bool here = c->rows * w.pitch * sizeof(E) <= kGatherHere * (c->groups < kGatherGroups ? c->groups : kGatherGroups);
     const uint64_t blocks = (c->rows + 3) / 4;
     const dim3 by_rows(static_cast<uint32_t>(blocks < kMostRowBlocks ? blocks : kMostRowBlocks));
     if (g.lift && !here) hipLaunchKernelGGL(scores_reach_kernel<T>, by_rows, dim3(256), 0, q, taking, g);

@@ -479,3 +479,21 @@ def test_small_hidden_states_in_fp16(bounds, rows, vocab, dim, small):
         inside = slice(bounds[0], bounds[-1])
         for k, got, x, f in (("dh", dh[inside], want["dh"][inside], far["dh"][inside]), ("de", de, want["de"], far["de"])):
             assert bool(((got.double() - x).abs() <= f).all()), (k, piece, float(((got.double() - x).abs() / f.clamp(min=1e-300)).max()))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows", [60, 240])
+@pytest.mark.parametrize("which", [0, 5, 8])
+def test_gradients_of_rows_in_one_of_nine_groups(dtype, rows, which):
+    """One group holds them all, the others are empty: on both sides of the bound up to which the group's own block copies its rows."""
+    bounds = [0] * (which + 1) + [rows] * (9 - which)
+    gen, h, e, target = inputs(dtype, bounds, rows, 90, 520, 0, 600 + which)
+    a, b = torch.randn(rows, generator=gen, device="cuda"), torch.randn(rows, generator=gen, device="cuda") * 0.1
+    dh, de = torch.full_like(h, float("nan")), torch.full_like(e, float("nan"))
+    c, out = scores_call(dtype, bounds, h, e, target, grad=True, d_logp=a, d_entropy=b, dh=dh, de=de)
+    P.token_scores(torch.cuda.current_stream(), c)
+    P.token_scores_grad(torch.cuda.current_stream(), c)
+    want, far = exact_scores(bounds, h, e, target, 1.0, a, b)
+    check_scores(out, want, far, bounds, rows, target)
+    for k, got in (("dh", dh), ("de", de)):
+        assert bool(((got.double() - want[k]).abs() <= far[k]).all()), k
