@@ -675,15 +675,17 @@ int cocod_adamw(void *stream, const cocod_adamw_call *c);
 
 /*
  * For tests: how the products of a call would run.  Makes no GPU call and reads no memory that the description points to.  Of the loss: the logits'
- * statistics, the slopes, the gradients of the hidden states and of the table (splits 0: no such product).
+ * statistics, the slopes, the gradients of the hidden states and of the table (splits 0: no such product).  Of the token scores: the logits' statistics
+ * alone, or the slopes and the two gradients, by direction.
  */
 typedef struct cocod_product_plan {
     uint32_t tile;                  /* of the result: 0 256x256, 1 128x128, 2 32x64, 3 128x128 with four slices in flight, 4 192x128, 5 64x64 */
     uint32_t splits;                /* of the sums */
-    uint32_t operands;              /* 0: both go to LDS directly, 1: through registers, 2: the first one is codes */
+    uint32_t operands;              /* 0: both go to LDS directly, 1: through registers, 2: the first one is codes, 3: both directly, the second past the caches */
 } cocod_product_plan;
 int cocod_debug_grouped_plan(const cocod_grouped *g, int direction, cocod_product_plan *out);
 int cocod_debug_cross_entropy_plan(const cocod_cross_entropy_call *c, cocod_product_plan out[4], uint32_t *pieces);
+int cocod_debug_token_scores_plan(const cocod_token_scores_call *c, int direction, cocod_product_plan out[3], uint32_t *pieces);
 
 /* Last error text of ctx, or of the last failed cocod_create / context-free call when ctx is NULL.
    Never NULL; owned by the library; valid until the next call on the same context / thread. */

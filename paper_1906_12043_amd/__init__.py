@@ -11,7 +11,7 @@ from .binding import (  # noqa: F401
     TokenScores, token_scores_workspace, token_scores, token_scores_grad, TOKEN_SCORES_RELU_IN, TOKEN_SCORES_FORWARD, TOKEN_SCORES_GRAD,
     Route, route_workspace, route_sort, route_dispatch, route_dispatch_grad, route_combine, route_combine_grad,
     AdamW, AdamWTensor, AdamWNow, adamw_now, adamw, ADAMW_STATE_F32, ADAMW_STATE_8BIT,
-    debug_grouped_plan, debug_cross_entropy_plan,
+    debug_grouped_plan, debug_cross_entropy_plan, debug_token_scores_plan,
     F32, BF16, F16, GROUPED_RELU_OUT, GROUPED_RELU_IN, GROUPED_FORWARD, GROUPED_INPUT_GRAD, GROUPED_WEIGHT_GRAD, CROSS_ENTROPY_SUM, CROSS_ENTROPY_RELU_IN,
     GRAD_QUADRATIC, GRAD_MLP, GRAD_EXTERNAL, SCHED_OVERLAP, SCHED_SERIAL, SCHED_FUSED, SCHED_HEAD, FLAG_DRY_RUN,
     OK, ERR_INVALID, ERR_STATE, ERR_HIP, ERR_NOMEM, ERR_UNSUPPORTED,

@@ -221,6 +221,7 @@ def lib():
             "cocod_cross_entropy": ([vp, P(CrossEntropy)], i32),
             "cocod_debug_grouped_plan": ([P(Grouped), i32, P(ProductPlan)], i32),
             "cocod_debug_cross_entropy_plan": ([P(CrossEntropy), P(ProductPlan), P(u32)], i32),
+            "cocod_debug_token_scores_plan": ([P(TokenScores), i32, P(ProductPlan), P(u32)], i32),
             "cocod_checkpoint_store": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_checkpoint_load": ([vp, i32, u64, u64, vp, u64, vp, u64, vp, u64], i32),
             "cocod_token_scores_workspace": ([P(TokenScores), i32, P(u64)], i32),
@@ -324,6 +325,13 @@ def debug_cross_entropy_plan(call):
     """[(tile, splits, operands)] of logits, slopes, gradient of the hidden states and of the table, and the number of pieces."""
     out, pieces = (ProductPlan * 4)(), C.c_uint32()
     _check(lib().cocod_debug_cross_entropy_plan(C.byref(call), out, C.byref(pieces)))
+    return [(p.tile, p.splits, p.operands) for p in out], pieces.value
+
+
+def debug_token_scores_plan(call, direction):
+    """[(tile, splits, operands)] of the logits (forward), or of slopes, gradient of the hidden states and of the table, and the number of pieces."""
+    out, pieces = (ProductPlan * 3)(), C.c_uint32()
+    _check(lib().cocod_debug_token_scores_plan(C.byref(call), direction, out, C.byref(pieces)))
     return [(p.tile, p.splits, p.operands) for p in out], pieces.value
 
 

@@ -681,6 +681,18 @@ ProductParams table_operands(const Workspace &w, const uint8_t *ws)
     p.b = ws + w.scaled; p.ldb = w.pitch;
     return p;
 }
+// Operands of the forward call.  Rows stay where they are if all of them take part or they are few, and the product can take them there.
+ProductParams forward_operands(const cocod_token_scores_call *c, const Workspace &w, const uint8_t *ws, bool &gathered)
+{
+    const Dtype t = kTypes[c->dtype];
+    const uint64_t s = dtype_bytes(t);
+    ProductParams z = logits_operands(c, w, ws, false);
+    gathered = (c->targets && c->rows * w.pitch * s > kLeaveHere * c->groups) || (t != Dtype::F32 && direct_b(Layout::Rows_NK, z) && !direct_a(Layout::Rows_NK, z));
+    if (gathered) z = logits_operands(c, w, ws, true);
+    // (one table for 16 groups of a row, 32000 entries of 1024: 113 us instead of 128 past the caches; 4 groups of two rows, 131072 of 2048: 213 against 209)
+    z.b_once = c->rows <= tile_size(t, Tile::Small).bm && static_cast<uint64_t>(z.b_group ? c->groups : 1) * c->vocab * c->dim * s > kLastLevelCache;
+    return z;
+}
 bool fits(const cocod_token_scores_call *c, Layout layout, const ProductPlan &plan, const ProductParams &p, uint32_t m, uint32_t n, uint32_t splits)
 {
     const Dtype t = kTypes[c->dtype];
@@ -788,10 +800,8 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     uint8_t *ws = static_cast<uint8_t *>(c->workspace);
     Taking taking{};
     taking.rows = {c->offsets, c->groups, c->rows, c->targets, c->vocab};
-    // Rows stay where they are if all of them take part or they are few, and the product can take them there.
-    ProductParams z = logits_operands(c, w, ws, false);
-    const bool gathered = (c->targets && c->rows * w.pitch * s > kLeaveHere * c->groups) || (t != Dtype::F32 && direct_b(Layout::Rows_NK, z) && !direct_a(Layout::Rows_NK, z));
-    if (gathered) z = logits_operands(c, w, ws, true);
+    bool gathered;
+    ProductParams z = forward_operands(c, w, ws, gathered);
     if (!fits(c, Layout::Rows_NK, w.logits, z, 0, c->vocab, 1)) return launch_status(hipErrorInvalidConfiguration, what);
     if (gathered)
         if (int rc = launch_status(t == Dtype::F32 ? launch_gather<F32>(q, taking, c, w, ws) : t == Dtype::BF16 ? launch_gather<Bf16>(q, taking, c, w, ws) : launch_gather<F16>(q, taking, c, w, ws), what)) return rc;
@@ -803,8 +813,6 @@ int cocod_token_scores(void *stream, const cocod_token_scores_call *c)
     z.target = !c->targets ? nullptr : gathered ? reinterpret_cast<const int32_t *>(ws + w.target) : c->targets;
     z.target_logit = reinterpret_cast<float *>(ws + w.target_logit);
     z.logit_scale = c->scale;
-    // (one table for 16 groups of a row, 32000 entries of 1024: 113 us instead of 128 past the caches; 4 groups of two rows, 131072 of 2048: 213 against 209)
-    z.b_once = c->rows <= tile_size(t, Tile::Small).bm && static_cast<uint64_t>(z.b_group ? c->groups : 1) * c->vocab * c->dim * s > kLastLevelCache;
     z.moments = reinterpret_cast<float4 *>(ws + w.moments);
     z.moment_tiles = (c->vocab + cols - 1) / cols;
     z.quads = c->top ? reinterpret_cast<float *>(ws + w.quads) : nullptr;
@@ -911,6 +919,35 @@ int cocod_token_scores_grad(void *stream, const cocod_token_scores_call *c)
             if (int rc = launch_status(launch_store(q, t, Layout::Weights, settle_tile(t, Layout::Weights, w.to_table.tile, d), d), what)) return rc;
         }
     }
+    return COCOD_OK;
+}
+
+int cocod_debug_token_scores_plan(const cocod_token_scores_call *c, int direction, cocod_product_plan out[3], uint32_t *pieces)
+{
+    if (!out || !pieces) return set_error(COCOD_ERR_INVALID, "out or pieces is NULL");
+    if (int rc = check(c)) return rc;
+    if (direction != COCOD_TOKEN_SCORES_FORWARD && direction != COCOD_TOKEN_SCORES_GRAD) return set_error(COCOD_ERR_INVALID, "unknown direction %d", direction);
+    const Dtype t = kTypes[c->dtype];
+    const bool grad = direction == COCOD_TOKEN_SCORES_GRAD;
+    const Workspace w = carve(c, grad);
+    const uint8_t *ws = static_cast<const uint8_t *>(c->workspace);
+    auto plan = [&](Layout layout, const ProductPlan &planned, const ProductParams &p) {
+        return plan_as_run(t, layout, settle_tile(t, layout, planned.tile, p), planned.splits, p);
+    };
+    const cocod_product_plan none = {0, 0, 0};
+    if (!grad) {
+        bool gathered;
+        const ProductParams z = forward_operands(c, w, ws, gathered);
+        out[0] = plan(Layout::Rows_NK, w.logits, z);
+        if (z.b_once && out[0].tile == static_cast<uint32_t>(Tile::Small) && out[0].operands == 0) out[0].operands = 3;
+        out[1] = out[2] = none;
+        *pieces = 1;
+        return COCOD_OK;
+    }
+    out[0] = plan(Layout::Rows_NK, w.logits, logits_operands(c, w, ws, true));
+    out[1] = c->dh ? plan(Layout::Rows_KN, w.to_hidden, hidden_operands(c, w, ws, 0, static_cast<uint32_t>(w.piece < c->vocab ? w.piece : c->vocab))) : none;
+    out[2] = c->de ? plan(Layout::Weights, w.to_table, table_operands(w, ws)) : none;
+    *pieces = w.pieces;
     return COCOD_OK;
 }
 

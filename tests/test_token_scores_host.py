@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_1906_12043_amd as P
+from tests import operator_plans as op
 from tests.operator_harness import TYPES
 from tests.scores_harness import exact_scores
 from tests.test_gpu_token_scores import LARGE, SHAPES
@@ -146,3 +147,54 @@ def test_every_tile_is_reached():
             seen.add((dtype, P.debug_cross_entropy_plan(x)[0][0][0]))
     want = {("fp32", 1), ("fp32", 2), ("fp32", 5)} | {(d, t) for d in ("bf16", "fp16") for t in (0, 1, 2, 3)}
     assert want <= seen, want - seen
+
+
+def planned(dtype, groups, rows, dim, vocab, piece=0):
+    f = dict(dtype=TYPES[dtype][0], groups=groups, rows=rows, dim=dim, vocab=vocab, offsets=A, h=1 << 41, ldh=dim, e=1 << 42, lde=dim, e_stride=vocab * dim, targets=1 << 43,
+             norms=1 << 44, dh=1 << 45, lddh=dim, de=1 << 46, ldde=dim, de_stride=vocab * dim, piece=piece, workspace=1 << 47, workspace_bytes=1 << 46)
+    return P.TokenScores(**f)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_every_product_is_reached_by_the_plans_of_the_calls_themselves(dtype):
+    """Tiles, sums whole and split, pieces and ways of the operands, as the calls would run at the sizes of operator_plans."""
+    seen = set()
+    for case in op.LOSSES:
+        call = planned(dtype, *case)
+        seen.add(("logits",) + P.debug_token_scores_plan(call, P.TOKEN_SCORES_FORWARD)[0][0][::2])
+        (slopes, dh, de), pieces = P.debug_token_scores_plan(call, P.TOKEN_SCORES_GRAD)
+        seen.add(("slopes",) + slopes[::2])
+        if case[2] >= op.COLUMNS[dh[0]]:
+            seen.add(("dh", dh[0], dh[1] > 1, pieces > 1, dh[2]))
+        if case[2] >= op.COLUMNS[de[0]]:
+            seen.add(("de", de[0], de[1] > 1))
+    both, logits = (False, True), ("logits", "slopes")
+    if dtype == "fp32":
+        tiles = (op.MEDIUM, op.SMALL, op.SQUARE)
+        want = {(k, tile, op.REGISTERS) for k in logits for tile in tiles} | {("dh", tile, split, pieces, op.REGISTERS) for tile in tiles for split in both for pieces in both}
+        want |= {("de", tile, split) for tile in tiles for split in both}
+    else:
+        tiles, few = (op.LARGE, op.MEDIUM, op.SMALL, op.DEEP), (op.MEDIUM, op.SMALL)
+        want = {(k, tile, op.DIRECT) for k in logits for tile in tiles} | {(k, tile, op.REGISTERS) for k in logits for tile in few}
+        want |= {("dh", tile, split, pieces, op.DIRECT) for tile in tiles + (op.TALL,) for split in both for pieces in both}
+        want |= {("dh", tile, split, pieces, op.REGISTERS) for tile in few for split in both for pieces in both} | {("de", tile, split) for tile in tiles for split in both}
+    assert seen == want, (seen - want, want - seen)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_large_table_that_few_rows_read_goes_past_the_caches(dtype):
+    def way(groups, rows, vocab, dim=520, **change):
+        call = planned(dtype, groups, rows, dim, vocab)
+        call.set(**change)
+        return P.debug_token_scores_plan(call, P.TOKEN_SCORES_FORWARD)[0][0]
+    assert way(1, 5, 300_001) == (op.SMALL, 1, 3) and way(2, 32, 150_000) == (op.SMALL, 1, 3)
+    assert way(1, 33, 300_001)[2] == op.DIRECT and way(1, 5, 200_001) == (op.SMALL, 1, op.DIRECT)
+    assert way(2, 32, 150_000, e_stride=0) == (op.SMALL, 1, op.DIRECT)                 # one table, within the caches
+    assert way(1, 5, 300_001, e=(1 << 42) + 2) == (op.SMALL, 1, op.REGISTERS)
+
+
+def test_plans_refuse_what_the_calls_refuse():
+    refused(P.debug_token_scores_plan, planned("bf16", 0, 7, 8, 8), 0, text="groups")
+    refused(P.debug_token_scores_plan, planned("bf16", 1, 7, 8, 8), 2, text="direction")
+    assert P.lib().cocod_debug_token_scores_plan(None, 0, None, None) == P.ERR_INVALID
+    assert P.debug_token_scores_plan(scores(dh=None, de=None), P.TOKEN_SCORES_GRAD)[0][1:] == [(0, 0, 0), (0, 0, 0)]
