@@ -622,6 +622,8 @@ template <class T> struct Moment {
     float below = 0.0f, largest = 0.0f, far = 0.0f;
     __device__ __forceinline__ void add(float z, float top)
     {
+        // z is a product, rounded, and `top` one of them: taken from it unrounded, the largest would not lie at distance zero, and the rounding of `top` in the place of what a sure row keeps apart.
+        #pragma clang fp contract(off)
         const float d = z - (top == -INFINITY ? 0.0f : top), e = T::exp(d, 0.0f);       // (what is not finite stays so in `below`)
         below += d == 0.0f ? 0.0f : e;
         largest += d == 0.0f ? 1.0f : 0.0f;

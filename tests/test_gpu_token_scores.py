@@ -497,3 +497,31 @@ def test_gradients_of_rows_in_one_of_nine_groups(dtype, rows, which):
     check_scores(out, want, far, bounds, rows, target)
     for k, got in (("dh", dh), ("de", de)):
         assert bool(((got.double() - want[k]).abs() <= far[k]).all()), k
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows, vocab, dim", [(20, 3001, 16), (300, 3001, 16), (600, 2050, 136), (1500, 8000, 136)])
+@pytest.mark.parametrize("gap, scale", [(20.3, 1.0 / 0.7), (33.1, 0.9), (12.7, 1.0 / 1.3)])
+def test_rows_that_are_sure_keep_their_digits_at_any_scale(dtype, rows, vocab, dim, gap, scale):
+    """As above, with a scale whose product with the largest logit is rounded (by half a step of itself, which moves the others' exponentials by gap / 2 steps), in every tile."""
+    t, scale = TYPES[dtype][1], float(torch.tensor(scale, dtype=torch.float32))
+    h, e = torch.zeros(rows, dim, dtype=t, device="cuda"), torch.zeros(1, vocab, dim, dtype=t, device="cuda")
+    h[:, 0] = gap
+    gap = float(h[0, 0]) * scale
+    e[0, 1234, 0] = 1.0
+    target = torch.full((rows,), 1234, dtype=torch.int32, device="cuda")
+    a, dh = torch.ones(rows, device="cuda"), torch.empty_like(h)
+    c, out = scores_call(dtype, [0, rows], h, e, target, grad=True, top=2, scale=scale, d_logp=a, dh=dh)
+    P.token_scores(torch.cuda.current_stream(), c)
+    P.token_scores_grad(torch.cuda.current_stream(), c)
+    rest = (vocab - 1) * math.exp(-gap)
+    logp, H = -math.log1p(rest), math.log1p(rest) + gap * rest / (1 + rest)
+    rel = (2 * gap + 40 + vocab / 64) * STEP
+    for got, want in ((out["logp"], logp), (out["entropy"], H), (out["top_logp"][:, 0], logp)):
+        assert bool(((got.double() - want).abs() <= rel * abs(want) * 1.01).all())
+    assert bool((out["top_ids"][:, 0] == 1234).all()) and bool((out["top_ids"][:, 1] == 0).all())
+    # dh[0] = scale a (1 - p) e[1234][0]; in 16 bits rounded twice
+    want = scale * rest / (1 + rest)
+    u = 2 * torch.finfo(t).eps if t != torch.float32 else 0.0
+    low = 2.0 ** -37 if t == torch.float16 else 0.0
+    assert bool(((dh[:, 0].double() - want).abs() <= (u + rel + 4 * STEP) * want * 1.01 + low + torch.finfo(t).smallest_normal * torch.finfo(t).eps).all())
