@@ -78,12 +78,14 @@ struct F32 : Bf16 {
     static __device__ __forceinline__ float exp(float x, float base) { return expf(x - base); }
 };
 
-// Slope of an entry whose logit lies d below the row's largest, from the row's two factors (Finish::Score).  Below -200 the exponential is zero, and so is
-// the slope, also where d is minus infinity.
+// Slope of an entry with the logit z, d below the row's largest, from the row's two factors (Finish::Score).  Below -200 the exponential is zero, and so is
+// the slope, also where d is minus infinity.  z is a product, rounded as `top` was: unrounded, the largest entry of a sure row would lie a rounding of `top`, not zero, from
+// itself, far more than its slope of the entropy.
 constexpr float kFarBelow = -200.0f;
-template <class T> __device__ __forceinline__ float score_slope(float d, float none, float one)
+template <class T> __device__ __forceinline__ float score_slope(float z, float top, float none, float one)
 {
-    d = fmaxf(d, kFarBelow);
+    #pragma clang fp contract(off)
+    const float d = fmaxf(z - top, kFarBelow);
     return T::exp(d, 0.0f) * fmaf(one, d, none);
 }
 

@@ -554,7 +554,7 @@ template <class T, bool WEIGHTS, Finish FINISH> struct RowFinish {
                 }
             } else if constexpr (FINISH == Finish::Score) {
                 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) { a[j] = score_slope<T>(a[j] * p.logit_scale - top, f, one); b[j] = score_slope<T>(b[j] * p.logit_scale - top, f, one); }
+                for (uint32_t j = 0; j < 4; ++j) { a[j] = score_slope<T>(a[j] * p.logit_scale, top, f, one); b[j] = score_slope<T>(b[j] * p.logit_scale, top, f, one); }
                 if (number - ca < 4 || number - cb < 4) {
                     const float t = p.target_slope[row];
                     #pragma unroll
@@ -790,7 +790,7 @@ __global__ __launch_bounds__(S::threads) void product_kernel(const ProductParams
             const int32_t target = p.target[at.row0 + r];
             #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = static_cast<int32_t>(p.v0 + c + j) == target ? slope : score_slope<T>(v[j] * p.logit_scale - top, none, one);
+                v[j] = static_cast<int32_t>(p.v0 + c + j) == target ? slope : score_slope<T>(v[j] * p.logit_scale, top, none, one);
                 if (c + j >= p.n) v[j] = 0.0f;
             }
             store_values<T>(p.out, (at.row0 + r) * p.ldc + c, v, 4, false);

@@ -525,3 +525,25 @@ def test_rows_that_are_sure_keep_their_digits_at_any_scale(dtype, rows, vocab, d
     u = 2 * torch.finfo(t).eps if t != torch.float32 else 0.0
     low = 2.0 ** -37 if t == torch.float16 else 0.0
     assert bool(((dh[:, 0].double() - want).abs() <= (u + rel + 4 * STEP) * want * 1.01 + low + torch.finfo(t).smallest_normal * torch.finfo(t).eps).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows, vocab, dim", [(20, 3001, 16), (300, 3001, 16), (600, 2050, 136), (1500, 8000, 136)])
+@pytest.mark.parametrize("gap, scale", [(20.0, 1.0), (20.3, 1.0 / 0.7), (33.1, 0.9), (12.7, 1.0 / 1.3)])
+def test_the_entropys_slope_of_a_sure_row_keeps_its_digits(dtype, rows, vocab, dim, gap, scale):
+    """The largest entry's slope is b p D, D = -gap rest / (1 + rest), with the error of D (that of H above), of p and one rounding, after the mantissa of the target's."""
+    t, scale = TYPES[dtype][1], float(torch.tensor(scale, dtype=torch.float32))
+    h, e = torch.zeros(rows, dim, dtype=t, device="cuda"), torch.zeros(1, vocab, dim, dtype=t, device="cuda")
+    h[:, 0] = gap
+    gap = float(h[0, 0]) * scale
+    e[0, 1234, 0] = 1.0
+    target = torch.full((rows,), 77, dtype=torch.int32, device="cuda")
+    b, dh = torch.ones(rows, device="cuda"), torch.empty_like(h)
+    c, out = scores_call(dtype, [0, rows], h, e, target, grad=True, scale=scale, d_entropy=b, dh=dh)
+    P.token_scores(torch.cuda.current_stream(), c)
+    P.token_scores_grad(torch.cuda.current_stream(), c)
+    rest = (vocab - 1) * math.exp(-gap)
+    want = -scale * gap * rest / (1 + rest) ** 2
+    rel = (2 * gap + 60 + vocab / 64) * STEP + (torch.finfo(t).eps if t != torch.float32 else 0.0)
+    low = 32 * 2.0 ** -38 * scale if t == torch.float16 else 0.0
+    assert bool(((dh[:, 0].double() - want).abs() <= rel * abs(want) * 1.01 + low + torch.finfo(t).smallest_normal * torch.finfo(t).eps).all())
