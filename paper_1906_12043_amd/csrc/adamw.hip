@@ -234,6 +234,8 @@ __device__ __forceinline__ Stored store_states(const f4 &m, const f4 &v, const f
 // An address in device memory from its number (said so, as accesses that might also go to LDS wait for it).
 __device__ __forceinline__ char *in_memory(uint64_t address) { return (char *)(__attribute__((address_space(1))) char *)address; }
 
+constexpr uint32_t kLeastNormal = 0x00800000u;       // bits of 2^-126
+
 // A tile of a tensor.  WHOLE: it lies within the tensor, so that nothing is decided between the loads, which are then all on their way at a time.
 struct Terms { float grad_scale, keep, step, root_bias2; uint32_t stream; };
 template <class TP, class TG, bool EIGHT, bool STREAM, bool WHOLE>
@@ -269,6 +271,7 @@ __device__ __forceinline__ void update(const AdamWParams &s, const Tensor &t, co
             v[u] *= v[u];
         }
         f4 root;
+        uint32_t least = ~0u;
         #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
             const float d = g[u][j] * now.grad_scale;
@@ -276,8 +279,16 @@ __device__ __forceinline__ void update(const AdamWParams &s, const Tensor &t, co
             v[u][j] = v[u][j] * s.beta2 + (d * s.rest2) * d;
             // (a code hangs on the last bit of the root only through its block's largest, of which store_states takes an exact one)
             root[j] = EIGHT ? __builtin_amdgcn_sqrtf(v[u][j]) : sqrtf(v[u][j]);
-            p[u][j] = fmaf(-now.step, m[u][j] * __builtin_amdgcn_rcpf(fmaf(root[j], now.root_bias2, s.eps)), p[u][j] * now.keep);
+            const uint32_t bits = __float_as_uint(v[u][j]) - 1;          // (zero, whose root is right, is far above)
+            least = least < bits ? least : bits;
         }
+        // the instruction takes what is below the normal numbers for zero: with an eps of zero the step would be infinite
+        if (EIGHT && __any(least < kLeastNormal - 1)) {
+            #pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) root[j] = sqrtf(v[u][j]);
+        }
+        #pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) p[u][j] = fmaf(-now.step, m[u][j] * __builtin_amdgcn_rcpf(fmaf(root[j], now.root_bias2, s.eps)), p[u][j] * now.keep);
         Four<TP, STREAM>::store(t.p, base, count[u], p[u]);
         if constexpr (sizeof(typename TP::elem) == 4) {
             if (t.copy && s.copy_dtype == COCOD_BF16) Four<Bf16, STREAM>::store(t.copy, base, count[u], p[u]);

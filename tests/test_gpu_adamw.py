@@ -464,3 +464,24 @@ def test_local_steps_of_workers_and_their_average():
         # six steps and two means, each off by a few roundings of values up to 5
         assert float((x[:, :d].double() - want).abs().max()) <= 6 * 20 * E * 5
         assert not bool(x[:, d:].any())
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("gradient", [1e-17, 1e-19, 3e-20])
+@pytest.mark.parametrize("n", [64, 2050])
+def test_squares_below_the_normal_numbers(eight, gradient, n):
+    """The first step without eps is lr whatever the gradient's size, its sign the gradient's; v of 1e-38 and less has steps of 2^-149, half of one moves its root by 2^-151 / v of itself."""
+    g = torch.full((n,), gradient, device="cuda")
+    g[1::2] *= -1
+    p = torch.ones(n, device="cuda")
+    block = -(-n // 32)
+    m, v = (torch.zeros(n, dtype=torch.uint8 if eight else torch.float32, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(block, dtype=torch.uint8, device="cuda") for _ in range(2))
+    one = dict(n=n, p=p, g=g, m=m, v=v, **(dict(m_scales=ms, v_scales=vs) if eight else {}))
+    call = P.AdamW(tensors=[one], dtype=P.F32, grad_dtype=P.F32, state=P.ADAMW_STATE_8BIT if eight else P.ADAMW_STATE_F32, lr=0.125, beta1=0.9, beta2=0.95, eps=0.0, step=1, seed=3)
+    P.adamw(torch.cuda.current_stream(), call)
+    want = 1.0 - 0.125 * torch.sign(g).double()
+    bound = 0.125 * (16 * E + 2 * 2.0 ** -151 / (0.05 * gradient ** 2)) + 2 * E
+    assert bool(((p.double() - want).abs() <= bound).all())
+    if eight:                                                  # (not zero is not stored as zero)
+        assert bool((v > 0).all())
