@@ -661,7 +661,7 @@ typedef struct cocod_adamw_call {
     uint64_t stride;                /* elements from worker to worker, of all arrays; a multiple of 32 for 8-bit states; not read with one worker */
     const cocod_adamw_tensor *tensors;            /* HOST memory, read during the call (a captured call keeps what it says) */
     uint64_t count;                 /* of tensors, up to 2^20 */
-    float lr, beta1, beta2, eps;    /* betas in 0 .. 1, 1 excluded; eps >= 0 */
+    float lr, beta1, beta2, eps;    /* betas in 0 .. 1, 1 excluded; eps 0 or at least 2^-126 */
     float grad_scale;               /* gradients are multiplied by it */
     uint32_t reserved;
     uint64_t step;                  /* the number of this step, from 1 */

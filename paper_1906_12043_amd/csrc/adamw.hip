@@ -377,6 +377,8 @@ int check_call(const cocod_adamw_call *c)
     if (c->count > (1u << 20)) return set_error(COCOD_ERR_INVALID, "at most 2^20 tensors");
     if (!finite_in(c->beta1, 0.0f, 1.0f) || !finite_in(c->beta2, 0.0f, 1.0f)) return set_error(COCOD_ERR_INVALID, "beta1 and beta2 must be in 0 .. 1, 1 excluded");
     if (!finite_in(c->eps, 0.0f, INFINITY)) return set_error(COCOD_ERR_INVALID, "eps must be finite and not negative");
+    // (the reciprocal's instruction takes what is below the normal numbers for zero, and a parameter without gradients would become NaN)
+    if (c->eps > 0.0f && c->eps < 0x1p-126f) return set_error(COCOD_ERR_INVALID, "eps must be 0 or at least 2^-126");
     if (c->now && (reinterpret_cast<uintptr_t>(c->now) & 3)) return set_error(COCOD_ERR_INVALID, "now is not 4-byte aligned");
     if (!c->now) {
         if (!std::isfinite(c->lr)) return set_error(COCOD_ERR_INVALID, "lr is not finite");

@@ -53,6 +53,13 @@ def test_states_of_8_bits_are_checked(change, more, text):
     refused(adamw([dict(EIGHT, **change)], state=P.ADAMW_STATE_8BIT, **more), text)
 
 
+@pytest.mark.parametrize("eps", [1e-45, 5e-39, 1.1754942e-38])
+def test_an_eps_below_the_normal_numbers_is_refused(eps):
+    refused(adamw(eps=eps), "eps must be 0 or at least 2^-126")
+    for fine in (0.0, 2.0 ** -126):
+        P.adamw(None, adamw([], eps=fine))
+
+
 def test_struct_and_null():
     c = adamw()
     c.struct_size += 4
