@@ -542,7 +542,9 @@ typedef struct cocod_token_scores_call {
     uint64_t workspace_bytes;
 } cocod_token_scores_call;
 
-/* Bytes of workspace that the call of this direction needs (with alternatives: rows * (vocab + 8 top) bytes, and a little); reads the sizes, top, piece, and whether dh and de are NULL. */
+/* Bytes of workspace that the call of this direction needs; reads dtype, groups and sizes, top, piece, and whether dh and de are NULL.  Forward: for every row one of dim elements,
+   16 bytes for every 128 entries of the vocabulary (64 where rows are few), with alternatives vocab + 8 top bytes more, and a little.  Gradient: for every row one of dim
+   elements (16-bit types with de: two) and one of `piece` elements, with several pieces and dh one of dim floats; partial sums; and a little. */
 int cocod_token_scores_workspace(const cocod_token_scores_call *c, int direction, uint64_t *bytes);
 int cocod_token_scores(void *stream, const cocod_token_scores_call *c);
 int cocod_token_scores_grad(void *stream, const cocod_token_scores_call *c);
@@ -572,7 +574,7 @@ int cocod_checkpoint_load(void *stream, int dtype, uint64_t rows, uint64_t cols,
  */
 typedef struct cocod_route {
     uint32_t struct_size;           /* sizeof(cocod_route); checked */
-    uint32_t dtype;                 /* cocod_dtype of x, xs, ys, y, dy, dys, dxs, dx (cocod_route_sort does not read it) */
+    uint32_t dtype;                 /* cocod_dtype of x, xs, ys, y, dy, dys, dxs, dx (to cocod_route_sort any of them is the same) */
     uint32_t groups;                /* 1 .. 65535 */
     uint32_t choices;               /* 1 .. 64 */
     uint64_t tokens;                /* tokens * choices < 2^31; 0 is legal */
@@ -650,6 +652,8 @@ typedef struct cocod_adamw_tensor {
  * element) alone.  The caller gives every step another seed.  A root that is not zero is not stored as zero.  The new p comes from
  * m and v before they are rounded.  A state that is not finite is stored as NaN and does not count for the scale.
  * Arrays may begin at any element.  The arrays of a call must not overlap each other; within a tensor and a worker that is checked.
+ * A launch takes up to 55 (8-bit states with copies) .. 64 tensors with up to 16 pairs of weight_decay and lr_scale; the next one begins behind them, and
+ * behind a tensor without elements between others.
  */
 typedef struct cocod_adamw_call {
     uint32_t struct_size;           /* sizeof(cocod_adamw_call); checked */

@@ -7,7 +7,7 @@
 // (the format of the 8-bit activations), whose range of 2^18 within a block would be 2^9 of v's roots if it held v.  A step changes v by a
 // thousandth of itself, a code's step is a sixteenth to an eighth: rounded to the nearest, v would stand still.  So a code is rounded up or down by chance,
 // with 16 random bits each, so that the stored m, and the SQUARE of the stored root of v, are m' and v' in the mean (to 2^-16 of a step).  The random bits are
-// a function of (seed, tensor, worker, element): a multiply-and-shift mixer of 32 bits, three multiplications an element, where a
+// a function of (seed, tensor, worker, element): the published mixer of 32 bits lowbias32 (C. Wellons, public domain), three multiplications an element, where a
 // ten-round counter generator would cost more time than the memory leaves.  p' comes from m' and v' before they are rounded.
 //
 // Bound by memory: fp32 with 16-bit gradients and copies 28 bytes an element (16 workers of 11.2 M: 842 us, 6.0 TB/s), with 8-bit states 16.1 (138 M: 404 us,
@@ -142,7 +142,7 @@ __device__ __forceinline__ void decode(uint32_t codes, uint8_t scale, f4 &v)
 // Random bits of element `at` of a tensor; those of the elements behind it follow by adding kNextElement to x.
 constexpr uint32_t kNextElement = 0x9E3779B1u;
 __device__ __forceinline__ uint32_t random_seed(uint64_t at, uint32_t stream) { return static_cast<uint32_t>(at) * kNextElement + static_cast<uint32_t>(at >> 32) * 0x85EBCA6Bu + stream; }
-__device__ __forceinline__ uint32_t mixed(uint32_t x)
+__device__ __forceinline__ uint32_t mixed(uint32_t x)        // lowbias32: its shifts and multipliers are the published ones
 {
     x = (x ^ (x >> 16)) * 0x7FEB352Du;
     x = (x ^ (x >> 15)) * 0x846CA68Bu;

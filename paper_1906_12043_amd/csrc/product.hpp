@@ -73,11 +73,11 @@ struct ProductParams {
     float logit_scale;                // logits are multiplied by it, > 0
     float4 *moments;                  // [rows][column tiles]: maximum, sum, sum of distances (target may be null then)
     uint32_t moment_tiles;
-    float *quads;                     // non-null: [rows][ld_quads], see quad_place
+    float *quads;                     // non-null: [rows][ld_quads], see quad_order
     uint64_t ld_quads;                // a multiple of 64
     const float *slope_one;           // [rows]: slope of an entry d below the largest is e^d (inverse + slope_one d)
     const float *group_scale;         // Weights, non-null: C of a group is multiplied by this instead of scale
-    uint32_t ldc_zero;                // Slope: columns up to here are stored, those from n on as zeros
+    uint32_t ldc_zero;                // Slope, Score: columns up to here are stored, those from n on as zeros
 };
 
 // Tile shapes a launch can take (plan_product picks one).

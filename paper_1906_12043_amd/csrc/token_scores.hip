@@ -19,8 +19,8 @@
 // of the target's slope is taken out of the row's slopes, which leaves a power of two there: dh is multiplied by it in fp32, and the product for dE
 // takes rows of h times it (a row whose entry no other row has for its target is then rounded once, as its last rounding would; 4096 rows, 32003 entries of 1024,
 // error against 64 bits: dh 1.00 and dE 1.23 times that of a plain form in fp32, both 1.41 times without).  fp16 slopes are also taken times a power of two per
-// group that brings their bound below 2^14: p |d - D| is below 22 for any vocabulary up to 2^30, so |a| + 32 |b| bounds a slope.  Rows whose slopes a and
-// b are both zero take no part.
+// group that brings their bound below 2^14: p |d - D| is below 22 for any vocabulary up to 2^30, so |a| + 32 |b| bounds a slope; and the rows of h for dE times one that brings the
+// group's largest number to 2^14.  Rows whose slopes a and b are both zero take no part.
 #include "vocabulary.hpp"
 #include "row_access.hpp"
 

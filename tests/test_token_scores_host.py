@@ -198,3 +198,12 @@ def test_plans_refuse_what_the_calls_refuse():
     refused(P.debug_token_scores_plan, planned("bf16", 1, 7, 8, 8), 2, text="direction")
     assert P.lib().cocod_debug_token_scores_plan(None, 0, None, None) == P.ERR_INVALID
     assert P.debug_token_scores_plan(scores(dh=None, de=None), P.TOKEN_SCORES_GRAD)[0][1:] == [(0, 0, 0), (0, 0, 0)]
+
+
+@pytest.mark.parametrize("rows, dim, vocab, top", [(4096, 4096, 1000, 8), (4096, 1024, 32003, 0), (4, 2048, 131072, 8), (509, 512, 5003, 5)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_the_header_says_how_much_workspace_a_forward_call_needs(dtype, rows, dim, vocab, top):
+    size = 4 if dtype == "fp32" else 2
+    need = P.token_scores_workspace(P.TokenScores(dtype=TYPES[dtype][0], groups=1, rows=rows, dim=dim, vocab=vocab, top=top), P.TOKEN_SCORES_FORWARD)
+    least, most = (rows * (dim * size + 16 * -(-vocab // entries) + (vocab + 8 * top if top else 0)) for entries in (128, 64))
+    assert least <= need <= most + rows * (20 + (256 if top else 0)) + 8 * 256            # (a little: five numbers a row, and quads of whole tiles)
